@@ -107,6 +107,48 @@ int atom_k_colsum(int dtype, const void* x, int64_t rows, int cols, float* out, 
 int atom_k_xent(int dtype, const float* logits, int64_t ldz, const int32_t* tgt, void* dz, int64_t lddz,
                 float* loss_rows, int64_t rows, int V, float scale, void* stream);
 
+/* Cross-entropy of a linear head over a vocabulary, with no logits in memory
+ * (the "Logits" layer, Section III-B; atom_k_gemm and atom_k_xent do it with
+ * the logits of a range of tokens):
+ *   z[n][v] = sum_c x[n][c] w[v][c],  lse[n] = log sum_v exp z[n][v],
+ *   loss_rows[n] = lse[n] - z[n][tgt[n]].
+ * x [rows][ldx] and w [V][ldw] in dtype, d columns of each; tgt, lse and
+ * loss_rows [rows].  A token whose target is negative (ATOM_XENT_IGNORE) takes
+ * no part: lse and loss 0, whatever its row holds.  A target of V or more:
+ * loss NaN (it is never read).  Logits of a whole row at -infinity, or one at
+ * +infinity or NaN: loss NaN.
+ * Requirements: d a positive multiple of 8 (bf16) or 4 (fp32), ldx and ldw
+ * multiples of the same, at least d; x, w and ws 16-byte aligned; rows, V >= 1
+ * any numbers (rows 0: nothing is done) with less than 2^30 tiles of 32 x 32
+ * between any two of rows, V and d.  ws: device scratch of at least the bytes
+ * that the query returns (0 for sizes it refuses); calls that may overlap need
+ * scratch of their own. */
+#define ATOM_XENT_IGNORE (-1)
+uint64_t atom_k_linear_xent_fwd_ws_bytes(int dtype, int64_t rows, int V, int d);
+int atom_k_linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
+                           float* lse, float* loss_rows, int64_t rows, int V, int d, void* ws, uint64_t ws_bytes,
+                           void* stream);
+
+/* Its gradients, in pieces of the vocabulary:
+ *   dz[n][v] = (exp(z[n][v] - lse[n]) - [v = tgt[n]]) * drow[n]
+ *   dx[n][c] = scale * sum_v dz[n][v] w[v][c]   (dtype, [rows][lddx])
+ *   dw[v][c] = scale * sum_n dz[n][v] x[n][c]   ([V][lddw])
+ * z is computed again, `piece` columns at a time (rounded up to a multiple of
+ * 8, at most V; 0: the library's choice), and dz of a piece goes through the
+ * workspace in dtype.  lse comes from the forward call; drow (NULL: 1) weighs
+ * a token.  A token with a negative target or with drow 0 adds nothing,
+ * whatever its row of x holds, and its row of dx is zero; one with a target of
+ * V or more makes both gradients NaN.  dx or dw may be NULL (not wanted).
+ * dw_epi: ATOM_EPI_STORE (dw in dtype), ATOM_EPI_STORE_F32 or ATOM_EPI_ACC_F32
+ * (dw fp32, += the gradient).  rows 0: dw is zeroed, or kept by
+ * ATOM_EPI_ACC_F32.  dx and dw must not overlap the inputs.  Requirements as
+ * above, for dx and lddx, dw and lddw as well. */
+uint64_t atom_k_linear_xent_bwd_ws_bytes(int dtype, int64_t rows, int V, int d, int piece);
+int atom_k_linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
+                           const float* lse, const float* drow, float scale, void* dx, int64_t lddx, void* dw,
+                           int64_t lddw, int dw_epi, int64_t rows, int V, int d, int piece, void* ws,
+                           uint64_t ws_bytes, void* stream);
+
 /* Token and position embedding (node 0 of the layer chain):
  * x[n][c] = wte[tok[n]][c] + wpe[n % T][c]; x fp32 [n_tok][d].  A token id
  * outside [0, V) yields a NaN row (no out-of-range read). */

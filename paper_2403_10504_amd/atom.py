@@ -133,6 +133,12 @@ _SIGS = {
     "atom_k_colsum_part_floats": (I64, [I64, ctypes.c_int]),
     "atom_k_colsum": (ctypes.c_int, [ctypes.c_int, P, I64, ctypes.c_int, P, P, P]),
     "atom_k_xent": (ctypes.c_int, [ctypes.c_int, P, I64, P, P, I64, P, I64, ctypes.c_int, ctypes.c_float, P]),
+    "atom_k_linear_xent_fwd_ws_bytes": (U64, [ctypes.c_int, I64, ctypes.c_int, ctypes.c_int]),
+    "atom_k_linear_xent_fwd": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, P, P, P, I64, ctypes.c_int, ctypes.c_int, P,
+                                              U64, P]),
+    "atom_k_linear_xent_bwd_ws_bytes": (U64, [ctypes.c_int, I64] + [ctypes.c_int] * 3),
+    "atom_k_linear_xent_bwd": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, P, P, P, ctypes.c_float, P, I64, P, I64,
+                                              ctypes.c_int, I64] + [ctypes.c_int] * 3 + [P, U64, P]),
     "atom_k_embed_fwd": (ctypes.c_int, [ctypes.c_int, P, P, P, P, I64, ctypes.c_int, ctypes.c_int, ctypes.c_int, P]),
     "atom_k_copy": (ctypes.c_int, [P, P, I64, P]),
 }
@@ -479,6 +485,27 @@ def atom_k_colsum(dtype, x, rows, cols, out, part, stream=None):
 
 def atom_k_xent(dtype, logits, ldz, tgt, dz, lddz, loss_rows, rows, V, scale, stream=None):
     _kcall("atom_k_xent", dtype, logits, ldz, tgt, dz, lddz, loss_rows, rows, V, ctypes.c_float(scale), stream)
+
+
+ATOM_XENT_IGNORE = -1
+
+
+def atom_k_linear_xent_fwd_ws_bytes(dtype, rows, V, d):
+    return lib().atom_k_linear_xent_fwd_ws_bytes(dtype, rows, V, d)
+
+
+def atom_k_linear_xent_fwd(dtype, x, ldx, w, ldw, tgt, lse, loss_rows, rows, V, d, ws, ws_bytes, stream=None):
+    _kcall("atom_k_linear_xent_fwd", dtype, x, ldx, w, ldw, tgt, lse, loss_rows, rows, V, d, ws, ws_bytes, stream)
+
+
+def atom_k_linear_xent_bwd_ws_bytes(dtype, rows, V, d, piece=0):
+    return lib().atom_k_linear_xent_bwd_ws_bytes(dtype, rows, V, d, piece)
+
+
+def atom_k_linear_xent_bwd(dtype, x, ldx, w, ldw, tgt, lse, drow, scale, dx, lddx, dw, lddw, dw_epi, rows, V, d, piece,
+                           ws, ws_bytes, stream=None):
+    _kcall("atom_k_linear_xent_bwd", dtype, x, ldx, w, ldw, tgt, lse, drow, scale, dx, lddx, dw, lddw, dw_epi, rows, V,
+           d, piece, ws, ws_bytes, stream)
 
 
 def atom_k_embed_fwd(dtype, tok, wte, wpe, x, n_tok, T, V, d, stream=None):

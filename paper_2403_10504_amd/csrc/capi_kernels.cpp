@@ -15,6 +15,11 @@ inline int st(hipError_t e) {
 }
 inline hipStream_t S(void* s) { return static_cast<hipStream_t>(s); }
 inline bool dt_ok(int dt) { return dt == ATOM_F32 || dt == ATOM_BF16; }
+inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+// rows of d elements, ld apart, in whole 16-byte chunks
+inline bool rows_ok(int dt, const void* p, int64_t ld, int d) {
+  return p && !misaligned(p) && ld >= d && ld % (dt == ATOM_BF16 ? 8 : 4) == 0;
+}
 }  // namespace
 
 extern "C" {
@@ -89,6 +94,44 @@ int atom_k_xent(int dtype, const float* logits, int64_t ldz, const int32_t* tgt,
                 float* loss_rows, int64_t rows, int V, float scale, void* stream) {
   if (!dt_ok(dtype) || !logits || !tgt || !dz || !loss_rows) return ATOM_EINVAL;
   return st(xent_fwd_bwd(dtype, logits, ldz, tgt, dz, lddz, loss_rows, rows, V, scale, S(stream)));
+}
+
+uint64_t atom_k_linear_xent_fwd_ws_bytes(int dtype, int64_t rows, int V, int d) {
+  return dt_ok(dtype) && linear_xent_ok(dtype, rows, V, d) ? linear_xent_fwd_ws(dtype, rows, V, d) : 0;
+}
+
+int atom_k_linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
+                           float* lse, float* loss_rows, int64_t rows, int V, int d, void* ws, uint64_t ws_bytes,
+                           void* stream) {
+  if (!dt_ok(dtype) || !linear_xent_ok(dtype, rows, V, d)) return ATOM_EINVAL;
+  if (!rows_ok(dtype, x, ldx, d) || !rows_ok(dtype, w, ldw, d)) return ATOM_EINVAL;
+  if (!tgt || !lse || !loss_rows) return ATOM_EINVAL;
+  if (rows > 0 && (!ws || misaligned(ws) || ws_bytes < linear_xent_fwd_ws(dtype, rows, V, d))) return ATOM_EINVAL;
+  return st(linear_xent_fwd(dtype, x, ldx, w, ldw, tgt, lse, loss_rows, rows, V, d, ws, S(stream)));
+}
+
+uint64_t atom_k_linear_xent_bwd_ws_bytes(int dtype, int64_t rows, int V, int d, int piece) {
+  return dt_ok(dtype) && piece >= 0 && linear_xent_ok(dtype, rows, V, d) ? linear_xent_bwd_ws(dtype, rows, V, d, piece) : 0;
+}
+
+int atom_k_linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
+                           const float* lse, const float* drow, float scale, void* dx, int64_t lddx, void* dw,
+                           int64_t lddw, int dw_epi, int64_t rows, int V, int d, int piece, void* ws,
+                           uint64_t ws_bytes, void* stream) {
+  if (!dt_ok(dtype) || piece < 0 || !linear_xent_ok(dtype, rows, V, d)) return ATOM_EINVAL;
+  if (!rows_ok(dtype, x, ldx, d) || !rows_ok(dtype, w, ldw, d) || !tgt || !lse) return ATOM_EINVAL;
+  if ((dx && !rows_ok(dtype, dx, lddx, d)) || (dw && !rows_ok(dtype, dw, lddw, d))) return ATOM_EINVAL;
+  int epi;
+  switch (dw_epi) {
+    case ATOM_EPI_STORE: epi = EPI_SCALE; break;
+    case ATOM_EPI_STORE_F32: epi = EPI_SCALE_F32; break;
+    case ATOM_EPI_ACC_F32: epi = EPI_SCALE_ACC; break;
+    default: return ATOM_EINVAL;
+  }
+  if (!dx && !dw) return ATOM_OK;
+  if (rows > 0 && (!ws || misaligned(ws) || ws_bytes < linear_xent_bwd_ws(dtype, rows, V, d, piece))) return ATOM_EINVAL;
+  return st(linear_xent_bwd(dtype, x, ldx, w, ldw, tgt, lse, drow, scale, dx, lddx, dw, lddw, epi, rows, V, d, piece,
+                            ws, S(stream)));
 }
 
 int atom_k_embed_fwd(int dtype, const int32_t* tok, const void* wte, const void* wpe, float* x, int64_t n_tok, int T,

@@ -246,6 +246,22 @@ __device__ __forceinline__ void epilogue4(const GemmArgs& g, int m, int nb, floa
     load4<T>(static_cast<const T*>(g.aux) + aoff, u, vec && (g.ldaux & 3) == 0, nvalid);
     for (int r = 0; r < 4; ++r) v[r] *= gelu_grad_f(u[r]);
     store4<T>(static_cast<T*>(g.C) + off, v, vec, nvalid);
+  } else if constexpr (EPI == EPI_SCALE) {
+    for (int r = 0; r < 4; ++r) v[r] *= g.alpha;
+    store4<T>(static_cast<T*>(g.C) + off, v, vec, nvalid);
+  } else if constexpr (EPI == EPI_SCALE_F32) {
+    for (int r = 0; r < 4; ++r) v[r] *= g.alpha;
+    store4<float>(static_cast<float*>(g.C) + off, v, vec, nvalid);
+  } else if constexpr (EPI == EPI_SCALE_ACC) {
+    float o[4];
+    load4<float>(static_cast<const float*>(g.C) + off, o, vec, nvalid);
+    for (int r = 0; r < 4; ++r) v[r] = fmaf(g.alpha, v[r], o[r]);
+    store4<float>(static_cast<float*>(g.C) + off, v, vec, nvalid);
+  } else if constexpr (EPI == EPI_SUM_SCALE) {
+    float x[4];
+    load4<float>(g.resid + static_cast<int64_t>(m) * g.ldaux + nb, x, vec && (g.ldaux & 3) == 0, nvalid);
+    for (int r = 0; r < 4; ++r) v[r] = g.alpha * (x[r] + v[r]);
+    store4<T>(static_cast<T*>(g.C) + off, v, vec, nvalid);
   }
 }
 
@@ -423,6 +439,10 @@ hipError_t launch_reduce(const GemmArgs& g, int epi, int splits, hipStream_t s) 
     ATOM_CASE(EPI_BIAS_GELU)
     ATOM_CASE(EPI_BIAS_RESID)
     ATOM_CASE(EPI_GELU_BWD)
+    ATOM_CASE(EPI_SCALE)
+    ATOM_CASE(EPI_SCALE_F32)
+    ATOM_CASE(EPI_SCALE_ACC)
+    ATOM_CASE(EPI_SUM_SCALE)
 #undef ATOM_CASE
     default: return hipErrorInvalidValue;
   }
@@ -481,24 +501,28 @@ struct Choice {
 // FLOP, 192 or 128 columns where 256 divide N badly (16384x768x3072: 78 -> 75
 // us; 2048x5120x15360: 310 -> 273; 1000x8192x2048: 54 -> 40), 128x128 and 64x64
 // where there are too few big tiles for 256 CUs (1000x2048x8192: 157 -> 61, 44
-// split in two; 520x768x3072: 65 -> 17).
+// split in two; 520x768x3072: 65 -> 17).  The loss epilogues (epi[4], epi[5])
+// are fitted to 14 problems with bf16 rows of 128 to 5120: reducing the logits
+// in registers costs less than storing them (16384x50257x768: 1149 us, 128x128
+// 1393), and dz's exponentials 4 us a 256-row tile, which the second workgroup
+// of a CU hides behind 128x128 ones (8192x16384x128: 126 and 119).
 struct TileCfg {
   int bm, bn, occ;  // occ: workgroups a CU holds
-  double ktile, fixed, epi[4], call;
+  double ktile, fixed, epi[6], call;
 };
-constexpr TileCfg BF16_TILES[] = {{256, 256, 1, 0.604, 8.93, {3.26, 10.96, 7.39, 18.10}, 0.70},
-                                  {256, 192, 1, 0.486, 7.82, {1.66, 7.20, 8.13, 13.97}, 1.89},
-                                  {256, 128, 1, 0.412, 5.52, {1.34, 5.36, 4.31, 6.24}, 0.80},
-                                  {128, 128, 2, 0.249, 1.74, {0.63, 2.11, 1.82, 2.08}, 2.10},
-                                  {64, 64, 4, 0.131, 0.437, {0.255, 0.358, 0.373, 0.371}, 1.58}};
+constexpr TileCfg BF16_TILES[] = {{256, 256, 1, 0.604, 8.93, {3.26, 10.96, 7.39, 18.10, -1.8, 4.2}, 0.70},
+                                  {256, 192, 1, 0.486, 7.82, {1.66, 7.20, 8.13, 13.97, -0.7, 4.6}, 1.89},
+                                  {256, 128, 1, 0.412, 5.52, {1.34, 5.36, 4.31, 6.24, 0.0, 3.0}, 0.80},
+                                  {128, 128, 2, 0.249, 1.74, {0.63, 2.11, 1.82, 2.08, -1.1, 0.05}, 2.10},
+                                  {64, 64, 4, 0.131, 0.437, {0.255, 0.358, 0.373, 0.371, -0.08, 0.15}, 1.58}};
 // fp32: the matrix cores bound both direct-load tiles (512 and 128 MFMAs of 32
 // cycles per k tile); 64x64 is 5-10 % faster where it fills the chip.  The
 // register-staged 128x128 tile up to 256 k, where stores and starts dominate
 // (5020x1524x136: 44 -> 30 us; from there on it loses, and its one set of
 // accumulators sums more than 64 MFMAs in a row).
-constexpr TileCfg F32_TILES[] = {{64, 64, 2, 0.554, 1.138, {0.034, 0.195, 0.316, 0.443}, 2.93},
-                                 {32, 32, 4, 0.157, 0.353, {0.023, 0.048, 0.08, 0.169}, 2.90}};
-constexpr TileCfg F32_STAGED = {128, 128, 2, 2.258, 3.0, {-0.13, 3.88, 4.12, 6.15}, 5.12};
+constexpr TileCfg F32_TILES[] = {{64, 64, 2, 0.554, 1.138, {0.034, 0.195, 0.316, 0.443, 0.0, 0.4}, 2.93},
+                                 {32, 32, 4, 0.157, 0.353, {0.023, 0.048, 0.08, 0.169, 0.0, 0.15}, 2.90}};
+constexpr TileCfg F32_STAGED = {128, 128, 2, 2.258, 3.0, {-0.13, 3.88, 4.12, 6.15, 0.0, 0.0}, 5.12};
 constexpr int STAGED_MAX_K = 256;
 // A split over k: the second kernel's launch, every partial written and read
 // once, its epilogue as above, and per range.
@@ -529,17 +553,19 @@ int min_ranges(const GemmArgs& g, int esz, int epi) {
 }
 
 // The configuration and split count with the smallest predicted time.
-Choice choose(const GemmArgs& g, int esz, bool akc, bool bkc, int epi) {
+Choice choose(const GemmArgs& g, int esz, bool akc, bool bkc, int epi, double* us = nullptr) {
   const int quads = (g.K + 127) / 128, least = min_ranges(g, esz, epi);
   const double mn = static_cast<double>(g.M) * g.N;
   const SplitCost& sc = esz == 2 ? BF16_SPLIT : F32_SPLIT;
   // index into epi[], -1: to the element type
-  const int e = epi == EPI_STORE_F32 ? 0 : epi == EPI_ACC_F32 || epi == EPI_BIAS_RESID ? 1 : epi == EPI_BIAS_GELU ? 2
-              : epi == EPI_GELU_BWD ? 3 : -1;
+  const int e = epi == EPI_STORE_F32 || epi == EPI_SCALE_F32 ? 0
+                : epi == EPI_ACC_F32 || epi == EPI_BIAS_RESID || epi == EPI_SCALE_ACC || epi == EPI_SUM_SCALE ? 1
+                : epi == EPI_BIAS_GELU ? 2
+                : epi == EPI_GELU_BWD ? 3 : epi == EPI_LSE ? 4 : epi == EPI_DZ ? 5 : -1;
   Choice best{0, 0, 1, false};
   double best_t = 0.0;
   auto consider = [&](const TileCfg& c, bool staged) {
-    if (c.bm == 256 && c.bn < 256 && !gemm_main_combo(akc, bkc, epi)) return;
+    if (c.bm == 256 && c.bn < 256 && !gemm_main_combo(akc, bkc, epi) && !gemm_loss_combo(akc, bkc, epi)) return;
     const int64_t tiles = static_cast<int64_t>((g.M + c.bm - 1) / c.bm) * ((g.N + c.bn - 1) / c.bn);
     for (int want = 1; want <= (staged ? 1 : MAX_SPLITS); ++want) {
       const int per = (quads + want - 1) / want, splits = (quads + per - 1) / per;
@@ -566,6 +592,7 @@ Choice choose(const GemmArgs& g, int esz, bool akc, bool bkc, int epi) {
     for (const auto& c : F32_TILES) consider(c, false);
     if (g.K <= STAGED_MAX_K) consider(F32_STAGED, true);
   }
+  if (us) *us = best_t;
   return best;
 }
 
@@ -610,6 +637,26 @@ bool stream_result(const GemmArgs& g, int epi, int splits) {
 }
 
 template <typename T>
+hipError_t launch_tile(const GemmArgs& g, const Choice& c, bool akc, bool bkc, int epi, hipStream_t s) {
+  if (epi >= EPI_LSE) {
+    if constexpr (sizeof(T) == 4)
+      return c.bm == 64 ? gemm_loss_f32_64(g, akc, bkc, epi, s) : gemm_loss_f32_32(g, akc, bkc, epi, s);
+    return c.bm == 64    ? gemm_loss_64(g, akc, bkc, epi, s)
+           : c.bm == 128 ? gemm_loss_128(g, akc, bkc, epi, s)
+           : c.bn == 128 ? gemm_loss_256x128(g, akc, bkc, epi, s)
+           : c.bn == 192 ? gemm_loss_192(g, akc, bkc, epi, s)
+                         : gemm_loss_256(g, akc, bkc, epi, s);
+  }
+  if constexpr (sizeof(T) == 4)
+    return c.bm == 64 ? gemm_dl_f32_64(g, akc, bkc, epi, s) : gemm_dl_f32_32(g, akc, bkc, epi, s);
+  return c.bm == 64    ? gemm_dl_64(g, akc, bkc, epi, s)
+         : c.bm == 128 ? gemm_dl_128(g, akc, bkc, epi, s)
+         : c.bn == 128 ? gemm_dl_256x128(g, akc, bkc, epi, s)
+         : c.bn == 192 ? gemm_dl_192(g, akc, bkc, epi, s)
+                       : gemm_dl_256(g, akc, bkc, epi, s);
+}
+
+template <typename T>
 hipError_t launch_dl(GemmArgs g, const Choice& c, bool akc, bool bkc, int epi, hipStream_t s) {
   const int quads = (g.K + 127) / 128;
   g.kquads = (quads + c.splits - 1) / c.splits;
@@ -621,15 +668,7 @@ hipError_t launch_dl(GemmArgs g, const Choice& c, bool akc, bool bkc, int epi, h
     k.C = g.ws;
     k.ldc = g.N;
   }
-  hipError_t e;
-  if constexpr (sizeof(T) == 4)
-    e = c.bm == 64 ? gemm_dl_f32_64(k, akc, bkc, kepi, s) : gemm_dl_f32_32(k, akc, bkc, kepi, s);
-  else
-    e = c.bm == 64    ? gemm_dl_64(k, akc, bkc, kepi, s)
-        : c.bm == 128 ? gemm_dl_128(k, akc, bkc, kepi, s)
-        : c.bn == 128 ? gemm_dl_256x128(k, akc, bkc, kepi, s)
-        : c.bn == 192 ? gemm_dl_192(k, akc, bkc, kepi, s)
-                      : gemm_dl_256(k, akc, bkc, kepi, s);
+  const hipError_t e = launch_tile<T>(k, c, akc, bkc, kepi, s);
   if (e != hipSuccess || g.splits == 1) return e;
   return launch_reduce<T>(g, epi, g.splits, s);
 }
@@ -641,6 +680,18 @@ hipError_t launch_t(const GemmArgs& g, int epi, hipStream_t s) {
   if constexpr (sizeof(T) == 2)
     if (c.bm == 256) return launch_cfg<T, AKC, BKC, Big>(g, epi, 1, s);
   return launch_cfg<T, AKC, BKC, Small>(g, epi, c.splits, s);
+}
+
+// The loss products run on the direct-load kernel alone.
+Choice choose_loss(const GemmArgs& g, int esz, bool akc, bool bkc, int epi, double* us = nullptr) {
+  GemmArgs one = g;
+  if (epi == EPI_LSE || epi == EPI_DZ) one.ws = nullptr;  // their epilogues need whole sums
+  Choice c = choose(one, esz, akc, bkc, epi, us);
+  if (c.staged) {  // fp32 of a short k: 64 x 64 tiles where they fill the chip
+    const int64_t tiles = static_cast<int64_t>((g.M + 63) / 64) * ((g.N + 63) / 64);
+    c = tiles >= 2 * CUS ? Choice{64, 64, 1, false} : Choice{32, 32, 1, false};
+  }
+  return c;
 }
 
 }  // namespace
@@ -681,6 +732,35 @@ hipError_t gemm(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi, hipSt
   return launch_t<float, false, true>(g, epi, s);
 }
 
+hipError_t gemm_loss(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi, hipStream_t s) {
+  const int esz = dtype == DT_BF16 ? 2 : 4, e = 16 / esz;
+  if (!(gemm_loss_combo(akc, bkc, epi) || (epi == EPI_STORE_F32 && akc && !bkc))) return hipErrorInvalidValue;
+  // whole chunks in memory: leading dimensions, k of two k-contiguous operands
+  // (each is read in full chunks), columns of a not k-contiguous B
+  if (g.M <= 0 || g.N <= 0 || g.K <= 0 || g.lda % e || g.ldb % e || g.ldc % 4) return hipErrorInvalidValue;
+  if (bkc ? g.K % e : g.N % e) return hipErrorInvalidValue;
+  const int64_t kpad = (g.K + e - 1) / e * e, mpad = (g.M + e - 1) / e * e;
+  if (akc ? g.lda < kpad : g.lda < mpad) return hipErrorInvalidValue;
+  if (bkc ? g.ldb < g.K : g.ldb < g.N) return hipErrorInvalidValue;
+  if ((reinterpret_cast<uintptr_t>(g.A) | reinterpret_cast<uintptr_t>(g.B) | reinterpret_cast<uintptr_t>(g.C)) & 15)
+    return hipErrorInvalidValue;
+  if (epi == EPI_SUM_SCALE && g.ldaux % 4) return hipErrorInvalidValue;
+  const Choice c = choose_loss(g, esz, akc, bkc, epi);
+  return dtype == DT_BF16 ? launch_dl<bf16_t>(g, c, akc, bkc, epi, s) : launch_dl<float>(g, c, akc, bkc, epi, s);
+}
+
+double gemm_loss_us(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi) {
+  double us = 0.0;
+  choose_loss(g, dtype == DT_BF16 ? 2 : 4, akc, bkc, epi, &us);
+  return us;
+}
+
+int gemm_lse_width(int dtype, int M, int N, int K) {
+  GemmArgs g{};
+  g.M = M, g.N = N, g.K = K;
+  return choose_loss(g, dtype == DT_BF16 ? 2 : 4, true, true, EPI_LSE).bn / 2;
+}
+
 }  // namespace atom
 
 // What a product with contiguous operands and rows runs as (tests).
@@ -693,7 +773,9 @@ extern "C" void atom_gemm_choice(int dtype, int akc, int bkc, int epi, int M, in
   float some;
   g.ws = ws_bytes ? &some : nullptr;
   g.ws_bytes = ws_bytes;
-  const Choice c = choice_of(g, dtype == DT_BF16 ? 2 : 4, akc != 0, bkc != 0, epi);
+  const int esz = dtype == DT_BF16 ? 2 : 4;
+  const Choice c = epi >= EPI_LSE ? choose_loss(g, esz, akc != 0, bkc != 0, epi)
+                                  : choice_of(g, esz, akc != 0, bkc != 0, epi);
   out[0] = c.staged, out[1] = c.bm, out[2] = c.bn, out[3] = c.splits;
   out[4] = !c.staged && stream_result(g, epi, c.splits);
 }

@@ -24,8 +24,10 @@
 //     more, c ^ (2 ((k >> 1) & 1) + 4 ((k >> 3) & 1)) for rows of 8.  fp32:
 //     fragments by ds_read_b32, chunk c at c ^ (4 ((k >> 3) & 3)) (16 chunks)
 //     or c ^ (4 ((k >> 3) & 1)) (8 chunks).
-// Rows past the operand are clamped to its last valid row (or chunk of rows):
-// they only reach output rows or columns that are never stored.  k past the
+// Rows past the operand are clamped to its last valid row (or chunk of rows;
+// the last chunk of a not k-contiguous A may hold rows past M, which
+// gemm_loss allows): they only reach output rows or columns that are never
+// stored.  k past the
 // end reads 16 bytes of zeros instead, in both operands, so any k whose
 // chunks are whole works; the loop runs whole groups of four k tiles, then the
 // one to three that are left.
@@ -163,7 +165,8 @@ __device__ __forceinline__ void mfma_agpr(f32x4_t& acc, const Frag<bf16_t>& a, c
 
 template <int EPI>
 constexpr bool epi_reads_elem() {
-  return EPI == EPI_ACC_F32 || EPI == EPI_BIAS_RESID || EPI == EPI_GELU_BWD;
+  return EPI == EPI_ACC_F32 || EPI == EPI_BIAS_RESID || EPI == EPI_GELU_BWD || EPI == EPI_SCALE_ACC ||
+         EPI == EPI_SUM_SCALE;
 }
 template <int EPI>
 constexpr bool epi_has_bias() {
@@ -239,7 +242,7 @@ gemm_dl_kernel(GemmArgs g) {
   typename OA::Src sra[OA::LPT];
   typename OB::Src srb[OB::LPT];
 #pragma unroll
-  for (int q = 0; q < OA::LPT; ++q) sra[q].init(static_cast<const T*>(g.A), g.lda, m0, g.M, q * NT + tid);
+  for (int q = 0; q < OA::LPT; ++q) sra[q].init(static_cast<const T*>(g.A), g.lda, m0, AKC ? g.M : (g.M + OA::E - 1) / OA::E * OA::E, q * NT + tid);
 #pragma unroll
   for (int q = 0; q < OB::LPT; ++q) srb[q].init(static_cast<const T*>(g.B), g.ldb, n0, g.N, q * NT + tid);
   // k tiles of this workgroup: kquads groups of four per split, the rest in
@@ -383,6 +386,76 @@ gemm_dl_kernel(GemmArgs g) {
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = tot[i][j] + (acc[i][j] + acc2[i][j]);
   }
+  const int row0 = m0 + wm * TM * 16, col0 = n0 + wn * TN * 16;
+  // acc[i][j][r] is the logit of row row0 + 16 i + lr, column col0 + 16 j +
+  // 4 lg + r: the loss epilogues' row values are per lane and i.
+  constexpr bool LOSS = EPI == EPI_LSE || EPI == EPI_DZ;
+  constexpr float LOG2E = 1.4426950408889634f;
+  int trow[LOSS ? TM : 1];  // target column in this wave's block, or outside [0, 16 TN)
+  if constexpr (LOSS) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m = row0 + 16 * i + lr;
+      trow[i] = m < g.M ? g.tgt[m] : -1;
+    }
+  }
+  if constexpr (EPI == EPI_LSE) {
+    // One pass over the logits in registers: a lane's 4 TN values of a row,
+    // then the four lanes that share the row.  The exponentials (16 TM TN of a
+    // quarter-rate instruction per lane) are what this epilogue costs.
+    float2* part = static_cast<float2*>(g.C) + static_cast<int64_t>(pid_n * 2 + wn) * g.M;
+    const bool edge = col0 + TN * 16 > g.N;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m = row0 + 16 * i + lr;
+      const int t = trow[i] < 0 || trow[i] >= g.N ? -1 : trow[i] - col0;
+      const bool hit = t >= 0 && t < TN * 16 && (t >> 2 & 3) == lg;
+      if (__builtin_amdgcn_ballot_w64(hit) != 0) {
+        float z = 0.f;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) z = t == 16 * j + 4 * lg + r ? acc[i][j][r] : z;
+        if (hit) g.ztgt[m] = z;
+      }
+      float mx = -INFINITY;
+      if (edge) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (col0 + 16 * j + 4 * lg + r >= g.N) acc[i][j][r] = -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, acc[i][j][r]);
+      mx = rows4_max(mx) * LOG2E;
+      const float ref = mx == -INFINITY ? 0.f : mx;  // no column of the row in this block
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        float e[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e[r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -ref));
+        sum += (e[0] + e[1]) + (e[2] + e[3]);
+      }
+      sum = rows4_sum(sum);
+      if (lg == 0 && m < g.M) part[m] = make_float2(mx, sum);
+    }
+    return;
+  }
+  float lrow[EPI == EPI_DZ ? TM : 1], srow[EPI == EPI_DZ ? TM : 1];
+  if constexpr (EPI == EPI_DZ) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m = row0 + 16 * i + lr;
+      const bool on = m < g.M && trow[i] >= 0;
+      lrow[i] = on ? g.lse[m] * LOG2E : 0.f;
+      srow[i] = !on ? 0.f : trow[i] >= g.V ? NAN : g.rowscale ? g.rowscale[m] : 1.f;
+      trow[i] -= g.v0 + col0;
+    }
+  }
   // Epilogue through LDS, RB rows of the wave's block at a time: the
   // accumulators go to a wave-private [RB][BN/2] fp32 staging area, and each
   // lane takes back 4 consecutive columns of one row, so a wave's stores (and
@@ -390,7 +463,6 @@ gemm_dl_kernel(GemmArgs g) {
   // whole rows of the block instead of 32-byte pieces of 16 rows.
   barrier_after_reads();  // every wave is done with the stages
   float* stg = reinterpret_cast<float*>(lds) + w * (RB * PITCH);
-  const int row0 = m0 + wm * TM * 16, col0 = n0 + wn * TN * 16;
   // N, ldc and ldaux are multiples of 4 (the launcher checks): a lane's four
   // columns are all inside the matrix or all past it, and every access is one
   // 4-vector.  They are the same columns in every row the lane stores, so the
@@ -399,7 +471,9 @@ gemm_dl_kernel(GemmArgs g) {
   // lanes per row the rest of the wave idles).
   constexpr int LPR = TN * 4, RPP = LPR > 16 ? 2 : 64 / LPR, NQ = RB / RPP, NB = TM * 16 / RB;
   const int cc = 4 * (lane % LPR), nb = col0 + cc, rsub = lane / LPR;
-  const bool col_ok = nb < g.N && rsub < RPP;
+  // (the gradient of the logits: N is any number, and the columns up to the next
+  // chunk, which the products read, are stored as zeros)
+  const bool col_ok = nb < (EPI == EPI_DZ ? (g.N + OA::E - 1) / OA::E * OA::E : g.N) && rsub < RPP;
   const int rsub0 = LPR * RPP == 64 ? rsub : min(rsub, RPP - 1);
   float bv[4] = {0.f, 0.f, 0.f, 0.f};
   if constexpr (epi_has_bias<EPI>())
@@ -415,7 +489,8 @@ gemm_dl_kernel(GemmArgs g) {
   auto epilogue = [&](auto GUARD_, const GemmArgs& ga) {
     constexpr bool GUARD = decltype(GUARD_)::value;
     constexpr int E = EPI;
-    constexpr bool F32_OUT = E == EPI_STORE_F32 || E == EPI_ACC_F32 || E == EPI_BIAS_RESID;
+    constexpr bool F32_OUT = E == EPI_STORE_F32 || E == EPI_ACC_F32 || E == EPI_BIAS_RESID || E == EPI_SCALE_F32 ||
+                             E == EPI_SCALE_ACC;
     constexpr bool ELEM = epi_reads_elem<E>();
     constexpr bool AUX16 = E == EPI_GELU_BWD && sizeof(T) == 2;
     constexpr int AHEAD = std::min(AUX16 ? 2 : 1, NB - 1);
@@ -431,8 +506,10 @@ gemm_dl_kernel(GemmArgs g) {
           if constexpr (E == EPI_GELU_BWD)
             xr[h][q] = *reinterpret_cast<const Raw*>(static_cast<const T*>(ga.aux) +
                                                      static_cast<int64_t>(mq + RPP * q) * ga.ldaux + nb);
+          else if constexpr (E == EPI_SUM_SCALE)
+            xr[h][q] = *reinterpret_cast<const Raw*>(ga.resid + static_cast<int64_t>(mq + RPP * q) * ga.ldaux + nb);
           else
-            xr[h][q] = *reinterpret_cast<const Raw*>((E == EPI_ACC_F32 ? static_cast<const float*>(ga.C) : ga.resid) +
+            xr[h][q] = *reinterpret_cast<const Raw*>((E == EPI_ACC_F32 || E == EPI_SCALE_ACC ? static_cast<const float*>(ga.C) : ga.resid) +
                                                      static_cast<int64_t>(mq + RPP * q) * ga.ldc + nb);
         }
       }
@@ -451,7 +528,18 @@ gemm_dl_kernel(GemmArgs g) {
       for (int ii = 0; ii < RB / 16; ++ii)
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-          const f32x4_t& a = acc[h * (RB / 16) + ii][j];
+          f32x4_t& a = acc[h * (RB / 16) + ii][j];
+          if constexpr (E == EPI_DZ) {
+            // (softmax - onehot) * scale; a row of scale zero takes no part,
+            // whatever its logits hold
+            const int i = h * (RB / 16) + ii, c = 16 * j + 4 * lg;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float p = __builtin_amdgcn_exp2f(fmaf(a[r], LOG2E, -lrow[i]));
+              p = (p - (trow[i] == c + r ? 1.f : 0.f)) * srow[i];
+              a[r] = srow[i] == 0.f || (GUARD && col0 + c + r >= ga.N) ? 0.f : p;
+            }
+          }
           *reinterpret_cast<float4*>(stg + (ii * 16 + lr) * PITCH + j * 16 + lg * 4) = make_float4(a[0], a[1], a[2], a[3]);
         }
       float4 sv[NQ];
@@ -488,6 +576,12 @@ gemm_dl_kernel(GemmArgs g) {
           for (int r = 0; r < 4; ++r) v[r] = xe[r] + (v[r] + bv[r]);
         } else if constexpr (E == EPI_GELU_BWD) {
           for (int r = 0; r < 4; ++r) v[r] *= gelu_grad_f(xe[r]);
+        } else if constexpr (E == EPI_SCALE || E == EPI_SCALE_F32) {
+          for (int r = 0; r < 4; ++r) v[r] *= ga.alpha;
+        } else if constexpr (E == EPI_SCALE_ACC) {
+          for (int r = 0; r < 4; ++r) v[r] = fmaf(ga.alpha, v[r], xe[r]);
+        } else if constexpr (E == EPI_SUM_SCALE) {
+          for (int r = 0; r < 4; ++r) v[r] = ga.alpha * (xe[r] + v[r]);
         }
         if constexpr (E == EPI_STORE_F32) {
           if (g.stream) stream4(static_cast<float*>(ga.C) + off, v);
@@ -543,6 +637,34 @@ hipError_t launch(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s)
   ATOM_DL_LAYOUT(false, false)
   ATOM_DL_LAYOUT(false, true)
 #undef ATOM_DL_LAYOUT
+#undef ATOM_DL
+  return hipErrorInvalidValue;
+}
+
+// The same for the loss epilogues.
+template <typename T, int BM, int BN>
+hipError_t launch_loss(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s) {
+  const int tiles = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
+  const dim3 grid(static_cast<unsigned>(tiles * g.splits)), block(NT);
+  const bool tail = g.K % (4 * BK) != 0;
+#define ATOM_DL(AK, BK_, E)                                                                        \
+  if (akc == AK && bkc == BK_ && epi == E) {                                                       \
+    if constexpr (sizeof(T) == 2)                                                                  \
+      if (!tail) {                                                                                 \
+        hipLaunchKernelGGL((gemm_dl_kernel<T, AK, BK_, E, BM, BN, false>), grid, block, 0, s, g);  \
+        return hipGetLastError();                                                                  \
+      }                                                                                            \
+    hipLaunchKernelGGL((gemm_dl_kernel<T, AK, BK_, E, BM, BN, true>), grid, block, 0, s, g);       \
+    return hipGetLastError();                                                                      \
+  }
+  ATOM_DL(true, true, EPI_LSE)
+  ATOM_DL(true, true, EPI_DZ)
+  ATOM_DL(true, false, EPI_SCALE)
+  ATOM_DL(true, false, EPI_SCALE_ACC)
+  ATOM_DL(true, false, EPI_SUM_SCALE)
+  ATOM_DL(false, false, EPI_SCALE)
+  ATOM_DL(false, false, EPI_SCALE_F32)
+  ATOM_DL(false, false, EPI_SCALE_ACC)
 #undef ATOM_DL
   return hipErrorInvalidValue;
 }

@@ -1,0 +1,10 @@
+// gemm_dl instantiations with the loss epilogues: 128x128 tiles.
+#include "gemm_dl.h"
+
+namespace atom {
+
+hipError_t gemm_loss_128(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s) {
+  return dl::launch_loss<bf16_t, 128, 128>(g, akc, bkc, epi, s);
+}
+
+}  // namespace atom

@@ -1,0 +1,10 @@
+// gemm_dl instantiations with the loss epilogues: 256x256 tiles.
+#include "gemm_dl.h"
+
+namespace atom {
+
+hipError_t gemm_loss_256(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s) {
+  return dl::launch_loss<bf16_t, 256, 256>(g, akc, bkc, epi, s);
+}
+
+}  // namespace atom

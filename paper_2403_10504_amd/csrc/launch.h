@@ -17,6 +17,13 @@ enum Epilogue {
   EPI_BIAS_GELU = 4,   // aux = acc + bias[n]; C = GELU(aux)
   EPI_BIAS_RESID = 5,  // C = resid + (acc + bias[n])      (fp32)
   EPI_GELU_BWD = 6,    // C = acc * GELU'(aux)             (element type)
+  // the linear head's loss (loss.hip); not reachable through atom_k_gemm
+  EPI_LSE = 7,         // per row and half tile: max and sum of exponentials of acc
+  EPI_DZ = 8,          // C = (exp(acc - lse[m]) - [target]) * rowscale[m]  (element type)
+  EPI_SCALE = 9,       // C = alpha * acc                  (element type)
+  EPI_SCALE_F32 = 10,  // C = alpha * acc                  (fp32)
+  EPI_SCALE_ACC = 11,  // C += alpha * acc                 (fp32)
+  EPI_SUM_SCALE = 12,  // C = alpha * (resid + acc)        (element type; resid fp32)
 };
 
 struct GemmArgs {
@@ -32,6 +39,13 @@ struct GemmArgs {
   uint64_t ws_bytes;  // its size; a split needs splits * M * N * 4 bytes
   int splits, kquads; // set by the launcher: k ranges and the groups of 128 k of each
   bool stream;        // set by the launcher: fp32 results are stored past the caches
+  // the loss epilogues
+  float alpha;            // EPI_SCALE*, EPI_SUM_SCALE
+  const int32_t* tgt;     // EPI_LSE, EPI_DZ: target column of each row, negative: none
+  const float* lse;       // EPI_DZ: natural log-sum-exp of each row
+  const float* rowscale;  // EPI_DZ: factor of each row, null: 1
+  float* ztgt;            // EPI_LSE: receives acc at each row's target
+  int v0, V;              // EPI_DZ: column 0 is column v0 of the V of the vocabulary
 };
 
 // The layout and epilogue combinations of the training step: forward, data
@@ -40,6 +54,14 @@ constexpr bool gemm_main_combo(bool akc, bool bkc, int epi) {
   if (akc && bkc) return epi != EPI_ACC_F32 && epi != EPI_GELU_BWD;
   if (akc) return epi == EPI_STORE || epi == EPI_STORE_F32 || epi == EPI_GELU_BWD;
   return !bkc && (epi == EPI_STORE || epi == EPI_STORE_F32 || epi == EPI_ACC_F32);
+}
+
+// Those of the linear head's loss: logits, then both gradients.
+constexpr bool gemm_loss_combo(bool akc, bool bkc, int epi) {
+  if (epi == EPI_LSE || epi == EPI_DZ) return akc && bkc;
+  if (epi == EPI_SCALE || epi == EPI_SCALE_ACC) return !bkc;
+  if (epi == EPI_SCALE_F32) return !akc && !bkc;
+  return epi == EPI_SUM_SCALE && akc && !bkc;
 }
 
 // Tile configurations of the direct-load kernel (gemm_dl.h); 256x192 and
@@ -52,8 +74,27 @@ hipError_t gemm_dl_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_
 hipError_t gemm_dl_f32_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 hipError_t gemm_dl_f32_32(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 
+// The same tiles with the loss epilogues (gemm_loss_combo).
+hipError_t gemm_loss_256(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_loss_192(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_loss_256x128(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_loss_128(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_loss_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_loss_f32_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_loss_f32_32(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+
 hipError_t gemm_check(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig);
 hipError_t gemm(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, int epi, hipStream_t s);
+// The products of the linear head's loss: the epilogues of gemm_loss_combo, and
+// EPI_STORE_F32 with A k-contiguous and B not.  Unlike gemm(),
+// M and K may be any length where the memory of A holds whole chunks: rows of a
+// not k-contiguous A up to the next chunk may be read (they reach no output),
+// and a k-contiguous A holds zeros from K to the next chunk.
+hipError_t gemm_loss(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, int epi, hipStream_t s);
+// Its predicted time in us (the tile choice's model), at M, N, K and ws_bytes of g.
+double gemm_loss_us(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, int epi);
+// Columns of the part of a row that EPI_LSE reduces to one maximum and sum.
+int gemm_lse_width(int dtype, int M, int N, int K);
 
 // LayerNorm over rows of length d (d % 64 == 0, d <= 8192).
 //   y = (x - mean) * rstd * gamma + beta, x fp32, y element type.
@@ -118,6 +159,17 @@ hipError_t copy_words(const uint32_t* src, uint32_t* dst, int64_t n, hipStream_t
 // Makes device memory written by a DMA engine (after the host saw the copy
 // complete) visible to the kernels enqueued after it on stream s.
 hipError_t dma_acquire(hipStream_t s);
+
+// Loss of a linear head and its gradients (atom_k_linear_xent_*); false where
+// the sizes are refused.
+bool linear_xent_ok(int dtype, int64_t rows, int V, int d);
+uint64_t linear_xent_fwd_ws(int dtype, int64_t rows, int V, int d);
+hipError_t linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
+                           float* lse, float* loss_rows, int64_t rows, int V, int d, void* ws, hipStream_t s);
+uint64_t linear_xent_bwd_ws(int dtype, int64_t rows, int V, int d, int piece);
+hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
+                           const float* lse, const float* drow, float scale, void* dx, int64_t lddx, void* dw,
+                           int64_t lddw, int dw_epi, int64_t rows, int V, int d, int piece, void* ws, hipStream_t s);
 
 // Causal attention on a fused qkv [B*T][3*d] (element type), heads of dh in
 // {64, 128}.  o [B*T][d], lse [B][H][T] fp32 (natural log).

@@ -1,0 +1,278 @@
+// Cross-entropy of a linear head, and its gradients, without the logits in
+// memory (atom_k_linear_xent_fwd, atom_k_linear_xent_bwd).
+//
+//   z = x W^T,  lse_n = log sum_v exp z_nv,  loss_n = lse_n - z_n[t_n]
+//   dz_nv = (exp(z_nv - lse_n) - [v = t_n]) drow_n,  dx = scale dz W,
+//   dW = scale dz^T x
+//
+// Forward: one product whose epilogue (EPI_LSE, gemm_dl.h) turns the logits of
+// a wave's block, still in the accumulators, into a maximum and a sum of
+// exponentials per row, and keeps the logit at the row's target; a second
+// kernel joins a row's parts in their order.  Memory: x and W read, 8 bytes per
+// token and part written and read.
+// Backward: pieces of the vocabulary.  Per piece the logits are computed again,
+// become dz in the epilogue (EPI_DZ) and go to the workspace in the element
+// type, and two products read them: dx gains dz W (fp32 between pieces), and the
+// piece's rows of dW = dz^T x are done.  A piece of dz that fits the 256 MB
+// Infinity Cache is read from there.
+//
+// dz is held without `scale`, which multiplies the fp32 sums: the usual scale
+// 1 / tokens is no power of two, and rounding -scale at the target would put a
+// bf16 rounding error into every row's largest term, where -1 + p with a small
+// p has next to none (2.4e-3 -> 1.7e-3 relative, the rounding of the result).
+#include <algorithm>
+
+#include "common.h"
+#include "launch.h"
+
+namespace atom {
+namespace {
+
+constexpr float LN2 = 0.6931471805599453f;
+
+// RPB rows per workgroup, 256 / RPB threads per row, each over every
+// (256 / RPB)-th part; the threads' (max, sum) pairs join in LDS in a fixed
+// order.  16 rows read 128 bytes of a part's row; few rows take a workgroup each.
+template <int RPB>
+__global__ void __launch_bounds__(256) lse_join_kernel(const float2* __restrict__ part, int64_t rows, int parts,
+                                                       const int32_t* __restrict__ tgt,
+                                                       const float* __restrict__ ztgt, int V,
+                                                       float* __restrict__ lse, float* __restrict__ loss_rows) {
+  constexpr int TPR = 256 / RPB;
+  __shared__ float2 red[TPR][RPB];
+  const int r = threadIdx.x % RPB, s = threadIdx.x / RPB;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * RPB + r;
+  float m = -INFINITY, sum = 0.f;
+  if (row < rows) {
+#pragma unroll 4
+    for (int p = s; p < parts; p += TPR) {
+      const float2 v = part[static_cast<int64_t>(p) * rows + row];
+      const float n = fmaxf(m, v.x);
+      const float ref = n == -INFINITY ? 0.f : n;
+      sum = sum * __builtin_amdgcn_exp2f(m - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
+      m = n;
+    }
+  }
+  red[s][r] = make_float2(m, sum);
+  __syncthreads();
+#pragma unroll
+  for (int h = TPR / 2; h > 0; h >>= 1) {
+    if (s < h) {
+      const float2 a = red[s][r], b = red[s + h][r];
+      const float n = fmaxf(a.x, b.x);
+      const float ref = n == -INFINITY ? 0.f : n;
+      red[s][r] = make_float2(n, a.y * __builtin_amdgcn_exp2f(a.x - ref) + b.y * __builtin_amdgcn_exp2f(b.x - ref));
+    }
+    __syncthreads();
+  }
+  if (s == 0 && row < rows) {
+    const int t = tgt[row];
+    float l = 0.f, loss = 0.f;
+    if (t >= 0) {
+      l = (red[0][r].x + log2f(red[0][r].y)) * LN2;
+      loss = t < V ? l - ztgt[row] : NAN;
+    }
+    lse[row] = l;
+    loss_rows[row] = loss;
+  }
+}
+
+// x with the rows of tokens that take no part set to zero, so that whatever
+// they hold (dz is zero there, and 0 * NaN is not) stays out of dW.
+__global__ void __launch_bounds__(256) keep_rows_kernel(const uint4* __restrict__ x, int64_t ldc, int cpr,
+                                                        const int32_t* __restrict__ tgt,
+                                                        const float* __restrict__ drow, int64_t n,
+                                                        uint4* __restrict__ y) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t row = i / cpr;
+    const bool on = tgt[row] >= 0 && !(drow && drow[row] == 0.f);
+    y[i] = on ? x[row * ldc + (i - row * cpr)] : make_uint4(0, 0, 0, 0);
+  }
+}
+
+__global__ void __launch_bounds__(256) zero_rows_kernel(uint32_t* __restrict__ y, int64_t ldw, int wpr, int64_t n) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256)
+    y[i / wpr * ldw + i % wpr] = 0;
+}
+
+inline uint64_t up(uint64_t n) { return (n + 255) & ~255ull; }
+inline unsigned blocks(int64_t n) { return static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 4096)); }
+inline int esize(int dtype) { return dtype == DT_BF16 ? 2 : 4; }
+inline int64_t lse_parts(int dtype, int64_t rows, int V, int d) {
+  const int width = gemm_lse_width(dtype, static_cast<int>(rows), V, d);
+  return (V + 2 * width - 1) / (2 * width) * 2;
+}
+
+// Workspace for few rows: ranges of the vocabulary summed apart (dx), up to 16.
+uint64_t split_bytes(int64_t rows, int d) { return std::min<uint64_t>(up(16ull * rows * d * 4), 32ull << 20); }
+
+// Rows of dz start an odd number of 256-byte lines apart: pieces are multiples
+// of 4 KB or more, and rows that far apart crowd a few memory channels.
+int ld_of_dz(int dtype, int piece) {
+  const int line = 256 / esize(dtype);
+  return ((piece + line - 1) / line | 1) * line;
+}
+
+struct BwdWs {
+  uint64_t dz, x, dx, split, split_bytes, end;  // offsets
+};
+BwdWs bwd_ws(int dtype, int64_t rows, int V, int d, int piece) {
+  const uint64_t e = esize(dtype), n = rows;
+  const int ldz = ld_of_dz(dtype, piece);
+  BwdWs w;
+  w.dz = 0;
+  w.x = w.dz + up(n * ldz * e);
+  w.dx = w.x + up(n * d * e);
+  w.split = w.dx + (dtype == DT_BF16 && piece < V ? up(n * d * 4) : 0);
+  w.split_bytes = split_bytes(rows, d);
+  w.end = w.split + w.split_bytes;
+  return w;
+}
+
+// Predicted time of both gradients in pieces of `width` columns.
+double bwd_us(int dtype, int64_t rows, int V, int d, int width) {
+  GemmArgs z{}, dx{}, dw{};
+  float some;
+  z.M = dx.M = dw.K = static_cast<int>(rows);
+  z.K = dx.N = dw.N = d;
+  dx.ws = dw.ws = &some;
+  dx.ws_bytes = dw.ws_bytes = split_bytes(rows, d);
+  auto piece = [&](int n, int epi) {
+    z.N = dx.K = dw.M = n;
+    return gemm_loss_us(z, dtype, true, true, EPI_DZ) + gemm_loss_us(dx, dtype, true, false, epi) +
+           gemm_loss_us(dw, dtype, false, false, EPI_SCALE);
+  };
+  const int whole = V / width, rest = V % width;
+  return whole * piece(width, EPI_SCALE_ACC) + (rest ? piece(rest, EPI_SUM_SCALE) : 0.0);
+}
+
+// Columns of a piece: the caller's, or by default the whole vocabulary where dz
+// of it takes at most 128 MB, half of the Infinity Cache, through which the two
+// products read it; else the width within that (2048 at least) with the
+// smallest predicted time, of the vocabulary in equal parts and of multiples of
+// 4096.  What varies is how many rounds of tiles the three products take
+// (2048 x 5120, vocabulary 50257: 2991 us in pieces of 8192, with 640 tiles of
+// dW and 256 of z on 256 CUs).
+int piece_of(int dtype, int64_t rows, int V, int d, int piece) {
+  if (piece > 0) return static_cast<int>(std::min<int64_t>(V, (piece + 7ll) / 8 * 8));
+  const int64_t most = std::max<int64_t>(2048, (128ll << 20) / (rows * esize(dtype)));
+  if (V <= most) return V;
+  int best = 0;
+  double best_us = 0.0;
+  auto consider = [&](int64_t width) {
+    if (width > most || width < 1) return;
+    const double us = bwd_us(dtype, rows, V, d, static_cast<int>(width));
+    if (best == 0 || us < best_us) best = static_cast<int>(width), best_us = us;
+  };
+  consider(most / 256 * 256);
+  const int64_t n = (V + most - 1) / most;
+  for (int64_t k = n; k < n + 4; ++k) consider(((V + k - 1) / k + 255) / 256 * 256);
+  for (int64_t k = 1; k <= 4; ++k) consider(4096 * k);
+  return best;
+}
+
+}  // namespace
+
+// Tiles are counted in 32 bits, of 64 x 64 at least (bf16) or 32 x 32.
+bool linear_xent_ok(int dtype, int64_t rows, int V, int d) {
+  if (rows < 0 || rows > (1 << 30) || V <= 0 || V > (1 << 30) || d <= 0 || d % (dtype == DT_BF16 ? 8 : 4)) return false;
+  return ((rows + 31) / 32) * ((static_cast<int64_t>(V) + 31) / 32) < (1ll << 30) &&
+         ((static_cast<int64_t>(V) + 31) / 32) * ((static_cast<int64_t>(d) + 31) / 32) < (1ll << 30) &&
+         ((rows + 31) / 32) * ((static_cast<int64_t>(d) + 31) / 32) < (1ll << 30);
+}
+
+uint64_t linear_xent_fwd_ws(int dtype, int64_t rows, int V, int d) {
+  if (rows == 0) return 0;
+  return up(rows * sizeof(float)) + lse_parts(dtype, rows, V, d) * rows * sizeof(float2);
+}
+
+hipError_t linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
+                           float* lse, float* loss_rows, int64_t rows, int V, int d, void* ws, hipStream_t s) {
+  if (rows == 0) return hipSuccess;
+  const int64_t parts = lse_parts(dtype, rows, V, d);
+  GemmArgs g{};
+  g.A = x, g.lda = ldx, g.B = w, g.ldb = ldw;
+  g.M = static_cast<int>(rows), g.N = V, g.K = d;
+  g.ztgt = static_cast<float*>(ws);
+  g.C = static_cast<char*>(ws) + up(rows * sizeof(float));
+  g.tgt = tgt;
+  hipError_t e = gemm_loss(g, dtype, true, true, EPI_LSE, s);
+  if (e != hipSuccess) return e;
+  const float2* part = static_cast<const float2*>(g.C);
+  if (rows < 2048)
+    hipLaunchKernelGGL(lse_join_kernel<1>, dim3(static_cast<unsigned>(rows)), dim3(256), 0, s, part, rows,
+                       static_cast<int>(parts), tgt, g.ztgt, V, lse, loss_rows);
+  else
+    hipLaunchKernelGGL(lse_join_kernel<16>, dim3(static_cast<unsigned>((rows + 15) / 16)), dim3(256), 0, s, part, rows,
+                       static_cast<int>(parts), tgt, g.ztgt, V, lse, loss_rows);
+  return hipGetLastError();
+}
+
+uint64_t linear_xent_bwd_ws(int dtype, int64_t rows, int V, int d, int piece) {
+  return rows == 0 ? 0 : bwd_ws(dtype, rows, V, d, piece_of(dtype, rows, V, d, piece)).end;
+}
+
+hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
+                           const float* lse, const float* drow, float scale, void* dx, int64_t lddx, void* dw,
+                           int64_t lddw, int dw_epi, int64_t rows, int V, int d, int piece, void* ws, hipStream_t s) {
+  const int esz = esize(dtype);
+  const int wsz = dw_epi == EPI_SCALE ? esz : 4;  // bytes of an element of dw
+  if (rows == 0) {
+    if (!dw || dw_epi == EPI_SCALE_ACC) return hipSuccess;
+    const int wpr = d * wsz / 4;
+    const int64_t n = static_cast<int64_t>(V) * wpr;
+    hipLaunchKernelGGL(zero_rows_kernel, dim3(blocks(n)), dim3(256), 0, s, static_cast<uint32_t*>(dw), lddw * wsz / 4,
+                       wpr, n);
+    return hipGetLastError();
+  }
+  piece = piece_of(dtype, rows, V, d, piece);
+  const BwdWs o = bwd_ws(dtype, rows, V, d, piece);
+  char* base = static_cast<char*>(ws);
+  const int ldz = ld_of_dz(dtype, piece);
+  char* xz = base + o.x;
+  if (dw) {
+    const int cpr = d * esz / 16;
+    const int64_t n = rows * cpr;
+    hipLaunchKernelGGL(keep_rows_kernel, dim3(blocks(n)), dim3(256), 0, s, static_cast<const uint4*>(x),
+                       ldx * esz / 16, cpr, tgt, drow, n, reinterpret_cast<uint4*>(xz));
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  // the sum over the pieces: in dx itself (fp32), or beside it
+  float* sum = dtype == DT_BF16 ? reinterpret_cast<float*>(base + o.dx) : static_cast<float*>(dx);
+  const int64_t ldsum = dtype == DT_BF16 ? d : lddx;
+  for (int v0 = 0; v0 < V; v0 += piece) {
+    const int n = std::min(piece, V - v0);
+    const char* wp = static_cast<const char*>(w) + static_cast<int64_t>(v0) * ldw * esz;
+    GemmArgs g{};
+    g.A = x, g.lda = ldx, g.B = wp, g.ldb = ldw, g.C = base, g.ldc = ldz;
+    g.M = static_cast<int>(rows), g.N = n, g.K = d;
+    g.tgt = tgt, g.lse = lse, g.rowscale = drow, g.v0 = v0, g.V = V;
+    hipError_t e = gemm_loss(g, dtype, true, true, EPI_DZ, s);
+    if (e != hipSuccess) return e;
+    GemmArgs h{};
+    h.A = base, h.lda = ldz;
+    h.ws = reinterpret_cast<float*>(base + o.split), h.ws_bytes = o.split_bytes;
+    h.N = d, h.alpha = scale;
+    if (dx) {
+      const bool first = v0 == 0, last = v0 + n == V;
+      GemmArgs a = h;
+      a.B = wp, a.ldb = ldw, a.M = static_cast<int>(rows), a.K = n;
+      a.C = last ? dx : sum, a.ldc = last ? lddx : ldsum;
+      a.resid = sum, a.ldaux = ldsum;
+      if (!last) a.alpha = 1.f;
+      e = gemm_loss(a, dtype, true, false, last ? (first ? EPI_SCALE : EPI_SUM_SCALE) : first ? EPI_STORE_F32 : EPI_SCALE_ACC, s);
+      if (e != hipSuccess) return e;
+    }
+    if (dw) {
+      GemmArgs a = h;
+      a.B = xz, a.ldb = d, a.M = n, a.K = static_cast<int>(rows);
+      a.C = static_cast<char*>(dw) + static_cast<int64_t>(v0) * lddw * wsz, a.ldc = lddw;
+      e = gemm_loss(a, dtype, false, false, dw_epi, s);
+      if (e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+}  // namespace atom
