@@ -155,6 +155,36 @@ int atom_k_linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w,
 int atom_k_embed_fwd(int dtype, const int32_t* tok, const void* wte, const void* wpe, float* x, int64_t n_tok,
                      int T, int V, int d, void* stream);
 
+/* Orthogonalised update of a weight matrix by Newton-Schulz products (the
+ * Muon optimiser's step for the linear layers' weights), for `batch` matrices
+ * g [rows][ldg] in dtype, stride_g elements apart:
+ *   X = g / (|g|_F + 1e-7); for each step k, with A = X X^T,
+ *   X <- a_k X + (b_k A + c_k A A) X;  then, with O = scale * X,
+ *   out = O (ATOM_EPI_STORE: dtype; ATOM_EPI_STORE_F32: fp32), or
+ *   out = keep * out + O (ATOM_EPI_ACC_F32: fp32, the weights themselves with
+ *   scale = -lr * ... and keep = 1 - lr * decay).  `keep` is read by the last
+ *   form only.
+ * coef: HOST array [steps][3] of a, b, c, read before the call returns; NULL:
+ * the quintic (3.4445, -4.7750, 2.0315) in every step.  The products run on
+ * the shorter side: A = X^T X and X (...) where rows > cols.  A matrix of
+ * zeros gives zeros; one with an infinity or a NaN gives NaN throughout.
+ * bf16: products in fp16 with fp32 sums (X itself in 22 bits), off by about
+ * the result's own rounding; fp32: every factor in 22 bits.
+ * Any rows, cols >= 1 (with less than 2^30 tiles of 64 x 64), leading
+ * dimensions >= cols, 0 <= batch <= 65535 (0: nothing is done), 0 <= steps <=
+ * 64; stride_g >= 0; the outputs of a batch must not overlap: stride_o >=
+ * (rows - 1) * ldo + cols, or matrices side by side, cols <= stride_o with
+ * batch * stride_o <= ldo; any stride for one matrix.  g and out are aligned to
+ * their elements, ws to 16 bytes; out may be g itself (same type, ld and
+ * stride), else they must not overlap.  Steps whose polynomial takes singular
+ * values of [0, 1] beyond 4, or b t + c t^2 beyond 32 on the way, do not fit
+ * fp16: ATOM_EINVAL.  ws: as for atom_k_linear_xent_fwd. */
+#define ATOM_NS_MAX_STEPS 64
+uint64_t atom_k_orthogonalize_ws_bytes(int dtype, int batch, int rows, int cols);
+int atom_k_orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,
+                         int64_t stride_o, int out_epi, float keep, float scale, int batch, int rows, int cols,
+                         const float* coef, int steps, void* ws, uint64_t ws_bytes, void* stream);
+
 /* Plain device copy of `bytes` (a multiple of 16; both pointers 16-byte
  * aligned, not overlapping): reads and writes each byte once.  Measurement
  * only: its known traffic calibrates the HBM byte counters. */

@@ -140,6 +140,9 @@ _SIGS = {
     "atom_k_linear_xent_bwd": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, P, P, P, ctypes.c_float, P, I64, P, I64,
                                               ctypes.c_int, I64] + [ctypes.c_int] * 3 + [P, U64, P]),
     "atom_k_embed_fwd": (ctypes.c_int, [ctypes.c_int, P, P, P, P, I64, ctypes.c_int, ctypes.c_int, ctypes.c_int, P]),
+    "atom_k_orthogonalize_ws_bytes": (U64, [ctypes.c_int] * 4),
+    "atom_k_orthogonalize": (ctypes.c_int, [ctypes.c_int, P, I64, I64, P, I64, I64, ctypes.c_int, ctypes.c_float,
+                                            ctypes.c_float] + [ctypes.c_int] * 3 + [P, ctypes.c_int, P, U64, P]),
     "atom_k_copy": (ctypes.c_int, [P, P, I64, P]),
 }
 EXPORTED = tuple(_SIGS)
@@ -510,6 +513,28 @@ def atom_k_linear_xent_bwd(dtype, x, ldx, w, ldw, tgt, lse, drow, scale, dx, ldd
 
 def atom_k_embed_fwd(dtype, tok, wte, wpe, x, n_tok, T, V, d, stream=None):
     _kcall("atom_k_embed_fwd", dtype, tok, wte, wpe, x, n_tok, T, V, d, stream)
+
+
+ATOM_NS_MAX_STEPS = 64
+
+
+def atom_k_orthogonalize_ws_bytes(dtype, batch, rows, cols):
+    return lib().atom_k_orthogonalize_ws_bytes(dtype, batch, rows, cols)
+
+
+def atom_k_orthogonalize(dtype, g, ldg, stride_g, out, ldo, stride_o, out_epi, keep, scale, batch, rows, cols, coef, ws,
+                         ws_bytes, stream=None):
+    """coef: one (a, b, c) per step, or a number of steps of the default quintic."""
+    if isinstance(coef, int):
+        arr, steps = None, coef
+    else:
+        flat = [v for abc in coef for v in abc]
+        steps = len(coef)
+        if len(flat) != 3 * steps:
+            raise ValueError("coef must hold three numbers per step")
+        arr = (ctypes.c_float * len(flat))(*flat)
+    _kcall("atom_k_orthogonalize", dtype, g, ldg, stride_g, out, ldo, stride_o, out_epi, keep, scale, batch, rows, cols,
+           arr, steps, ws, ws_bytes, stream)
 
 
 def atom_k_copy(src, dst, nbytes, stream=None):

@@ -140,6 +140,32 @@ int atom_k_embed_fwd(int dtype, const int32_t* tok, const void* wte, const void*
   return st(embed_fwd(dtype, tok, wte, wpe, x, n_tok, T, V, d, S(stream)));
 }
 
+uint64_t atom_k_orthogonalize_ws_bytes(int dtype, int batch, int rows, int cols) {
+  return dt_ok(dtype) && batch > 0 && orthogonalize_ok(batch, rows, cols) ? orthogonalize_ws(dtype, batch, rows, cols) : 0;
+}
+
+int atom_k_orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,
+                         int64_t stride_o, int out_epi, float keep, float scale, int batch, int rows, int cols,
+                         const float* coef, int steps, void* ws, uint64_t ws_bytes, void* stream) {
+  if (!dt_ok(dtype) || !g || !out || !orthogonalize_ok(batch, rows, cols)) return ATOM_EINVAL;
+  if (ldg < cols || ldo < cols || stride_g < 0) return ATOM_EINVAL;
+  if (out_epi != ATOM_EPI_STORE && out_epi != ATOM_EPI_STORE_F32 && out_epi != ATOM_EPI_ACC_F32) return ATOM_EINVAL;
+  const uintptr_t esz = dtype == ATOM_BF16 ? 2 : 4, osz = out_epi == ATOM_EPI_STORE ? esz : 4;
+  if (reinterpret_cast<uintptr_t>(g) % esz || reinterpret_cast<uintptr_t>(out) % osz) return ATOM_EINVAL;
+  if (batch > 1 && stride_o < (rows - 1) * ldo + cols && !(stride_o >= cols && stride_o <= ldo / batch)) return ATOM_EINVAL;
+  if (steps < 0 || steps > ATOM_NS_MAX_STEPS) return ATOM_EINVAL;
+  float own[3 * ATOM_NS_MAX_STEPS];
+  if (!coef) {
+    for (int k = 0; k < steps; ++k) own[3 * k] = 3.4445f, own[3 * k + 1] = -4.7750f, own[3 * k + 2] = 2.0315f;
+    coef = own;
+  }
+  if (!orthogonalize_coef_ok(coef, steps)) return ATOM_EINVAL;
+  if (batch == 0) return ATOM_OK;
+  if (!ws || misaligned(ws) || ws_bytes < orthogonalize_ws(dtype, batch, rows, cols)) return ATOM_EINVAL;
+  return st(orthogonalize(dtype, g, ldg, stride_g, out, ldo, stride_o, out_epi, keep, scale, batch, rows, cols, coef,
+                          steps, ws, S(stream)));
+}
+
 int atom_k_copy(const void* src, void* dst, int64_t bytes, void* stream) {
   if (!src || !dst || bytes < 0 || bytes % 16) return ATOM_EINVAL;
   return st(copy_bytes(src, dst, bytes, S(stream)));

@@ -1,6 +1,6 @@
 // Device-side helpers shared by the CDNA4 (gfx950) kernels of libatom.
 //
-// Element types: activations and weights are either fp32 (validation mode) or
+// Element types (but for orthogonalize.hip): activations and weights are either fp32 (validation mode) or
 // bfloat16 stored as raw uint16 bit patterns.  Accumulation is always fp32.
 //
 // MFMA convention used by every kernel.  A 16x16 output tile is produced by
@@ -19,6 +19,9 @@
 #include <stdint.h>
 
 typedef uint16_t bf16_t;
+// IEEE half, the element type of the Newton-Schulz products (orthogonalize.hip).
+typedef _Float16 f16_t;
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
@@ -50,6 +53,7 @@ template <> ATOM_DEV bf16_t from_f<bf16_t>(float v) { return f2bf(v); }
 // A fragment: eight consecutive-k elements of one operand row for one lane.
 template <typename T> struct Frag;
 template <> struct Frag<bf16_t> { uint4 v; };
+template <> struct Frag<f16_t> { uint4 v; };
 template <> struct Frag<float> { float4 lo, hi; };
 
 // Load a fragment from 8 contiguous elements (16-byte aligned for bf16,
@@ -131,6 +135,10 @@ ATOM_DEV uint2 ds_read_tr8(const void* p) {
 ATOM_DEV void mfma16(f32x4_t& acc, const Frag<bf16_t>& a, const Frag<bf16_t>& b) {
   acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a.v),
                                                  __builtin_bit_cast(bf16x8_t, b.v), acc, 0, 0, 0);
+}
+ATOM_DEV void mfma16(f32x4_t& acc, const Frag<f16_t>& a, const Frag<f16_t>& b) {
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a.v), __builtin_bit_cast(f16x8_t, b.v), acc,
+                                                0, 0, 0);
 }
 ATOM_DEV void mfma16(f32x4_t& acc, const Frag<float>& a, const Frag<float>& b) {
   acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.lo.x, b.lo.x, acc, 0, 0, 0);

@@ -89,6 +89,10 @@ struct Operand {
       if constexpr (TAIL) s = kt * BK + k < K ? s : static_cast<const void*>(zero_chunk);
       lds_dma16(s, __builtin_amdgcn_readfirstlane(lds_offset(stage) + group * 1024));
     }
+    // the tile's chunk `off` elements on (another plane), k whole tiles
+    __device__ __forceinline__ void load_plane(uint8_t* stage, int kt, int64_t off, int group) const {
+      lds_dma16(p + off + kt * kstep, __builtin_amdgcn_readfirstlane(lds_offset(stage) + group * 1024));
+    }
   };
 
   // Byte offsets inside a stage of this lane's fragment of tile rows
@@ -163,6 +167,12 @@ __device__ __forceinline__ void mfma_agpr(f32x4_t& acc, const Frag<bf16_t>& a, c
                : "v"(__builtin_bit_cast(bf16x8_t, a.v)), "v"(__builtin_bit_cast(bf16x8_t, b.v)));
 }
 
+__device__ __forceinline__ void mfma_agpr(f32x4_t& acc, const Frag<f16_t>& a, const Frag<f16_t>& b) {
+  asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0"
+               : "+a"(acc)
+               : "v"(__builtin_bit_cast(f16x8_t, a.v)), "v"(__builtin_bit_cast(f16x8_t, b.v)));
+}
+
 template <int EPI>
 constexpr bool epi_reads_elem() {
   return EPI == EPI_ACC_F32 || EPI == EPI_BIAS_RESID || EPI == EPI_GELU_BWD || EPI == EPI_SCALE_ACC ||
@@ -191,6 +201,26 @@ __device__ __forceinline__ void pack4(T* p, const float* v) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
 }
 
+// Four fp16 values of a plane (hi), or of two (lo not null).
+__device__ __forceinline__ void unpack_planes(uint2 hi, uint2 lo, bool two, float* v) {
+  typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+  const h4 a = __builtin_bit_cast(h4, hi), b = __builtin_bit_cast(h4, lo);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = static_cast<float>(a[r]) + (two ? static_cast<float>(b[r]) : 0.f);
+}
+// v = hi + lo, each rounded to the nearest fp16.
+__device__ __forceinline__ void pack_planes(const float* v, uint2& hi, uint2& lo) {
+  typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+  h4 a, b;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    a[r] = static_cast<_Float16>(v[r]);
+    b[r] = static_cast<_Float16>(v[r] - static_cast<float>(a[r]));
+  }
+  hi = __builtin_bit_cast(uint2, a);
+  lo = __builtin_bit_cast(uint2, b);
+}
+
 // Workgroups a CU holds: one of the 256-row tiles (their LDS and, with one
 // wave per SIMD, the AGPR accumulators), else what four stages leave room for.
 template <typename T, int BM, int BN>
@@ -204,12 +234,15 @@ constexpr int occupancy() {
 // whole group of four, the last tile may reach past k, and every load tests its
 // chunk (three vector instructions: 3-4 % at 4096x12288x4096, so whole groups
 // take the copy without).
-template <typename T, bool AKC, bool BKC, int EPI, int BM, int BN, bool TAIL>
+// PASSES (Newton-Schulz products of two planes): k runs three times, over hi
+// hi, hi lo and lo hi of A and B; lo lo is below the sums' own rounding.
+template <typename T, bool AKC, bool BKC, int EPI, int BM, int BN, bool TAIL, int PASSES = 1>
 __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(occupancy<T, BM, BN>(), occupancy<T, BM, BN>())))
 gemm_dl_kernel(GemmArgs g) {
   using OA = Operand<T, AKC, BM>;
   using OB = Operand<T, BKC, BN>;
-  constexpr bool PIN = BM == 256;  // accumulators in AGPRs, one wave per SIMD
+  constexpr bool PIN = BM >= 192;  // accumulators in AGPRs, one wave per SIMD
+  constexpr bool NS = EPI >= EPI_NS_GRAM, SYM = EPI == EPI_NS_GRAM || EPI == EPI_NS_POLY;
   constexpr int TM = BM / 32, TN = BN / 32;
   static_assert(TM >= TN, "fragment rows");
   constexpr int LT = OA::LPT + OB::LPT;  // loads per thread and k tile
@@ -226,18 +259,28 @@ gemm_dl_kernel(GemmArgs g) {
   // panels through its L2); items are the tiles of the first k range, then of
   // the next; tiles go in groups of 8 row tiles sweeping the columns.
   const int tiles_m = (g.M + BM - 1) / BM, tiles_n = (g.N + BN - 1) / BN;
-  const int tiles = tiles_m * tiles_n, total = static_cast<int>(gridDim.x);
+  const int tiles = SYM ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n, total = static_cast<int>(gridDim.x);
   const int xcd = blockIdx.x & 7, rem = total & 7;
   int pid = xcd * (total >> 3) + min(xcd, rem) + (blockIdx.x >> 3);
-  const int split = pid / tiles;
+  const int split = pid / tiles;  // Newton-Schulz products: the matrix of the batch
   pid -= split * tiles;
   constexpr int GROUP = 8;
   const int per_group = GROUP * tiles_n;
   const int first_m = (pid / per_group) * GROUP;
   const int gsize = min(tiles_m - first_m, GROUP);
-  const int pid_m = first_m + (pid % per_group) % gsize;
-  const int pid_n = (pid % per_group) / gsize;
+  int pid_m = first_m + (pid % per_group) % gsize;
+  int pid_n = (pid % per_group) / gsize;
+  if constexpr (SYM) {  // tiles on and below the diagonal, row by row
+    pid_m = static_cast<int>((sqrtf(8.f * pid + 1.f) - 1.f) * 0.5f);
+    while (pid_m * (pid_m + 1) / 2 > pid) --pid_m;
+    while ((pid_m + 1) * (pid_m + 2) / 2 <= pid) ++pid_m;
+    pid_n = pid - pid_m * (pid_m + 1) / 2;
+  }
   const int m0 = pid_m * BM, n0 = pid_n * BN;
+  if constexpr (NS) {
+    g.A = static_cast<const T*>(g.A) + split * g.ns.sa;
+    g.B = static_cast<const T*>(g.B) + split * g.ns.sb;
+  }
 
   typename OA::Src sra[OA::LPT];
   typename OB::Src srb[OB::LPT];
@@ -250,8 +293,8 @@ gemm_dl_kernel(GemmArgs g) {
   // may be short: only the tiles that hold k are loaded and multiplied
   // (4096x8192x576: 49.0 us with a whole last group, 47.0; 8192x8192x352: 81, 78).
   const int quads = (g.K + 4 * BK - 1) / (4 * BK);
-  const int kbase = split * g.kquads * 4;
-  const int nk4 = min(g.kquads, quads - split * g.kquads) * 4;
+  const int kbase = NS ? 0 : split * g.kquads * 4;
+  const int nk4 = NS ? quads * 4 : min(g.kquads, quads - split * g.kquads) * 4;
   const int nk = TAIL ? min(nk4, (g.K + BK - 1) / BK - kbase) : nk4;
   // Each XCD starts its k loop at its own eighth of the range (the tile's
   // sum is rotated, the same for every launch of the shape).  Workgroups
@@ -260,7 +303,9 @@ gemm_dl_kernel(GemmArgs g) {
   // k are 32 KB apart and those addresses share their low bits, which crowds
   // a few memory channels (4096x4096x16384: 500 -> 418 us).  The workgroups
   // of one XCD share operand tiles through its L2, so they keep one offset.
-  const int koff = (xcd * (nk4 >> 3)) & ~3;
+  // (Newton-Schulz products: the tile's eighth of its matrix's tiles, which is
+  // about the same; equal matrices of a batch get equal bits.)
+  const int koff = ((NS ? pid * 8 / tiles : xcd) * (nk4 >> 3)) & ~3;
   auto rot = [&](int kt) {
     const int r = kt + koff;
     return kbase + (r >= nk ? r - nk : r);
@@ -297,7 +342,15 @@ gemm_dl_kernel(GemmArgs g) {
   auto stage_a = [&](int s) -> uint8_t* { return lds + s * OA::BYTES; };
   auto stage_b = [&](int s) -> uint8_t* { return lds + STAGES * OA::BYTES + s * OB::BYTES; };
   auto load = [&](int s, int kt, int l) {
-    if (l < OA::LPT) sra[l < OA::LPT ? l : 0].template load<TAIL>(stage_a(s), kt, g.K, l * 4 + w);
+    if constexpr (NS) {
+      int64_t oa = 0, ob = 0;
+      if constexpr (PASSES == 3) {
+        if (kt >= 2 * g.ns.kp) kt -= 2 * g.ns.kp, oa = g.ns.pa;
+        else if (kt >= g.ns.kp) kt -= g.ns.kp, ob = g.ns.pb;
+      }
+      if (l < OA::LPT) sra[l < OA::LPT ? l : 0].load_plane(stage_a(s), kt, oa, l * 4 + w);
+      else srb[l < OA::LPT ? 0 : l - OA::LPT].load_plane(stage_b(s), kt, ob, (l - OA::LPT) * 4 + w);
+    } else if (l < OA::LPT) sra[l < OA::LPT ? l : 0].template load<TAIL>(stage_a(s), kt, g.K, l * 4 + w);
     else srb[l < OA::LPT ? 0 : l - OA::LPT].template load<TAIL>(stage_b(s), kt, g.K, (l - OA::LPT) * 4 + w);
   };
 
@@ -488,7 +541,7 @@ gemm_dl_kernel(GemmArgs g) {
   // which defeats the loads issued ahead.
   auto epilogue = [&](auto GUARD_, const GemmArgs& ga) {
     constexpr bool GUARD = decltype(GUARD_)::value;
-    constexpr int E = EPI;
+    constexpr int E = NS ? static_cast<int>(EPI_STORE_F32) : EPI;  // (NS has returned)
     constexpr bool F32_OUT = E == EPI_STORE_F32 || E == EPI_ACC_F32 || E == EPI_BIAS_RESID || E == EPI_SCALE_F32 ||
                              E == EPI_SCALE_ACC;
     constexpr bool ELEM = epi_reads_elem<E>();
@@ -591,6 +644,113 @@ gemm_dl_kernel(GemmArgs g) {
       }
     }
   };
+  if constexpr (NS) {
+    // Lengths are multiples of 32 and RB is 32, so a block of rows is inside or
+    // outside as a whole; loads take clamped columns instead of tests.  A lane
+    // puts its values back into the staging area, from where the tile's mirror
+    // image is stored: four consecutive rows of a column, which are four
+    // consecutive columns there, 64 bytes by eight lanes.
+    constexpr bool LO = EPI == EPI_NS_STEP || PASSES == 3, AUX = EPI != EPI_NS_GRAM;
+    const NsArgs& ns = g.ns;
+    const bool col_in = nb < g.N && rsub < RPP, last = EPI == EPI_NS_STEP && ns.out_mode != 3;
+    const int64_t base = split * ns.sc;
+    const int nc = min(nb, g.N - 4);
+    uint2 xh[NB][NQ], xl[NB][NQ];
+    auto load_block = [&](int h) {
+      if (row0 + h * RB >= g.M) return;
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        const int64_t at = base + static_cast<int64_t>(row0 + h * RB + RPP * q + rsub0) * g.ldc + nc;
+        xh[h][q] = *reinterpret_cast<const uint2*>(static_cast<const f16_t*>(ns.aux) + at);
+        if constexpr (LO) xl[h][q] = *reinterpret_cast<const uint2*>(static_cast<const f16_t*>(ns.aux_lo) + at);
+      }
+    };
+    if constexpr (AUX) load_block(0);
+#pragma unroll
+    for (int h = 0; h < NB; ++h) {
+      if (row0 + h * RB >= g.M) break;
+      if constexpr (AUX)
+        if (h + 1 < NB) load_block(h + 1);
+#pragma unroll
+      for (int ii = 0; ii < RB / 16; ++ii)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const f32x4_t& a = acc[h * (RB / 16) + ii][j];
+          *reinterpret_cast<float4*>(stg + (ii * 16 + lr) * PITCH + j * 16 + lg * 4) = make_float4(a[0], a[1], a[2], a[3]);
+        }
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        float* sp = stg + (RPP * q + rsub0) * PITCH + cc;
+        const float4 s4 = *reinterpret_cast<const float4*>(sp);
+        float v[4] = {s4.x, s4.y, s4.z, s4.w};
+        if constexpr (AUX) {
+          float x[4];
+          unpack_planes(xh[h][q], LO ? xl[h][q] : make_uint2(0, 0), LO, x);
+          for (int r = 0; r < 4; ++r) v[r] = fmaf(g.alpha, v[r], ns.beta * x[r]);
+        } else {
+          for (int r = 0; r < 4; ++r) v[r] *= g.alpha;
+        }
+        const int m = row0 + h * RB + RPP * q + rsub;
+        if (last) {
+          if (m >= ns.orows || rsub >= RPP) continue;
+          const int64_t at = split * ns.so + static_cast<int64_t>(m) * ns.ldo + nb;
+          for (int r = 0; r < 4; ++r) v[r] *= ns.scale;
+          if (ns.vec) {
+            if (nb >= ns.ocols) continue;
+            if (ns.out_mode == 0) {
+              pack4(static_cast<bf16_t*>(ns.out) + at, v);
+            } else {
+              float* o = static_cast<float*>(ns.out) + at;
+              if (ns.out_mode == 2) {
+                const float4 c = *reinterpret_cast<const float4*>(o);
+                v[0] = fmaf(ns.keep, c.x, v[0]); v[1] = fmaf(ns.keep, c.y, v[1]);
+                v[2] = fmaf(ns.keep, c.z, v[2]); v[3] = fmaf(ns.keep, c.w, v[3]);
+              }
+              pack4(o, v);
+            }
+          } else {
+            for (int r = 0; r < 4; ++r) {
+              if (nb + r >= ns.ocols) break;
+              if (ns.out_mode == 0) static_cast<bf16_t*>(ns.out)[at + r] = f2bf(v[r]);
+              else {
+                float* o = static_cast<float*>(ns.out) + at + r;
+                *o = ns.out_mode == 2 ? fmaf(ns.keep, *o, v[r]) : v[r];
+              }
+            }
+          }
+          continue;
+        }
+        uint2 hi, lo;
+        pack_planes(v, hi, lo);
+        const int64_t at = base + static_cast<int64_t>(m) * g.ldc + nb;
+        if (col_in) {
+          *reinterpret_cast<uint2*>(static_cast<f16_t*>(g.C) + at) = hi;
+          if constexpr (LO) *reinterpret_cast<uint2*>(static_cast<f16_t*>(ns.C_lo) + at) = lo;
+        }
+        if constexpr (SYM)
+          if (rsub < RPP) *reinterpret_cast<float4*>(sp) = make_float4(v[0], v[1], v[2], v[3]);
+      }
+      if constexpr (SYM) {
+        if (pid_m == pid_n) continue;
+        asm volatile("" ::: "memory");  // the wave's LDS accesses are in order
+#pragma unroll
+        for (int p = 0; p < TN * 2; ++p) {
+          const int r4 = 4 * (lane & 7), c = (lane >> 3) + 8 * p;
+          float v[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = stg[(r4 + r) * PITCH + c];
+          uint2 hi, lo;
+          pack_planes(v, hi, lo);
+          if (col0 + c >= g.N) continue;
+          const int64_t at = base + static_cast<int64_t>(col0 + c) * g.ldc + row0 + h * RB + r4;
+          *reinterpret_cast<uint2*>(static_cast<f16_t*>(g.C) + at) = hi;
+          if constexpr (LO) *reinterpret_cast<uint2*>(static_cast<f16_t*>(ns.C_lo) + at) = lo;
+        }
+        asm volatile("" ::: "memory");
+      }
+    }
+    return;
+  }
   const bool interior = row0 + TM * 16 <= g.M && col0 + TN * 16 <= g.N;
   if constexpr (EPI == EPI_STORE_F32) {
     // a split over k: the raw fp32 sums go to C[split][M][N] (the workspace),
@@ -665,6 +825,27 @@ hipError_t launch_loss(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream
   ATOM_DL(false, false, EPI_SCALE)
   ATOM_DL(false, false, EPI_SCALE_F32)
   ATOM_DL(false, false, EPI_SCALE_ACC)
+#undef ATOM_DL
+  return hipErrorInvalidValue;
+}
+
+// Newton-Schulz products: square tiles, k of whole tiles (g.K counts all passes).
+template <int BS, int PASSES>
+hipError_t launch_ns(const GemmArgs& g, int batch, bool akc, bool bkc, int epi, hipStream_t s) {
+  const int64_t tm = (g.M + BS - 1) / BS, tn = (g.N + BS - 1) / BS;
+  const int64_t tiles = epi == EPI_NS_STEP ? tm * tn : tm * (tm + 1) / 2;
+  if (tiles * batch > (1ll << 30)) return hipErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(tiles * batch)), block(NT);
+#define ATOM_DL(AK, BK_, E)                                                                              \
+  if (akc == AK && bkc == BK_ && epi == E) {                                                             \
+    hipLaunchKernelGGL((gemm_dl_kernel<f16_t, AK, BK_, E, BS, BS, true, PASSES>), grid, block, 0, s, g); \
+    return hipGetLastError();                                                                            \
+  }
+  ATOM_DL(true, true, EPI_NS_GRAM)
+  ATOM_DL(false, false, EPI_NS_GRAM)
+  ATOM_DL(true, true, EPI_NS_POLY)
+  ATOM_DL(true, false, EPI_NS_STEP)
+  ATOM_DL(true, true, EPI_NS_STEP)
 #undef ATOM_DL
   return hipErrorInvalidValue;
 }

@@ -1,0 +1,10 @@
+// gemm_dl instantiations for the Newton-Schulz products: 128x128 tiles.
+#include "gemm_dl.h"
+
+namespace atom {
+
+hipError_t gemm_ns_128(const GemmArgs& g, int planes, int batch, bool akc, bool bkc, int epi, hipStream_t s) {
+  return planes == 1 ? dl::launch_ns<128, 1>(g, batch, akc, bkc, epi, s) : dl::launch_ns<128, 3>(g, batch, akc, bkc, epi, s);
+}
+
+}  // namespace atom

@@ -24,6 +24,30 @@ enum Epilogue {
   EPI_SCALE_F32 = 10,  // C = alpha * acc                  (fp32)
   EPI_SCALE_ACC = 11,  // C += alpha * acc                 (fp32)
   EPI_SUM_SCALE = 12,  // C = alpha * (resid + acc)        (element type; resid fp32)
+  // the Newton-Schulz products (orthogonalize.hip); see NsArgs
+  EPI_NS_GRAM = 13,    // C = alpha * acc, symmetric
+  EPI_NS_POLY = 14,    // C = alpha * acc + beta * aux, symmetric
+  EPI_NS_STEP = 15,    // C = alpha * acc + beta * aux, or the result from it
+};
+
+// The epilogues of the Newton-Schulz products.  Matrices are fp16 in one or two
+// planes (value = hi + lo); every length is a multiple of 32.  A symmetric
+// product computes the tiles on and below the diagonal and stores each on both
+// sides of it.
+struct NsArgs {
+  int64_t sa, sb, sc;        // elements from one matrix of the batch to the next: A, B; C and aux
+  int64_t pa, pb;            // elements from the hi to the lo plane of A and B
+  int kp;                    // k tiles of 32 of one pass over k (two planes: three passes)
+  const void *aux, *aux_lo;  // as C
+  void* C_lo;
+  float beta;
+  // the last step: out = scale * (...), of orows x ocols, instead of C
+  void* out;
+  int64_t ldo, so;
+  int out_mode;              // 0 bf16, 1 fp32, 2 fp32 out = keep * out + ..., 3 none (C)
+  int orows, ocols;
+  bool vec;                  // out's rows hold whole aligned 4-vectors
+  float scale, keep;
 };
 
 struct GemmArgs {
@@ -46,6 +70,7 @@ struct GemmArgs {
   const float* rowscale;  // EPI_DZ: factor of each row, null: 1
   float* ztgt;            // EPI_LSE: receives acc at each row's target
   int v0, V;              // EPI_DZ: column 0 is column v0 of the V of the vocabulary
+  NsArgs ns;
 };
 
 // The layout and epilogue combinations of the training step: forward, data
@@ -82,6 +107,10 @@ hipError_t gemm_loss_128(const GemmArgs& g, bool akc, bool bkc, int epi, hipStre
 hipError_t gemm_loss_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 hipError_t gemm_loss_f32_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 hipError_t gemm_loss_f32_32(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+
+// Newton-Schulz products on square tiles of bs (64, 128, 192 or 256); planes 1
+// or 2, `batch` matrices.
+hipError_t gemm_ns(const GemmArgs& g, int bs, int planes, int batch, bool akc, bool bkc, int epi, hipStream_t s);
 
 hipError_t gemm_check(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig);
 hipError_t gemm(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, int epi, hipStream_t s);
@@ -170,6 +199,15 @@ uint64_t linear_xent_bwd_ws(int dtype, int64_t rows, int V, int d, int piece);
 hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
                            const float* lse, const float* drow, float scale, void* dx, int64_t lddx, void* dw,
                            int64_t lddw, int dw_epi, int64_t rows, int V, int d, int piece, void* ws, hipStream_t s);
+
+// Newton-Schulz orthogonalisation (atom_k_orthogonalize).  out_epi: EPI_STORE,
+// EPI_STORE_F32 or EPI_ACC_F32; coef: host [steps][3].
+bool orthogonalize_ok(int batch, int rows, int cols);
+bool orthogonalize_coef_ok(const float* coef, int steps);
+uint64_t orthogonalize_ws(int dtype, int batch, int rows, int cols);
+hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,
+                         int64_t stride_o, int out_epi, float keep, float scale, int batch, int rows, int cols,
+                         const float* coef, int steps, void* ws, hipStream_t s);
 
 // Causal attention on a fused qkv [B*T][3*d] (element type), heads of dh in
 // {64, 128}.  o [B*T][d], lse [B][H][T] fp32 (natural log).

@@ -1,0 +1,317 @@
+// Newton-Schulz orthogonalisation of a matrix (atom_k_orthogonalize): the
+// update of the Muon optimiser, U V^T of the singular value decomposition G =
+// U S V^T but for the singular values, which end near 1 instead of at 1.
+//
+//   X = G / (|G|_F + 1e-7); per step  A = X X^T,  B = b A + c A^2,
+//   X <- a X + B X;  with A = X^T X and X B for matrices taller than wide.
+//
+// Every step works on the singular values alone, s <- a s + b s^3 + c s^5.
+// All products run on the direct-load kernel (gemm_dl.h) in fp16 MFMAs with
+// fp32 sums, on matrices scaled by 2^10 and padded with zeros to multiples of
+// 32, and each step's sums and scalings are its products' epilogues: three
+// launches a step.  A and B are symmetric, so their products take the tiles on
+// and below the diagonal.
+//
+// Precision.  X is kept as two fp16 planes, hi + lo (22 bits): rounding X to
+// one would mix its strong directions into the weak ones, which later steps
+// raise by up to a per step (a gradient of rank 8 over noise of 1e-3, 512 x
+// 512: 4e-2 off in relative norm; 3e-4 with two planes).  The product B X may
+// take hi alone, because B is small where X's directions are weak, and so may A
+// and B be one plane: bf16 results are within 2e-3 of the definition, about
+// what their own rounding is off (fp16, with 11 bits, not bf16: 1.5e-2).  fp32
+// results take two planes of all three, and each product three passes over k
+// (hi hi, hi lo, lo hi), at three eighths of the fp16 rate and still about
+// three times that of fp32 MFMAs; 2.5e-7 to 1.4e-6 from the definition, fp32
+// arithmetic 1.5e-7 to 9e-7.
+#include <algorithm>
+#include <cmath>
+
+#include "common.h"
+#include "launch.h"
+
+namespace atom {
+
+hipError_t gemm_ns_256(const GemmArgs& g, int planes, int batch, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_ns_192(const GemmArgs& g, int planes, int batch, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_ns_128(const GemmArgs& g, int planes, int batch, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_ns_64(const GemmArgs& g, int planes, int batch, bool akc, bool bkc, int epi, hipStream_t s);
+
+hipError_t gemm_ns(const GemmArgs& g, int bs, int planes, int batch, bool akc, bool bkc, int epi, hipStream_t s) {
+  return bs == 256   ? gemm_ns_256(g, planes, batch, akc, bkc, epi, s)
+         : bs == 192 ? gemm_ns_192(g, planes, batch, akc, bkc, epi, s)
+         : bs == 128 ? gemm_ns_128(g, planes, batch, akc, bkc, epi, s)
+                     : gemm_ns_64(g, planes, batch, akc, bkc, epi, s);
+}
+
+namespace {
+
+constexpr float SCALE = 1024.f;  // of every fp16 matrix: entries of 2^-24 of the norm are still held
+constexpr double EPS = 1e-7;
+constexpr int NORM_BLOCKS = 256;  // most partial sums of squares of a matrix
+
+// Partial sums of squares in 64 bits: no entry's square over- or underflows,
+// and long sums lose nothing.  Block b of a matrix takes every gridDim.x-th run
+// of 1024 elements of a row's order.
+template <typename T>
+__global__ void __launch_bounds__(256) norm_kernel(const T* __restrict__ g, int64_t ldg, int64_t stride, int rows,
+                                                   int cols, double* __restrict__ part) {
+  __shared__ double red[4];
+  g += blockIdx.y * stride;
+  double s = 0.0;
+  const int64_t runs = (cols + 1023) / 1024, n = runs * rows;
+  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const int64_t row = i / runs;
+    const int c0 = static_cast<int>(i - row * runs) * 1024 + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int c = c0 + 256 * k;
+      const double v = c < cols ? static_cast<double>(to_f<T>(g[row * ldg + c])) : 0.0;
+      s = fma(v, v, s);
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// X = SCALE * g / (norm + EPS) in two planes [rp][cp], zeros past the matrix.
+// A norm that is not finite makes all of X NaN.
+template <typename T>
+__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ g, int64_t ldg, int64_t stride, int rows,
+                                                   int cols, int rp, int cp, const double* __restrict__ part, int parts,
+                                                   f16_t* __restrict__ hi, f16_t* __restrict__ lo, int64_t sx) {
+  __shared__ double red[4];
+  g += blockIdx.y * stride;
+  hi += blockIdx.y * sx;
+  lo += blockIdx.y * sx;
+  double s = static_cast<int>(threadIdx.x) < parts ? part[blockIdx.y * parts + threadIdx.x] : 0.0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = (red[0] + red[1]) + (red[2] + red[3]);
+  const double f = s < INFINITY ? SCALE / (sqrt(s) + EPS) : NAN;
+  const int64_t n = static_cast<int64_t>(rp) * (cp / 4);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t row = i / (cp / 4);
+    const int c = static_cast<int>(i - row * (cp / 4)) * 4;
+    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+    h4 a, b;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float v = row < rows && c + k < cols
+                          ? static_cast<float>(static_cast<double>(to_f<T>(g[row * ldg + c + k])) * f) : 0.f;
+      a[k] = static_cast<_Float16>(v);
+      b[k] = static_cast<_Float16>(v - static_cast<float>(a[k]));
+    }
+    *reinterpret_cast<h4*>(hi + row * cp + c) = a;
+    *reinterpret_cast<h4*>(lo + row * cp + c) = b;
+  }
+}
+
+// No steps: out from X itself.
+template <typename TO, bool ACC>
+__global__ void __launch_bounds__(256) unpack_kernel(const f16_t* __restrict__ hi, const f16_t* __restrict__ lo,
+                                                     int64_t sx, int cp, TO* __restrict__ out, int64_t ldo, int64_t so,
+                                                     int rows, int cols, float scale, float keep) {
+  const int64_t n = static_cast<int64_t>(rows) * cols;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t row = i / cols, c = i - row * cols, at = blockIdx.y * sx + row * cp + c;
+    const float v = scale * (static_cast<float>(hi[at]) + static_cast<float>(lo[at]));
+    TO* o = out + blockIdx.y * so + row * ldo + c;
+    *o = ACC ? from_f<TO>(fmaf(keep, to_f<TO>(*o), v)) : from_f<TO>(v);
+  }
+}
+
+inline uint64_t up(uint64_t n) { return (n + 255) & ~255ull; }
+
+// Workspace: partial sums, X (hi and lo, each twice: a step reads one and
+// writes the other; one plane's lo is read and written by the same lanes, so it
+// is there once), A, B.  n: bytes of a plane of X and of A, all matrices.
+struct Ws {
+  int rp, cp, k;  // padded lengths, the smaller of them
+  uint64_t part, x[2], xl[2], a, al, b, bl, end;
+};
+Ws layout(int dtype, int batch, int rows, int cols) {
+  Ws w;
+  w.rp = (rows + 31) / 32 * 32, w.cp = (cols + 31) / 32 * 32, w.k = std::min(w.rp, w.cp);
+  const uint64_t x = up(2ull * batch * w.rp * w.cp), a = up(2ull * batch * w.k * w.k);
+  const bool two = dtype == DT_F32;
+  uint64_t at = 0;
+  auto take = [&](uint64_t n) { const uint64_t o = at; at += n; return o; };
+  w.part = take(up(8ull * batch * NORM_BLOCKS));
+  w.x[0] = take(x);
+  w.xl[0] = take(x);
+  w.x[1] = take(x);
+  w.xl[1] = two ? take(x) : w.xl[0];
+  w.a = take(a);
+  w.al = two ? take(a) : w.a;
+  w.b = take(a);
+  w.bl = two ? take(a) : w.b;
+  w.end = at;
+  return w;
+}
+
+constexpr int CUS = 256;
+
+// Tile of a product: the smallest predicted time, as for other products
+// (gemm.hip): the most workgroups a CU gets x (k tiles x the time of one + a
+// fixed time).
+int tile_of(int M, int N, int ktiles, int batch, bool sym) {
+  struct {
+    int bs, occ;
+    double ktile, fixed;
+  } const cfg[] = {{256, 1, 0.604, 10.0}, {192, 1, 0.375, 7.0}, {128, 2, 0.249, 2.4}, {64, 4, 0.131, 0.7}};
+  int best = 0;
+  double best_us = 0.0;
+  for (const auto& c : cfg) {
+    const int64_t tm = (M + c.bs - 1) / c.bs, tn = (N + c.bs - 1) / c.bs;
+    const int64_t tiles = (sym ? tm * (tm + 1) / 2 : tm * tn) * batch;
+    const double us = static_cast<double>((tiles + CUS - 1) / CUS) * (ktiles * c.ktile + c.fixed);
+    if (best == 0 || us < best_us) best = c.bs, best_us = us;
+  }
+  return best;
+}
+
+}  // namespace
+
+// Tiles are counted in 32 bits, of 64 x 64 at least.
+bool orthogonalize_ok(int batch, int rows, int cols) {
+  if (batch < 0 || rows <= 0 || cols <= 0 || batch > 65535 || rows > (1 << 24) || cols > (1 << 24)) return false;
+  const int64_t tr = (rows + 63) / 64, tc = (cols + 63) / 64;
+  return tr * tc * std::max(batch, 1) < (1ll << 30) && std::min(tr, tc) * std::min(tr, tc) * std::max(batch, 1) < (1ll << 30);
+}
+
+// Coefficients whose steps keep the singular values, which start in [0, 1], and
+// the entries of b A + c A^2 in fp16's range: bounds of s <- |a s + b s^3 + c
+// s^5| and |b t + c t^2|, t = s^2, from their extrema.
+bool orthogonalize_coef_ok(const float* coef, int steps) {
+  double top = 1.0;
+  for (int k = 0; k < steps; ++k) {
+    const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    const double t = top * top;
+    auto p = [&](double x) { return std::fabs(b * x + c * x * x); };
+    double poly = p(t);
+    if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < t) poly = std::max(poly, p(-b / (2 * c)));
+    auto f = [&](double s) { return std::fabs(s * (a + s * s * (b + c * s * s))); };
+    double next = f(top);
+    // a + 3 b x + 5 c x^2 = 0, x = s^2
+    const double disc = 9 * b * b - 20 * a * c;
+    if (c != 0.0 && disc >= 0.0) {
+      for (const double x : {(-3 * b + std::sqrt(disc)) / (10 * c), (-3 * b - std::sqrt(disc)) / (10 * c)})
+        if (x > 0.0 && x < t) next = std::max(next, f(std::sqrt(x)));
+    } else if (c == 0.0 && b != 0.0 && -a / (3 * b) > 0.0 && -a / (3 * b) < t) {
+      next = std::max(next, f(std::sqrt(-a / (3 * b))));
+    }
+    top = next;
+    if (poly > 32.0 || top > 4.0 || std::fabs(a) > 32.0) return false;
+  }
+  return true;
+}
+
+uint64_t orthogonalize_ws(int dtype, int batch, int rows, int cols) { return layout(dtype, batch, rows, cols).end; }
+
+hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,
+                         int64_t stride_o, int out_epi, float keep, float scale, int batch, int rows, int cols,
+                         const float* coef, int steps, void* ws, hipStream_t s) {
+  const Ws o = layout(dtype, batch, rows, cols);
+  char* base = static_cast<char*>(ws);
+  auto at = [&](uint64_t off) { return reinterpret_cast<f16_t*>(base + off); };
+  const int64_t sx = static_cast<int64_t>(o.rp) * o.cp, sa = static_cast<int64_t>(o.k) * o.k;
+  double* part = reinterpret_cast<double*>(base + o.part);
+  // one block per 8192 elements, at most NORM_BLOCKS a matrix
+  const int64_t n = static_cast<int64_t>(rows) * cols;
+  const int parts = static_cast<int>(std::min<int64_t>(NORM_BLOCKS, (n + 8191) / 8192));
+  const dim3 ngrid(parts, batch), pgrid(static_cast<unsigned>(std::min<int64_t>((sx / 4 + 255) / 256, 2048)), batch);
+  if (dtype == DT_BF16) {
+    const bf16_t* x = static_cast<const bf16_t*>(g);
+    hipLaunchKernelGGL(norm_kernel<bf16_t>, ngrid, dim3(256), 0, s, x, ldg, stride_g, rows, cols, part);
+    hipLaunchKernelGGL(pack_kernel<bf16_t>, pgrid, dim3(256), 0, s, x, ldg, stride_g, rows, cols, o.rp, o.cp, part,
+                       parts, at(o.x[0]), at(o.xl[0]), sx);
+  } else {
+    const float* x = static_cast<const float*>(g);
+    hipLaunchKernelGGL(norm_kernel<float>, ngrid, dim3(256), 0, s, x, ldg, stride_g, rows, cols, part);
+    hipLaunchKernelGGL(pack_kernel<float>, pgrid, dim3(256), 0, s, x, ldg, stride_g, rows, cols, o.rp, o.cp, part,
+                       parts, at(o.x[0]), at(o.xl[0]), sx);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int out_mode = out_epi == EPI_ACC_F32 ? 2 : out_epi == EPI_STORE_F32 || dtype == DT_F32 ? 1 : 0;
+  scale /= SCALE;
+  if (steps == 0) {
+    const dim3 ugrid(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 2048)), batch);
+#define ATOM_UNPACK(TO, ACC)                                                                                     \
+  hipLaunchKernelGGL((unpack_kernel<TO, ACC>), ugrid, dim3(256), 0, s, at(o.x[0]), at(o.xl[0]), sx, o.cp,        \
+                     static_cast<TO*>(out), ldo, stride_o, rows, cols, scale, keep)
+    if (out_mode == 0) ATOM_UNPACK(bf16_t, false);
+    else if (out_mode == 1) ATOM_UNPACK(float, false);
+    else ATOM_UNPACK(float, true);
+#undef ATOM_UNPACK
+    return hipGetLastError();
+  }
+  const bool wide = rows <= cols, two = dtype == DT_F32;
+  const int planes = two ? 2 : 1, passes = two ? 3 : 1;
+  const int osz = out_mode == 0 ? 2 : 4;
+  for (int k = 0; k < steps; ++k) {
+    const int i = k & 1;
+    const float a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
+    auto product = [&](GemmArgs& p, int len, bool akc, bool bkc, int epi) {
+      p.ns.kp = len / 32;
+      p.K = passes * len;
+      p.splits = 1;
+      return gemm_ns(p, tile_of(p.M, p.N, passes * p.ns.kp, batch, epi != EPI_NS_STEP), planes, batch, akc, bkc, epi, s);
+    };
+    GemmArgs p{};
+    p.A = p.B = at(o.x[i]), p.lda = p.ldb = o.cp, p.C = at(o.a), p.ldc = o.k;
+    p.M = p.N = o.k;
+    p.alpha = 1.f / SCALE;
+    p.ns.sa = p.ns.sb = sx, p.ns.sc = sa;
+    p.ns.pa = p.ns.pb = at(o.xl[i]) - at(o.x[i]);
+    p.ns.C_lo = at(o.al);
+    e = product(p, wide ? o.cp : o.rp, wide, wide, EPI_NS_GRAM);
+    if (e != hipSuccess) return e;
+    GemmArgs q{};
+    q.A = q.B = at(o.a), q.lda = q.ldb = o.k, q.C = at(o.b), q.ldc = o.k;
+    q.M = q.N = o.k;
+    q.alpha = c / SCALE;
+    q.ns.sa = q.ns.sb = q.ns.sc = sa;
+    q.ns.pa = q.ns.pb = at(o.al) - at(o.a);
+    q.ns.aux = at(o.a), q.ns.aux_lo = at(o.al), q.ns.beta = b, q.ns.C_lo = at(o.bl);
+    e = product(q, o.k, true, true, EPI_NS_POLY);
+    if (e != hipSuccess) return e;
+    GemmArgs r{};
+    r.A = wide ? at(o.b) : at(o.x[i]), r.B = wide ? at(o.x[i]) : at(o.b);
+    r.lda = wide ? o.k : o.cp, r.ldb = wide ? o.cp : o.k;
+    r.C = at(o.x[1 - i]), r.ldc = o.cp;
+    r.M = o.rp, r.N = o.cp;
+    r.alpha = 1.f / SCALE;
+    r.ns.sa = wide ? sa : sx, r.ns.sb = wide ? sx : sa, r.ns.sc = sx;
+    r.ns.pa = wide ? at(o.bl) - at(o.b) : at(o.xl[i]) - at(o.x[i]);
+    r.ns.pb = wide ? at(o.xl[i]) - at(o.x[i]) : at(o.bl) - at(o.b);
+    r.ns.aux = at(o.x[i]), r.ns.aux_lo = at(o.xl[i]), r.ns.beta = a, r.ns.C_lo = at(o.xl[1 - i]);
+    r.ns.out_mode = 3;
+    if (k == steps - 1) {
+      r.ns.out = out, r.ns.ldo = ldo, r.ns.so = stride_o, r.ns.out_mode = out_mode;
+      r.ns.orows = rows, r.ns.ocols = cols, r.ns.scale = scale, r.ns.keep = keep;
+      r.ns.vec = cols % 4 == 0 && ldo % 4 == 0 && stride_o % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * osz) == 0;
+    }
+    e = product(r, o.k, true, !wide, EPI_NS_STEP);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace atom
+
+// Tiles of a step's three products (tests).
+extern "C" void atom_ns_choice(int dtype, int batch, int rows, int cols, int* out) {
+  using namespace atom;
+  const Ws o = layout(dtype, batch, rows, cols);
+  const int passes = dtype == DT_F32 ? 3 : 1, lng = std::max(o.rp, o.cp);
+  out[0] = tile_of(o.k, o.k, passes * lng / 32, batch, true);
+  out[1] = tile_of(o.k, o.k, passes * o.k / 32, batch, true);
+  out[2] = tile_of(o.rp, o.cp, passes * o.k / 32, batch, false);
+}

@@ -125,3 +125,16 @@ def attn_choice(B, T, H, dh):
     f.argtypes, f.restype = [ctypes.c_int] * 4, ctypes.c_int
     bits = f(B, T, H, dh)
     return tuple(bool(bits >> i & 1) for i in range(4))
+
+
+def ns_choice(dtype, batch, rows, cols):
+    """Tiles atom_k_orthogonalize takes for a step's three products, by the library's own rule."""
+    import ctypes
+
+    from paper_2403_10504_amd import atom as A
+
+    out = (ctypes.c_int * 3)()
+    f = A.lib().atom_ns_choice
+    f.argtypes, f.restype = [ctypes.c_int] * 4 + [ctypes.c_void_p], None
+    f(dt_code(dtype), batch, rows, cols, ctypes.addressof(out))
+    return tuple(out)
