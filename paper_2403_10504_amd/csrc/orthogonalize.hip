@@ -47,67 +47,120 @@ namespace {
 
 constexpr float SCALE = 1024.f;  // of every fp16 matrix: entries of 2^-24 of the norm are still held
 constexpr double EPS = 1e-7;
-constexpr int NORM_BLOCKS = 256;  // most partial sums of squares of a matrix
+constexpr int NORM_BLOCKS = 1024;  // most partial sums of squares of a matrix
 
+// Eight elements of a row from column c on, zeros from `cols` on.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* p, int c, int cols, float* v) {
+  if (VEC && c + 8 <= cols) {
+    if constexpr (sizeof(T) == 2) {
+      const uint4 w = *reinterpret_cast<const uint4*>(p + c);
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[2 * k] = bf2f(u[k] & 0xffff), v[2 * k + 1] = bf2f(u[k] >> 16);
+    } else {
+      const float4 a = *reinterpret_cast<const float4*>(p + c), b = *reinterpret_cast<const float4*>(p + c + 4);
+      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? to_f<T>(p[c + k]) : 0.f;
+  }
+}
+
+// A workgroup takes 256 >> lx rows at a time, 1 << lx threads a row, eight
+// columns a thread.  VEC: rows of g start on 16 bytes.
+//
 // Partial sums of squares in 64 bits: no entry's square over- or underflows,
-// and long sums lose nothing.  Block b of a matrix takes every gridDim.x-th run
-// of 1024 elements of a row's order.
-template <typename T>
+// and long sums lose nothing.
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) norm_kernel(const T* __restrict__ g, int64_t ldg, int64_t stride, int rows,
-                                                   int cols, double* __restrict__ part) {
+                                                   int cols, int lx, double* __restrict__ part) {
   __shared__ double red[4];
   g += blockIdx.y * stride;
-  double s = 0.0;
-  const int64_t runs = (cols + 1023) / 1024, n = runs * rows;
-  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-    const int64_t row = i / runs;
-    const int c0 = static_cast<int>(i - row * runs) * 1024 + threadIdx.x;
+  const int x = threadIdx.x & ((1 << lx) - 1), rpb = 256 >> lx;
+  double s[2] = {0.0, 0.0};
+  for (int r = blockIdx.x * rpb + (threadIdx.x >> lx); r < rows; r += gridDim.x * rpb) {
+    const T* p = g + r * ldg;
+#pragma unroll 4
+    for (int c = 8 * x; c < cols; c += 8 << lx) {
+      float v[8];
+      load8<T, VEC>(p, c, cols, v);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int c = c0 + 256 * k;
-      const double v = c < cols ? static_cast<double>(to_f<T>(g[row * ldg + c])) : 0.0;
-      s = fma(v, v, s);
+      for (int k = 0; k < 8; ++k) s[k & 1] = fma(static_cast<double>(v[k]), static_cast<double>(v[k]), s[k & 1]);
     }
   }
+  double t = s[0] + s[1];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
   __syncthreads();
   if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
 // X = SCALE * g / (norm + EPS) in two planes [rp][cp], zeros past the matrix.
 // A norm that is not finite makes all of X NaN.
-template <typename T>
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ g, int64_t ldg, int64_t stride, int rows,
-                                                   int cols, int rp, int cp, const double* __restrict__ part, int parts,
-                                                   f16_t* __restrict__ hi, f16_t* __restrict__ lo, int64_t sx) {
+                                                   int cols, int rp, int cp, int lx, const double* __restrict__ part,
+                                                   int parts, f16_t* __restrict__ hi, f16_t* __restrict__ lo,
+                                                   int64_t sx) {
   __shared__ double red[4];
   g += blockIdx.y * stride;
   hi += blockIdx.y * sx;
   lo += blockIdx.y * sx;
-  double s = static_cast<int>(threadIdx.x) < parts ? part[blockIdx.y * parts + threadIdx.x] : 0.0;
+  double s = 0.0;
+  for (int i = threadIdx.x; i < parts; i += 256) s += part[blockIdx.y * parts + i];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
   s = (red[0] + red[1]) + (red[2] + red[3]);
   const double f = s < INFINITY ? SCALE / (sqrt(s) + EPS) : NAN;
-  const int64_t n = static_cast<int64_t>(rp) * (cp / 4);
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t row = i / (cp / 4);
-    const int c = static_cast<int>(i - row * (cp / 4)) * 4;
-    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-    h4 a, b;
+  const int x = threadIdx.x & ((1 << lx) - 1), rpb = 256 >> lx;
+  for (int r = blockIdx.x * rpb + (threadIdx.x >> lx); r < rp; r += gridDim.x * rpb) {
+    const T* p = g + r * ldg;
+#pragma unroll 2
+    for (int c = 8 * x; c < cp; c += 8 << lx) {
+      float v[8];
+      load8<T, VEC>(p, c, r < rows ? cols : 0, v);
+      f16x8_t a, b;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float v = row < rows && c + k < cols
-                          ? static_cast<float>(static_cast<double>(to_f<T>(g[row * ldg + c + k])) * f) : 0.f;
-      a[k] = static_cast<_Float16>(v);
-      b[k] = static_cast<_Float16>(v - static_cast<float>(a[k]));
+      for (int k = 0; k < 8; ++k) {
+        const float y = static_cast<float>(static_cast<double>(v[k]) * f);
+        a[k] = static_cast<_Float16>(y);
+        b[k] = static_cast<_Float16>(y - static_cast<float>(a[k]));
+      }
+      *reinterpret_cast<f16x8_t*>(hi + static_cast<int64_t>(r) * cp + c) = a;
+      *reinterpret_cast<f16x8_t*>(lo + static_cast<int64_t>(r) * cp + c) = b;
     }
-    *reinterpret_cast<h4*>(hi + row * cp + c) = a;
-    *reinterpret_cast<h4*>(lo + row * cp + c) = b;
+  }
+}
+
+template <typename T>
+void launch_pack(const void* g, int64_t ldg, int64_t stride, int batch, int rows, int cols, int rp, int cp,
+                 double* part, f16_t* hi, f16_t* lo, hipStream_t s) {
+  const T* p = static_cast<const T*>(g);
+  const int e = 16 / static_cast<int>(sizeof(T));
+  const bool vec = reinterpret_cast<uintptr_t>(g) % 16 == 0 && ldg % e == 0 && stride % e == 0;
+  int lx = 0;
+  while (lx < 8 && 8 << lx < cols) ++lx;
+  const int64_t runs = (rows + (256 >> lx) - 1) / (256 >> lx);  // of rows a workgroup takes at once
+  const int64_t pruns = (rp + (256 >> lx) - 1) / (256 >> lx);
+  // a few thousand workgroups over the batch: each of the second kernel's sums
+  // all parts of its matrix
+  const int parts = static_cast<int>(std::min<int64_t>(std::max(64, NORM_BLOCKS / batch), runs));
+  const int64_t packs = std::min<int64_t>(std::max(64, 2048 / batch), pruns);
+  const dim3 ngrid(parts, batch), pgrid(static_cast<unsigned>(packs), batch), block(256);
+  const int64_t sx = static_cast<int64_t>(rp) * cp;
+  if (vec) {
+    hipLaunchKernelGGL((norm_kernel<T, true>), ngrid, block, 0, s, p, ldg, stride, rows, cols, lx, part);
+    hipLaunchKernelGGL((pack_kernel<T, true>), pgrid, block, 0, s, p, ldg, stride, rows, cols, rp, cp, lx, part, parts,
+                       hi, lo, sx);
+  } else {
+    hipLaunchKernelGGL((norm_kernel<T, false>), ngrid, block, 0, s, p, ldg, stride, rows, cols, lx, part);
+    hipLaunchKernelGGL((pack_kernel<T, false>), pgrid, block, 0, s, p, ldg, stride, rows, cols, rp, cp, lx, part,
+                       parts, hi, lo, sx);
   }
 }
 
@@ -156,20 +209,27 @@ Ws layout(int dtype, int batch, int rows, int cols) {
 
 constexpr int CUS = 256;
 
-// Tile of a product: the smallest predicted time, as for other products
-// (gemm.hip): the most workgroups a CU gets x (k tiles x the time of one + a
-// fixed time).
-int tile_of(int M, int N, int ktiles, int batch, bool sym) {
+// Tile of a product (0 A, 1 B, 2 X): the smallest predicted time.  A CU's k tile
+// (32) takes `lat` us of one workgroup alone on it and `ktile` of each of
+// several, a workgroup's start and epilogue `fixed`.  Fitted to 33 products of 256 to
+// 20480 in one and three passes; B X reads and writes both planes of X, 8 bytes
+// an entry that no product hides in 256x256 tiles (4096 x 4096: 25 of 130 us).
+// 4096 x 4096, A: 192x192 tiles fill 253 CUs and take 78 us, 256x256 136 CUs and
+// 91, 128x128 two or three to a CU and 107; 12 x 768 x 768, B X: 24 us in
+// 128x128, 28 in 192x192, 40 in 256x256.
+int tile_of(int product, int M, int N, int ktiles, int batch) {
   struct {
-    int bs, occ;
-    double ktile, fixed;
-  } const cfg[] = {{256, 1, 0.604, 10.0}, {192, 1, 0.375, 7.0}, {128, 2, 0.249, 2.4}, {64, 4, 0.131, 0.7}};
+    int bs;
+    double lat, ktile, fixed[3];
+  } const cfg[] = {{256, 0.74, 0.74, {8.0, 9.5, 20.0}}, {192, 0.45, 0.48, {9.0, 10.0, 11.0}},
+                   {128, 0.30, 0.25, {2.5, 3.2, 4.0}}, {64, 0.147, 0.117, {0.8, 0.9, 0.7}}};
   int best = 0;
   double best_us = 0.0;
   for (const auto& c : cfg) {
     const int64_t tm = (M + c.bs - 1) / c.bs, tn = (N + c.bs - 1) / c.bs;
-    const int64_t tiles = (sym ? tm * (tm + 1) / 2 : tm * tn) * batch;
-    const double us = static_cast<double>((tiles + CUS - 1) / CUS) * (ktiles * c.ktile + c.fixed);
+    const int64_t tiles = (product < 2 ? tm * (tm + 1) / 2 : tm * tn) * batch;
+    const double share = static_cast<double>((tiles + CUS - 1) / CUS);
+    const double us = ktiles * std::max(c.lat, share * c.ktile) + share * c.fixed[product];
     if (best == 0 || us < best_us) best = c.bs, best_us = us;
   }
   return best;
@@ -222,21 +282,11 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
   auto at = [&](uint64_t off) { return reinterpret_cast<f16_t*>(base + off); };
   const int64_t sx = static_cast<int64_t>(o.rp) * o.cp, sa = static_cast<int64_t>(o.k) * o.k;
   double* part = reinterpret_cast<double*>(base + o.part);
-  // one block per 8192 elements, at most NORM_BLOCKS a matrix
   const int64_t n = static_cast<int64_t>(rows) * cols;
-  const int parts = static_cast<int>(std::min<int64_t>(NORM_BLOCKS, (n + 8191) / 8192));
-  const dim3 ngrid(parts, batch), pgrid(static_cast<unsigned>(std::min<int64_t>((sx / 4 + 255) / 256, 2048)), batch);
-  if (dtype == DT_BF16) {
-    const bf16_t* x = static_cast<const bf16_t*>(g);
-    hipLaunchKernelGGL(norm_kernel<bf16_t>, ngrid, dim3(256), 0, s, x, ldg, stride_g, rows, cols, part);
-    hipLaunchKernelGGL(pack_kernel<bf16_t>, pgrid, dim3(256), 0, s, x, ldg, stride_g, rows, cols, o.rp, o.cp, part,
-                       parts, at(o.x[0]), at(o.xl[0]), sx);
-  } else {
-    const float* x = static_cast<const float*>(g);
-    hipLaunchKernelGGL(norm_kernel<float>, ngrid, dim3(256), 0, s, x, ldg, stride_g, rows, cols, part);
-    hipLaunchKernelGGL(pack_kernel<float>, pgrid, dim3(256), 0, s, x, ldg, stride_g, rows, cols, o.rp, o.cp, part,
-                       parts, at(o.x[0]), at(o.xl[0]), sx);
-  }
+  if (dtype == DT_BF16)
+    launch_pack<bf16_t>(g, ldg, stride_g, batch, rows, cols, o.rp, o.cp, part, at(o.x[0]), at(o.xl[0]), s);
+  else
+    launch_pack<float>(g, ldg, stride_g, batch, rows, cols, o.rp, o.cp, part, at(o.x[0]), at(o.xl[0]), s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int out_mode = out_epi == EPI_ACC_F32 ? 2 : out_epi == EPI_STORE_F32 || dtype == DT_F32 ? 1 : 0;
@@ -262,7 +312,7 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
       p.ns.kp = len / 32;
       p.K = passes * len;
       p.splits = 1;
-      return gemm_ns(p, tile_of(p.M, p.N, passes * p.ns.kp, batch, epi != EPI_NS_STEP), planes, batch, akc, bkc, epi, s);
+      return gemm_ns(p, tile_of(epi - EPI_NS_GRAM, p.M, p.N, passes * p.ns.kp, batch), planes, batch, akc, bkc, epi, s);
     };
     GemmArgs p{};
     p.A = p.B = at(o.x[i]), p.lda = p.ldb = o.cp, p.C = at(o.a), p.ldc = o.k;
@@ -311,7 +361,7 @@ extern "C" void atom_ns_choice(int dtype, int batch, int rows, int cols, int* ou
   using namespace atom;
   const Ws o = layout(dtype, batch, rows, cols);
   const int passes = dtype == DT_F32 ? 3 : 1, lng = std::max(o.rp, o.cp);
-  out[0] = tile_of(o.k, o.k, passes * lng / 32, batch, true);
-  out[1] = tile_of(o.k, o.k, passes * o.k / 32, batch, true);
-  out[2] = tile_of(o.rp, o.cp, passes * o.k / 32, batch, false);
+  out[0] = tile_of(0, o.k, o.k, passes * lng / 32, batch);
+  out[1] = tile_of(1, o.k, o.k, passes * o.k / 32, batch);
+  out[2] = tile_of(2, o.rp, o.cp, passes * o.k / 32, batch);
 }

@@ -214,8 +214,17 @@ def test_extreme_values(dtype):
 
 
 # type, batch, rows, cols, tiles of the three products by the library's rule
-TILES = [("bf16", 1, 1500, 1500, (64, 64, 128)), ("bf16", 12, 700, 760, (128, 128, 192)), ("bf16", 2, 2048, 2050, (192, 192, 192)),
-         ("bf16", 4, 2100, 2048, (256, 256, 192)), ("f32", 2, 2100, 2048, (192, 192, 192)), ("f32", 4, 2048, 2048, (256, 256, 256))]
+TILES = [("bf16", 1, 1500, 1500, (64, 64, 128)),
+         ("bf16", 12, 700, 760, (128, 128, 128)),
+         ("bf16", 2, 2048, 2050, (128, 128, 192)),
+         ("bf16", 4, 2100, 2048, (256, 256, 192)),
+         ("f32", 2, 2100, 2048, (128, 192, 192)),
+         ("f32", 4, 2048, 2048, (256, 256, 256)),
+         ("bf16", 1, 4096, 4160, (192, 192, 192)),
+         ("bf16", 1, 4200, 4096, (192, 192, 192)),
+         ("f32", 1, 3300, 3200, (192, 192, 128)),
+         ("f32", 3, 700, 640, (64, 64, 64)),
+         ("f32", 12, 640, 700, (128, 128, 128))]
 
 
 @pytest.mark.gpu
