@@ -694,6 +694,35 @@ Choice choose_loss(const GemmArgs& g, int esz, bool akc, bool bkc, int epi, doub
   return c;
 }
 
+// Parts of a row of one launch with EPI_LSE: half tiles.
+int lse_parts(const GemmArgs& g, int esz) {
+  const int bn = choose_loss(g, esz, true, true, EPI_LSE).bn;
+  return (g.N + bn - 1) / bn * 2;
+}
+
+// A product along the vocabulary (columns of the logits, rows of dW) runs in
+// two ranges where the first fills whole rounds of the chip with 256x256 tiles,
+// the rest takes smaller ones, and both take less time than tiles of one kind,
+// whose last round is mostly empty (999 rows, vocabulary 50257, width 2048: 788
+// tiles of the logits, three rounds and 20 tiles).  Returns the length of the
+// first range, 0 for one.
+int first_range(const GemmArgs& g, int esz, bool akc, bool bkc, int epi) {
+  const bool cols = epi == EPI_LSE || epi == EPI_DZ;
+  if (esz != 2 || !(cols || !akc)) return 0;
+  const int len = cols ? g.N : g.M;
+  const int64_t across = ((cols ? g.M : g.N) + 255) / 256, along = (len + 255) / 256;
+  const int64_t rounds = across * along / CUS, fit = rounds * CUS / across * 256;
+  if (rounds == 0 || fit >= len) return 0;
+  GemmArgs a = g, b = g;
+  (cols ? a.N : a.M) = static_cast<int>(fit);
+  (cols ? b.N : b.M) = static_cast<int>(len - fit);
+  double one, first, rest;
+  choose_loss(g, esz, akc, bkc, epi, &one);
+  choose_loss(a, esz, akc, bkc, epi, &first);
+  choose_loss(b, esz, akc, bkc, epi, &rest);
+  return first + rest + 3.0 < one ? static_cast<int>(fit) : 0;
+}
+
 }  // namespace
 
 // Shape and alignment rules checked before launch (bounds inside the kernel
@@ -745,20 +774,38 @@ hipError_t gemm_loss(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi, 
   if ((reinterpret_cast<uintptr_t>(g.A) | reinterpret_cast<uintptr_t>(g.B) | reinterpret_cast<uintptr_t>(g.C)) & 15)
     return hipErrorInvalidValue;
   if (epi == EPI_SUM_SCALE && g.ldaux % 4) return hipErrorInvalidValue;
-  const Choice c = choose_loss(g, esz, akc, bkc, epi);
-  return dtype == DT_BF16 ? launch_dl<bf16_t>(g, c, akc, bkc, epi, s) : launch_dl<float>(g, c, akc, bkc, epi, s);
+  auto run = [&](const GemmArgs& r) {
+    const Choice c = choose_loss(r, esz, akc, bkc, epi);
+    return dtype == DT_BF16 ? launch_dl<bf16_t>(r, c, akc, bkc, epi, s) : launch_dl<float>(r, c, akc, bkc, epi, s);
+  };
+  const int cut = first_range(g, esz, akc, bkc, epi);
+  if (cut == 0) return run(g);
+  GemmArgs a = g, b = g;
+  const bool cols = epi == EPI_LSE || epi == EPI_DZ;
+  (cols ? a.N : a.M) = cut;
+  if (cols) {
+    b.N = g.N - cut;
+    b.B = static_cast<const char*>(g.B) + cut * g.ldb * esz;
+    b.v0 = g.v0 + cut;
+    b.C = epi == EPI_DZ ? static_cast<void*>(static_cast<char*>(g.C) + static_cast<int64_t>(cut) * esz)
+                        : static_cast<void*>(static_cast<float2*>(g.C) + lse_parts(a, esz) * g.M);
+  } else {
+    b.M = g.M - cut;
+    b.A = static_cast<const char*>(g.A) + static_cast<int64_t>(cut) * esz;
+    b.C = static_cast<char*>(g.C) + cut * g.ldc * (epi == EPI_SCALE ? esz : 4);
+  }
+  const hipError_t err = run(a);
+  return err == hipSuccess ? run(b) : err;
 }
 
-double gemm_loss_us(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi) {
-  double us = 0.0;
-  choose_loss(g, dtype == DT_BF16 ? 2 : 4, akc, bkc, epi, &us);
-  return us;
-}
-
-int gemm_lse_width(int dtype, int M, int N, int K) {
+int gemm_lse_parts(int dtype, int M, int N, int K) {
   GemmArgs g{};
   g.M = M, g.N = N, g.K = K;
-  return choose_loss(g, dtype == DT_BF16 ? 2 : 4, true, true, EPI_LSE).bn / 2;
+  const int esz = dtype == DT_BF16 ? 2 : 4, cut = first_range(g, esz, true, true, EPI_LSE);
+  if (cut == 0) return lse_parts(g, esz);
+  GemmArgs a = g, b = g;
+  a.N = cut, b.N = N - cut;
+  return lse_parts(a, esz) + lse_parts(b, esz);
 }
 
 }  // namespace atom

@@ -249,7 +249,11 @@ gemm_dl_kernel(GemmArgs g) {
   // epilogue staging: RB rows of a wave's block at a time, PITCH floats per row
   constexpr int RB = TM * 16 < 32 ? TM * 16 : 32, PITCH = TN * 16 + 4;
   constexpr int LDS = std::max(STAGES * (OA::BYTES + OB::BYTES), 4 * RB * PITCH * 4);
+  constexpr bool LOSS = EPI == EPI_LSE || EPI == EPI_DZ;
+  constexpr float LOG2E = 1.4426950408889634f;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[LDS];
+  __shared__ int row_tgt[LOSS ? BM : 1];                           // of the tile's rows: target column,
+  __shared__ float2 row_lse_scale[EPI == EPI_DZ ? BM : 1];         // lse (base 2), factor
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int lr = lane & 15, lg = lane >> 4;
   const int wm = w >> 1, wn = w & 1;
@@ -280,6 +284,20 @@ gemm_dl_kernel(GemmArgs g) {
   if constexpr (NS) {
     g.A = static_cast<const T*>(g.A) + split * g.ns.sa;
     g.B = static_cast<const T*>(g.B) + split * g.ns.sb;
+  }
+
+  // The loss epilogues' row values, requested here and put into LDS behind the
+  // loop, where their latency would be in every tile's way.
+  int my_tgt = -1;
+  float my_lse = 0.f, my_scale = 1.f;
+  if constexpr (LOSS) {
+    if (tid < BM && m0 + tid < g.M) {
+      my_tgt = g.tgt[m0 + tid];
+      if constexpr (EPI == EPI_DZ) {
+        my_lse = g.lse[m0 + tid];
+        if (g.rowscale) my_scale = g.rowscale[m0 + tid];
+      }
+    }
   }
 
   typename OA::Src sra[OA::LPT];
@@ -440,16 +458,25 @@ gemm_dl_kernel(GemmArgs g) {
       for (int j = 0; j < TN; ++j) acc[i][j] = tot[i][j] + (acc[i][j] + acc2[i][j]);
   }
   const int row0 = m0 + wm * TM * 16, col0 = n0 + wn * TN * 16;
+  if constexpr (LOSS) {
+    // (a row of scale zero takes no part, and one with a bad target none but NaN)
+    if (tid < BM) {
+      const bool on = my_tgt >= 0;
+      row_tgt[tid] = my_tgt;
+      if constexpr (EPI == EPI_DZ)
+        row_lse_scale[tid] = on && my_scale != 0.f ? make_float2(my_lse * LOG2E, my_tgt < g.V ? my_scale : NAN)
+                                                   : make_float2(0.f, 0.f);
+    }
+    barrier_after_reads();  // also: every wave is done with the stages
+  }
   // acc[i][j][r] is the logit of row row0 + 16 i + lr, column col0 + 16 j +
   // 4 lg + r: the loss epilogues' row values are per lane and i.
-  constexpr bool LOSS = EPI == EPI_LSE || EPI == EPI_DZ;
-  constexpr float LOG2E = 1.4426950408889634f;
   int trow[LOSS ? TM : 1];  // target column in this wave's block, or outside [0, 16 TN)
   if constexpr (LOSS) {
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int m = row0 + 16 * i + lr;
-      trow[i] = m < g.M ? g.tgt[m] : -1;
+      const int t = row_tgt[wm * TM * 16 + 16 * i + lr];
+      trow[i] = t < 0 || t >= g.V ? -1 : t - g.v0 - col0;
     }
   }
   if constexpr (EPI == EPI_LSE) {
@@ -460,8 +487,7 @@ gemm_dl_kernel(GemmArgs g) {
     const bool edge = col0 + TN * 16 > g.N;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int m = row0 + 16 * i + lr;
-      const int t = trow[i] < 0 || trow[i] >= g.N ? -1 : trow[i] - col0;
+      const int m = row0 + 16 * i + lr, t = trow[i];
       const bool hit = t >= 0 && t < TN * 16 && (t >> 2 & 3) == lg;
       if (__builtin_amdgcn_ballot_w64(hit) != 0) {
         float z = 0.f;
@@ -498,23 +524,12 @@ gemm_dl_kernel(GemmArgs g) {
     }
     return;
   }
-  float lrow[EPI == EPI_DZ ? TM : 1], srow[EPI == EPI_DZ ? TM : 1];
-  if constexpr (EPI == EPI_DZ) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int m = row0 + 16 * i + lr;
-      const bool on = m < g.M && trow[i] >= 0;
-      lrow[i] = on ? g.lse[m] * LOG2E : 0.f;
-      srow[i] = !on ? 0.f : trow[i] >= g.V ? NAN : g.rowscale ? g.rowscale[m] : 1.f;
-      trow[i] -= g.v0 + col0;
-    }
-  }
   // Epilogue through LDS, RB rows of the wave's block at a time: the
   // accumulators go to a wave-private [RB][BN/2] fp32 staging area, and each
   // lane takes back 4 consecutive columns of one row, so a wave's stores (and
   // the epilogue's reads of bias, residual or saved pre-activations) cover
   // whole rows of the block instead of 32-byte pieces of 16 rows.
-  barrier_after_reads();  // every wave is done with the stages
+  if constexpr (!LOSS) barrier_after_reads();  // every wave is done with the stages
   float* stg = reinterpret_cast<float*>(lds) + w * (RB * PITCH);
   // N, ldc and ldaux are multiples of 4 (the launcher checks): a lane's four
   // columns are all inside the matrix or all past it, and every access is one
@@ -578,23 +593,34 @@ gemm_dl_kernel(GemmArgs g) {
       const int mq = row0 + h * RB + rsub;  // row of q = 0; row q is mq + RPP q
       const int64_t cq = static_cast<int64_t>(mq) * ga.ldc + nb, aq = static_cast<int64_t>(mq) * ga.ldaux + nb;
 #pragma unroll
-      for (int ii = 0; ii < RB / 16; ++ii)
+      for (int ii = 0; ii < RB / 16; ++ii) {
+        const int i = h * (RB / 16) + ii;
+        if constexpr (E == EPI_DZ) {
+          // dz = (softmax - onehot) * scale; a row that takes no part has logits
+          // of zero (its row of A is zero) and scale zero.  Four instructions
+          // and the exponential per logit; the one-hot only where it is.
+          const float2 ls = row_lse_scale[wm * TM * 16 + 16 * i + lr];
+          const bool hit = trow[i] >= 0 && trow[i] < TN * 16;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          f32x4_t& a = acc[h * (RB / 16) + ii][j];
-          if constexpr (E == EPI_DZ) {
-            // (softmax - onehot) * scale; a row of scale zero takes no part,
-            // whatever its logits hold
-            const int i = h * (RB / 16) + ii, c = 16 * j + 4 * lg;
+          for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float p = __builtin_amdgcn_exp2f(fmaf(a[r], LOG2E, -lrow[i]));
-              p = (p - (trow[i] == c + r ? 1.f : 0.f)) * srow[i];
-              a[r] = srow[i] == 0.f || (GUARD && col0 + c + r >= ga.N) ? 0.f : p;
+              const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -ls.x)) * ls.y;
+              acc[i][j][r] = GUARD && col0 + 16 * j + 4 * lg + r >= ga.N ? 0.f : p;
             }
+          if (__builtin_amdgcn_ballot_w64(hit) != 0) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[i][j][r] -= trow[i] == 16 * j + 4 * lg + r ? ls.y : 0.f;
           }
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const f32x4_t& a = acc[i][j];
           *reinterpret_cast<float4*>(stg + (ii * 16 + lr) * PITCH + j * 16 + lg * 4) = make_float4(a[0], a[1], a[2], a[3]);
         }
+      }
       float4 sv[NQ];
 #pragma unroll
       for (int q = 0; q < NQ; ++q)

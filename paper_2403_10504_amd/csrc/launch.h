@@ -120,10 +120,8 @@ hipError_t gemm(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, in
 // not k-contiguous A up to the next chunk may be read (they reach no output),
 // and a k-contiguous A holds zeros from K to the next chunk.
 hipError_t gemm_loss(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, int epi, hipStream_t s);
-// Its predicted time in us (the tile choice's model), at M, N, K and ws_bytes of g.
-double gemm_loss_us(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, int epi);
-// Columns of the part of a row that EPI_LSE reduces to one maximum and sum.
-int gemm_lse_width(int dtype, int M, int N, int K);
+// Parts of a row (a maximum and a sum each) that EPI_LSE writes, [part][M].
+int gemm_lse_parts(int dtype, int M, int N, int K);
 
 // LayerNorm over rows of length d (d % 64 == 0, d <= 8192).
 //   y = (x - mean) * rstd * gamma + beta, x fp32, y element type.

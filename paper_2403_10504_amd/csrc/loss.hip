@@ -78,7 +78,8 @@ __global__ void __launch_bounds__(256) lse_join_kernel(const float2* __restrict_
 }
 
 // x with the rows of tokens that take no part set to zero, so that whatever
-// they hold (dz is zero there, and 0 * NaN is not) stays out of dW.
+// they hold stays out of dz (their logits are zero) and of dW (dz is zero there,
+// and 0 * NaN is not).
 __global__ void __launch_bounds__(256) keep_rows_kernel(const uint4* __restrict__ x, int64_t ldc, int cpr,
                                                         const int32_t* __restrict__ tgt,
                                                         const float* __restrict__ drow, int64_t n,
@@ -99,8 +100,34 @@ inline uint64_t up(uint64_t n) { return (n + 255) & ~255ull; }
 inline unsigned blocks(int64_t n) { return static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 4096)); }
 inline int esize(int dtype) { return dtype == DT_BF16 ? 2 : 4; }
 inline int64_t lse_parts(int dtype, int64_t rows, int V, int d) {
-  const int width = gemm_lse_width(dtype, static_cast<int>(rows), V, d);
-  return (V + 2 * width - 1) / (2 * width) * 2;
+  return gemm_lse_parts(dtype, static_cast<int>(rows), V, d);
+}
+
+// The pieces of the vocabulary: `width` columns each, the last one what is left.
+struct Pieces {
+  int width, last;  // last: columns of the last piece, at most 9/8 width
+  int next(int v0, int V) const { return V - v0 <= last ? V - v0 : width; }
+};
+
+// The caller's width, or by default the whole vocabulary where dz of it takes
+// at most 128 MB, half of the Infinity Cache, through which the two products
+// read it, else the largest power of two from 2048 to 16384 within that.
+// Vocabulary 50257, pieces of 4096, 8192, 16384, 32768: 2048 x 5120 3184, 2704,
+// 2595, 2750 us; 4096 x 4096 4057, 3883, 3876, 3908; 999 x 2048 988, 771, 672,
+// 638, whole 660; only with more rows are larger ones faster than this takes
+// (16384 x 768: 3866, 3751, 3524, 3472).  A short rest joins the last piece.
+Pieces pieces_of(int dtype, int64_t rows, int V, int piece) {
+  if (piece > 0) {
+    const int w = static_cast<int>(std::min<int64_t>(V, (piece + 7ll) / 8 * 8));
+    return Pieces{w, w};
+  }
+  const int64_t most = (128ll << 20) / (rows * esize(dtype));
+  if (V <= most) return Pieces{V, V};
+  int w = 16384;
+  while (w > 2048 && w > most) w /= 2;
+  w = std::min(V, w);
+  const int rest = V % w;
+  return Pieces{w, rest > 0 && rest <= w / 8 ? w + rest : w};
 }
 
 // Workspace for few rows: ranges of the vocabulary summed apart (dx), up to 16.
@@ -116,59 +143,17 @@ int ld_of_dz(int dtype, int piece) {
 struct BwdWs {
   uint64_t dz, x, dx, split, split_bytes, end;  // offsets
 };
-BwdWs bwd_ws(int dtype, int64_t rows, int V, int d, int piece) {
+BwdWs bwd_ws(int dtype, int64_t rows, int V, int d, const Pieces& p) {
   const uint64_t e = esize(dtype), n = rows;
-  const int ldz = ld_of_dz(dtype, piece);
+  const int ldz = ld_of_dz(dtype, p.last);
   BwdWs w;
   w.dz = 0;
   w.x = w.dz + up(n * ldz * e);
   w.dx = w.x + up(n * d * e);
-  w.split = w.dx + (dtype == DT_BF16 && piece < V ? up(n * d * 4) : 0);
+  w.split = w.dx + (dtype == DT_BF16 && p.last < V ? up(n * d * 4) : 0);
   w.split_bytes = split_bytes(rows, d);
   w.end = w.split + w.split_bytes;
   return w;
-}
-
-// Predicted time of both gradients in pieces of `width` columns.
-double bwd_us(int dtype, int64_t rows, int V, int d, int width) {
-  GemmArgs z{}, dx{}, dw{};
-  float some;
-  z.M = dx.M = dw.K = static_cast<int>(rows);
-  z.K = dx.N = dw.N = d;
-  dx.ws = dw.ws = &some;
-  dx.ws_bytes = dw.ws_bytes = split_bytes(rows, d);
-  auto piece = [&](int n, int epi) {
-    z.N = dx.K = dw.M = n;
-    return gemm_loss_us(z, dtype, true, true, EPI_DZ) + gemm_loss_us(dx, dtype, true, false, epi) +
-           gemm_loss_us(dw, dtype, false, false, EPI_SCALE);
-  };
-  const int whole = V / width, rest = V % width;
-  return whole * piece(width, EPI_SCALE_ACC) + (rest ? piece(rest, EPI_SUM_SCALE) : 0.0);
-}
-
-// Columns of a piece: the caller's, or by default the whole vocabulary where dz
-// of it takes at most 128 MB, half of the Infinity Cache, through which the two
-// products read it; else the width within that (2048 at least) with the
-// smallest predicted time, of the vocabulary in equal parts and of multiples of
-// 4096.  What varies is how many rounds of tiles the three products take
-// (2048 x 5120, vocabulary 50257: 2991 us in pieces of 8192, with 640 tiles of
-// dW and 256 of z on 256 CUs).
-int piece_of(int dtype, int64_t rows, int V, int d, int piece) {
-  if (piece > 0) return static_cast<int>(std::min<int64_t>(V, (piece + 7ll) / 8 * 8));
-  const int64_t most = std::max<int64_t>(2048, (128ll << 20) / (rows * esize(dtype)));
-  if (V <= most) return V;
-  int best = 0;
-  double best_us = 0.0;
-  auto consider = [&](int64_t width) {
-    if (width > most || width < 1) return;
-    const double us = bwd_us(dtype, rows, V, d, static_cast<int>(width));
-    if (best == 0 || us < best_us) best = static_cast<int>(width), best_us = us;
-  };
-  consider(most / 256 * 256);
-  const int64_t n = (V + most - 1) / most;
-  for (int64_t k = n; k < n + 4; ++k) consider(((V + k - 1) / k + 255) / 256 * 256);
-  for (int64_t k = 1; k <= 4; ++k) consider(4096 * k);
-  return best;
 }
 
 }  // namespace
@@ -195,7 +180,7 @@ hipError_t linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w,
   g.M = static_cast<int>(rows), g.N = V, g.K = d;
   g.ztgt = static_cast<float*>(ws);
   g.C = static_cast<char*>(ws) + up(rows * sizeof(float));
-  g.tgt = tgt;
+  g.tgt = tgt, g.V = V;
   hipError_t e = gemm_loss(g, dtype, true, true, EPI_LSE, s);
   if (e != hipSuccess) return e;
   const float2* part = static_cast<const float2*>(g.C);
@@ -209,7 +194,7 @@ hipError_t linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w,
 }
 
 uint64_t linear_xent_bwd_ws(int dtype, int64_t rows, int V, int d, int piece) {
-  return rows == 0 ? 0 : bwd_ws(dtype, rows, V, d, piece_of(dtype, rows, V, d, piece)).end;
+  return rows == 0 ? 0 : bwd_ws(dtype, rows, V, d, pieces_of(dtype, rows, V, piece)).end;
 }
 
 hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
@@ -225,12 +210,12 @@ hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w,
                        wpr, n);
     return hipGetLastError();
   }
-  piece = piece_of(dtype, rows, V, d, piece);
-  const BwdWs o = bwd_ws(dtype, rows, V, d, piece);
+  const Pieces pc = pieces_of(dtype, rows, V, piece);
+  const BwdWs o = bwd_ws(dtype, rows, V, d, pc);
   char* base = static_cast<char*>(ws);
-  const int ldz = ld_of_dz(dtype, piece);
+  const int ldz = ld_of_dz(dtype, pc.last);
   char* xz = base + o.x;
-  if (dw) {
+  {
     const int cpr = d * esz / 16;
     const int64_t n = rows * cpr;
     hipLaunchKernelGGL(keep_rows_kernel, dim3(blocks(n)), dim3(256), 0, s, static_cast<const uint4*>(x),
@@ -241,11 +226,11 @@ hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w,
   // the sum over the pieces: in dx itself (fp32), or beside it
   float* sum = dtype == DT_BF16 ? reinterpret_cast<float*>(base + o.dx) : static_cast<float*>(dx);
   const int64_t ldsum = dtype == DT_BF16 ? d : lddx;
-  for (int v0 = 0; v0 < V; v0 += piece) {
-    const int n = std::min(piece, V - v0);
+  for (int v0 = 0, n; v0 < V; v0 += n) {
+    n = pc.next(v0, V);
     const char* wp = static_cast<const char*>(w) + static_cast<int64_t>(v0) * ldw * esz;
     GemmArgs g{};
-    g.A = x, g.lda = ldx, g.B = wp, g.ldb = ldw, g.C = base, g.ldc = ldz;
+    g.A = xz, g.lda = d, g.B = wp, g.ldb = ldw, g.C = base, g.ldc = ldz;
     g.M = static_cast<int>(rows), g.N = n, g.K = d;
     g.tgt = tgt, g.lse = lse, g.rowscale = drow, g.v0 = v0, g.V = V;
     hipError_t e = gemm_loss(g, dtype, true, true, EPI_DZ, s);
