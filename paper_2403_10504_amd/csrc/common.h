@@ -42,6 +42,24 @@ ATOM_DEV uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2v{a, b}), b2v));
 }
 
+// v = h + m + l in three bf16 planes (p[0] h): 24 bits, each the rest's nearest
+// bf16; h is cut, not rounded, where rounding would overflow a finite value.
+ATOM_DEV void pack_three(const float* v, uint2* p) {
+  float r[4], h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = v[i];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[i] = bf2f(f2bf(r[i]));
+      if (k == 0 && __builtin_isinf(h[i])) h[i] = __uint_as_float(__float_as_uint(r[i]) & 0xffff0000u);
+      r[i] -= h[i];
+    }
+    p[k] = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
+  }
+}
+
 template <typename T> ATOM_DEV float to_f(T v);
 template <> ATOM_DEV float to_f<float>(float v) { return v; }
 template <> ATOM_DEV float to_f<bf16_t>(bf16_t v) { return bf2f(v); }

@@ -638,6 +638,12 @@ bool stream_result(const GemmArgs& g, int epi, int splits) {
 
 template <typename T>
 hipError_t launch_tile(const GemmArgs& g, const Choice& c, bool akc, bool bkc, int epi, hipStream_t s) {
+  if (g.pl.kp)
+    return c.bm == 64    ? gemm_planes_64(g, akc, bkc, epi, s)
+           : c.bm == 128 ? gemm_planes_128(g, akc, bkc, epi, s)
+           : c.bn == 128 ? gemm_planes_256x128(g, akc, bkc, epi, s)
+           : c.bn == 192 ? gemm_planes_192(g, akc, bkc, epi, s)
+                         : gemm_planes_256(g, akc, bkc, epi, s);
   if (epi >= EPI_LSE) {
     if constexpr (sizeof(T) == 4)
       return c.bm == 64 ? gemm_loss_f32_64(g, akc, bkc, epi, s) : gemm_loss_f32_32(g, akc, bkc, epi, s);
@@ -762,21 +768,24 @@ hipError_t gemm(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi, hipSt
 }
 
 hipError_t gemm_loss(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi, hipStream_t s) {
-  const int esz = dtype == DT_BF16 ? 2 : 4, e = 16 / esz;
-  if (!(gemm_loss_combo(akc, bkc, epi) || (epi == EPI_STORE_F32 && akc && !bkc))) return hipErrorInvalidValue;
+  const bool planes = g.pl.kp > 0;
+  const int esz = dtype == DT_BF16 || planes ? 2 : 4, e = 16 / esz;
+  if (planes ? !(epi == EPI_LSE || epi == EPI_DZ || epi == EPI_SCALE_F32 || epi == EPI_SCALE_ACC) || (bkc && !akc)
+             : !(gemm_loss_combo(akc, bkc, epi) || (epi == EPI_STORE_F32 && akc && !bkc))) return hipErrorInvalidValue;
   // whole chunks in memory: leading dimensions, k of two k-contiguous operands
   // (each is read in full chunks), columns of a not k-contiguous B
   if (g.M <= 0 || g.N <= 0 || g.K <= 0 || g.lda % e || g.ldb % e || g.ldc % 4) return hipErrorInvalidValue;
-  if (bkc ? g.K % e : g.N % e) return hipErrorInvalidValue;
-  const int64_t kpad = (g.K + e - 1) / e * e, mpad = (g.M + e - 1) / e * e;
-  if (akc ? g.lda < kpad : g.lda < mpad) return hipErrorInvalidValue;
-  if (bkc ? g.ldb < g.K : g.ldb < g.N) return hipErrorInvalidValue;
+  if (planes ? g.N % 4 && epi != EPI_LSE && epi != EPI_DZ : bkc ? g.K % e : g.N % e) return hipErrorInvalidValue;
+  auto whole = [&](int n) { return (n + static_cast<int64_t>(e) - 1) / e * e; };
+  const int k = planes ? g.pl.k : g.K;
+  if (akc ? g.lda < whole(k) : g.lda < whole(g.M)) return hipErrorInvalidValue;
+  if (bkc ? g.ldb < whole(k) : g.ldb < whole(g.N)) return hipErrorInvalidValue;
   if ((reinterpret_cast<uintptr_t>(g.A) | reinterpret_cast<uintptr_t>(g.B) | reinterpret_cast<uintptr_t>(g.C)) & 15)
     return hipErrorInvalidValue;
   if (epi == EPI_SUM_SCALE && g.ldaux % 4) return hipErrorInvalidValue;
   auto run = [&](const GemmArgs& r) {
     const Choice c = choose_loss(r, esz, akc, bkc, epi);
-    return dtype == DT_BF16 ? launch_dl<bf16_t>(r, c, akc, bkc, epi, s) : launch_dl<float>(r, c, akc, bkc, epi, s);
+    return dtype == DT_BF16 || planes ? launch_dl<bf16_t>(r, c, akc, bkc, epi, s) : launch_dl<float>(r, c, akc, bkc, epi, s);
   };
   const int cut = first_range(g, esz, akc, bkc, epi);
   if (cut == 0) return run(g);

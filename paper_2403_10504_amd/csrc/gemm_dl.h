@@ -89,6 +89,12 @@ struct Operand {
       if constexpr (TAIL) s = kt * BK + k < K ? s : static_cast<const void*>(zero_chunk);
       lds_dma16(s, __builtin_amdgcn_readfirstlane(lds_offset(stage) + group * 1024));
     }
+    template <bool TAIL>
+    __device__ __forceinline__ void load_plane(uint8_t* stage, int kt, int K, int64_t off, int group) const {
+      const void* s = p + off + kt * kstep;
+      if constexpr (TAIL) s = kt * BK + k < K ? s : static_cast<const void*>(zero_chunk);
+      lds_dma16(s, __builtin_amdgcn_readfirstlane(lds_offset(stage) + group * 1024));
+    }
     // the tile's chunk `off` elements on (another plane), k whole tiles
     __device__ __forceinline__ void load_plane(uint8_t* stage, int kt, int64_t off, int group) const {
       lds_dma16(p + off + kt * kstep, __builtin_amdgcn_readfirstlane(lds_offset(stage) + group * 1024));
@@ -234,8 +240,10 @@ constexpr int occupancy() {
 // whole group of four, the last tile may reach past k, and every load tests its
 // chunk (three vector instructions: 3-4 % at 4096x12288x4096, so whole groups
 // take the copy without).
-// PASSES (Newton-Schulz products of two planes): k runs three times, over hi
-// hi, hi lo and lo hi of A and B; lo lo is below the sums' own rounding.
+// PASSES (Newton-Schulz products of two planes, 3): k runs three times, over hi
+// hi, hi lo and lo hi of A and B; lo lo is below the sums' own rounding.  6
+// (fp32 as three bf16 planes): h l, l h, m m, h m, m h and h h, the small ones
+// first, while the sums are small; m l, l m and l l are below 2^-23.
 template <typename T, bool AKC, bool BKC, int EPI, int BM, int BN, bool TAIL, int PASSES = 1>
 __global__ void __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(occupancy<T, BM, BN>(), occupancy<T, BM, BN>())))
 gemm_dl_kernel(GemmArgs g) {
@@ -305,7 +313,7 @@ gemm_dl_kernel(GemmArgs g) {
 #pragma unroll
   for (int q = 0; q < OA::LPT; ++q) sra[q].init(static_cast<const T*>(g.A), g.lda, m0, AKC ? g.M : (g.M + OA::E - 1) / OA::E * OA::E, q * NT + tid);
 #pragma unroll
-  for (int q = 0; q < OB::LPT; ++q) srb[q].init(static_cast<const T*>(g.B), g.ldb, n0, g.N, q * NT + tid);
+  for (int q = 0; q < OB::LPT; ++q) srb[q].init(static_cast<const T*>(g.B), g.ldb, n0, BKC ? g.N : (g.N + OB::E - 1) / OB::E * OB::E, q * NT + tid);
   // k tiles of this workgroup: kquads groups of four per split, the rest in
   // the last one (the launcher leaves none empty).  With TAIL the last group
   // may be short: only the tiles that hold k are loaded and multiplied
@@ -323,7 +331,8 @@ gemm_dl_kernel(GemmArgs g) {
   // of one XCD share operand tiles through its L2, so they keep one offset.
   // (Newton-Schulz products: the tile's eighth of its matrix's tiles, which is
   // about the same; equal matrices of a batch get equal bits.)
-  const int koff = ((NS ? pid * 8 / tiles : xcd) * (nk4 >> 3)) & ~3;
+  // (Three planes: the passes keep their order.)
+  const int koff = PASSES == 6 ? 0 : ((NS ? pid * 8 / tiles : xcd) * (nk4 >> 3)) & ~3;
   auto rot = [&](int kt) {
     const int r = kt + koff;
     return kbase + (r >= nk ? r - nk : r);
@@ -360,7 +369,16 @@ gemm_dl_kernel(GemmArgs g) {
   auto stage_a = [&](int s) -> uint8_t* { return lds + s * OA::BYTES; };
   auto stage_b = [&](int s) -> uint8_t* { return lds + STAGES * OA::BYTES + s * OB::BYTES; };
   auto load = [&](int s, int kt, int l) {
-    if constexpr (NS) {
+    if constexpr (PASSES == 6) {
+      const int kp = g.pl.kp;
+      int pass = 0;
+#pragma unroll
+      for (int i = 1; i < 6; ++i) pass += kt >= i * kp;
+      kt -= pass * kp;
+      const int64_t oa = (0x010120 >> 4 * pass & 3) * g.pl.pa, ob = (0x001102 >> 4 * pass & 3) * g.pl.pb;
+      if (l < OA::LPT) sra[l < OA::LPT ? l : 0].template load_plane<true>(stage_a(s), kt, g.pl.k, oa, l * 4 + w);
+      else srb[l < OA::LPT ? 0 : l - OA::LPT].template load_plane<true>(stage_b(s), kt, g.pl.k, ob, (l - OA::LPT) * 4 + w);
+    } else if constexpr (NS) {
       int64_t oa = 0, ob = 0;
       if constexpr (PASSES == 3) {
         if (kt >= 2 * g.ns.kp) kt -= 2 * g.ns.kp, oa = g.ns.pa;
@@ -666,7 +684,11 @@ gemm_dl_kernel(GemmArgs g) {
           if (g.stream) stream4(static_cast<float*>(ga.C) + off, v);
           else pack4(static_cast<float*>(ga.C) + off, v);
         } else if constexpr (F32_OUT) pack4(static_cast<float*>(ga.C) + off, v);
-        else pack4(static_cast<T*>(ga.C) + off, v);
+        else if constexpr (PASSES == 6) {
+          uint2 pl[3];
+          pack_three(v, pl);
+          for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(static_cast<T*>(ga.C) + i * ga.pl.pc + off) = pl[i];
+        } else pack4(static_cast<T*>(ga.C) + off, v);
       }
     }
   };
@@ -849,6 +871,29 @@ hipError_t launch_loss(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream
   ATOM_DL(true, false, EPI_SCALE_ACC)
   ATOM_DL(true, false, EPI_SUM_SCALE)
   ATOM_DL(false, false, EPI_SCALE)
+  ATOM_DL(false, false, EPI_SCALE_F32)
+  ATOM_DL(false, false, EPI_SCALE_ACC)
+#undef ATOM_DL
+  return hipErrorInvalidValue;
+}
+
+// The loss products of fp32 operands in three bf16 planes (g.K counts all
+// passes).
+template <int BM, int BN>
+hipError_t launch_planes(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s) {
+  const int tiles = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
+  const dim3 grid(static_cast<unsigned>(tiles * g.splits)), block(NT);
+#define ATOM_DL(AK, BK_, E)                                                                           \
+  if (akc == AK && bkc == BK_ && epi == E) {                                                          \
+    hipLaunchKernelGGL((gemm_dl_kernel<bf16_t, AK, BK_, E, BM, BN, true, 6>), grid, block, 0, s, g);  \
+    return hipGetLastError();                                                                         \
+  }
+  ATOM_DL(true, true, EPI_LSE)
+  ATOM_DL(true, true, EPI_DZ)
+  ATOM_DL(true, false, EPI_STORE_F32)
+  ATOM_DL(true, false, EPI_SCALE_F32)
+  ATOM_DL(true, false, EPI_SCALE_ACC)
+  ATOM_DL(false, false, EPI_STORE_F32)
   ATOM_DL(false, false, EPI_SCALE_F32)
   ATOM_DL(false, false, EPI_SCALE_ACC)
 #undef ATOM_DL

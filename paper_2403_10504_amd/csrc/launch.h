@@ -37,7 +37,7 @@ enum Epilogue {
 struct NsArgs {
   int64_t sa, sb, sc;        // elements from one matrix of the batch to the next: A, B; C and aux
   int64_t pa, pb;            // elements from the hi to the lo plane of A and B
-  int kp;                    // k tiles of 32 of one pass over k (two planes: three passes)
+  int kp;                    // k tiles of 32 of one pass over k (two planes: three passes, three: six)
   const void *aux, *aux_lo;  // as C
   void* C_lo;
   float beta;
@@ -48,6 +48,14 @@ struct NsArgs {
   int orows, ocols;
   bool vec;                  // out's rows hold whole aligned 4-vectors
   float scale, keep;
+};
+
+// A product of fp32 operands held as three bf16 planes each (x = h + m + l,
+// loss.hip): pa, pb and kp above, the k of one pass, and the planes of EPI_DZ's
+// result.
+struct PlaneArgs {
+  int64_t pa, pb, pc;
+  int kp, k;  // kp 0: not such a product
 };
 
 struct GemmArgs {
@@ -71,6 +79,7 @@ struct GemmArgs {
   float* ztgt;            // EPI_LSE: receives acc at each row's target
   int v0, V;              // EPI_DZ: column 0 is column v0 of the V of the vocabulary
   NsArgs ns;
+  PlaneArgs pl;
 };
 
 // The layout and epilogue combinations of the training step: forward, data
@@ -105,6 +114,11 @@ hipError_t gemm_loss_192(const GemmArgs& g, bool akc, bool bkc, int epi, hipStre
 hipError_t gemm_loss_256x128(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 hipError_t gemm_loss_128(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 hipError_t gemm_loss_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_planes_256(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);  // three planes
+hipError_t gemm_planes_192(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_planes_256x128(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_planes_128(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
+hipError_t gemm_planes_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 hipError_t gemm_loss_f32_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 hipError_t gemm_loss_f32_32(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 
@@ -118,10 +132,13 @@ hipError_t gemm(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, in
 // EPI_STORE_F32 with A k-contiguous and B not.  Unlike gemm(),
 // M and K may be any length where the memory of A holds whole chunks: rows of a
 // not k-contiguous A up to the next chunk may be read (they reach no output),
-// and a k-contiguous A holds zeros from K to the next chunk.
+// and a k-contiguous A holds zeros from K to the next chunk.  With g.pl.kp, A
+// and B are three bf16 planes, N and K any multiples of 4 (operands hold zeros
+// up to whole chunks), and the results fp32: EPI_LSE, EPI_DZ (three planes),
+// EPI_SCALE_F32 and EPI_SCALE_ACC.
 hipError_t gemm_loss(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, int epi, hipStream_t s);
 // Parts of a row (a maximum and a sum each) that EPI_LSE writes, [part][M].
-int gemm_lse_parts(int dtype, int M, int N, int K);
+int gemm_lse_parts(int dtype, int M, int N, int K);  // (three planes: bf16, six times the k)
 
 // LayerNorm over rows of length d (d % 64 == 0, d <= 8192).
 //   y = (x - mean) * rstd * gamma + beta, x fp32, y element type.

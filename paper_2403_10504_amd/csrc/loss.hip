@@ -29,6 +29,7 @@ namespace atom {
 namespace {
 
 constexpr float LN2 = 0.6931471805599453f;
+constexpr int PLANE_ROWS = 256;
 
 // RPB rows per workgroup, 256 / RPB threads per row, each over every
 // (256 / RPB)-th part; the threads' (max, sum) pairs join in LDS in a fixed
@@ -91,6 +92,30 @@ __global__ void __launch_bounds__(256) keep_rows_kernel(const uint4* __restrict_
   }
 }
 
+// Rows of an fp32 matrix as three bf16 planes [rows][dp], zeros from column d
+// on; with tgt, rows that take no part are zero, as above.
+__global__ void __launch_bounds__(256) planes_kernel(const float* __restrict__ x, int64_t ldx, int d, int dp,
+                                                     const int32_t* __restrict__ tgt, const float* __restrict__ drow,
+                                                     int64_t n, bf16_t* __restrict__ y, int64_t plane) {
+  const int cpr = dp / 8;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t row = i / cpr;
+    const int c = static_cast<int>(i - row * cpr) * 8;
+    const bool on = !tgt || (tgt[row] >= 0 && !(drow && drow[row] == 0.f));
+    uint2 p[2][3];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // d is a multiple of 4
+      const float4 v = on && c + 4 * h < d ? *reinterpret_cast<const float4*>(x + row * ldx + c + 4 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float f[4] = {v.x, v.y, v.z, v.w};
+      pack_three(f, p[h]);
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      *reinterpret_cast<uint4*>(y + k * plane + row * dp + c) = make_uint4(p[0][k].x, p[0][k].y, p[1][k].x, p[1][k].y);
+  }
+}
+
 __global__ void __launch_bounds__(256) zero_rows_kernel(uint32_t* __restrict__ y, int64_t ldw, int wpr, int64_t n) {
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256)
     y[i / wpr * ldw + i % wpr] = 0;
@@ -99,8 +124,32 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(uint32_t* __restrict__ y
 inline uint64_t up(uint64_t n) { return (n + 255) & ~255ull; }
 inline unsigned blocks(int64_t n) { return static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 4096)); }
 inline int esize(int dtype) { return dtype == DT_BF16 ? 2 : 4; }
-inline int64_t lse_parts(int dtype, int64_t rows, int V, int d) {
-  return gemm_lse_parts(dtype, static_cast<int>(rows), V, d);
+
+// fp32 as three bf16 planes (x = h + m + l, 24 bits) and six passes of bf16
+// MFMAs, two to three times the rate of fp32 ones; w's planes, 10 bytes of
+// memory traffic an entry each time, want rows to pay for them.
+bool planes(int dtype, int64_t rows) { return dtype == DT_F32 && rows >= PLANE_ROWS; }
+// Columns of a row of planes, an odd number of 128-byte lines.
+int plane_ld(int d) { return ((d + 63) / 64 | 1) * 64; }
+// Rows of w that are planes at a time: 96 MB, 1024 rows at least.
+int plane_rows(int V, int d) {
+  return static_cast<int>(std::min<int64_t>(V, std::max<int64_t>(1024, (96ll << 20) / (6 * plane_ld(d)) / 256 * 256)));
+}
+GemmArgs plane_args(const bf16_t* A, int64_t lda, int64_t pa, const bf16_t* B, int64_t ldb, int64_t pb, int M, int N, int K) {
+  GemmArgs g{};
+  g.A = A, g.lda = lda, g.B = B, g.ldb = ldb;
+  g.M = M, g.N = N;
+  g.pl = PlaneArgs{pa, pb, 0, (K + 31) / 32, K};
+  g.K = 6 * 32 * g.pl.kp;
+  return g;
+}
+hipError_t to_planes(const void* x, int64_t ldx, int64_t rows, int d, const int32_t* tgt, const float* drow, bf16_t* y,
+                     hipStream_t s) {
+  const int dp = plane_ld(d);
+  const int64_t n = rows * (dp / 8);
+  hipLaunchKernelGGL(planes_kernel, dim3(blocks(n)), dim3(256), 0, s, static_cast<const float*>(x), ldx, d, dp, tgt,
+                     drow, n, y, rows * dp);
+  return hipGetLastError();
 }
 
 // The pieces of the vocabulary: `width` columns each, the last one what is left.
@@ -116,12 +165,14 @@ struct Pieces {
 // 2595, 2750 us; 4096 x 4096 4057, 3883, 3876, 3908; 999 x 2048 988, 771, 672,
 // 638, whole 660; only with more rows are larger ones faster than this takes
 // (16384 x 768: 3866, 3751, 3524, 3472).  A short rest joins the last piece.
-Pieces pieces_of(int dtype, int64_t rows, int V, int piece) {
+// (Three planes: within 128 MB of dz and of w's planes.)
+Pieces pieces_of(int dtype, int64_t rows, int V, int d, int piece) {
   if (piece > 0) {
     const int w = static_cast<int>(std::min<int64_t>(V, (piece + 7ll) / 8 * 8));
     return Pieces{w, w};
   }
-  const int64_t most = (128ll << 20) / (rows * esize(dtype));
+  const int64_t most = planes(dtype, rows) ? (128ll << 20) / (6 * std::max<int64_t>(rows, plane_ld(d)))
+                                           : (128ll << 20) / (rows * esize(dtype));
   if (V <= most) return Pieces{V, V};
   int w = 16384;
   while (w > 2048 && w > most) w /= 2;
@@ -135,21 +186,24 @@ uint64_t split_bytes(int64_t rows, int d) { return std::min<uint64_t>(up(16ull *
 
 // Rows of dz start an odd number of 256-byte lines apart: pieces are multiples
 // of 4 KB or more, and rows that far apart crowd a few memory channels.
-int ld_of_dz(int dtype, int piece) {
-  const int line = 256 / esize(dtype);
+int ld_of_dz(int dtype, int64_t rows, int piece) {
+  const int line = 256 / (planes(dtype, rows) ? 2 : esize(dtype));
   return ((piece + line - 1) / line | 1) * line;
 }
 
 struct BwdWs {
-  uint64_t dz, x, dx, split, split_bytes, end;  // offsets
+  uint64_t dz, x, w, dx, split, split_bytes, end;  // offsets
 };
 BwdWs bwd_ws(int dtype, int64_t rows, int V, int d, const Pieces& p) {
-  const uint64_t e = esize(dtype), n = rows;
-  const int ldz = ld_of_dz(dtype, p.last);
+  const bool three = planes(dtype, rows);
+  const uint64_t e = three ? 6 : esize(dtype), n = rows;
+  const int ldz = ld_of_dz(dtype, rows, p.last);
+  const uint64_t wide = three ? plane_ld(d) : d;
   BwdWs w;
   w.dz = 0;
   w.x = w.dz + up(n * ldz * e);
-  w.dx = w.x + up(n * d * e);
+  w.w = w.x + up(n * wide * e);
+  w.dx = w.w + (three ? up(p.last * wide * e) : 0);
   w.split = w.dx + (dtype == DT_BF16 && p.last < V ? up(n * d * 4) : 0);
   w.split_bytes = split_bytes(rows, d);
   w.end = w.split + w.split_bytes;
@@ -166,35 +220,77 @@ bool linear_xent_ok(int dtype, int64_t rows, int V, int d) {
          ((rows + 31) / 32) * ((static_cast<int64_t>(d) + 31) / 32) < (1ll << 30);
 }
 
+namespace {
+struct FwdWs {
+  uint64_t ztgt, x, w, part, end;  // offsets
+  int64_t parts;
+  int range;  // rows of w at a time
+};
+FwdWs fwd_ws(int dtype, int64_t rows, int V, int d) {
+  FwdWs w;
+  const bool three = planes(dtype, rows);
+  const int m = static_cast<int>(rows);
+  w.range = three ? plane_rows(V, d) : V;
+  w.parts = 0;
+  for (int v0 = 0; v0 < V; v0 += w.range) {
+    const int n = std::min(w.range, V - v0);
+    w.parts += three ? gemm_lse_parts(DT_BF16, m, n, 6 * 32 * ((d + 31) / 32)) : gemm_lse_parts(dtype, m, n, d);
+  }
+  w.ztgt = 0;
+  w.x = up(rows * sizeof(float));
+  w.w = w.x + (three ? up(6ull * rows * plane_ld(d)) : 0);
+  w.part = w.w + (three ? up(6ull * w.range * plane_ld(d)) : 0);
+  w.end = w.part + w.parts * rows * sizeof(float2);
+  return w;
+}
+}  // namespace
+
 uint64_t linear_xent_fwd_ws(int dtype, int64_t rows, int V, int d) {
-  if (rows == 0) return 0;
-  return up(rows * sizeof(float)) + lse_parts(dtype, rows, V, d) * rows * sizeof(float2);
+  return rows == 0 ? 0 : fwd_ws(dtype, rows, V, d).end;
 }
 
 hipError_t linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
                            float* lse, float* loss_rows, int64_t rows, int V, int d, void* ws, hipStream_t s) {
   if (rows == 0) return hipSuccess;
-  const int64_t parts = lse_parts(dtype, rows, V, d);
-  GemmArgs g{};
-  g.A = x, g.lda = ldx, g.B = w, g.ldb = ldw;
-  g.M = static_cast<int>(rows), g.N = V, g.K = d;
-  g.ztgt = static_cast<float*>(ws);
-  g.C = static_cast<char*>(ws) + up(rows * sizeof(float));
-  g.tgt = tgt, g.V = V;
-  hipError_t e = gemm_loss(g, dtype, true, true, EPI_LSE, s);
+  const FwdWs o = fwd_ws(dtype, rows, V, d);
+  char* base = static_cast<char*>(ws);
+  float* ztgt = reinterpret_cast<float*>(base + o.ztgt);
+  float2* part = reinterpret_cast<float2*>(base + o.part);
+  const int m = static_cast<int>(rows);
+  hipError_t e;
+  if (planes(dtype, rows)) {
+    const int dp = plane_ld(d);
+    bf16_t *xp = reinterpret_cast<bf16_t*>(base + o.x), *wp = reinterpret_cast<bf16_t*>(base + o.w);
+    e = to_planes(x, ldx, rows, d, nullptr, nullptr, xp, s);
+    float2* at = part;
+    for (int v0 = 0; v0 < V && e == hipSuccess; v0 += o.range) {
+      const int n = std::min(o.range, V - v0);
+      e = to_planes(static_cast<const float*>(w) + v0 * ldw, ldw, n, d, nullptr, nullptr, wp, s);
+      if (e != hipSuccess) return e;
+      GemmArgs g = plane_args(xp, dp, rows * dp, wp, dp, static_cast<int64_t>(n) * dp, m, n, d);
+      g.ztgt = ztgt, g.C = at, g.tgt = tgt, g.v0 = v0, g.V = V;
+      e = gemm_loss(g, dtype, true, true, EPI_LSE, s);
+      at += gemm_lse_parts(DT_BF16, m, n, g.K) * rows;
+    }
+  } else {
+    GemmArgs g{};
+    g.A = x, g.lda = ldx, g.B = w, g.ldb = ldw;
+    g.M = m, g.N = V, g.K = d;
+    g.ztgt = ztgt, g.C = part, g.tgt = tgt, g.V = V;
+    e = gemm_loss(g, dtype, true, true, EPI_LSE, s);
+  }
   if (e != hipSuccess) return e;
-  const float2* part = static_cast<const float2*>(g.C);
   if (rows < 2048)
     hipLaunchKernelGGL(lse_join_kernel<1>, dim3(static_cast<unsigned>(rows)), dim3(256), 0, s, part, rows,
-                       static_cast<int>(parts), tgt, g.ztgt, V, lse, loss_rows);
+                       static_cast<int>(o.parts), tgt, ztgt, V, lse, loss_rows);
   else
     hipLaunchKernelGGL(lse_join_kernel<16>, dim3(static_cast<unsigned>((rows + 15) / 16)), dim3(256), 0, s, part, rows,
-                       static_cast<int>(parts), tgt, g.ztgt, V, lse, loss_rows);
+                       static_cast<int>(o.parts), tgt, ztgt, V, lse, loss_rows);
   return hipGetLastError();
 }
 
 uint64_t linear_xent_bwd_ws(int dtype, int64_t rows, int V, int d, int piece) {
-  return rows == 0 ? 0 : bwd_ws(dtype, rows, V, d, pieces_of(dtype, rows, V, piece)).end;
+  return rows == 0 ? 0 : bwd_ws(dtype, rows, V, d, pieces_of(dtype, rows, V, d, piece)).end;
 }
 
 hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
@@ -210,11 +306,40 @@ hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w,
                        wpr, n);
     return hipGetLastError();
   }
-  const Pieces pc = pieces_of(dtype, rows, V, piece);
+  const Pieces pc = pieces_of(dtype, rows, V, d, piece);
   const BwdWs o = bwd_ws(dtype, rows, V, d, pc);
   char* base = static_cast<char*>(ws);
-  const int ldz = ld_of_dz(dtype, pc.last);
+  const int ldz = ld_of_dz(dtype, rows, pc.last);
   char* xz = base + o.x;
+  if (planes(dtype, rows)) {
+    const int dp = plane_ld(d), m = static_cast<int>(rows);
+    bf16_t *zp = reinterpret_cast<bf16_t*>(base), *xp = reinterpret_cast<bf16_t*>(xz), *wp = reinterpret_cast<bf16_t*>(base + o.w);
+    const int64_t px = rows * dp, pz = rows * ldz;
+    hipError_t e = to_planes(x, ldx, rows, d, tgt, drow, xp, s);
+    for (int v0 = 0, n; v0 < V && e == hipSuccess; v0 += n) {
+      n = pc.next(v0, V);
+      const int64_t pw = static_cast<int64_t>(n) * dp;
+      e = to_planes(static_cast<const float*>(w) + v0 * ldw, ldw, n, d, nullptr, nullptr, wp, s);
+      if (e != hipSuccess) return e;
+      GemmArgs g = plane_args(xp, dp, px, wp, dp, pw, m, n, d);
+      g.C = zp, g.ldc = ldz, g.pl.pc = pz;
+      g.tgt = tgt, g.lse = lse, g.rowscale = drow, g.v0 = v0, g.V = V;
+      e = gemm_loss(g, dtype, true, true, EPI_DZ, s);
+      if (e == hipSuccess && dx) {
+        GemmArgs a = plane_args(zp, ldz, pz, wp, dp, pw, m, d, n);
+        a.C = dx, a.ldc = lddx, a.alpha = scale;
+        a.ws = reinterpret_cast<float*>(base + o.split), a.ws_bytes = o.split_bytes;
+        e = gemm_loss(a, dtype, true, false, v0 == 0 ? EPI_SCALE_F32 : EPI_SCALE_ACC, s);
+      }
+      if (e == hipSuccess && dw) {
+        GemmArgs a = plane_args(zp, ldz, pz, xp, dp, px, n, d, m);
+        a.C = static_cast<float*>(dw) + v0 * lddw, a.ldc = lddw, a.alpha = scale;
+        a.ws = reinterpret_cast<float*>(base + o.split), a.ws_bytes = o.split_bytes;
+        e = gemm_loss(a, dtype, false, false, dw_epi == EPI_SCALE_ACC ? EPI_SCALE_ACC : EPI_SCALE_F32, s);
+      }
+    }
+    return e;
+  }
   {
     const int cpr = d * esz / 16;
     const int64_t n = rows * cpr;

@@ -62,7 +62,8 @@ def _ref(x, w, tgt, d):
 FWD = [("bf16", 1, 1, 8, 0), ("bf16", 1, 50257, 64, 0), ("bf16", 5, 7, 72, 8), ("bf16", 257, 1000, 136, 16),
        ("bf16", 999, 2049, 768, 0), ("bf16", 4100, 50257, 128, 0), ("bf16", 2048, 3333, 1024, 8),
        ("bf16", 3, 4096, 4104, 0), ("f32", 1, 1, 4, 0), ("f32", 33, 65, 68, 4), ("f32", 300, 5003, 260, 0),
-       ("f32", 1025, 2049, 516, 4), ("f32", 2, 30011, 4096, 0)]
+       ("f32", 1025, 2049, 516, 4), ("f32", 2, 30011, 4096, 0),
+       ("f32", 255, 1001, 100, 0), ("f32", 256, 1001, 100, 4), ("f32", 700, 9001, 1028, 0), ("f32", 2100, 4097, 36, 0)]
 
 
 @pytest.mark.gpu
@@ -158,7 +159,9 @@ BWD = [("bf16", 1, 1, 8, 0, 0), ("bf16", 1, 3000, 256, 0, 0), ("bf16", 5, 7, 72,
        ("bf16", 257, 1003, 136, 250, 8), ("bf16", 999, 2049, 768, 1024, 0), ("bf16", 4100, 9001, 128, 0, 0),
        ("bf16", 2048, 17000, 512, 0, 0), ("bf16", 130, 4097, 1032, 4096, 0), ("f32", 1, 1, 4, 0, 0),
        ("f32", 33, 65, 68, 8, 4), ("f32", 300, 3003, 260, 1000, 0), ("f32", 1025, 2049, 516, 0, 4),
-       ("f32", 2, 9001, 1028, 4096, 0)]
+       ("f32", 2, 9001, 1028, 4096, 0),
+       ("f32", 256, 1003, 100, 250, 4), ("f32", 700, 9001, 1028, 0, 0), ("f32", 2100, 4097, 36, 0, 0),
+       ("f32", 259, 20000, 772, 2048, 4)]
 
 
 @pytest.mark.gpu
@@ -198,10 +201,11 @@ def test_backward_forms(dtype, epi, want):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_tokens_without_part(dtype):
+@pytest.mark.parametrize("rows", [150, 400])
+def test_tokens_without_part(dtype, rows):
     """Rows of masked tokens may hold anything; a batch of masked tokens only has no loss and no gradient."""
     t = U.torch()
-    rows, V, d = 150, 700, 128
+    V, d = 700, 128
     x, w, tgt = _case(dtype, rows, V, d, 0.5, 4)
     clean = x.clone()
     off = tgt < 0
