@@ -250,7 +250,8 @@ gemm_dl_kernel(GemmArgs g) {
   using OA = Operand<T, AKC, BM>;
   using OB = Operand<T, BKC, BN>;
   constexpr bool PIN = BM >= 192;  // accumulators in AGPRs, one wave per SIMD
-  constexpr bool NS = EPI >= EPI_NS_GRAM, SYM = EPI == EPI_NS_GRAM || EPI == EPI_NS_POLY;
+  constexpr bool NS = EPI >= EPI_NS_GRAM, SYM = EPI == EPI_NS_GRAM || EPI == EPI_NS_POLY || EPI == EPI_NS_PART;
+  constexpr bool PART = EPI == EPI_NS_PART;
   constexpr int TM = BM / 32, TN = BN / 32;
   static_assert(TM >= TN, "fragment rows");
   constexpr int LT = OA::LPT + OB::LPT;  // loads per thread and k tile
@@ -274,8 +275,11 @@ gemm_dl_kernel(GemmArgs g) {
   const int tiles = SYM ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n, total = static_cast<int>(gridDim.x);
   const int xcd = blockIdx.x & 7, rem = total & 7;
   int pid = xcd * (total >> 3) + min(xcd, rem) + (blockIdx.x >> 3);
-  const int split = pid / tiles;  // Newton-Schulz products: the matrix of the batch
+  int split = pid / tiles;  // Newton-Schulz products: the matrix of the batch
+  const int item = pid;
   pid -= split * tiles;
+  const int part = PART ? split % g.ns.ranges : 0;  // the range of k
+  if constexpr (PART) split /= g.ns.ranges;
   constexpr int GROUP = 8;
   const int per_group = GROUP * tiles_n;
   const int first_m = (pid / per_group) * GROUP;
@@ -319,9 +323,10 @@ gemm_dl_kernel(GemmArgs g) {
   // may be short: only the tiles that hold k are loaded and multiplied
   // (4096x8192x576: 49.0 us with a whole last group, 47.0; 8192x8192x352: 81, 78).
   const int quads = (g.K + 4 * BK - 1) / (4 * BK);
-  const int kbase = NS ? 0 : split * g.kquads * 4;
-  const int nk4 = NS ? quads * 4 : min(g.kquads, quads - split * g.kquads) * 4;
-  const int nk = TAIL ? min(nk4, (g.K + BK - 1) / BK - kbase) : nk4;
+  const int kbase = PART ? part * g.ns.range : NS ? 0 : split * g.kquads * 4;
+  const int nk4 = PART ? (min(g.ns.range, g.K / BK - kbase) + 3) / 4 * 4
+                  : NS ? quads * 4 : min(g.kquads, quads - split * g.kquads) * 4;
+  const int nk = PART ? min(g.ns.range, g.K / BK - kbase) : TAIL ? min(nk4, (g.K + BK - 1) / BK - kbase) : nk4;
   // Each XCD starts its k loop at its own eighth of the range (the tile's
   // sum is rotated, the same for every launch of the shape).  Workgroups
   // walk k in step, so without it the whole GPU reads the same column range
@@ -692,6 +697,16 @@ gemm_dl_kernel(GemmArgs g) {
       }
     }
   };
+  if constexpr (PART) {
+    // the tile's sums as they lie, [item][BM][BN]; rows and columns past the
+    // matrix as well, which the joining kernel does not read
+    float* out = static_cast<float*>(g.C) + static_cast<int64_t>(item) * (BM * BN) + wm * TM * 16 * BN + wn * TN * 16;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) *reinterpret_cast<f32x4_t*>(out + (16 * i + lr) * BN + 16 * j + 4 * lg) = acc[i][j];
+    return;
+  }
   if constexpr (NS) {
     // Lengths are multiples of 32 and RB is 32, so a block of rows is inside or
     // outside as a whole; loads take clamped columns instead of tests.  A lane
@@ -904,13 +919,17 @@ hipError_t launch_planes(const GemmArgs& g, bool akc, bool bkc, int epi, hipStre
 template <int BS, int PASSES>
 hipError_t launch_ns(const GemmArgs& g, int batch, bool akc, bool bkc, int epi, hipStream_t s) {
   const int64_t tm = (g.M + BS - 1) / BS, tn = (g.N + BS - 1) / BS;
-  const int64_t tiles = epi == EPI_NS_STEP ? tm * tn : tm * (tm + 1) / 2;
+  const int64_t tiles = (epi == EPI_NS_STEP ? tm * tn : tm * (tm + 1) / 2) * (epi == EPI_NS_PART ? g.ns.ranges : 1);
   if (tiles * batch > (1ll << 30)) return hipErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(tiles * batch)), block(NT);
 #define ATOM_DL(AK, BK_, E)                                                                              \
   if (akc == AK && bkc == BK_ && epi == E) {                                                             \
     hipLaunchKernelGGL((gemm_dl_kernel<f16_t, AK, BK_, E, BS, BS, true, PASSES>), grid, block, 0, s, g); \
     return hipGetLastError();                                                                            \
+  }
+  if constexpr (BS == 64) {
+    ATOM_DL(true, true, EPI_NS_PART)
+    ATOM_DL(false, false, EPI_NS_PART)
   }
   ATOM_DL(true, true, EPI_NS_GRAM)
   ATOM_DL(false, false, EPI_NS_GRAM)

@@ -28,6 +28,7 @@ enum Epilogue {
   EPI_NS_GRAM = 13,    // C = alpha * acc, symmetric
   EPI_NS_POLY = 14,    // C = alpha * acc + beta * aux, symmetric
   EPI_NS_STEP = 15,    // C = alpha * acc + beta * aux, or the result from it
+  EPI_NS_PART = 16,    // a range of k of EPI_NS_GRAM: raw fp32 tiles to C
 };
 
 // The epilogues of the Newton-Schulz products.  Matrices are fp16 in one or two
@@ -38,6 +39,7 @@ struct NsArgs {
   int64_t sa, sb, sc;        // elements from one matrix of the batch to the next: A, B; C and aux
   int64_t pa, pb;            // elements from the hi to the lo plane of A and B
   int kp;                    // k tiles of 32 of one pass over k (two planes: three passes, three: six)
+  int ranges, range;         // EPI_NS_PART: ranges of k, k tiles of each (the last may be shorter)
   const void *aux, *aux_lo;  // as C
   void* C_lo;
   float beta;
@@ -122,8 +124,8 @@ hipError_t gemm_planes_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStr
 hipError_t gemm_loss_f32_64(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 hipError_t gemm_loss_f32_32(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);
 
-// Newton-Schulz products on square tiles of bs (64, 128, 192 or 256); planes 1
-// or 2, `batch` matrices.
+// Newton-Schulz products on square tiles of bs (64, 128, 192 or 256; EPI_NS_PART:
+// 64 alone); planes 1 or 2, `batch` matrices.
 hipError_t gemm_ns(const GemmArgs& g, int bs, int planes, int batch, bool akc, bool bkc, int epi, hipStream_t s);
 
 hipError_t gemm_check(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig);

@@ -164,6 +164,50 @@ void launch_pack(const void* g, int64_t ldg, int64_t stride, int batch, int rows
   }
 }
 
+// Joins the ranges of k of A = X X^T (EPI_NS_PART, 64x64 tiles on and below the
+// diagonal, item [matrix][range][tile]) in range order: a workgroup per 32x32
+// block of a tile, stored on both sides of the diagonal.
+__global__ void __launch_bounds__(256) gram_join_kernel(const float* __restrict__ part, int ranges, int tiles, int M,
+                                                        float alpha, f16_t* __restrict__ hi, f16_t* __restrict__ lo,
+                                                        int two, int64_t sa) {
+  __shared__ float s[32][33];
+  const int tile = blockIdx.x >> 2, sub = blockIdx.x & 3, b = blockIdx.y;
+  int tm = static_cast<int>((sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
+  while (tm * (tm + 1) / 2 > tile) --tm;
+  while ((tm + 1) * (tm + 2) / 2 <= tile) ++tm;
+  const int tn = tile - tm * (tm + 1) / 2;
+  const int r0 = (sub >> 1) * 32, c0 = (sub & 1) * 32;
+  if (tm * 64 + r0 >= M || tn * 64 + c0 >= M) return;  // lengths are multiples of 32
+  const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 4;
+  const float* p = part + (static_cast<int64_t>(b) * ranges * tiles + tile) * 4096 + (r0 + r) * 64 + c0 + c;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int k = 0; k < ranges; ++k) {
+    const float4 x = *reinterpret_cast<const float4*>(p + static_cast<int64_t>(k) * tiles * 4096);
+    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+  }
+  typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+  auto store = [&](int row, int col) {
+    h4 a, l;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      a[k] = static_cast<_Float16>(v[k]);
+      l[k] = static_cast<_Float16>(v[k] - static_cast<float>(a[k]));
+    }
+    const int64_t at = b * sa + static_cast<int64_t>(row) * M + col;
+    *reinterpret_cast<h4*>(hi + at) = a;
+    if (two) *reinterpret_cast<h4*>(lo + at) = l;
+  };
+#pragma unroll
+  for (int k = 0; k < 4; ++k) s[r][c + k] = v[k] *= alpha;
+  store(tm * 64 + r0 + r, tn * 64 + c0 + c);
+  if (tm == tn) return;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = s[c + k][r];
+  store(tn * 64 + c0 + r, tm * 64 + r0 + c);
+}
+
 // No steps: out from X itself.
 template <typename TO, bool ACC>
 __global__ void __launch_bounds__(256) unpack_kernel(const f16_t* __restrict__ hi, const f16_t* __restrict__ lo,
@@ -180,12 +224,61 @@ __global__ void __launch_bounds__(256) unpack_kernel(const f16_t* __restrict__ h
 
 inline uint64_t up(uint64_t n) { return (n + 255) & ~255ull; }
 
+constexpr int CUS = 256;
+
+// Tile of a product (0 A, 1 B, 2 X): the smallest predicted time.  A CU's k tile
+// (32) takes `lat` us of one workgroup alone on it and `ktile` of each of
+// several, a workgroup's start and epilogue `fixed`.  Fitted to 33 products of 256 to
+// 20480 in one and three passes; B X reads and writes both planes of X, 8 bytes
+// an entry that no product hides in 256x256 tiles (4096 x 4096: 25 of 130 us).
+// 4096 x 4096, A: 192x192 tiles fill 253 CUs and take 78 us, 256x256 136 CUs and
+// 91, 128x128 two or three to a CU and 107; 12 x 768 x 768, B X: 24 us in
+// 128x128, 28 in 192x192, 40 in 256x256.
+int tile_of(int product, int M, int N, int ktiles, int batch, double* us_out = nullptr) {
+  struct {
+    int bs;
+    double lat, ktile, fixed[3];
+  } const cfg[] = {{256, 0.74, 0.74, {8.0, 9.5, 20.0}}, {192, 0.45, 0.48, {9.0, 10.0, 11.0}},
+                   {128, 0.30, 0.25, {2.5, 3.2, 4.0}}, {64, 0.147, 0.117, {0.8, 0.9, 0.7}}};
+  int best = 0;
+  double best_us = 0.0;
+  for (const auto& c : cfg) {
+    const int64_t tm = (M + c.bs - 1) / c.bs, tn = (N + c.bs - 1) / c.bs;
+    const int64_t tiles = (product < 2 ? tm * (tm + 1) / 2 : tm * tn) * batch;
+    const double share = static_cast<double>((tiles + CUS - 1) / CUS);
+    const double us = ktiles * std::max(c.lat, share * c.ktile) + share * c.fixed[product];
+    if (best == 0 || us < best_us) best = c.bs, best_us = us;
+  }
+  if (us_out) *us_out = best_us;
+  return best;
+}
+
+// Ranges of k for A = X X^T of a short side M: 64x64 tiles in ranges and the
+// joining kernel (4 us and its partial sums' way through memory) where that takes
+// less time than the best tile alone, as with few tiles and a long k.
+int ranges_of(int M, int ktiles, int batch) {
+  double whole, best_us;
+  tile_of(0, M, M, ktiles, batch, &whole);
+  int best = 1;
+  best_us = whole;
+  const int64_t t = (M + 63) / 64, tiles = t * (t + 1) / 2 * batch;
+  for (int n = 2; n <= 64; n *= 2) {
+    if (ktiles < 8 * n || tiles * n > 4 * CUS) break;
+    const double share = static_cast<double>((tiles * n + CUS - 1) / CUS), kt = static_cast<double>((ktiles + n - 1) / n);
+    const double us = kt * std::max(0.147, share * 0.117) + share * 0.8 + 4.0 + tiles * n * 16384 * 2 / 4e6;
+    if (us < best_us) best = n, best_us = us;
+  }
+  return best;
+}
+
+
 // Workspace: partial sums, X (hi and lo, each twice: a step reads one and
 // writes the other; one plane's lo is read and written by the same lanes, so it
 // is there once), A, B.  n: bytes of a plane of X and of A, all matrices.
 struct Ws {
   int rp, cp, k;  // padded lengths, the smaller of them
-  uint64_t part, x[2], xl[2], a, al, b, bl, end;
+  int ranges;     // of k that A is the sum of
+  uint64_t part, x[2], xl[2], a, al, b, bl, sums, end;
 };
 Ws layout(int dtype, int batch, int rows, int cols) {
   Ws w;
@@ -203,36 +296,11 @@ Ws layout(int dtype, int batch, int rows, int cols) {
   w.al = two ? take(a) : w.a;
   w.b = take(a);
   w.bl = two ? take(a) : w.b;
+  w.ranges = ranges_of(w.k, (two ? 3 : 1) * std::max(w.rp, w.cp) / 32, batch);
+  const uint64_t t = (w.k + 63) / 64;
+  w.sums = take(w.ranges > 1 ? t * (t + 1) / 2 * w.ranges * batch * 4096 * 4 : 0);
   w.end = at;
   return w;
-}
-
-constexpr int CUS = 256;
-
-// Tile of a product (0 A, 1 B, 2 X): the smallest predicted time.  A CU's k tile
-// (32) takes `lat` us of one workgroup alone on it and `ktile` of each of
-// several, a workgroup's start and epilogue `fixed`.  Fitted to 33 products of 256 to
-// 20480 in one and three passes; B X reads and writes both planes of X, 8 bytes
-// an entry that no product hides in 256x256 tiles (4096 x 4096: 25 of 130 us).
-// 4096 x 4096, A: 192x192 tiles fill 253 CUs and take 78 us, 256x256 136 CUs and
-// 91, 128x128 two or three to a CU and 107; 12 x 768 x 768, B X: 24 us in
-// 128x128, 28 in 192x192, 40 in 256x256.
-int tile_of(int product, int M, int N, int ktiles, int batch) {
-  struct {
-    int bs;
-    double lat, ktile, fixed[3];
-  } const cfg[] = {{256, 0.74, 0.74, {8.0, 9.5, 20.0}}, {192, 0.45, 0.48, {9.0, 10.0, 11.0}},
-                   {128, 0.30, 0.25, {2.5, 3.2, 4.0}}, {64, 0.147, 0.117, {0.8, 0.9, 0.7}}};
-  int best = 0;
-  double best_us = 0.0;
-  for (const auto& c : cfg) {
-    const int64_t tm = (M + c.bs - 1) / c.bs, tn = (N + c.bs - 1) / c.bs;
-    const int64_t tiles = (product < 2 ? tm * (tm + 1) / 2 : tm * tn) * batch;
-    const double share = static_cast<double>((tiles + CUS - 1) / CUS);
-    const double us = ktiles * std::max(c.lat, share * c.ktile) + share * c.fixed[product];
-    if (best == 0 || us < best_us) best = c.bs, best_us = us;
-  }
-  return best;
 }
 
 }  // namespace
@@ -321,7 +389,23 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
     p.ns.sa = p.ns.sb = sx, p.ns.sc = sa;
     p.ns.pa = p.ns.pb = at(o.xl[i]) - at(o.x[i]);
     p.ns.C_lo = at(o.al);
-    e = product(p, wide ? o.cp : o.rp, wide, wide, EPI_NS_GRAM);
+    if (o.ranges > 1) {
+      const int len = wide ? o.cp : o.rp;
+      p.ns.kp = len / 32;
+      p.K = passes * len;
+      p.splits = 1;
+      p.C = base + o.sums;
+      p.ns.range = (passes * p.ns.kp + o.ranges - 1) / o.ranges;
+      p.ns.ranges = (passes * p.ns.kp + p.ns.range - 1) / p.ns.range;  // none empty
+      e = gemm_ns(p, 64, planes, batch, wide, wide, EPI_NS_PART, s);
+      if (e != hipSuccess) return e;
+      const int t = (o.k + 63) / 64, tiles = t * (t + 1) / 2;
+      hipLaunchKernelGGL(gram_join_kernel, dim3(4 * tiles, batch), dim3(256), 0, s, reinterpret_cast<float*>(base + o.sums),
+                         p.ns.ranges, tiles, o.k, 1.f / SCALE, at(o.a), at(o.al), two ? 1 : 0, sa);
+      e = hipGetLastError();
+    } else {
+      e = product(p, wide ? o.cp : o.rp, wide, wide, EPI_NS_GRAM);
+    }
     if (e != hipSuccess) return e;
     GemmArgs q{};
     q.A = q.B = at(o.a), q.lda = q.ldb = o.k, q.C = at(o.b), q.ldc = o.k;
@@ -356,7 +440,7 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
 
 }  // namespace atom
 
-// Tiles of a step's three products (tests).
+// Tiles of a step's three products and ranges of k of the first (tests).
 extern "C" void atom_ns_choice(int dtype, int batch, int rows, int cols, int* out) {
   using namespace atom;
   const Ws o = layout(dtype, batch, rows, cols);
@@ -364,4 +448,5 @@ extern "C" void atom_ns_choice(int dtype, int batch, int rows, int cols, int* ou
   out[0] = tile_of(0, o.k, o.k, passes * lng / 32, batch);
   out[1] = tile_of(1, o.k, o.k, passes * o.k / 32, batch);
   out[2] = tile_of(2, o.rp, o.cp, passes * o.k / 32, batch);
+  out[3] = o.ranges;
 }

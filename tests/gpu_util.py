@@ -128,12 +128,13 @@ def attn_choice(B, T, H, dh):
 
 
 def ns_choice(dtype, batch, rows, cols):
-    """Tiles atom_k_orthogonalize takes for a step's three products, by the library's own rule."""
+    """Tiles atom_k_orthogonalize takes for a step's three products, and the ranges of k of the first, by the library's
+    own rule."""
     import ctypes
 
     from paper_2403_10504_amd import atom as A
 
-    out = (ctypes.c_int * 3)()
+    out = (ctypes.c_int * 4)()
     f = A.lib().atom_ns_choice
     f.argtypes, f.restype = [ctypes.c_int] * 4 + [ctypes.c_void_p], None
     f(dt_code(dtype), batch, rows, cols, ctypes.addressof(out))

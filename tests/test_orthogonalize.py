@@ -213,18 +213,23 @@ def test_extreme_values(dtype):
         assert t.equal(got[0], base[0]) and got[1].isnan().all()
 
 
-# type, batch, rows, cols, tiles of the three products by the library's rule
-TILES = [("bf16", 1, 1500, 1500, (64, 64, 128)),
-         ("bf16", 12, 700, 760, (128, 128, 128)),
-         ("bf16", 2, 2048, 2050, (128, 128, 192)),
-         ("bf16", 4, 2100, 2048, (256, 256, 192)),
-         ("f32", 2, 2100, 2048, (128, 192, 192)),
-         ("f32", 4, 2048, 2048, (256, 256, 256)),
-         ("bf16", 1, 4096, 4160, (192, 192, 192)),
-         ("bf16", 1, 4200, 4096, (192, 192, 192)),
-         ("f32", 1, 3300, 3200, (192, 192, 128)),
-         ("f32", 3, 700, 640, (64, 64, 64)),
-         ("f32", 12, 640, 700, (128, 128, 128))]
+# type, batch, rows, cols, tiles of the three products and ranges of k of the first by the library's rule
+TILES = [("bf16", 1, 1500, 1500, (64, 64, 128, 1)),
+         ("bf16", 12, 700, 760, (128, 128, 128, 1)),
+         ("bf16", 2, 2048, 2050, (128, 128, 192, 1)),
+         ("bf16", 4, 2100, 2048, (256, 256, 192, 1)),
+         ("f32", 2, 2100, 2048, (128, 192, 192, 1)),
+         ("f32", 4, 2048, 2048, (256, 256, 256, 1)),
+         ("bf16", 1, 4096, 4160, (192, 192, 192, 1)),
+         ("bf16", 1, 4200, 4096, (192, 192, 192, 1)),
+         ("f32", 1, 3300, 3200, (192, 192, 128, 1)),
+         ("f32", 3, 700, 640, (64, 64, 64, 1)),
+         ("f32", 12, 640, 700, (128, 128, 128, 1)),
+         ("bf16", 1, 70, 20000, (64, 64, 64, 64)),
+         ("bf16", 1, 20000, 70, (64, 64, 64, 64)),
+         ("f32", 2, 100, 5000, (64, 64, 64, 32)),
+         ("f32", 1, 768, 256, (64, 64, 64, 8)),
+         ("bf16", 3, 700, 9001, (64, 64, 128, 2))]
 
 
 @pytest.mark.gpu
