@@ -119,9 +119,9 @@ int atom_k_xent(int dtype, const float* logits, int64_t ldz, const int32_t* tgt,
  * +infinity or NaN: loss NaN (fp32 with 256 rows or more, whose products run on
  * three bf16 planes: infinite inputs too).
  * Requirements: d a positive multiple of 8 (bf16) or 4 (fp32), ldx and ldw
- * multiples of the same, at least d; x, w and ws 16-byte aligned; rows, V >= 1
- * any numbers (rows 0: nothing is done) with less than 2^30 tiles of 32 x 32
- * between any two of rows, V and d.  ws: device scratch of at least the bytes
+ * multiples of the same, at least d; x, w and ws 16-byte aligned; rows up to
+ * 2^28 (0: nothing is done, and no pointer looked at), V from 1 to 2^28, d up to
+ * 2^24, with less than 2^30 tiles of 32 x 32 between any two of them.  ws: device scratch of at least the bytes
  * that the query returns (0 for sizes it refuses); calls that may overlap need
  * scratch of their own. */
 #define ATOM_XENT_IGNORE (-1)
@@ -142,7 +142,7 @@ int atom_k_linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w,
  * V or more makes both gradients NaN.  dx or dw may be NULL (not wanted).
  * dw_epi: ATOM_EPI_STORE (dw in dtype), ATOM_EPI_STORE_F32 or ATOM_EPI_ACC_F32
  * (dw fp32, += the gradient).  rows 0: dw is zeroed, or kept by
- * ATOM_EPI_ACC_F32.  dx and dw must not overlap the inputs.  Requirements as
+ * ATOM_EPI_ACC_F32, and no other pointer looked at.  dx and dw must not overlap the inputs.  Requirements as
  * above, for dx and lddx, dw and lddw as well. */
 uint64_t atom_k_linear_xent_bwd_ws_bytes(int dtype, int64_t rows, int V, int d, int piece);
 int atom_k_linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,

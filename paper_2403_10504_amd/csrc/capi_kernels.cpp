@@ -104,9 +104,10 @@ int atom_k_linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w,
                            float* lse, float* loss_rows, int64_t rows, int V, int d, void* ws, uint64_t ws_bytes,
                            void* stream) {
   if (!dt_ok(dtype) || !linear_xent_ok(dtype, rows, V, d)) return ATOM_EINVAL;
+  if (rows == 0) return ATOM_OK;
   if (!rows_ok(dtype, x, ldx, d) || !rows_ok(dtype, w, ldw, d)) return ATOM_EINVAL;
   if (!tgt || !lse || !loss_rows) return ATOM_EINVAL;
-  if (rows > 0 && (!ws || misaligned(ws) || ws_bytes < linear_xent_fwd_ws(dtype, rows, V, d))) return ATOM_EINVAL;
+  if (!ws || misaligned(ws) || ws_bytes < linear_xent_fwd_ws(dtype, rows, V, d)) return ATOM_EINVAL;
   return st(linear_xent_fwd(dtype, x, ldx, w, ldw, tgt, lse, loss_rows, rows, V, d, ws, S(stream)));
 }
 
@@ -119,8 +120,9 @@ int atom_k_linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w,
                            int64_t lddw, int dw_epi, int64_t rows, int V, int d, int piece, void* ws,
                            uint64_t ws_bytes, void* stream) {
   if (!dt_ok(dtype) || piece < 0 || !linear_xent_ok(dtype, rows, V, d)) return ATOM_EINVAL;
-  if (!rows_ok(dtype, x, ldx, d) || !rows_ok(dtype, w, ldw, d) || !tgt || !lse) return ATOM_EINVAL;
-  if ((dx && !rows_ok(dtype, dx, lddx, d)) || (dw && !rows_ok(dtype, dw, lddw, d))) return ATOM_EINVAL;
+  if (rows > 0 && (!rows_ok(dtype, x, ldx, d) || !rows_ok(dtype, w, ldw, d) || !tgt || !lse)) return ATOM_EINVAL;
+  if (rows > 0 && dx && !rows_ok(dtype, dx, lddx, d)) return ATOM_EINVAL;
+  if (dw && !rows_ok(dtype, dw, lddw, d)) return ATOM_EINVAL;
   int epi;
   switch (dw_epi) {
     case ATOM_EPI_STORE: epi = EPI_SCALE; break;
@@ -147,9 +149,10 @@ uint64_t atom_k_orthogonalize_ws_bytes(int dtype, int batch, int rows, int cols)
 int atom_k_orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,
                          int64_t stride_o, int out_epi, float keep, float scale, int batch, int rows, int cols,
                          const float* coef, int steps, void* ws, uint64_t ws_bytes, void* stream) {
-  if (!dt_ok(dtype) || !g || !out || !orthogonalize_ok(batch, rows, cols)) return ATOM_EINVAL;
+  if (!dt_ok(dtype) || !orthogonalize_ok(batch, rows, cols)) return ATOM_EINVAL;
   if (ldg < cols || ldo < cols || stride_g < 0) return ATOM_EINVAL;
   if (out_epi != ATOM_EPI_STORE && out_epi != ATOM_EPI_STORE_F32 && out_epi != ATOM_EPI_ACC_F32) return ATOM_EINVAL;
+  if (batch > 0 && (!g || !out)) return ATOM_EINVAL;
   const uintptr_t esz = dtype == ATOM_BF16 ? 2 : 4, osz = out_epi == ATOM_EPI_STORE ? esz : 4;
   if (reinterpret_cast<uintptr_t>(g) % esz || reinterpret_cast<uintptr_t>(out) % osz) return ATOM_EINVAL;
   if (batch > 1 && stride_o < (rows - 1) * ldo + cols && !(stride_o >= cols && stride_o <= ldo / batch)) return ATOM_EINVAL;

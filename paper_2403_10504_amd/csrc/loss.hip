@@ -212,12 +212,12 @@ BwdWs bwd_ws(int dtype, int64_t rows, int V, int d, const Pieces& p) {
 
 }  // namespace
 
-// Tiles are counted in 32 bits, of 64 x 64 at least (bf16) or 32 x 32.
+// Lengths whose tiles (32 x 32 at least) and passes over k are counted in 32 bits.
 bool linear_xent_ok(int dtype, int64_t rows, int V, int d) {
-  if (rows < 0 || rows > (1 << 30) || V <= 0 || V > (1 << 30) || d <= 0 || d % (dtype == DT_BF16 ? 8 : 4)) return false;
-  return ((rows + 31) / 32) * ((static_cast<int64_t>(V) + 31) / 32) < (1ll << 30) &&
-         ((static_cast<int64_t>(V) + 31) / 32) * ((static_cast<int64_t>(d) + 31) / 32) < (1ll << 30) &&
-         ((rows + 31) / 32) * ((static_cast<int64_t>(d) + 31) / 32) < (1ll << 30);
+  if (rows < 0 || rows > (1 << 28) || V <= 0 || V > (1 << 28) || d <= 0 || d > (1 << 24)) return false;
+  if (d % (dtype == DT_BF16 ? 8 : 4)) return false;
+  const int64_t tr = (rows + 31) / 32, tv = (static_cast<int64_t>(V) + 31) / 32, td = (d + 31) / 32;
+  return tr * tv < (1ll << 30) && tv * td < (1ll << 30) && tr * td < (1ll << 30);
 }
 
 namespace {

@@ -5,6 +5,8 @@ python -m paper_2403_10504_amd.kernel_bench gemm [iters]
 python -m paper_2403_10504_amd.kernel_bench gemm_layouts [iters]
 python -m paper_2403_10504_amd.kernel_bench layernorm [iters]
 python -m paper_2403_10504_amd.kernel_bench xent [iters]
+python -m paper_2403_10504_amd.kernel_bench linear_xent [iters]
+python -m paper_2403_10504_amd.kernel_bench orthogonalize [iters]
 
 attention: causal attention at the 6.7B shape (B 2, T 2048, 32 heads of 128),
 GPT-3 Small's (B 8, 12 heads of 64) and 13B's (B 1, 40 heads of 128); the
@@ -14,7 +16,10 @@ the 6.7B layer shapes for k = 2048, 4096, 8192, with the fit t = a + b k.
 gemm_layouts: the 6.7B block's GEMMs in the three operand layouts the step
 uses (forward, data gradient, weight gradient), store epilogue.
 layernorm: the LayerNorm backward (accumulate, bf16 copy, both partial sums)
-and forward (bf16 output, row statistics) at the four GPT-3 widths.  One line per measurement; times from HIP events.
+and forward (bf16 output, row statistics) at the four GPT-3 widths.
+linear_xent: the head's loss without logits, and its gradients, at the four
+GPT-3 widths; orthogonalize: five Newton-Schulz steps of the weight matrices of
+a block at those widths.  One line per measurement; times from HIP events.
 """
 from __future__ import annotations
 
@@ -155,6 +160,45 @@ def xent(iters=20):
               f"(fp32 logits read once, bf16 dz written once)", flush=True)
 
 
+def linear_xent(iters=10):
+    """The head's loss without its logits, and both gradients (GPT-3 widths, their token counts and vocabulary)."""
+    V = 50257
+    for N, d in ((16384, 768), (8192, 2048), (4096, 4096), (2048, 5120)):
+        x = torch.randn(N, d, device="cuda").to(torch.bfloat16)
+        w = (torch.randn(V, d, device="cuda") * (2.5 / d ** 0.5)).to(torch.bfloat16)
+        tgt = torch.randint(0, V, (N,), device="cuda", dtype=torch.int32)
+        lse, loss = torch.empty(N, device="cuda"), torch.empty(N, device="cuda")
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        nf, nb = A.atom_k_linear_xent_fwd_ws_bytes(1, N, V, d), A.atom_k_linear_xent_bwd_ws_bytes(1, N, V, d)
+        ws = torch.empty(max(nf, nb), device="cuda", dtype=torch.uint8)
+        fwd = lambda: A.atom_k_linear_xent_fwd(1, x.data_ptr(), d, w.data_ptr(), d, tgt.data_ptr(),  # noqa: E731
+                                               lse.data_ptr(), loss.data_ptr(), N, V, d, ws.data_ptr(), nf)
+        bwd = lambda: A.atom_k_linear_xent_bwd(1, x.data_ptr(), d, w.data_ptr(), d, tgt.data_ptr(),  # noqa: E731
+                                               lse.data_ptr(), None, 1.0 / N, dx.data_ptr(), d, dw.data_ptr(), d,
+                                               A.ATOM_EPI_STORE, N, V, d, 0, ws.data_ptr(), nb)
+        for name, fn, mult, ws_bytes in (("loss", fwd, 2, nf), ("gradients", bwd, 6, nb)):
+            us = _time(fn, iters)
+            print(f"linear_xent {name} rows={N} d={d} V={V}: {us:.1f} us, {mult * N * V * d / us / 1e6:.0f} TFLOP/s, "
+                  f"workspace {ws_bytes / 1e6:.0f} MB", flush=True)
+
+
+def orthogonalize(iters=10):
+    """Five Newton-Schulz steps of a block's weight matrices at the GPT-3 widths (bf16 gradients, bf16 results)."""
+    for rows, cols, batch in ((768, 768, 12), (2048, 2048, 1), (8192, 2048, 1), (4096, 4096, 1),
+                              (4096, 16384, 1), (5120, 20480, 1)):
+        g = (torch.randn(batch, rows, cols, device="cuda") * 1e-3).to(torch.bfloat16)
+        out = torch.empty_like(g)
+        n = A.atom_k_orthogonalize_ws_bytes(1, batch, rows, cols)
+        ws = torch.empty(n, device="cuda", dtype=torch.uint8)
+        us = _time(lambda: A.atom_k_orthogonalize(1, g.data_ptr(), cols, rows * cols, out.data_ptr(), cols, rows * cols,
+                                                  A.ATOM_EPI_STORE, 0.0, 1.0, batch, rows, cols, 5, ws.data_ptr(), n),
+                   iters)
+        m, k = min(rows, cols), max(rows, cols)
+        flop = batch * 5 * (m * m * k + m ** 3 + 2 * m * m * k)  # symmetric products count half
+        print(f"orthogonalize {batch} x {rows} x {cols}: {us:.1f} us, {flop / us / 1e6:.0f} TFLOP/s, "
+              f"workspace {n / 1e6:.0f} MB", flush=True)
+
+
 def main(argv):
     if not torch.cuda.is_available():
         raise SystemExit("kernel_bench needs a GPU")
@@ -167,6 +211,10 @@ def main(argv):
         gemm_layouts(int(argv[2]) if len(argv) > 2 else 20)
     elif what == "xent":
         xent(int(argv[2]) if len(argv) > 2 else 20)
+    elif what == "linear_xent":
+        linear_xent(int(argv[2]) if len(argv) > 2 else 10)
+    elif what == "orthogonalize":
+        orthogonalize(int(argv[2]) if len(argv) > 2 else 10)
     elif what == "layernorm":
         layernorm(int(argv[2]) if len(argv) > 2 else 50)
     else:

@@ -347,7 +347,8 @@ def test_refusals():
 
     common = [dict(dtype=2), dict(x=None), dict(w=None), dict(tgt=None), dict(lse=None), dict(ws=None), dict(x=P + 8),
               dict(w=P + 2), dict(ws=P + 4), dict(d=0), dict(d=60), dict(d=72), dict(ldx=63), dict(ldx=68), dict(ldw=56),
-              dict(V=0), dict(V=-1), dict(rows=-1), dict(rows=1 << 31), dict(rows=1 << 29, V=1 << 24), dict(n=0)]
+              dict(V=0), dict(V=-1), dict(rows=-1), dict(rows=1 << 31), dict(rows=1 << 27, V=1 << 24),
+              dict(rows=(1 << 28) + 1), dict(V=(1 << 28) + 1), dict(d=(1 << 24) + 8, ldx=1 << 25, ldw=1 << 25), dict(n=0)]
     for call, more in ((fwd, [dict(loss=None), dict(n=A.atom_k_linear_xent_fwd_ws_bytes(1, 10, 100, 64) - 1)]),
                        (bwd, [dict(piece=-1), dict(epi=3), dict(epi=-1), dict(dx=P + 8), dict(dw=P + 8), dict(lddx=60),
                               dict(lddw=68), dict(n=A.atom_k_linear_xent_bwd_ws_bytes(1, 10, 100, 64, 0) - 1)])):
@@ -356,9 +357,9 @@ def test_refusals():
                 call(**k)
             assert e.value.status == A.ATOM_EINVAL, (call.__name__, k)
     # nothing to do: no launch, no workspace
-    fwd(rows=0, ws=None, n=0)
+    fwd(rows=0, x=None, w=None, tgt=None, lse=None, loss=None, ws=None, n=0)
     bwd(dx=None, dw=None)
-    bwd(rows=0, ws=None, n=0, dw=None)
+    bwd(rows=0, x=None, w=None, tgt=None, lse=None, dx=None, ws=None, n=0, dw=None)
     for bad in ((2, 10, 100, 64), (1, -1, 100, 64), (1, 10, 0, 64), (1, 10, 100, 4)):
         assert A.atom_k_linear_xent_fwd_ws_bytes(*bad) == 0 and A.atom_k_linear_xent_bwd_ws_bytes(*bad, 0) == 0
     assert A.atom_k_linear_xent_bwd_ws_bytes(1, 10, 100, 64, -1) == 0
@@ -376,6 +377,6 @@ def test_no_tokens():
     lse = t.empty(1, device="cuda")
     for epi, want in ((A.ATOM_EPI_STORE, 0.0), (A.ATOM_EPI_STORE_F32, 0.0), (A.ATOM_EPI_ACC_F32, 3.0)):
         dw = t.full((34, 72), 3.0, device="cuda", dtype=t.bfloat16 if epi == A.ATOM_EPI_STORE else t.float32)
-        A.atom_k_linear_xent_bwd(A.ATOM_BF16, w.data_ptr(), 64, w.data_ptr(), 64, lse.data_ptr(), lse.data_ptr(), None,
-                                 1.0, None, 0, dw.data_ptr(), 72, epi, 0, 33, 64, 0, None, 0)
+        A.atom_k_linear_xent_bwd(A.ATOM_BF16, x.data_ptr(), 64, w.data_ptr(), 64, tgt.data_ptr(), lse.data_ptr(), None,
+                                 1.0, x.data_ptr(), 64, dw.data_ptr(), 72, epi, 0, 33, 64, 0, None, 0)
         assert (dw[:33, :64] == want).all() and (dw[33] == 3.0).all() and (dw[:, 64:] == 3.0).all()

@@ -297,7 +297,7 @@ def test_refusals():
         with pytest.raises(A.AtomError) as e:
             call(**k)
         assert e.value.status == A.ATOM_EINVAL, k
-    call(batch=0, ws=None, n=0)  # nothing to do
+    call(batch=0, g=None, out=None, ws=None, n=0)  # nothing to do
     with pytest.raises(ValueError):
         call(coef=[(1.0, 2.0)])
     for bad in ((2, 3, 100, 64), (1, 0, 100, 64), (1, 3, 0, 64), (1, 3, 100, -4)):
