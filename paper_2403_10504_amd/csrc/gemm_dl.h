@@ -25,12 +25,11 @@
 //     fragments by ds_read_b32, chunk c at c ^ (4 ((k >> 3) & 3)) (16 chunks)
 //     or c ^ (4 ((k >> 3) & 1)) (8 chunks).
 // Rows past the operand are clamped to its last valid row (or chunk of rows;
-// the last chunk of a not k-contiguous A may hold rows past M, which
-// gemm_loss allows): they only reach output rows or columns that are never
-// stored.  k past the
-// end reads 16 bytes of zeros instead, in both operands, so any k whose
-// chunks are whole works; the loop runs whole groups of four k tiles, then the
-// one to three that are left.
+// the last chunk of an operand that is not k-contiguous may hold rows past it,
+// which gemm_loss allows): they only reach output rows or columns that are
+// never stored.  k past the end reads 16 bytes of zeros instead, in both
+// operands, so any k whose chunks are whole works; the loop runs whole groups of
+// four k tiles, then the one to three that are left.
 #pragma once
 
 #include <algorithm>
@@ -43,6 +42,7 @@ namespace atom {
 namespace dl {
 
 constexpr int BK = 32, NT = 256, STAGES = 4;
+constexpr int RESIDENT = 256;  // workgroups that stay for all tiles (see STAY): one per CU
 
 // What direct loads read for k past the end.
 static __device__ __attribute__((aligned(16))) uint32_t zero_chunk[4];
@@ -89,13 +89,14 @@ struct Operand {
       if constexpr (TAIL) s = kt * BK + k < K ? s : static_cast<const void*>(zero_chunk);
       lds_dma16(s, __builtin_amdgcn_readfirstlane(lds_offset(stage) + group * 1024));
     }
+    // the same, `off` elements on (another plane)
     template <bool TAIL>
     __device__ __forceinline__ void load_plane(uint8_t* stage, int kt, int K, int64_t off, int group) const {
       const void* s = p + off + kt * kstep;
       if constexpr (TAIL) s = kt * BK + k < K ? s : static_cast<const void*>(zero_chunk);
       lds_dma16(s, __builtin_amdgcn_readfirstlane(lds_offset(stage) + group * 1024));
     }
-    // the tile's chunk `off` elements on (another plane), k whole tiles
+    // the same, k whole tiles
     __device__ __forceinline__ void load_plane(uint8_t* stage, int kt, int64_t off, int group) const {
       lds_dma16(p + off + kt * kstep, __builtin_amdgcn_readfirstlane(lds_offset(stage) + group * 1024));
     }
@@ -261,8 +262,9 @@ gemm_dl_kernel(GemmArgs g) {
   constexpr bool LOSS = EPI == EPI_LSE || EPI == EPI_DZ;
   constexpr float LOG2E = 1.4426950408889634f;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[LDS];
-  __shared__ int row_tgt[LOSS ? BM : 1];                           // of the tile's rows: target column,
-  __shared__ float2 row_lse_scale[EPI == EPI_DZ ? BM : 1];         // lse (base 2), factor
+  // of the tile's rows: target column; lse (base 2) and factor
+  __shared__ int row_tgt[LOSS ? BM : 1];
+  __shared__ float2 row_lse_scale[EPI == EPI_DZ ? BM : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int lr = lane & 15, lg = lane >> 4;
   const int wm = w >> 1, wn = w & 1;
@@ -272,20 +274,37 @@ gemm_dl_kernel(GemmArgs g) {
   // panels through its L2); items are the tiles of the first k range, then of
   // the next; tiles go in groups of 8 row tiles sweeping the columns.
   const int tiles_m = (g.M + BM - 1) / BM, tiles_n = (g.N + BN - 1) / BN;
-  const int tiles = SYM ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n, total = static_cast<int>(gridDim.x);
-  const int xcd = blockIdx.x & 7, rem = total & 7;
-  int pid = xcd * (total >> 3) + min(xcd, rem) + (blockIdx.x >> 3);
+  const int tiles = SYM ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n;
+  // STAY: one workgroup per CU stays for every RESIDENT-th tile and loads the
+  // first k tiles of the next one before this one's epilogue, which leaves the
+  // stages alone (EPI_LSE): with a short k, the start of a tile is a good part of
+  // its time.
+  constexpr bool STAY = EPI == EPI_LSE && BM == 256;
+  const int total = STAY ? tiles : static_cast<int>(gridDim.x);
+  constexpr int GROUP = 8;
+  auto item_of = [&](int block) {
+    const int rem = total & 7;
+    return (block & 7) * (total >> 3) + min(block & 7, rem) + (block >> 3);
+  };
+  auto tile_of = [&](int pid, int& pid_m, int& pid_n) {
+    const int per_group = GROUP * tiles_n;
+    const int first_m = (pid / per_group) * GROUP;
+    const int gsize = min(tiles_m - first_m, GROUP);
+    pid_m = first_m + (pid % per_group) % gsize;
+    pid_n = (pid % per_group) / gsize;
+  };
+  int block = static_cast<int>(blockIdx.x);
+  bool loaded = false;  // STAY: the first k tiles are in their stages
+next_tile:
+  const int xcd = block & 7;
+  int pid = item_of(block);
   int split = pid / tiles;  // Newton-Schulz products: the matrix of the batch
   const int item = pid;
   pid -= split * tiles;
   const int part = PART ? split % g.ns.ranges : 0;  // the range of k
   if constexpr (PART) split /= g.ns.ranges;
-  constexpr int GROUP = 8;
-  const int per_group = GROUP * tiles_n;
-  const int first_m = (pid / per_group) * GROUP;
-  const int gsize = min(tiles_m - first_m, GROUP);
-  int pid_m = first_m + (pid % per_group) % gsize;
-  int pid_n = (pid % per_group) / gsize;
+  int pid_m, pid_n;
+  tile_of(pid, pid_m, pid_n);
   if constexpr (SYM) {  // tiles on and below the diagonal, row by row
     pid_m = static_cast<int>((sqrtf(8.f * pid + 1.f) - 1.f) * 0.5f);
     while (pid_m * (pid_m + 1) / 2 > pid) --pid_m;
@@ -314,10 +333,15 @@ gemm_dl_kernel(GemmArgs g) {
 
   typename OA::Src sra[OA::LPT];
   typename OB::Src srb[OB::LPT];
+  auto init_src = [&](int m0, int n0) {
 #pragma unroll
-  for (int q = 0; q < OA::LPT; ++q) sra[q].init(static_cast<const T*>(g.A), g.lda, m0, AKC ? g.M : (g.M + OA::E - 1) / OA::E * OA::E, q * NT + tid);
+    for (int q = 0; q < OA::LPT; ++q)
+      sra[q].init(static_cast<const T*>(g.A), g.lda, m0, AKC ? g.M : (g.M + OA::E - 1) / OA::E * OA::E, q * NT + tid);
 #pragma unroll
-  for (int q = 0; q < OB::LPT; ++q) srb[q].init(static_cast<const T*>(g.B), g.ldb, n0, BKC ? g.N : (g.N + OB::E - 1) / OB::E * OB::E, q * NT + tid);
+    for (int q = 0; q < OB::LPT; ++q)
+      srb[q].init(static_cast<const T*>(g.B), g.ldb, n0, BKC ? g.N : (g.N + OB::E - 1) / OB::E * OB::E, q * NT + tid);
+  };
+  init_src(m0, n0);
   // k tiles of this workgroup: kquads groups of four per split, the rest in
   // the last one (the launcher leaves none empty).  With TAIL the last group
   // may be short: only the tiles that hold k are loaded and multiplied
@@ -399,13 +423,18 @@ gemm_dl_kernel(GemmArgs g) {
   // prologue: tiles 0..3 in flight, fragments of tile 0 in set 0.  Loads
   // past the last tile repeat it (into stages nobody reads again), so every
   // iteration has the same loads outstanding; they land before the exit.
+  auto first_loads = [&] {
 #pragma unroll
-  for (int s = 0; s < STAGES; ++s) {
-    const int kt = rot(TAIL ? min(s, nk - 1) : s);
+    for (int s = 0; s < STAGES; ++s) {
+      const int kt = rot(TAIL ? min(s, nk - 1) : s);
 #pragma unroll
-    for (int l = 0; l < LT; ++l) load(s, kt, l);
+      for (int l = 0; l < LT; ++l) load(s, kt, l);
+    }
+  };
+  if (!STAY || !loaded) {
+    first_loads();
+    wait_loads<3 * LT>();
   }
-  wait_loads<3 * LT>();
   barrier_after_reads();
 #pragma unroll
   for (int i = 0; i < TM; ++i) OA::frag(fa0[i], stage_a(0), foa[i]);
@@ -503,48 +532,74 @@ gemm_dl_kernel(GemmArgs g) {
     }
   }
   if constexpr (EPI == EPI_LSE) {
+    float2* part = static_cast<float2*>(g.C) + static_cast<int64_t>(pid_n * 2 + wn) * g.M;
+    const bool edge = col0 + TN * 16 > g.N;
+    if constexpr (STAY) {
+      block += RESIDENT;
+      loaded = block < total;
+      if (loaded) {
+        int next_m, next_n;
+        tile_of(item_of(block), next_m, next_n);
+        init_src(next_m * BM, next_n * BN);
+        first_loads();
+      }
+    }
     // One pass over the logits in registers: a lane's 4 TN values of a row,
     // then the four lanes that share the row.  The exponentials (16 TM TN of a
     // quarter-rate instruction per lane) are what this epilogue costs.
-    float2* part = static_cast<float2*>(g.C) + static_cast<int64_t>(pid_n * 2 + wn) * g.M;
-    const bool edge = col0 + TN * 16 > g.N;
+    float mx[TM], sum[TM], zt[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int m = row0 + 16 * i + lr, t = trow[i];
-      const bool hit = t >= 0 && t < TN * 16 && (t >> 2 & 3) == lg;
-      if (__builtin_amdgcn_ballot_w64(hit) != 0) {
-        float z = 0.f;
+      const int t = trow[i];
+      float z[TN][4];
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          z[j][r] = acc[i][j][r];
+          asm volatile("" : "+v"(z[j][r]));  // out of its AGPR once, not for each use
+        }
+      zt[i] = 0.f;
+      if (__builtin_amdgcn_ballot_w64(t >= 0 && t < TN * 16) != 0) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) z = t == 16 * j + 4 * lg + r ? acc[i][j][r] : z;
-        if (hit) g.ztgt[m] = z;
+          for (int r = 0; r < 4; ++r) zt[i] = t == 16 * j + 4 * lg + r ? z[j][r] : zt[i];
       }
-      float mx = -INFINITY;
       if (edge) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (col0 + 16 * j + 4 * lg + r >= g.N) acc[i][j][r] = -INFINITY;
+            if (col0 + 16 * j + 4 * lg + r >= g.N) z[j][r] = -INFINITY;
       }
+      float m = -INFINITY;
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, acc[i][j][r]);
-      mx = rows4_max(mx) * LOG2E;
-      const float ref = mx == -INFINITY ? 0.f : mx;  // no column of the row in this block
-      float sum = 0.f;
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, z[j][r]);
+      mx[i] = rows4_max(m) * LOG2E;
+      const float ref = mx[i] == -INFINITY ? 0.f : mx[i];  // no column of the row in this block
+      float s = 0.f;
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         float e[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) e[r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -ref));
-        sum += (e[0] + e[1]) + (e[2] + e[3]);
+        for (int r = 0; r < 4; ++r) e[r] = __builtin_amdgcn_exp2f(fmaf(z[j][r], LOG2E, -ref));
+        s += (e[0] + e[1]) + (e[2] + e[3]);
       }
-      sum = rows4_sum(sum);
-      if (lg == 0 && m < g.M) part[m] = make_float2(mx, sum);
+      sum[i] = rows4_sum(s);
     }
+    // the next tile's loads have landed; the stores are left in flight
+    if constexpr (STAY) wait_loads<0>();
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int m = row0 + 16 * i + lr, t = trow[i];
+      if (t >= 0 && t < TN * 16 && (t >> 2 & 3) == lg) g.ztgt[m] = zt[i];
+      if (lg == 0 && m < g.M) part[m] = make_float2(mx[i], sum[i]);
+    }
+    if constexpr (STAY)
+      if (loaded) goto next_tile;
     return;
   }
   // Epilogue through LDS, RB rows of the wave's block at a time: the
@@ -620,28 +675,33 @@ gemm_dl_kernel(GemmArgs g) {
         const int i = h * (RB / 16) + ii;
         if constexpr (E == EPI_DZ) {
           // dz = (softmax - onehot) * scale; a row that takes no part has logits
-          // of zero (its row of A is zero) and scale zero.  Four instructions
-          // and the exponential per logit; the one-hot only where it is.
+          // of zero (its row of A is zero) and scale zero.  An FMA, the
+          // exponential and a product per logit; the one-hot only where it is.
           const float2 ls = row_lse_scale[wm * TM * 16 + 16 * i + lr];
           const bool hit = trow[i] >= 0 && trow[i] < TN * 16;
+          float z[TN][4];
 #pragma unroll
           for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -ls.x)) * ls.y;
-              acc[i][j][r] = GUARD && col0 + 16 * j + 4 * lg + r >= ga.N ? 0.f : p;
+              z[j][r] = GUARD && col0 + 16 * j + 4 * lg + r >= ga.N ? 0.f : p;
             }
           if (__builtin_amdgcn_ballot_w64(hit) != 0) {
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) acc[i][j][r] -= trow[i] == 16 * j + 4 * lg + r ? ls.y : 0.f;
+              for (int r = 0; r < 4; ++r) z[j][r] -= trow[i] == 16 * j + 4 * lg + r ? ls.y : 0.f;
           }
-        }
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const f32x4_t& a = acc[i][j];
-          *reinterpret_cast<float4*>(stg + (ii * 16 + lr) * PITCH + j * 16 + lg * 4) = make_float4(a[0], a[1], a[2], a[3]);
+          for (int j = 0; j < TN; ++j)
+            *reinterpret_cast<float4*>(stg + (ii * 16 + lr) * PITCH + j * 16 + lg * 4) = make_float4(z[j][0], z[j][1], z[j][2], z[j][3]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const f32x4_t& a = acc[i][j];
+            *reinterpret_cast<float4*>(stg + (ii * 16 + lr) * PITCH + j * 16 + lg * 4) = make_float4(a[0], a[1], a[2], a[3]);
+          }
         }
       }
       float4 sv[NQ];
@@ -868,7 +928,7 @@ hipError_t launch(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s)
 template <typename T, int BM, int BN>
 hipError_t launch_loss(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s) {
   const int tiles = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
-  const dim3 grid(static_cast<unsigned>(tiles * g.splits)), block(NT);
+  const dim3 grid(static_cast<unsigned>(epi == EPI_LSE && BM == 256 ? std::min(tiles, RESIDENT) : tiles * g.splits)), block(NT);
   const bool tail = g.K % (4 * BK) != 0;
 #define ATOM_DL(AK, BK_, E)                                                                        \
   if (akc == AK && bkc == BK_ && epi == E) {                                                       \
@@ -897,7 +957,7 @@ hipError_t launch_loss(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream
 template <int BM, int BN>
 hipError_t launch_planes(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s) {
   const int tiles = ((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
-  const dim3 grid(static_cast<unsigned>(tiles * g.splits)), block(NT);
+  const dim3 grid(static_cast<unsigned>(epi == EPI_LSE && BM == 256 ? std::min(tiles, RESIDENT) : tiles * g.splits)), block(NT);
 #define ATOM_DL(AK, BK_, E)                                                                           \
   if (akc == AK && bkc == BK_ && epi == E) {                                                          \
     hipLaunchKernelGGL((gemm_dl_kernel<bf16_t, AK, BK_, E, BM, BN, true, 6>), grid, block, 0, s, g);  \
