@@ -116,8 +116,8 @@ int atom_k_xent(int dtype, const float* logits, int64_t ldz, const int32_t* tgt,
  * loss_rows [rows].  A token whose target is negative (ATOM_XENT_IGNORE) takes
  * no part: lse and loss 0, whatever its row holds.  A target of V or more:
  * loss NaN (it is never read).  Logits of a whole row at -infinity, or one at
- * +infinity or NaN: loss NaN (fp32 with 256 rows or more, whose products run on
- * three bf16 planes: infinite inputs too).
+ * +infinity or NaN: loss NaN (fp32 of 768 rows and 2^32 products or more,
+ * which runs on three bf16 planes: infinite inputs too).
  * Requirements: d a positive multiple of 8 (bf16) or 4 (fp32), ldx and ldw
  * multiples of the same, at least d; x, w and ws 16-byte aligned; rows up to
  * 2^28 (0: nothing is done, and no pointer looked at), V from 1 to 2^28, d up to

@@ -29,7 +29,6 @@ namespace atom {
 namespace {
 
 constexpr float LN2 = 0.6931471805599453f;
-constexpr int PLANE_ROWS = 256;
 
 // RPB rows per workgroup, 256 / RPB threads per row, each over every
 // (256 / RPB)-th part; the threads' (max, sum) pairs join in LDS in a fixed
@@ -125,15 +124,24 @@ inline uint64_t up(uint64_t n) { return (n + 255) & ~255ull; }
 inline unsigned blocks(int64_t n) { return static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 4096)); }
 inline int esize(int dtype) { return dtype == DT_BF16 ? 2 : 4; }
 
-// fp32 as three bf16 planes (x = h + m + l, 24 bits) and six passes of bf16
-// MFMAs, two to three times the rate of fp32 ones; w's planes, 10 bytes of
-// memory traffic an entry each time, want rows to pay for them.
-bool planes(int dtype, int64_t rows) { return dtype == DT_F32 && rows >= PLANE_ROWS; }
+// Whether fp32 operands become three bf16 planes (x = h + m + l, 24 bits), with
+// six passes of bf16 MFMAs at two to three times the rate of fp32 ones: w's
+// planes, 16 bytes of memory traffic an entry, want rows and work to pay for
+// them.  54 problems, fp32 MFMAs against planes: loss 4096 x 512, vocabulary
+// 8000, 309 and 190 us; 1024 x 512, 8000, 85 and 75; 512 x 512, 8000, 47 and 55; 1024 x
+// 2048, 1000, 45 and 87; gradients 4096 x 2048, 8000, 3336 and 2354; 512 x 2048,
+// 8000, 460 and 381; 256 x 2048, 50257, 1461 and 1737; 1024 x 128, 50257, 455 and 619.
+bool planes(int dtype, int64_t rows, int V, int d, bool grad) {
+  return dtype == DT_F32 && rows >= (grad ? 512 : 768) && d >= (grad ? 256 : 1) &&
+         static_cast<double>(rows) * V * d >= 4294967296.0;
+}
 // Columns of a row of planes, an odd number of 128-byte lines.
 int plane_ld(int d) { return ((d + 63) / 64 | 1) * 64; }
-// Rows of w that are planes at a time: 96 MB, 1024 rows at least.
+// Rows of w that are planes at a time (forward): equal parts of 192 MB at most,
+// 1024 rows at least.
 int plane_rows(int V, int d) {
-  return static_cast<int>(std::min<int64_t>(V, std::max<int64_t>(1024, (96ll << 20) / (6 * plane_ld(d)) / 256 * 256)));
+  const int64_t most = std::max<int64_t>(1024, (192ll << 20) / (6 * plane_ld(d)) / 256 * 256), n = (V + most - 1) / most;
+  return static_cast<int>(std::min<int64_t>(V, ((V + n - 1) / n + 255) / 256 * 256));
 }
 GemmArgs plane_args(const bf16_t* A, int64_t lda, int64_t pa, const bf16_t* B, int64_t ldb, int64_t pb, int M, int N, int K) {
   GemmArgs g{};
@@ -171,7 +179,7 @@ Pieces pieces_of(int dtype, int64_t rows, int V, int d, int piece) {
     const int w = static_cast<int>(std::min<int64_t>(V, (piece + 7ll) / 8 * 8));
     return Pieces{w, w};
   }
-  const int64_t most = planes(dtype, rows) ? (128ll << 20) / (6 * std::max<int64_t>(rows, plane_ld(d)))
+  const int64_t most = planes(dtype, rows, V, d, true) ? (128ll << 20) / (6 * std::max<int64_t>(rows, plane_ld(d)))
                                            : (128ll << 20) / (rows * esize(dtype));
   if (V <= most) return Pieces{V, V};
   int w = 16384;
@@ -186,8 +194,8 @@ uint64_t split_bytes(int64_t rows, int d) { return std::min<uint64_t>(up(16ull *
 
 // Rows of dz start an odd number of 256-byte lines apart: pieces are multiples
 // of 4 KB or more, and rows that far apart crowd a few memory channels.
-int ld_of_dz(int dtype, int64_t rows, int piece) {
-  const int line = 256 / (planes(dtype, rows) ? 2 : esize(dtype));
+int ld_of_dz(int esz, int piece) {
+  const int line = 256 / esz;
   return ((piece + line - 1) / line | 1) * line;
 }
 
@@ -195,9 +203,9 @@ struct BwdWs {
   uint64_t dz, x, w, dx, split, split_bytes, end;  // offsets
 };
 BwdWs bwd_ws(int dtype, int64_t rows, int V, int d, const Pieces& p) {
-  const bool three = planes(dtype, rows);
+  const bool three = planes(dtype, rows, V, d, true);
   const uint64_t e = three ? 6 : esize(dtype), n = rows;
-  const int ldz = ld_of_dz(dtype, rows, p.last);
+  const int ldz = ld_of_dz(three ? 2 : esize(dtype), p.last);
   const uint64_t wide = three ? plane_ld(d) : d;
   BwdWs w;
   w.dz = 0;
@@ -228,7 +236,7 @@ struct FwdWs {
 };
 FwdWs fwd_ws(int dtype, int64_t rows, int V, int d) {
   FwdWs w;
-  const bool three = planes(dtype, rows);
+  const bool three = planes(dtype, rows, V, d, false);
   const int m = static_cast<int>(rows);
   w.range = three ? plane_rows(V, d) : V;
   w.parts = 0;
@@ -258,7 +266,7 @@ hipError_t linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w,
   float2* part = reinterpret_cast<float2*>(base + o.part);
   const int m = static_cast<int>(rows);
   hipError_t e;
-  if (planes(dtype, rows)) {
+  if (planes(dtype, rows, V, d, false)) {
     const int dp = plane_ld(d);
     bf16_t *xp = reinterpret_cast<bf16_t*>(base + o.x), *wp = reinterpret_cast<bf16_t*>(base + o.w);
     e = to_planes(x, ldx, rows, d, nullptr, nullptr, xp, s);
@@ -309,9 +317,10 @@ hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w,
   const Pieces pc = pieces_of(dtype, rows, V, d, piece);
   const BwdWs o = bwd_ws(dtype, rows, V, d, pc);
   char* base = static_cast<char*>(ws);
-  const int ldz = ld_of_dz(dtype, rows, pc.last);
+  const bool three = planes(dtype, rows, V, d, true);
+  const int ldz = ld_of_dz(three ? 2 : esize(dtype), pc.last);
   char* xz = base + o.x;
-  if (planes(dtype, rows)) {
+  if (three) {
     const int dp = plane_ld(d), m = static_cast<int>(rows);
     bf16_t *zp = reinterpret_cast<bf16_t*>(base), *xp = reinterpret_cast<bf16_t*>(xz), *wp = reinterpret_cast<bf16_t*>(base + o.w);
     const int64_t px = rows * dp, pz = rows * ldz;

@@ -63,7 +63,8 @@ FWD = [("bf16", 1, 1, 8, 0), ("bf16", 1, 50257, 64, 0), ("bf16", 5, 7, 72, 8), (
        ("bf16", 999, 2049, 768, 0), ("bf16", 4100, 50257, 128, 0), ("bf16", 2048, 3333, 1024, 8),
        ("bf16", 3, 4096, 4104, 0), ("f32", 1, 1, 4, 0), ("f32", 33, 65, 68, 4), ("f32", 300, 5003, 260, 0),
        ("f32", 1025, 2049, 516, 4), ("f32", 2, 30011, 4096, 0),
-       ("f32", 255, 1001, 100, 0), ("f32", 256, 1001, 100, 4), ("f32", 700, 9001, 1028, 0), ("f32", 2100, 4097, 36, 0)]
+       ("f32", 255, 1001, 100, 0), ("f32", 256, 1001, 100, 4), ("f32", 700, 9001, 1028, 0), ("f32", 2100, 4097, 36, 0),
+       ("f32", 768, 43000, 132, 4), ("f32", 1030, 8201, 516, 0), ("f32", 2100, 4097, 516, 4), ("f32", 1100, 2001, 2052, 0)]
 
 
 @pytest.mark.gpu
@@ -161,7 +162,8 @@ BWD = [("bf16", 1, 1, 8, 0, 0), ("bf16", 1, 3000, 256, 0, 0), ("bf16", 5, 7, 72,
        ("f32", 33, 65, 68, 8, 4), ("f32", 300, 3003, 260, 1000, 0), ("f32", 1025, 2049, 516, 0, 4),
        ("f32", 2, 9001, 1028, 4096, 0),
        ("f32", 256, 1003, 100, 250, 4), ("f32", 700, 9001, 1028, 0, 0), ("f32", 2100, 4097, 36, 0, 0),
-       ("f32", 259, 20000, 772, 2048, 4)]
+       ("f32", 259, 20000, 772, 2048, 4), ("f32", 1030, 8201, 516, 0, 0), ("f32", 2100, 4097, 516, 1000, 4),
+       ("f32", 512, 33000, 260, 0, 4), ("f32", 1100, 2001, 2052, 0, 0)]
 
 
 @pytest.mark.gpu
@@ -201,11 +203,10 @@ def test_backward_forms(dtype, epi, want):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows", [150, 400])
-def test_tokens_without_part(dtype, rows):
+@pytest.mark.parametrize("rows,V,d", [(150, 700, 128), (400, 700, 128), (1100, 8000, 512)])
+def test_tokens_without_part(dtype, rows, V, d):
     """Rows of masked tokens may hold anything; a batch of masked tokens only has no loss and no gradient."""
     t = U.torch()
-    V, d = 700, 128
     x, w, tgt = _case(dtype, rows, V, d, 0.5, 4)
     clean = x.clone()
     off = tgt < 0
@@ -380,3 +381,26 @@ def test_no_tokens():
         A.atom_k_linear_xent_bwd(A.ATOM_BF16, x.data_ptr(), 64, w.data_ptr(), 64, tgt.data_ptr(), lse.data_ptr(), None,
                                  1.0, x.data_ptr(), 64, dw.data_ptr(), 72, epi, 0, 33, 64, 0, None, 0)
         assert (dw[:33, :64] == want).all() and (dw[33] == 3.0).all() and (dw[:, 64:] == 3.0).all()
+
+
+@pytest.mark.gpu
+def test_far_rows():
+    """Rows of W, dW and x more than 2^31 elements from the first."""
+    t = U.torch()
+    rows, V, d, ld = 9, 1040, 64, 1 << 21
+    x, w, tgt = _case("bf16", rows, V, d, 0.2, 50)
+    tgt[0] = V - 1
+    loss, lse, _ = _fwd("bf16", x, w, tgt, d)
+    dx, dw = _bwd("bf16", x, w, tgt, lse, d)
+    far = t.empty(V * ld, device="cuda", dtype=t.bfloat16)
+    wf = far.as_strided((V, d), (ld, 1))
+    wf.copy_(w)
+    l2, s2, _ = _fwd("bf16", x, wf, tgt, d)
+    assert t.equal(loss, l2) and t.equal(lse, s2)
+    ws = t.empty(A.atom_k_linear_xent_bwd_ws_bytes(A.ATOM_BF16, rows, V, d), device="cuda", dtype=t.uint8)
+    df = far.as_strided((V, d), (ld, 1), 4096)
+    x2 = t.empty_like(x)
+    A.atom_k_linear_xent_bwd(A.ATOM_BF16, x.data_ptr(), d, wf.data_ptr(), ld, tgt.data_ptr(), lse.data_ptr(), None, 1.0,
+                             x2.data_ptr(), d, df.data_ptr(), ld, A.ATOM_EPI_STORE, rows, V, d, 0, ws.data_ptr(),
+                             ws.numel())
+    assert t.equal(x2, dx) and t.equal(df, dw)

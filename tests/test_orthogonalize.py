@@ -302,3 +302,19 @@ def test_refusals():
         call(coef=[(1.0, 2.0)])
     for bad in ((2, 3, 100, 64), (1, 0, 100, 64), (1, 3, 0, 64), (1, 3, 100, -4)):
         assert A.atom_k_orthogonalize_ws_bytes(*bad) == 0
+
+
+@pytest.mark.gpu
+def test_far_rows():
+    """Rows of the gradient and of the result more than 2^31 elements from the first."""
+    t = U.torch()
+    rows, cols, ld = 1040, 48, 1 << 21
+    g = _matrix(rows, cols, "bf16", 60)
+    want = _run("bf16", g[None], 5)[0]
+    far = t.empty(rows * ld, device="cuda", dtype=t.bfloat16)
+    src, dst = far.as_strided((rows, cols), (ld, 1)), far.as_strided((rows, cols), (ld, 1), 4097)
+    src.copy_(g)
+    ws = t.empty(A.atom_k_orthogonalize_ws_bytes(A.ATOM_BF16, 1, rows, cols), device="cuda", dtype=t.uint8)
+    A.atom_k_orthogonalize(A.ATOM_BF16, src.data_ptr(), ld, 0, dst.data_ptr(), ld, 0, A.ATOM_EPI_STORE, 0.0, 1.0, 1, rows,
+                           cols, 5, ws.data_ptr(), ws.numel())
+    assert t.equal(dst, want)
