@@ -42,8 +42,8 @@ HBM_PEAK_GBS = 8000.0
 # --copy-calibration 2147483648`, each scaled by what the counter reads for
 # the plain copy kernel of known size (profiles/gemm_wgrad_6.7b_hbm_traffic.md).
 # Valid only for the kernel sources it was measured on.
-WGRAD_TRAFFIC = {"sources_sha256": "fdb77e2684147a47a0610f98eb910edd0690dbb2d74258b31162bf977a991bdd",
-                 "bytes_per_launch": 725825619}
+WGRAD_TRAFFIC = {"sources_sha256": "b21c2b66e4276ad8c7020a55fb7828d04f85679f86ec7fce5e935b39eceb3882",
+                 "bytes_per_launch": 725817103}
 TRAFFIC_SOURCES = ("gemm.hip", "gemm_dl.h", "gemm_dl_256.hip", "common.h", "launch.h")
 
 
