@@ -189,8 +189,10 @@ Pieces pieces_of(int dtype, int64_t rows, int V, int d, int piece) {
   return Pieces{w, rest > 0 && rest <= w / 8 ? w + rest : w};
 }
 
-// Workspace for few rows: ranges of the vocabulary summed apart (dx), up to 16.
-uint64_t split_bytes(int64_t rows, int d) { return std::min<uint64_t>(up(16ull * rows * d * 4), 32ull << 20); }
+// Workspace for few rows: ranges of the vocabulary summed apart (dx), up to 16
+// in 64 MB (32, 64, 128 MB: 999 x 4096, vocabulary 50257, 1280, 1212, 1178 us; 1500 x
+// 2048 1030, 988, 982; 512 x 4096 741, 699, 697; 2048 x 5120 2735, 2745, 2797).
+uint64_t split_bytes(int64_t rows, int d) { return std::min<uint64_t>(up(16ull * rows * d * 4), 64ull << 20); }
 
 // Rows of dz start an odd number of 256-byte lines apart: pieces are multiples
 // of 4 KB or more, and rows that far apart crowd a few memory channels.
