@@ -129,8 +129,8 @@ inline int esize(int dtype) { return dtype == DT_BF16 ? 2 : 4; }
 // planes, 16 bytes of memory traffic an entry, want rows and work to pay for
 // them.  54 problems, fp32 MFMAs against planes: loss 4096 x 512, vocabulary
 // 8000, 309 and 190 us; 1024 x 512, 8000, 85 and 75; 512 x 512, 8000, 47 and 55; 1024 x
-// 2048, 1000, 45 and 87; gradients 4096 x 2048, 8000, 3336 and 2354; 512 x 2048,
-// 8000, 460 and 381; 256 x 2048, 50257, 1461 and 1737; 1024 x 128, 50257, 455 and 619.
+// 2048, 1000, 45 and 87; gradients 4096 x 2048, 8000, 3336 and 2087; 512 x 2048,
+// 8000, 460 and 358; 256 x 2048, 50257, 1461 and 1737; 1024 x 128, 50257, 455 and 619.
 bool planes(int dtype, int64_t rows, int V, int d, bool grad) {
   return dtype == DT_F32 && rows >= (grad ? 512 : 768) && d >= (grad ? 256 : 1) &&
          static_cast<double>(rows) * V * d >= 4294967296.0;
@@ -168,22 +168,25 @@ struct Pieces {
 
 // The caller's width, or by default the whole vocabulary where dz of it takes
 // at most 128 MB, half of the Infinity Cache, through which the two products
-// read it, else the largest power of two from 2048 to 16384 within that.
-// Vocabulary 50257, pieces of 4096, 8192, 16384, 32768: 2048 x 5120 3184, 2704,
-// 2595, 2750 us; 4096 x 4096 4057, 3883, 3876, 3908; 999 x 2048 988, 771, 672,
-// 638, whole 660; only with more rows are larger ones faster than this takes
-// (16384 x 768: 3866, 3751, 3524, 3472).  A short rest joins the last piece.
-// (Three planes: within 128 MB of dz and of w's planes.)
+// read it, else the largest power of two from 2048 to 16384 within that.  A
+// narrow d reads dz less often, and short pieces cost it more: 256 MB, and 512
+// for the piece.  Vocabulary 50257, pieces of 4096, 8192, 16384, 32768: 2048 x
+// 5120 3306, 2784, 2658, 2815 us; 4096 x 4096 4129, 3955, 3971, 3958; 999 x 2048
+// 1039, 787, 679, 636, whole 600; 16384 x 768 3849, 3711, 3589, 3553.  Within
+// 128 MB and as here: 1500 x 2048 1003 and 942; 32768 x 768 8212 and 7179; 16384 x
+// 2560 11143 and 10491; but whole, 4096 x 2560 (412 MB) 2720 and 2822, 2048 x 5120
+// (206 MB) 2659 and 2786.  A short rest joins the last piece.  (Three planes:
+// bytes of dz or of w's planes; 600 x 2048 2923 and 2595.)
 Pieces pieces_of(int dtype, int64_t rows, int V, int d, int piece) {
   if (piece > 0) {
     const int w = static_cast<int>(std::min<int64_t>(V, (piece + 7ll) / 8 * 8));
     return Pieces{w, w};
   }
-  const int64_t most = planes(dtype, rows, V, d, true) ? (128ll << 20) / (6 * std::max<int64_t>(rows, plane_ld(d)))
-                                           : (128ll << 20) / (rows * esize(dtype));
-  if (V <= most) return Pieces{V, V};
+  const bool narrow = d <= 2560;
+  const int64_t column = planes(dtype, rows, V, d, true) ? 6 * std::max<int64_t>(rows, plane_ld(d)) : rows * esize(dtype);
+  if (V <= (narrow ? 256ll << 20 : 128ll << 20) / column) return Pieces{V, V};
   int w = 16384;
-  while (w > 2048 && w > most) w /= 2;
+  while (w > 2048 && w > (narrow ? 512ll << 20 : 128ll << 20) / column) w /= 2;
   w = std::min(V, w);
   const int rest = V % w;
   return Pieces{w, rest > 0 && rest <= w / 8 ? w + rest : w};
