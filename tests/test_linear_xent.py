@@ -163,7 +163,8 @@ BWD = [("bf16", 1, 1, 8, 0, 0), ("bf16", 1, 3000, 256, 0, 0), ("bf16", 5, 7, 72,
        ("f32", 2, 9001, 1028, 4096, 0),
        ("f32", 256, 1003, 100, 250, 4), ("f32", 700, 9001, 1028, 0, 0), ("f32", 2100, 4097, 36, 0, 0),
        ("f32", 259, 20000, 772, 2048, 4), ("f32", 1030, 8201, 516, 0, 0), ("f32", 2100, 4097, 516, 1000, 4),
-       ("f32", 512, 33000, 260, 0, 4), ("f32", 1100, 2001, 2052, 0, 0)]
+       ("f32", 512, 33000, 260, 0, 4), ("f32", 1100, 2001, 2052, 0, 0), ("bf16", 4100, 40001, 72, 0, 8),
+       ("bf16", 2100, 33001, 2568, 0, 0), ("f32", 1300, 40001, 260, 0, 4)]
 
 
 @pytest.mark.gpu
