@@ -135,8 +135,9 @@ int atom_k_linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w,
  *   dx[n][c] = scale * sum_v dz[n][v] w[v][c]   (dtype, [rows][lddx])
  *   dw[v][c] = scale * sum_n dz[n][v] x[n][c]   ([V][lddw])
  * z is computed again, `piece` columns at a time (rounded up to a multiple of
- * 8, at most V; 0: the library's choice), and dz of a piece goes through the
- * workspace in dtype.  lse comes from the forward call; drow (NULL: 1) weighs
+ * 8, at most V; 0: the library's choice, dz of up to 512 MB and 2048 columns at
+ * least), and dz of a piece goes through the
+ * workspace in dtype (fewer columns take less of it and more time).  lse comes from the forward call; drow (NULL: 1) weighs
  * a token.  A token with a negative target or with drow 0 adds nothing,
  * whatever its row of x holds, and its row of dx is zero; one with a target of
  * V or more makes both gradients NaN.  dx or dw may be NULL (not wanted).
