@@ -706,6 +706,11 @@ int lse_parts(const GemmArgs& g, int esz) {
   return (g.N + bn - 1) / bn * 2;
 }
 
+// Where a launch with EPI_LSE on the columns behind this one's puts its parts:
+// float2 entries behind this one's (2^31 and more of them for some millions of
+// rows).
+int64_t lse_entries(const GemmArgs& g, int esz) { return static_cast<int64_t>(lse_parts(g, esz)) * g.M; }
+
 // A product along the vocabulary (columns of the logits, rows of dW) runs in
 // two ranges where the first fills whole rounds of the chip with 256x256 tiles,
 // the rest takes smaller ones, and both take less time than tiles of one kind,
@@ -797,7 +802,7 @@ hipError_t gemm_loss(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi, 
     b.B = static_cast<const char*>(g.B) + cut * g.ldb * esz;
     b.v0 = g.v0 + cut;
     b.C = epi == EPI_DZ ? static_cast<void*>(static_cast<char*>(g.C) + static_cast<int64_t>(cut) * esz)
-                        : static_cast<void*>(static_cast<float2*>(g.C) + lse_parts(a, esz) * g.M);
+                        : static_cast<void*>(static_cast<float2*>(g.C) + lse_entries(a, esz));
   } else {
     b.M = g.M - cut;
     b.A = static_cast<const char*>(g.A) + static_cast<int64_t>(cut) * esz;
@@ -834,4 +839,18 @@ extern "C" void atom_gemm_choice(int dtype, int akc, int bkc, int epi, int M, in
                                   : choice_of(g, esz, akc != 0, bkc != 0, epi);
   out[0] = c.staged, out[1] = c.bm, out[2] = c.bn, out[3] = c.splits;
   out[4] = !c.staged && stream_result(g, epi, c.splits);
+}
+
+// How gemm_loss cuts EPI_LSE of M rows and N columns (tests): columns of the
+// first launch (0: one launch), and the entries that the second one's parts
+// start behind.
+extern "C" void atom_lse_cut(int dtype, int M, int N, int K, int64_t* out) {
+  using namespace atom;
+  GemmArgs g{};
+  g.M = M, g.N = N, g.K = K;
+  const int esz = dtype == DT_BF16 ? 2 : 4;
+  out[0] = first_range(g, esz, true, true, EPI_LSE);
+  GemmArgs a = g;
+  a.N = static_cast<int>(out[0]);
+  out[1] = out[0] ? lse_entries(a, esz) : 0;
 }

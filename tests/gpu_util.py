@@ -139,3 +139,17 @@ def ns_choice(dtype, batch, rows, cols):
     f.argtypes, f.restype = [ctypes.c_int] * 4 + [ctypes.c_void_p], None
     f(dt_code(dtype), batch, rows, cols, ctypes.addressof(out))
     return tuple(out)
+
+
+def lse_cut(dtype, rows, V, d):
+    """Columns of the first of the two launches that the loss of a linear head takes (0: one launch), and how many
+    (maximum, sum) pairs its parts are, behind which the second launch's start."""
+    import ctypes
+
+    from paper_2403_10504_amd import atom as A
+
+    out = (ctypes.c_int64 * 2)()
+    f = A.lib().atom_lse_cut
+    f.argtypes, f.restype = [ctypes.c_int] * 4 + [ctypes.c_void_p], None
+    f(dt_code(dtype), rows, V, d, ctypes.addressof(out))
+    return tuple(out)

@@ -405,3 +405,16 @@ def test_far_rows():
                              x2.data_ptr(), d, df.data_ptr(), ld, A.ATOM_EPI_STORE, rows, V, d, 0, ws.data_ptr(),
                              ws.numel())
     assert t.equal(x2, dx) and t.equal(df, dw)
+
+
+@pytest.mark.parametrize("rows,V,d", [(2755581, 151936, 768), (2561241, 108983, 1024), (5923305, 50257, 4096)])
+def test_parts_of_two_launches(rows, V, d):
+    """Where the vocabulary is cut in two launches, the second one's parts lie behind the first one's and inside the
+    workspace, also when that is more than 2^31 pairs (no GPU needed)."""
+    cut, entries = U.lse_cut("bf16", rows, V, d)
+    assert 0 < cut < V and entries % (2 * rows) == 0
+    # a part is half a tile of 64 to 256 columns
+    assert -(-cut // 128) <= entries // rows <= 2 * -(-cut // 64)
+    assert entries > 2 ** 31
+    rest = -(-(V - cut) // 128)
+    assert 8 * (entries + rest * rows) <= A.atom_k_linear_xent_fwd_ws_bytes(A.ATOM_BF16, rows, V, d)
