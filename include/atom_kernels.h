@@ -121,9 +121,11 @@ int atom_k_xent(int dtype, const float* logits, int64_t ldz, const int32_t* tgt,
  * Requirements: d a positive multiple of 8 (bf16) or 4 (fp32), ldx and ldw
  * multiples of the same, at least d; x, w and ws 16-byte aligned; rows up to
  * 2^28 (0: nothing is done, and no pointer looked at), V from 1 to 2^28, d up to
- * 2^24, with less than 2^30 tiles of 32 x 32 between any two of them.  ws: device scratch of at least the bytes
- * that the query returns (0 for sizes it refuses); calls that may overlap need
- * scratch of their own. */
+ * 2^24, with less than 2^30 tiles of 32 x 32 between any two of them, and for
+ * the forward call less than 2^24 tiles of logits where it takes tiles of less
+ * than 256 rows (fp32 of less than 768 rows: 64 x 64).  ws: device scratch of at
+ * least the bytes that the query returns (0 for sizes it refuses); calls that
+ * may overlap need scratch of their own. */
 #define ATOM_XENT_IGNORE (-1)
 uint64_t atom_k_linear_xent_fwd_ws_bytes(int dtype, int64_t rows, int V, int d);
 int atom_k_linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
@@ -172,7 +174,8 @@ int atom_k_embed_fwd(int dtype, const int32_t* tok, const void* wte, const void*
  * zeros gives zeros; one with an infinity or a NaN gives NaN throughout.
  * bf16: products in fp16 with fp32 sums (X itself in 22 bits), off by about
  * the result's own rounding; fp32: every factor in 22 bits.
- * Any rows, cols >= 1 (with less than 2^30 tiles of 64 x 64), leading
+ * Any rows, cols >= 1 (with less than 2^30 tiles of 64 x 64, and 2^24 of the
+ * products' tiles of 64 to 256, in a batch), leading
  * dimensions >= cols, 0 <= batch <= 65535 (0: nothing is done), 0 <= steps <=
  * 64; stride_g >= 0; the outputs of a batch must not overlap: stride_o >=
  * (rows - 1) * ldo + cols, or matrices side by side, cols <= stride_o with

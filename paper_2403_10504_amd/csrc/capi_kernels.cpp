@@ -97,13 +97,13 @@ int atom_k_xent(int dtype, const float* logits, int64_t ldz, const int32_t* tgt,
 }
 
 uint64_t atom_k_linear_xent_fwd_ws_bytes(int dtype, int64_t rows, int V, int d) {
-  return dt_ok(dtype) && linear_xent_ok(dtype, rows, V, d) ? linear_xent_fwd_ws(dtype, rows, V, d) : 0;
+  return dt_ok(dtype) && linear_xent_fwd_ok(dtype, rows, V, d) ? linear_xent_fwd_ws(dtype, rows, V, d) : 0;
 }
 
 int atom_k_linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
                            float* lse, float* loss_rows, int64_t rows, int V, int d, void* ws, uint64_t ws_bytes,
                            void* stream) {
-  if (!dt_ok(dtype) || !linear_xent_ok(dtype, rows, V, d)) return ATOM_EINVAL;
+  if (!dt_ok(dtype) || !linear_xent_fwd_ok(dtype, rows, V, d)) return ATOM_EINVAL;
   if (rows == 0) return ATOM_OK;
   if (!rows_ok(dtype, x, ldx, d) || !rows_ok(dtype, w, ldw, d)) return ATOM_EINVAL;
   if (!tgt || !lse || !loss_rows) return ATOM_EINVAL;
@@ -143,13 +143,13 @@ int atom_k_embed_fwd(int dtype, const int32_t* tok, const void* wte, const void*
 }
 
 uint64_t atom_k_orthogonalize_ws_bytes(int dtype, int batch, int rows, int cols) {
-  return dt_ok(dtype) && batch > 0 && orthogonalize_ok(batch, rows, cols) ? orthogonalize_ws(dtype, batch, rows, cols) : 0;
+  return dt_ok(dtype) && batch > 0 && orthogonalize_ok(dtype, batch, rows, cols) ? orthogonalize_ws(dtype, batch, rows, cols) : 0;
 }
 
 int atom_k_orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,
                          int64_t stride_o, int out_epi, float keep, float scale, int batch, int rows, int cols,
                          const float* coef, int steps, void* ws, uint64_t ws_bytes, void* stream) {
-  if (!dt_ok(dtype) || !orthogonalize_ok(batch, rows, cols)) return ATOM_EINVAL;
+  if (!dt_ok(dtype) || !orthogonalize_ok(dtype, batch, rows, cols)) return ATOM_EINVAL;
   if (ldg < cols || ldo < cols || stride_g < 0) return ATOM_EINVAL;
   if (out_epi != ATOM_EPI_STORE && out_epi != ATOM_EPI_STORE_F32 && out_epi != ATOM_EPI_ACC_F32) return ATOM_EINVAL;
   if (batch > 0 && (!g || !out)) return ATOM_EINVAL;

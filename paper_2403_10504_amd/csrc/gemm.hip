@@ -822,6 +822,19 @@ int gemm_lse_parts(int dtype, int M, int N, int K) {
   return lse_parts(a, esz) + lse_parts(b, esz);
 }
 
+bool gemm_lse_fits(int dtype, int M, int N, int K) {
+  GemmArgs g{};
+  g.M = M, g.N = N, g.K = K;
+  const int esz = dtype == DT_BF16 ? 2 : 4, cut = first_range(g, esz, true, true, EPI_LSE);
+  auto fits = [&](int n) {
+    g.N = n;
+    const Choice c = choose_loss(g, esz, true, true, EPI_LSE);
+    const int64_t tiles = static_cast<int64_t>((M + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn);
+    return c.bm == 256 || tiles < MAX_WORKGROUPS;  // 256-row tiles: workgroups that stay
+  };
+  return fits(cut ? cut : N) && (cut == 0 || fits(N - cut));
+}
+
 }  // namespace atom
 
 // What a product with contiguous operands and rows runs as (tests).

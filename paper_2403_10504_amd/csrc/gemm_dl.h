@@ -980,7 +980,7 @@ template <int BS, int PASSES>
 hipError_t launch_ns(const GemmArgs& g, int batch, bool akc, bool bkc, int epi, hipStream_t s) {
   const int64_t tm = (g.M + BS - 1) / BS, tn = (g.N + BS - 1) / BS;
   const int64_t tiles = (epi == EPI_NS_STEP ? tm * tn : tm * (tm + 1) / 2) * (epi == EPI_NS_PART ? g.ns.ranges : 1);
-  if (tiles * batch > (1ll << 30)) return hipErrorInvalidValue;
+  if (tiles * batch >= MAX_WORKGROUPS) return hipErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(tiles * batch)), block(NT);
 #define ATOM_DL(AK, BK_, E)                                                                              \
   if (akc == AK && bkc == BK_ && epi == E) {                                                             \

@@ -31,6 +31,9 @@ enum Epilogue {
   EPI_NS_PART = 16,    // a range of k of EPI_NS_GRAM: raw fp32 tiles to C
 };
 
+// A dispatch counts its threads along a dimension in 32 bits: workgroups of 256.
+constexpr int64_t MAX_WORKGROUPS = 1 << 24;
+
 // The epilogues of the Newton-Schulz products.  Matrices are fp16 in one or two
 // planes (value = hi + lo); every length is a multiple of 32.  A symmetric
 // product computes the tiles on and below the diagonal and stores each on both
@@ -141,6 +144,8 @@ hipError_t gemm(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, in
 hipError_t gemm_loss(const GemmArgs& g, int dtype, bool a_kcontig, bool b_kcontig, int epi, hipStream_t s);
 // Parts of a row (a maximum and a sum each) that EPI_LSE writes, [part][M].
 int gemm_lse_parts(int dtype, int M, int N, int K);  // (three planes: bf16, six times the k)
+// Whether its launches have less than MAX_WORKGROUPS.
+bool gemm_lse_fits(int dtype, int M, int N, int K);
 
 // LayerNorm over rows of length d (d % 64 == 0, d <= 8192).
 //   y = (x - mean) * rstd * gamma + beta, x fp32, y element type.
@@ -209,6 +214,7 @@ hipError_t dma_acquire(hipStream_t s);
 // Loss of a linear head and its gradients (atom_k_linear_xent_*); false where
 // the sizes are refused.
 bool linear_xent_ok(int dtype, int64_t rows, int V, int d);
+bool linear_xent_fwd_ok(int dtype, int64_t rows, int V, int d);
 uint64_t linear_xent_fwd_ws(int dtype, int64_t rows, int V, int d);
 hipError_t linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
                            float* lse, float* loss_rows, int64_t rows, int V, int d, void* ws, hipStream_t s);
@@ -219,7 +225,7 @@ hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w,
 
 // Newton-Schulz orthogonalisation (atom_k_orthogonalize).  out_epi: EPI_STORE,
 // EPI_STORE_F32 or EPI_ACC_F32; coef: host [steps][3].
-bool orthogonalize_ok(int batch, int rows, int cols);
+bool orthogonalize_ok(int dtype, int batch, int rows, int cols);
 bool orthogonalize_coef_ok(const float* coef, int steps);
 uint64_t orthogonalize_ws(int dtype, int batch, int rows, int cols);
 hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,

@@ -33,6 +33,7 @@ constexpr float LN2 = 0.6931471805599453f;
 // RPB rows per workgroup, 256 / RPB threads per row, each over every
 // (256 / RPB)-th part; the threads' (max, sum) pairs join in LDS in a fixed
 // order.  16 rows read 128 bytes of a part's row; few rows take a workgroup each.
+// (A loop over the rows: 2^28 of them are more workgroups than a dispatch counts.)
 template <int RPB>
 __global__ void __launch_bounds__(256) lse_join_kernel(const float2* __restrict__ part, int64_t rows, int parts,
                                                        const int32_t* __restrict__ tgt,
@@ -41,39 +42,42 @@ __global__ void __launch_bounds__(256) lse_join_kernel(const float2* __restrict_
   constexpr int TPR = 256 / RPB;
   __shared__ float2 red[TPR][RPB];
   const int r = threadIdx.x % RPB, s = threadIdx.x / RPB;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * RPB + r;
-  float m = -INFINITY, sum = 0.f;
-  if (row < rows) {
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * RPB; row0 < rows; row0 += static_cast<int64_t>(gridDim.x) * RPB) {
+    const int64_t row = row0 + r;
+    float m = -INFINITY, sum = 0.f;
+    if (row < rows) {
 #pragma unroll 4
-    for (int p = s; p < parts; p += TPR) {
-      const float2 v = part[static_cast<int64_t>(p) * rows + row];
-      const float n = fmaxf(m, v.x);
-      const float ref = n == -INFINITY ? 0.f : n;
-      sum = sum * __builtin_amdgcn_exp2f(m - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
-      m = n;
+      for (int p = s; p < parts; p += TPR) {
+        const float2 v = part[static_cast<int64_t>(p) * rows + row];
+        const float n = fmaxf(m, v.x);
+        const float ref = n == -INFINITY ? 0.f : n;
+        sum = sum * __builtin_amdgcn_exp2f(m - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
+        m = n;
+      }
     }
-  }
-  red[s][r] = make_float2(m, sum);
-  __syncthreads();
-#pragma unroll
-  for (int h = TPR / 2; h > 0; h >>= 1) {
-    if (s < h) {
-      const float2 a = red[s][r], b = red[s + h][r];
-      const float n = fmaxf(a.x, b.x);
-      const float ref = n == -INFINITY ? 0.f : n;
-      red[s][r] = make_float2(n, a.y * __builtin_amdgcn_exp2f(a.x - ref) + b.y * __builtin_amdgcn_exp2f(b.x - ref));
-    }
+    red[s][r] = make_float2(m, sum);
     __syncthreads();
-  }
-  if (s == 0 && row < rows) {
-    const int t = tgt[row];
-    float l = 0.f, loss = 0.f;
-    if (t >= 0) {
-      l = (red[0][r].x + log2f(red[0][r].y)) * LN2;
-      loss = t < V ? l - ztgt[row] : NAN;
+#pragma unroll
+    for (int h = TPR / 2; h > 0; h >>= 1) {
+      if (s < h) {
+        const float2 a = red[s][r], b = red[s + h][r];
+        const float n = fmaxf(a.x, b.x);
+        const float ref = n == -INFINITY ? 0.f : n;
+        red[s][r] = make_float2(n, a.y * __builtin_amdgcn_exp2f(a.x - ref) + b.y * __builtin_amdgcn_exp2f(b.x - ref));
+      }
+      __syncthreads();
     }
-    lse[row] = l;
-    loss_rows[row] = loss;
+    if (s == 0 && row < rows) {
+      const int t = tgt[row];
+      float l = 0.f, loss = 0.f;
+      if (t >= 0) {
+        l = (red[0][r].x + log2f(red[0][r].y)) * LN2;
+        loss = t < V ? l - ztgt[row] : NAN;
+      }
+      lse[row] = l;
+      loss_rows[row] = loss;
+    }
+    __syncthreads();  // red
   }
 }
 
@@ -258,6 +262,15 @@ FwdWs fwd_ws(int dtype, int64_t rows, int V, int d) {
 }
 }  // namespace
 
+bool linear_xent_fwd_ok(int dtype, int64_t rows, int V, int d) {
+  if (!linear_xent_ok(dtype, rows, V, d)) return false;
+  if (rows == 0) return true;
+  const int m = static_cast<int>(rows);
+  if (!planes(dtype, rows, V, d, false)) return gemm_lse_fits(dtype, m, V, d);
+  const int range = plane_rows(V, d), k = 6 * 32 * ((d + 31) / 32), rest = V % range;
+  return gemm_lse_fits(DT_BF16, m, range, k) && (rest == 0 || gemm_lse_fits(DT_BF16, m, rest, k));
+}
+
 uint64_t linear_xent_fwd_ws(int dtype, int64_t rows, int V, int d) {
   return rows == 0 ? 0 : fwd_ws(dtype, rows, V, d).end;
 }
@@ -297,8 +310,8 @@ hipError_t linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w,
     hipLaunchKernelGGL(lse_join_kernel<1>, dim3(static_cast<unsigned>(rows)), dim3(256), 0, s, part, rows,
                        static_cast<int>(o.parts), tgt, ztgt, V, lse, loss_rows);
   else
-    hipLaunchKernelGGL(lse_join_kernel<16>, dim3(static_cast<unsigned>((rows + 15) / 16)), dim3(256), 0, s, part, rows,
-                       static_cast<int>(o.parts), tgt, ztgt, V, lse, loss_rows);
+    hipLaunchKernelGGL(lse_join_kernel<16>, dim3(static_cast<unsigned>(std::min<int64_t>((rows + 15) / 16, 1 << 20))),
+                       dim3(256), 0, s, part, rows, static_cast<int>(o.parts), tgt, ztgt, V, lse, loss_rows);
   return hipGetLastError();
 }
 

@@ -305,11 +305,20 @@ Ws layout(int dtype, int batch, int rows, int cols) {
 
 }  // namespace
 
-// Tiles are counted in 32 bits, of 64 x 64 at least.
-bool orthogonalize_ok(int batch, int rows, int cols) {
+// Tiles are counted in 32 bits, of 64 x 64 at least, and each is a workgroup.
+bool orthogonalize_ok(int dtype, int batch, int rows, int cols) {
   if (batch < 0 || rows <= 0 || cols <= 0 || batch > 65535 || rows > (1 << 24) || cols > (1 << 24)) return false;
   const int64_t tr = (rows + 63) / 64, tc = (cols + 63) / 64;
-  return tr * tc * std::max(batch, 1) < (1ll << 30) && std::min(tr, tc) * std::min(tr, tc) * std::max(batch, 1) < (1ll << 30);
+  if (batch == 0) return tr * tc < (1ll << 30);
+  if (tr * tc * batch >= (1ll << 30) || std::min(tr, tc) * std::min(tr, tc) * batch >= (1ll << 30)) return false;
+  const Ws o = layout(dtype, batch, rows, cols);
+  const int k = o.k / 32 * (dtype == DT_F32 ? 3 : 1), n = std::max(o.rp, o.cp) / 32 * (dtype == DT_F32 ? 3 : 1);
+  auto fits = [&](int product, int M, int N, int ktiles) {
+    const int bs = tile_of(product, M, N, ktiles, batch);
+    const int64_t tm = (M + bs - 1) / bs, tn = (N + bs - 1) / bs;
+    return (product < 2 ? tm * (tm + 1) / 2 : tm * tn) * batch < MAX_WORKGROUPS;
+  };
+  return fits(0, o.k, o.k, n) && fits(1, o.k, o.k, k) && fits(2, o.rp, o.cp, k);
 }
 
 // Coefficients whose steps keep the singular values, which start in [0, 1], and

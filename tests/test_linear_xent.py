@@ -418,3 +418,32 @@ def test_parts_of_two_launches(rows, V, d):
     assert entries > 2 ** 31
     rest = -(-(V - cut) // 128)
     assert 8 * (entries + rest * rows) <= A.atom_k_linear_xent_fwd_ws_bytes(A.ATOM_BF16, rows, V, d)
+
+
+def test_refuses_more_workgroups_than_a_dispatch():
+    """A dispatch counts its threads in 32 bits; sizes that need more in one launch are refused (no GPU needed)."""
+    P = 1 << 20  # never read
+    for dtype, rows, V, d in ((A.ATOM_F32, 700, 1 << 27, 4), (A.ATOM_BF16, 1 << 24, 1 << 15, 8)):
+        assert A.atom_k_linear_xent_fwd_ws_bytes(dtype, rows, V, d) == 0
+        with pytest.raises(A.AtomError) as e:
+            A.atom_k_linear_xent_fwd(dtype, P, d, P, d, P, P, P, rows, V, d, P, 1 << 60)
+        assert e.value.status == A.ATOM_EINVAL
+    assert A.atom_k_linear_xent_fwd_ws_bytes(A.ATOM_F32, 700, 1 << 22, 4) > 0
+    assert A.atom_k_linear_xent_fwd_ws_bytes(A.ATOM_BF16, 1 << 28, 8, 8) > 0
+
+
+@pytest.mark.gpu
+def test_most_tokens():
+    """2^28 tokens, a block of them over and over: its loss over and over."""
+    t = U.torch()
+    n, rows, V, d = 1 << 16, 1 << 28, 8, 8
+    x, w, tgt = _case("bf16", n, V, d, 0.2, 70)
+    want, wlse, _ = _fwd("bf16", x, w, tgt, d)
+    rl, rs, z, terms = _ref(x, w, tgt, d)
+    bound = _gamma(d) * terms + 2 ** -22 * (z.abs().max().item() + rs.abs().max().item()) + 2 ** -20
+    assert (want[:-1] - rl).abs().max().item() <= 2 * bound
+    loss, lse, behind = _fwd("bf16", x.repeat(rows // n, 1), w, tgt.repeat(rows // n), d)
+    assert loss[rows] == 77.0 and lse[rows] == 77.0 and (behind == 0xA5).all()
+    # (another tile for so many tokens: other sums)
+    assert (loss[:rows].view(-1, n) - want[:-1]).abs().max().item() <= 4 * bound
+    assert (lse[:rows].view(-1, n) - wlse[:-1]).abs().max().item() <= 2 * bound

@@ -318,3 +318,9 @@ def test_far_rows():
     A.atom_k_orthogonalize(A.ATOM_BF16, src.data_ptr(), ld, 0, dst.data_ptr(), ld, 0, A.ATOM_EPI_STORE, 0.0, 1.0, 1, rows,
                            cols, 5, ws.data_ptr(), ws.numel())
     assert t.equal(dst, want)
+
+
+def test_refuses_more_workgroups_than_a_dispatch():
+    """A dispatch counts its threads in 32 bits; batches that need more in one launch are refused (no GPU needed)."""
+    assert A.atom_k_orthogonalize_ws_bytes(A.ATOM_F32, 65535, 1, 64 * 1000) == 0
+    assert A.atom_k_orthogonalize_ws_bytes(A.ATOM_BF16, 65535, 1, 64) > 0
