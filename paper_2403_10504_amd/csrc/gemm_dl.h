@@ -546,7 +546,10 @@ next_tile:
     }
     // One pass over the logits in registers: a lane's 4 TN values of a row,
     // then the four lanes that share the row.  The exponentials (16 TM TN of a
-    // quarter-rate instruction per lane) are what this epilogue costs.
+    // quarter-rate instruction per lane) are what this epilogue costs.  The
+    // difference from the maximum is taken before the factor log2(e): it is exact
+    // next to the maximum, whose own term is 1, and no logit that fp32 holds
+    // overflows on the way.
     float mx[TM], sum[TM], zt[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -578,14 +581,14 @@ next_tile:
       for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) m = fmaxf(m, z[j][r]);
-      mx[i] = rows4_max(m) * LOG2E;
+      mx[i] = rows4_max(m);
       const float ref = mx[i] == -INFINITY ? 0.f : mx[i];  // no column of the row in this block
       float s = 0.f;
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         float e[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) e[r] = __builtin_amdgcn_exp2f(fmaf(z[j][r], LOG2E, -ref));
+        for (int r = 0; r < 4; ++r) e[r] = __builtin_amdgcn_exp2f((z[j][r] - ref) * LOG2E);
         s += (e[0] + e[1]) + (e[2] + e[3]);
       }
       sum[i] = rows4_sum(s);

@@ -28,7 +28,7 @@
 namespace atom {
 namespace {
 
-constexpr float LN2 = 0.6931471805599453f;
+constexpr float LOG2E = 1.4426950408889634f;
 
 // RPB rows per workgroup, 256 / RPB threads per row, each over every
 // (256 / RPB)-th part; the threads' (max, sum) pairs join in LDS in a fixed
@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(256) lse_join_kernel(const float2* __restrict_
         const float2 v = part[static_cast<int64_t>(p) * rows + row];
         const float n = fmaxf(m, v.x);
         const float ref = n == -INFINITY ? 0.f : n;
-        sum = sum * __builtin_amdgcn_exp2f(m - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
+        sum = sum * __builtin_amdgcn_exp2f((m - ref) * LOG2E) + v.y * __builtin_amdgcn_exp2f((v.x - ref) * LOG2E);
         m = n;
       }
     }
@@ -63,7 +63,8 @@ __global__ void __launch_bounds__(256) lse_join_kernel(const float2* __restrict_
         const float2 a = red[s][r], b = red[s + h][r];
         const float n = fmaxf(a.x, b.x);
         const float ref = n == -INFINITY ? 0.f : n;
-        red[s][r] = make_float2(n, a.y * __builtin_amdgcn_exp2f(a.x - ref) + b.y * __builtin_amdgcn_exp2f(b.x - ref));
+        red[s][r] = make_float2(n, a.y * __builtin_amdgcn_exp2f((a.x - ref) * LOG2E) +
+                                       b.y * __builtin_amdgcn_exp2f((b.x - ref) * LOG2E));
       }
       __syncthreads();
     }
@@ -71,8 +72,11 @@ __global__ void __launch_bounds__(256) lse_join_kernel(const float2* __restrict_
       const int t = tgt[row];
       float l = 0.f, loss = 0.f;
       if (t >= 0) {
-        l = (red[0][r].x + log2f(red[0][r].y)) * LN2;
-        loss = t < V ? l - ztgt[row] : NAN;
+        const float m = red[0][r].x, g = logf(red[0][r].y);
+        l = m + g;
+        // not l - z: what l rounds off would be all of the loss of a token whose
+        // target has nearly the whole sum
+        loss = t < V ? (m - ztgt[row]) + g : NAN;
       }
       lse[row] = l;
       loss_rows[row] = loss;

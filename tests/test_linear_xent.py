@@ -447,3 +447,76 @@ def test_most_tokens():
     # (another tile for so many tokens: other sums)
     assert (loss[:rows].view(-1, n) - want[:-1]).abs().max().item() <= 4 * bound
     assert (lse[:rows].view(-1, n) - wlse[:-1]).abs().max().item() <= 2 * bound
+
+
+def _exact_case(dtype, rows, V, d, unit, gap, seed):
+    """Logits that every product gives exactly: row n of x has `unit` at column n % d, w holds small integers there, and
+    the target's is `gap` above all others."""
+    t = U.torch()
+    g = t.Generator(device="cuda").manual_seed(seed)
+    dt = t.bfloat16 if dtype == "bf16" else t.float32
+    x = t.zeros((rows, d), device="cuda", dtype=dt)
+    n = t.arange(rows, device="cuda")
+    x[n, n % d] = unit
+    w = t.randint(-16, 9, (V, d), device="cuda", generator=g).to(dt)
+    top = t.randint(0, V, (d,), device="cuda", generator=g)
+    w[top, t.arange(d, device="cuda")] = 8.0 + gap
+    return x, w, top[n % d].int()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,rows,V,d", [("bf16", 300, 777, 64), ("bf16", 4100, 9001, 128), ("f32", 300, 777, 64),
+                                            ("f32", 1100, 2001, 2052), ("bf16", 70, 50257, 64)])
+def test_small_losses_of_large_logits(dtype, rows, V, d):
+    """A target whose logit (1088) stands 64 above all others: the loss is nearly 0, and never below."""
+    x, w, tgt = _exact_case(dtype, rows, V, d, 64.0, 9.0, 60)
+    loss, lse, _ = _fwd(dtype, x, w, tgt, d)
+    rl, rs, z, _ = _ref(x, w, tgt, d)
+    assert z.max().item() == 64 * 17 and rl.max().item() < V * 1e-27
+    assert (loss[:rows] >= 0).all() and loss[:rows].max().item() < V * 1e-27
+    assert (lse[:rows] == 64 * 17).all()
+    # 0 to 4 above the rest: the sum (1 to V) is off by at most 32 roundings (adds
+    # of 8 columns, lanes, parts) and an exponential of up to 2^-20
+    x, w, tgt = _exact_case(dtype, rows, V, d, 4.0, 1.0, 61)
+    w += 200.0  # logits of 768 to 836
+    loss, lse, _ = _fwd(dtype, x, w, tgt, d)
+    rl, rs, z, _ = _ref(x, w, tgt, d)
+    assert z.max().item() == 836
+    assert (loss[:rows] - rl).abs().max().item() <= 32 * U32 + 2 ** -20 + U32 * rl.max().item()
+    assert ((lse[:rows] - rs).abs().max().item() <= 32 * U32 + 2 ** -20 + U32 * 850)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_column(dtype):
+    """A vocabulary of one: lse is the logit, the loss exactly 0."""
+    t = U.torch()
+    x, w, tgt = _case(dtype, 50, 1, 72, 0.2, 62, 0, 300.0)
+    loss, lse, _ = _fwd(dtype, x, w, tgt, 72)
+    z = (x[:, :72].double() @ w[:, :72].double().T)[:, 0]
+    terms = (x.double().abs() @ w.double().abs().T).max().item()
+    assert (loss[:50] == 0).all()
+    assert (lse[:50] - t.where(tgt >= 0, z, 0.0)).abs().max().item() <= _gamma(72) * terms
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_largest_logits(dtype):
+    """Logits next to the largest number of fp32, of both signs, alike and alone: loss and lse are those of the definition."""
+    t = U.torch()
+    V, d = 100, 64
+    big = t.tensor(1.7e19).to(t.bfloat16).item()  # big^2 is 2.9e38
+    dt = t.bfloat16 if dtype == "bf16" else t.float32
+    x = t.zeros((4, d), device="cuda", dtype=dt)
+    w = t.zeros((V, d), device="cuda", dtype=dt)
+    for r, v in enumerate((big, -big, big, -big)):
+        x[r, r] = v
+    w[:, 0], w[:, 1], w[:, 2] = big, big, -big  # all alike: the largest, the lowest, the lowest
+    w[:, 3], w[7, 3] = big, -big                # one largest among lowest
+    tgt = t.tensor([5, 5, 5, 7], device="cuda", dtype=t.int32)
+    loss, lse, _ = _fwd(dtype, x, w, tgt, d)
+    want = t.tensor([1.0, 1.0, 1.0, 0.0], device="cuda") * np.log(V)
+    # a sum of 100 ones is exact, its logarithm within 2^-22
+    assert (loss[:4] - want).abs().max().item() <= 2 ** -21
+    top = t.tensor([big * big, -big * big, -big * big, big * big], device="cuda", dtype=t.float32)
+    assert ((lse[:4] - top).abs() <= 2.0 ** -22 * top.abs()).all()
