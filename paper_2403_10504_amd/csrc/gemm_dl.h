@@ -262,7 +262,7 @@ gemm_dl_kernel(GemmArgs g) {
   constexpr bool LOSS = EPI == EPI_LSE || EPI == EPI_DZ;
   constexpr float LOG2E = 1.4426950408889634f;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[LDS];
-  // of the tile's rows: target column; lse (base 2) and factor
+  // of the tile's rows: target column; lse and factor
   __shared__ int row_tgt[LOSS ? BM : 1];
   __shared__ float2 row_lse_scale[EPI == EPI_DZ ? BM : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -516,7 +516,7 @@ next_tile:
       const bool on = my_tgt >= 0;
       row_tgt[tid] = my_tgt;
       if constexpr (EPI == EPI_DZ)
-        row_lse_scale[tid] = on && my_scale != 0.f ? make_float2(my_lse * LOG2E, my_tgt < g.V ? my_scale : NAN)
+        row_lse_scale[tid] = on && my_scale != 0.f ? make_float2(my_lse, my_tgt < g.V ? my_scale : NAN)
                                                    : make_float2(0.f, 0.f);
     }
     barrier_after_reads();  // also: every wave is done with the stages
@@ -678,8 +678,9 @@ next_tile:
         const int i = h * (RB / 16) + ii;
         if constexpr (E == EPI_DZ) {
           // dz = (softmax - onehot) * scale; a row that takes no part has logits
-          // of zero (its row of A is zero) and scale zero.  An FMA, the
-          // exponential and a product per logit; the one-hot only where it is.
+          // of zero (its row of A is zero) and scale zero.  A difference (exact
+          // next to lse, where a target that has nearly the whole sum is), two
+          // products and the exponential per logit; the one-hot only where it is.
           const float2 ls = row_lse_scale[wm * TM * 16 + 16 * i + lr];
           const bool hit = trow[i] >= 0 && trow[i] < TN * 16;
           float z[TN][4];
@@ -687,7 +688,7 @@ next_tile:
           for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -ls.x)) * ls.y;
+              const float p = __builtin_amdgcn_exp2f((acc[i][j][r] - ls.x) * LOG2E) * ls.y;
               z[j][r] = GUARD && col0 + 16 * j + 4 * lg + r >= ga.N ? 0.f : p;
             }
           if (__builtin_amdgcn_ballot_w64(hit) != 0) {

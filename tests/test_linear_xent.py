@@ -520,3 +520,13 @@ def test_largest_logits(dtype):
     assert (loss[:4] - want).abs().max().item() <= 2 ** -21
     top = t.tensor([big * big, -big * big, -big * big, big * big], device="cuda", dtype=t.float32)
     assert ((lse[:4] - top).abs() <= 2.0 ** -22 * top.abs()).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,rows,V,d", [("bf16", 300, 777, 64), ("f32", 300, 777, 64), ("f32", 1100, 2001, 2052)])
+def test_small_gradients_of_large_logits(dtype, rows, V, d):
+    """The same targets' dz is p - 1 with p the nearest to 1: what is left are the other logits, e^-64 and less."""
+    x, w, tgt = _exact_case(dtype, rows, V, d, 64.0, 9.0, 60)
+    _, lse, _ = _fwd(dtype, x, w, tgt, d)
+    dx, dw = _bwd(dtype, x, w, tgt, lse, d)
+    assert dx.abs().max().item() <= V * 16 * 2e-28 and dw.abs().max().item() <= rows * 64 * 2e-28
