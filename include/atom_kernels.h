@@ -171,7 +171,9 @@ int atom_k_embed_fwd(int dtype, const int32_t* tok, const void* wte, const void*
  * coef: HOST array [steps][3] of a, b, c, read before the call returns; NULL:
  * the quintic (3.4445, -4.7750, 2.0315) in every step.  The products run on
  * the shorter side: A = X^T X and X (...) where rows > cols.  A matrix of
- * zeros gives zeros; one with an infinity or a NaN gives NaN throughout.
+ * zeros gives zeros; one with an infinity or a NaN gives NaN throughout.  Where
+ * |g|_F is far below 1e-7 X is small, and as accurate as any other: it is held
+ * relative to a bound of its singular values (22 bits, down to 2^-35 of the bound).
  * bf16: products in fp16 with fp32 sums (X itself in 22 bits), off by about
  * the result's own rounding; fp32: every factor in 22 bits.
  * Any rows, cols >= 1 (with less than 2^30 tiles of 64 x 64, and 2^24 of the

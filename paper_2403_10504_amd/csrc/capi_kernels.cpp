@@ -157,6 +157,7 @@ int atom_k_orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
   if (reinterpret_cast<uintptr_t>(g) % esz || reinterpret_cast<uintptr_t>(out) % osz) return ATOM_EINVAL;
   if (batch > 1 && stride_o < (rows - 1) * ldo + cols && !(stride_o >= cols && stride_o <= ldo / batch)) return ATOM_EINVAL;
   if (steps < 0 || steps > ATOM_NS_MAX_STEPS) return ATOM_EINVAL;
+  static_assert(ATOM_NS_MAX_STEPS == NS_EXPS, "steps");
   float own[3 * ATOM_NS_MAX_STEPS];
   if (!coef) {
     for (int k = 0; k < steps; ++k) own[3 * k] = 3.4445f, own[3 * k + 1] = -4.7750f, own[3 * k + 2] = 2.0315f;

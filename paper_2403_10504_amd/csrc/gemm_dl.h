@@ -331,6 +331,13 @@ next_tile:
     }
   }
 
+  // the scales of X in this step and the next (the result has none)
+  int e0 = 0, e1 = 0;
+  if constexpr (EPI == EPI_NS_POLY || EPI == EPI_NS_STEP) {
+    e0 = g.ns.exps[split * NS_EXPS];
+    if (EPI == EPI_NS_STEP && g.ns.out_mode == 3) e1 = g.ns.exps[split * NS_EXPS + 1];
+  }
+
   typename OA::Src sra[OA::LPT];
   typename OB::Src srb[OB::LPT];
   auto init_src = [&](int m0, int n0) {
@@ -779,6 +786,9 @@ next_tile:
     // consecutive columns there, 64 bytes by eight lanes.
     constexpr bool LO = EPI == EPI_NS_STEP || PASSES == 3, AUX = EPI != EPI_NS_GRAM;
     const NsArgs& ns = g.ns;
+    // X = 2^-e0 Y, A = 2^-2e0 Y Y^T: B = b A + c A^2, and 2^e1 (a X + B X)
+    const float alpha = ldexpf(g.alpha, EPI == EPI_NS_POLY ? -4 * e0 : EPI == EPI_NS_STEP ? e1 - e0 : 0);
+    const float beta = ldexpf(ns.beta, EPI == EPI_NS_POLY ? -2 * e0 : e1 - e0);
     const bool col_in = nb < g.N && rsub < RPP, last = EPI == EPI_NS_STEP && ns.out_mode != 3;
     const int64_t base = split * ns.sc;
     const int nc = min(nb, g.N - 4);
@@ -813,9 +823,9 @@ next_tile:
         if constexpr (AUX) {
           float x[4];
           unpack_planes(xh[h][q], LO ? xl[h][q] : make_uint2(0, 0), LO, x);
-          for (int r = 0; r < 4; ++r) v[r] = fmaf(g.alpha, v[r], ns.beta * x[r]);
+          for (int r = 0; r < 4; ++r) v[r] = fmaf(alpha, v[r], beta * x[r]);
         } else {
-          for (int r = 0; r < 4; ++r) v[r] *= g.alpha;
+          for (int r = 0; r < 4; ++r) v[r] *= alpha;
         }
         const int m = row0 + h * RB + RPP * q + rsub;
         if (last) {

@@ -38,6 +38,7 @@ constexpr int64_t MAX_WORKGROUPS = 1 << 24;
 // planes (value = hi + lo); every length is a multiple of 32.  A symmetric
 // product computes the tiles on and below the diagonal and stores each on both
 // sides of it.
+constexpr int NS_EXPS = 64;  // most steps
 struct NsArgs {
   int64_t sa, sb, sc;        // elements from one matrix of the batch to the next: A, B; C and aux
   int64_t pa, pb;            // elements from the hi to the lo plane of A and B
@@ -46,6 +47,9 @@ struct NsArgs {
   const void *aux, *aux_lo;  // as C
   void* C_lo;
   float beta;
+  // X of a step is held times 2^e, e per matrix and step (orthogonalize.hip):
+  // this step's of matrix 0, the next step's behind it, matrices NS_EXPS apart
+  const int* exps;
   // the last step: out = scale * (...), of orows x ocols, instead of C
   void* out;
   int64_t ldo, so;

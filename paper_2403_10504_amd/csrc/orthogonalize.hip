@@ -7,8 +7,8 @@
 //
 // Every step works on the singular values alone, s <- a s + b s^3 + c s^5.
 // All products run on the direct-load kernel (gemm_dl.h) in fp16 MFMAs with
-// fp32 sums, on matrices scaled by 2^10 and padded with zeros to multiples of
-// 32, and each step's sums and scalings are its products' epilogues: three
+// fp32 sums, on matrices scaled by 2^10 (X also by a power of two per matrix
+// and step, see pack_kernel) and padded with zeros to multiples of 32, and each step's sums and scalings are its products' epilogues: three
 // launches a step.  A and B are symmetric, so their products take the tiles on
 // and below the diagonal.
 //
@@ -98,13 +98,46 @@ __global__ void __launch_bounds__(256) norm_kernel(const T* __restrict__ g, int6
   if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// X = SCALE * g / (norm + EPS) in two planes [rp][cp], zeros past the matrix.
-// A norm that is not finite makes all of X NaN.
+// Largest |a s + b s^3 + c s^5| of s in [0, top], from its extrema: a + 3 b x +
+// 5 c x^2 = 0, x = s^2.
+__host__ __device__ inline double step_bound(double a, double b, double c, double top) {
+  auto f = [=](double s) { return fabs(s * (a + s * s * (b + c * s * s))); };
+  const double t = top * top, disc = 9 * b * b - 20 * a * c;
+  double most = f(top);
+  if (c != 0.0 && disc >= 0.0) {
+    const double q = sqrt(disc), x0 = (-3 * b + q) / (10 * c), x1 = (-3 * b - q) / (10 * c);
+    if (x0 > 0.0 && x0 < t) most = fmax(most, f(sqrt(x0)));
+    if (x1 > 0.0 && x1 < t) most = fmax(most, f(sqrt(x1)));
+  } else if (c == 0.0 && b != 0.0) {
+    const double x = -a / (3 * b);
+    if (x > 0.0 && x < t) most = fmax(most, f(sqrt(x)));
+  }
+  return most;
+}
+
+// The power of two that a matrix of norm at most r is held times: r 2^e in [1/2,
+// 1); none for r of 1/2 and more, and 2^126 at most (a norm of 2^-150).
+__host__ __device__ inline int exponent_of(double r) {
+  if (!(r < 0.5 && r > 0.0)) return 0;
+  const int e = -1 - ilogb(r);
+  return e < 126 ? e : 126;
+}
+
+struct Steps {
+  float coef[3 * NS_EXPS];
+  int exps[NS_EXPS];  // of a norm of 1
+  int n;
+};
+
+// X = SCALE * 2^e * g / (norm + EPS) in two planes [rp][cp], zeros past the
+// matrix.  A norm that is not finite makes all of X NaN.  The EPS makes X small
+// where the norm is far below it, and planes are fixed-point: 2^e, from the
+// bound on the singular values, keeps their 22 bits.  exps: e of every step.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ g, int64_t ldg, int64_t stride, int rows,
                                                    int cols, int rp, int cp, int lx, const double* __restrict__ part,
-                                                   int parts, f16_t* __restrict__ hi, f16_t* __restrict__ lo,
-                                                   int64_t sx) {
+                                                   int parts, Steps steps, int* __restrict__ exps,
+                                                   f16_t* __restrict__ hi, f16_t* __restrict__ lo, int64_t sx) {
   __shared__ double red[4];
   g += blockIdx.y * stride;
   hi += blockIdx.y * sx;
@@ -116,7 +149,18 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ g, int6
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
   s = (red[0] + red[1]) + (red[2] + red[3]);
-  const double f = s < INFINITY ? SCALE / (sqrt(s) + EPS) : NAN;
+  const double norm = sqrt(s), ratio = norm / (norm + EPS);
+  const int e0 = exponent_of(ratio);
+  const double f = s < INFINITY ? ldexp(SCALE / (norm + EPS), e0) : NAN;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    int* e = exps + blockIdx.y * NS_EXPS;
+    e[0] = e0;
+    double r = ratio;
+    for (int k = 1; k < steps.n; ++k) {
+      if (e0 > 0) r = step_bound(steps.coef[3 * k - 3], steps.coef[3 * k - 2], steps.coef[3 * k - 1], r);
+      e[k] = e0 > 0 ? exponent_of(r) : steps.exps[k];
+    }
+  }
   const int x = threadIdx.x & ((1 << lx) - 1), rpb = 256 >> lx;
   for (int r = blockIdx.x * rpb + (threadIdx.x >> lx); r < rp; r += gridDim.x * rpb) {
     const T* p = g + r * ldg;
@@ -139,7 +183,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ g, int6
 
 template <typename T>
 void launch_pack(const void* g, int64_t ldg, int64_t stride, int batch, int rows, int cols, int rp, int cp,
-                 double* part, f16_t* hi, f16_t* lo, hipStream_t s) {
+                 double* part, const Steps& steps, int* exps, f16_t* hi, f16_t* lo, hipStream_t s) {
   const T* p = static_cast<const T*>(g);
   const int e = 16 / static_cast<int>(sizeof(T));
   const bool vec = reinterpret_cast<uintptr_t>(g) % 16 == 0 && ldg % e == 0 && stride % e == 0;
@@ -156,11 +200,11 @@ void launch_pack(const void* g, int64_t ldg, int64_t stride, int batch, int rows
   if (vec) {
     hipLaunchKernelGGL((norm_kernel<T, true>), ngrid, block, 0, s, p, ldg, stride, rows, cols, lx, part);
     hipLaunchKernelGGL((pack_kernel<T, true>), pgrid, block, 0, s, p, ldg, stride, rows, cols, rp, cp, lx, part, parts,
-                       hi, lo, sx);
+                       steps, exps, hi, lo, sx);
   } else {
     hipLaunchKernelGGL((norm_kernel<T, false>), ngrid, block, 0, s, p, ldg, stride, rows, cols, lx, part);
     hipLaunchKernelGGL((pack_kernel<T, false>), pgrid, block, 0, s, p, ldg, stride, rows, cols, rp, cp, lx, part,
-                       parts, hi, lo, sx);
+                       parts, steps, exps, hi, lo, sx);
   }
 }
 
@@ -211,12 +255,13 @@ __global__ void __launch_bounds__(256) gram_join_kernel(const float* __restrict_
 // No steps: out from X itself.
 template <typename TO, bool ACC>
 __global__ void __launch_bounds__(256) unpack_kernel(const f16_t* __restrict__ hi, const f16_t* __restrict__ lo,
-                                                     int64_t sx, int cp, TO* __restrict__ out, int64_t ldo, int64_t so,
-                                                     int rows, int cols, float scale, float keep) {
+                                                     int64_t sx, int cp, const int* __restrict__ exps,
+                                                     TO* __restrict__ out, int64_t ldo, int64_t so, int rows, int cols,
+                                                     float scale, float keep) {
   const int64_t n = static_cast<int64_t>(rows) * cols;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
     const int64_t row = i / cols, c = i - row * cols, at = blockIdx.y * sx + row * cp + c;
-    const float v = scale * (static_cast<float>(hi[at]) + static_cast<float>(lo[at]));
+    const float v = scale * ldexpf(static_cast<float>(hi[at]) + static_cast<float>(lo[at]), -exps[blockIdx.y * NS_EXPS]);
     TO* o = out + blockIdx.y * so + row * ldo + c;
     *o = ACC ? from_f<TO>(fmaf(keep, to_f<TO>(*o), v)) : from_f<TO>(v);
   }
@@ -278,7 +323,7 @@ int ranges_of(int M, int ktiles, int batch) {
 struct Ws {
   int rp, cp, k;  // padded lengths, the smaller of them
   int ranges;     // of k that A is the sum of
-  uint64_t part, x[2], xl[2], a, al, b, bl, sums, end;
+  uint64_t part, exps, x[2], xl[2], a, al, b, bl, sums, end;
 };
 Ws layout(int dtype, int batch, int rows, int cols) {
   Ws w;
@@ -288,6 +333,7 @@ Ws layout(int dtype, int batch, int rows, int cols) {
   uint64_t at = 0;
   auto take = [&](uint64_t n) { const uint64_t o = at; at += n; return o; };
   w.part = take(up(8ull * batch * NORM_BLOCKS));
+  w.exps = take(up(sizeof(int) * NS_EXPS * batch));
   w.x[0] = take(x);
   w.xl[0] = take(x);
   w.x[1] = take(x);
@@ -333,17 +379,7 @@ bool orthogonalize_coef_ok(const float* coef, int steps) {
     auto p = [&](double x) { return std::fabs(b * x + c * x * x); };
     double poly = p(t);
     if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < t) poly = std::max(poly, p(-b / (2 * c)));
-    auto f = [&](double s) { return std::fabs(s * (a + s * s * (b + c * s * s))); };
-    double next = f(top);
-    // a + 3 b x + 5 c x^2 = 0, x = s^2
-    const double disc = 9 * b * b - 20 * a * c;
-    if (c != 0.0 && disc >= 0.0) {
-      for (const double x : {(-3 * b + std::sqrt(disc)) / (10 * c), (-3 * b - std::sqrt(disc)) / (10 * c)})
-        if (x > 0.0 && x < t) next = std::max(next, f(std::sqrt(x)));
-    } else if (c == 0.0 && b != 0.0 && -a / (3 * b) > 0.0 && -a / (3 * b) < t) {
-      next = std::max(next, f(std::sqrt(-a / (3 * b))));
-    }
-    top = next;
+    top = step_bound(a, b, c, top);
     if (poly > 32.0 || top > 4.0 || std::fabs(a) > 32.0) return false;
   }
   return true;
@@ -359,11 +395,20 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
   auto at = [&](uint64_t off) { return reinterpret_cast<f16_t*>(base + off); };
   const int64_t sx = static_cast<int64_t>(o.rp) * o.cp, sa = static_cast<int64_t>(o.k) * o.k;
   double* part = reinterpret_cast<double*>(base + o.part);
+  int* exps = reinterpret_cast<int*>(base + o.exps);
   const int64_t n = static_cast<int64_t>(rows) * cols;
+  Steps st{};
+  st.n = steps;
+  double r = 1.0;
+  for (int k = 0; k < steps; ++k) {
+    for (int i = 0; i < 3; ++i) st.coef[3 * k + i] = coef[3 * k + i];
+    st.exps[k] = exponent_of(r);
+    r = step_bound(coef[3 * k], coef[3 * k + 1], coef[3 * k + 2], r);
+  }
   if (dtype == DT_BF16)
-    launch_pack<bf16_t>(g, ldg, stride_g, batch, rows, cols, o.rp, o.cp, part, at(o.x[0]), at(o.xl[0]), s);
+    launch_pack<bf16_t>(g, ldg, stride_g, batch, rows, cols, o.rp, o.cp, part, st, exps, at(o.x[0]), at(o.xl[0]), s);
   else
-    launch_pack<float>(g, ldg, stride_g, batch, rows, cols, o.rp, o.cp, part, at(o.x[0]), at(o.xl[0]), s);
+    launch_pack<float>(g, ldg, stride_g, batch, rows, cols, o.rp, o.cp, part, st, exps, at(o.x[0]), at(o.xl[0]), s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int out_mode = out_epi == EPI_ACC_F32 ? 2 : out_epi == EPI_STORE_F32 || dtype == DT_F32 ? 1 : 0;
@@ -371,7 +416,7 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
   if (steps == 0) {
     const dim3 ugrid(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 2048)), batch);
 #define ATOM_UNPACK(TO, ACC)                                                                                     \
-  hipLaunchKernelGGL((unpack_kernel<TO, ACC>), ugrid, dim3(256), 0, s, at(o.x[0]), at(o.xl[0]), sx, o.cp,        \
+  hipLaunchKernelGGL((unpack_kernel<TO, ACC>), ugrid, dim3(256), 0, s, at(o.x[0]), at(o.xl[0]), sx, o.cp, exps,  \
                      static_cast<TO*>(out), ldo, stride_o, rows, cols, scale, keep)
     if (out_mode == 0) ATOM_UNPACK(bf16_t, false);
     else if (out_mode == 1) ATOM_UNPACK(float, false);
@@ -423,6 +468,7 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
     q.ns.sa = q.ns.sb = q.ns.sc = sa;
     q.ns.pa = q.ns.pb = at(o.al) - at(o.a);
     q.ns.aux = at(o.a), q.ns.aux_lo = at(o.al), q.ns.beta = b, q.ns.C_lo = at(o.bl);
+    q.ns.exps = exps + k;
     e = product(q, o.k, true, true, EPI_NS_POLY);
     if (e != hipSuccess) return e;
     GemmArgs r{};
@@ -435,6 +481,7 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
     r.ns.pa = wide ? at(o.bl) - at(o.b) : at(o.xl[i]) - at(o.x[i]);
     r.ns.pb = wide ? at(o.xl[i]) - at(o.x[i]) : at(o.bl) - at(o.b);
     r.ns.aux = at(o.x[i]), r.ns.aux_lo = at(o.xl[i]), r.ns.beta = a, r.ns.C_lo = at(o.xl[1 - i]);
+    r.ns.exps = exps + k;
     r.ns.out_mode = 3;
     if (k == steps - 1) {
       r.ns.out = out, r.ns.ldo = ldo, r.ns.so = stride_o, r.ns.out_mode = out_mode;

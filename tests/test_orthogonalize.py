@@ -324,3 +324,82 @@ def test_refuses_more_workgroups_than_a_dispatch():
     """A dispatch counts its threads in 32 bits; batches that need more in one launch are refused (no GPU needed)."""
     assert A.atom_k_orthogonalize_ws_bytes(A.ATOM_F32, 65535, 1, 64 * 1000) == 0
     assert A.atom_k_orthogonalize_ws_bytes(A.ATOM_BF16, 65535, 1, 64) > 0
+
+
+def _small_norm_check(dtype, got, g, coef, scale=1.0):
+    """The result against the recursion in 64 bits, bounded by the error of the recursion with the kernels' planes, which
+    are taken of X times the power of two that brings the bound of its singular values into [1/2, 1)."""
+    t = U.torch()
+    x = g.double()
+    ref = _recursion(x, coef) * scale
+    tall = x.shape[0] > x.shape[1]
+    y = x.T if tall else x
+    y = y / (t.linalg.vector_norm(y) + 1e-7)
+    f = 2 if dtype == "f32" else 1
+    r = t.linalg.vector_norm(y).item()
+    for a, b, c in coef:
+        a, b, c = (float(np.float32(v)) for v in (a, b, c))
+        e = 2.0 ** max(0.0, np.floor(-np.log2(r)))
+        v = np.linspace(0.0, r, 4097)
+        r = np.abs(a * v + b * v ** 3 + c * v ** 5).max()
+        y = _planes(y * e, 2)
+        yf = _planes(y, f)
+        s = _planes(yf @ yf.T, f)
+        p = _planes(b / e ** 2 * s + c / e ** 4 * (s @ s), f)
+        y = (a * y + p @ yf) / e
+    y = (y.T if tall else y) * scale
+    size = t.linalg.vector_norm(ref).item()
+    off = t.linalg.vector_norm(y - ref).item()
+    k = max(g.shape)
+    # as in _check; off counts four times: a bound next to a power of two may take
+    # the other exponent
+    sums = size * 2.0 ** -24 * (4 + (3 * k / 32) ** 0.5) * len(coef) * (8.0 if dtype == "f32" else 100.0)
+    bound = 4.0 * off + sums + size * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) + 2.0 ** -149 * (g.numel() ** 0.5)
+    err = t.linalg.vector_norm(got.double() - ref).item()
+    assert size > 0 and err <= bound, (err / size, bound / size, off / size)
+    assert bound <= size * (2.0 ** -5 if dtype == "bf16" else 2.0 ** -12)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("coef", [[], [QUINTIC] * 5, [(1.5, -0.5, 0.0)] * 20, [(0.25, 0.1, 0.0)] * 3 + [QUINTIC] * 8])
+@pytest.mark.parametrize("rows,cols", [(40, 72), (200, 130)])
+def test_small_norms(dtype, coef, rows, cols):
+    """Norms far below the 1e-7 in the divisor, down to a few of the type's smallest numbers: X is small, and keeps its
+    bits.  Beside matrices of ordinary norms in a batch, which stay as they are alone."""
+    t = U.torch()
+    base = _matrix(rows, cols, "f32", 71, "gauss").double()
+    base = base / t.linalg.vector_norm(base)
+    dt = t.bfloat16 if dtype == "bf16" else t.float32
+    norms = [1.0, 1e-6, 3e-8, 1e-9, 1e-11, 1e-14, 1e-20, 1e-30, 1e-36]
+    g = t.stack([(base * v).to(dt) for v in norms])
+    # the result's scale keeps it out of the subnormal numbers
+    got = _run(dtype, g, coef, scale=2.0 ** 40)
+    for i, v in enumerate(norms):
+        _small_norm_check(dtype, got[i], g[i], coef, 2.0 ** 40)
+        assert t.equal(got[i], _run(dtype, g[i:i + 1], coef, scale=2.0 ** 40)[0]), v
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_entry(dtype):
+    """A single entry is the norm itself, also the type's smallest: g / (g + 1e-7), and the recursion of a number."""
+    t = U.torch()
+    dt = t.bfloat16 if dtype == "bf16" else t.float32
+    least = 2.0 ** -133 if dtype == "bf16" else 2.0 ** -149
+    for v in (1.0, -3e-8, 1e-12, -1e-25, 1e-37, least, -7 * least):
+        g = t.zeros((1, 33, 70), device="cuda", dtype=dt)
+        g[0, 20, 50] = v
+        v = g[0, 20, 50].double().item()
+        x = v / (abs(v) + 1e-7)
+        for coef in ([], [QUINTIC] * 5):
+            want = x
+            for a, b, c in coef:
+                a, b, c = (float(np.float32(k)) for k in (a, b, c))
+                want = a * want + b * want ** 3 + c * want ** 5
+            got = _run(dtype, g, coef, A.ATOM_EPI_STORE_F32)[0]
+            # per step X, A and B in 22 bits: B is off by (|b| x^2 + 2 |c| x^4 + |B|) 2^-23, up to 12 of them, and a step
+            # next to |x| = 1 takes an error times 1.2.  bf16: A and B in 11, nothing beside a while X is small
+            off = (2.0 ** -21 * (len(coef) + 1) * 8 if dtype == "f32" or abs(x) < 0.01 or not coef else 2.0 ** -5) * abs(want)
+            assert abs(got[20, 50].item() - want) <= off + 2.0 ** -149
+            assert (got != 0).sum().item() == 1
