@@ -174,8 +174,10 @@ int atom_k_embed_fwd(int dtype, const int32_t* tok, const void* wte, const void*
  * zeros gives zeros; one with an infinity or a NaN gives NaN throughout.  Where
  * |g|_F is far below 1e-7 X is small, and as accurate as any other: it is held
  * relative to a bound of its singular values (22 bits, down to 2^-35 of the bound).
- * bf16: products in fp16 with fp32 sums (X itself in 22 bits), off by about
- * the result's own rounding; fp32: every factor in 22 bits.
+ * The result's type sets the precision: in bf16, products in fp16 with fp32 sums
+ * (X itself in 22 bits), off by about the result's own rounding; in fp32 (of bf16
+ * gradients too, ATOM_EPI_STORE_F32 and ATOM_EPI_ACC_F32), every factor in 22
+ * bits, in 2.1 to 2.9 times the time.
  * Any rows, cols >= 1 (with less than 2^30 tiles of 64 x 64, and 2^24 of the
  * products' tiles of 64 to 256, in a batch), leading
  * dimensions >= cols, 0 <= batch <= 65535 (0: nothing is done), 0 <= steps <=

@@ -143,13 +143,13 @@ int atom_k_embed_fwd(int dtype, const int32_t* tok, const void* wte, const void*
 }
 
 uint64_t atom_k_orthogonalize_ws_bytes(int dtype, int batch, int rows, int cols) {
-  return dt_ok(dtype) && batch > 0 && orthogonalize_ok(dtype, batch, rows, cols) ? orthogonalize_ws(dtype, batch, rows, cols) : 0;
+  return dt_ok(dtype) && batch > 0 && orthogonalize_ok(batch, rows, cols) ? orthogonalize_ws(batch, rows, cols) : 0;
 }
 
 int atom_k_orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,
                          int64_t stride_o, int out_epi, float keep, float scale, int batch, int rows, int cols,
                          const float* coef, int steps, void* ws, uint64_t ws_bytes, void* stream) {
-  if (!dt_ok(dtype) || !orthogonalize_ok(dtype, batch, rows, cols)) return ATOM_EINVAL;
+  if (!dt_ok(dtype) || !orthogonalize_ok(batch, rows, cols)) return ATOM_EINVAL;
   if (ldg < cols || ldo < cols || stride_g < 0) return ATOM_EINVAL;
   if (out_epi != ATOM_EPI_STORE && out_epi != ATOM_EPI_STORE_F32 && out_epi != ATOM_EPI_ACC_F32) return ATOM_EINVAL;
   if (batch > 0 && (!g || !out)) return ATOM_EINVAL;
@@ -165,7 +165,7 @@ int atom_k_orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
   }
   if (!orthogonalize_coef_ok(coef, steps)) return ATOM_EINVAL;
   if (batch == 0) return ATOM_OK;
-  if (!ws || misaligned(ws) || ws_bytes < orthogonalize_ws(dtype, batch, rows, cols)) return ATOM_EINVAL;
+  if (!ws || misaligned(ws) || ws_bytes < orthogonalize_ws(batch, rows, cols)) return ATOM_EINVAL;
   return st(orthogonalize(dtype, g, ldg, stride_g, out, ldo, stride_o, out_epi, keep, scale, batch, rows, cols, coef,
                           steps, ws, S(stream)));
 }

@@ -229,9 +229,9 @@ hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w,
 
 // Newton-Schulz orthogonalisation (atom_k_orthogonalize).  out_epi: EPI_STORE,
 // EPI_STORE_F32 or EPI_ACC_F32; coef: host [steps][3].
-bool orthogonalize_ok(int dtype, int batch, int rows, int cols);
+bool orthogonalize_ok(int batch, int rows, int cols);
 bool orthogonalize_coef_ok(const float* coef, int steps);
-uint64_t orthogonalize_ws(int dtype, int batch, int rows, int cols);
+uint64_t orthogonalize_ws(int batch, int rows, int cols);
 hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,
                          int64_t stride_o, int out_epi, float keep, float scale, int batch, int rows, int cols,
                          const float* coef, int steps, void* ws, hipStream_t s);

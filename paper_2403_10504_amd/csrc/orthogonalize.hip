@@ -8,21 +8,24 @@
 // Every step works on the singular values alone, s <- a s + b s^3 + c s^5.
 // All products run on the direct-load kernel (gemm_dl.h) in fp16 MFMAs with
 // fp32 sums, on matrices scaled by 2^10 (X also by a power of two per matrix
-// and step, see pack_kernel) and padded with zeros to multiples of 32, and each step's sums and scalings are its products' epilogues: three
-// launches a step.  A and B are symmetric, so their products take the tiles on
-// and below the diagonal.
+// and step, see pack_kernel) and padded with zeros to multiples of 32, and each
+// step's sums and scalings are its products' epilogues: three launches a step,
+// four where A is summed in ranges of k.  A and B are symmetric, so their
+// products take the tiles on and below the diagonal.
 //
 // Precision.  X is kept as two fp16 planes, hi + lo (22 bits): rounding X to
 // one would mix its strong directions into the weak ones, which later steps
 // raise by up to a per step (a gradient of rank 8 over noise of 1e-3, 512 x
 // 512: 4e-2 off in relative norm; 3e-4 with two planes).  The product B X may
-// take hi alone, because B is small where X's directions are weak, and so may A
-// and B be one plane: bf16 results are within 2e-3 of the definition, about
-// what their own rounding is off (fp16, with 11 bits, not bf16: 1.5e-2).  fp32
-// results take two planes of all three, and each product three passes over k
-// (hi hi, hi lo, lo hi), at three eighths of the fp16 rate and still about
-// three times that of fp32 MFMAs; 2.5e-7 to 1.4e-6 from the definition, fp32
-// arithmetic 1.5e-7 to 9e-7.
+// take hi alone where the result is bf16, because B is small where X's
+// directions are weak, and so may A and B be one plane: the result is 1.7e-3 to
+// 2.4e-3 from the definition, whose own rounding is 1.66e-3 off (fp16, with 11
+// bits, not bf16: 1.5e-2).  fp32 results, of bf16 gradients too, take two planes
+// of all three, and each product three passes over k (hi hi, hi lo, lo hi), at
+// three eighths of the fp16 rate and still about three times that of fp32 MFMAs:
+// 1.1e-6 to 4.7e-6 from the definition, fp32 arithmetic 1.7e-6 to 6.4e-6 (256 x
+// 768 to 2048 x 8192 and 4096 x 4096; gradients of a few strong directions,
+// Gaussian ones, singular values over four decades).
 #include <algorithm>
 #include <cmath>
 
@@ -325,11 +328,11 @@ struct Ws {
   int ranges;     // of k that A is the sum of
   uint64_t part, exps, x[2], xl[2], a, al, b, bl, sums, end;
 };
-Ws layout(int dtype, int batch, int rows, int cols) {
+// two: both planes of every factor (results in fp32).
+Ws layout(bool two, int batch, int rows, int cols) {
   Ws w;
   w.rp = (rows + 31) / 32 * 32, w.cp = (cols + 31) / 32 * 32, w.k = std::min(w.rp, w.cp);
   const uint64_t x = up(2ull * batch * w.rp * w.cp), a = up(2ull * batch * w.k * w.k);
-  const bool two = dtype == DT_F32;
   uint64_t at = 0;
   auto take = [&](uint64_t n) { const uint64_t o = at; at += n; return o; };
   w.part = take(up(8ull * batch * NORM_BLOCKS));
@@ -352,19 +355,22 @@ Ws layout(int dtype, int batch, int rows, int cols) {
 }  // namespace
 
 // Tiles are counted in 32 bits, of 64 x 64 at least, and each is a workgroup.
-bool orthogonalize_ok(int dtype, int batch, int rows, int cols) {
+bool orthogonalize_ok(int batch, int rows, int cols) {
   if (batch < 0 || rows <= 0 || cols <= 0 || batch > 65535 || rows > (1 << 24) || cols > (1 << 24)) return false;
   const int64_t tr = (rows + 63) / 64, tc = (cols + 63) / 64;
   if (batch == 0) return tr * tc < (1ll << 30);
   if (tr * tc * batch >= (1ll << 30) || std::min(tr, tc) * std::min(tr, tc) * batch >= (1ll << 30)) return false;
-  const Ws o = layout(dtype, batch, rows, cols);
-  const int k = o.k / 32 * (dtype == DT_F32 ? 3 : 1), n = std::max(o.rp, o.cp) / 32 * (dtype == DT_F32 ? 3 : 1);
-  auto fits = [&](int product, int M, int N, int ktiles) {
-    const int bs = tile_of(product, M, N, ktiles, batch);
-    const int64_t tm = (M + bs - 1) / bs, tn = (N + bs - 1) / bs;
-    return (product < 2 ? tm * (tm + 1) / 2 : tm * tn) * batch < MAX_WORKGROUPS;
-  };
-  return fits(0, o.k, o.k, n) && fits(1, o.k, o.k, k) && fits(2, o.rp, o.cp, k);
+  for (const bool two : {false, true}) {
+    const Ws o = layout(two, batch, rows, cols);
+    const int passes = two ? 3 : 1, k = o.k / 32 * passes, n = std::max(o.rp, o.cp) / 32 * passes;
+    auto fits = [&](int product, int M, int N, int ktiles) {
+      const int bs = tile_of(product, M, N, ktiles, batch);
+      const int64_t tm = (M + bs - 1) / bs, tn = (N + bs - 1) / bs;
+      return (product < 2 ? tm * (tm + 1) / 2 : tm * tn) * batch < MAX_WORKGROUPS;
+    };
+    if (!fits(0, o.k, o.k, n) || !fits(1, o.k, o.k, k) || !fits(2, o.rp, o.cp, k)) return false;
+  }
+  return true;
 }
 
 // Coefficients whose steps keep the singular values, which start in [0, 1], and
@@ -385,12 +391,17 @@ bool orthogonalize_coef_ok(const float* coef, int steps) {
   return true;
 }
 
-uint64_t orthogonalize_ws(int dtype, int batch, int rows, int cols) { return layout(dtype, batch, rows, cols).end; }
+// Enough for either type of result.
+uint64_t orthogonalize_ws(int batch, int rows, int cols) {
+  return std::max(layout(false, batch, rows, cols).end, layout(true, batch, rows, cols).end);
+}
 
 hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g, void* out, int64_t ldo,
                          int64_t stride_o, int out_epi, float keep, float scale, int batch, int rows, int cols,
                          const float* coef, int steps, void* ws, hipStream_t s) {
-  const Ws o = layout(dtype, batch, rows, cols);
+  const int out_mode = out_epi == EPI_ACC_F32 ? 2 : out_epi == EPI_STORE_F32 || dtype == DT_F32 ? 1 : 0;
+  const bool two = out_mode != 0;  // of an fp32 result every factor has both planes
+  const Ws o = layout(two, batch, rows, cols);
   char* base = static_cast<char*>(ws);
   auto at = [&](uint64_t off) { return reinterpret_cast<f16_t*>(base + off); };
   const int64_t sx = static_cast<int64_t>(o.rp) * o.cp, sa = static_cast<int64_t>(o.k) * o.k;
@@ -411,7 +422,6 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
     launch_pack<float>(g, ldg, stride_g, batch, rows, cols, o.rp, o.cp, part, st, exps, at(o.x[0]), at(o.xl[0]), s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int out_mode = out_epi == EPI_ACC_F32 ? 2 : out_epi == EPI_STORE_F32 || dtype == DT_F32 ? 1 : 0;
   scale /= SCALE;
   if (steps == 0) {
     const dim3 ugrid(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 2048)), batch);
@@ -424,7 +434,7 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
 #undef ATOM_UNPACK
     return hipGetLastError();
   }
-  const bool wide = rows <= cols, two = dtype == DT_F32;
+  const bool wide = rows <= cols;
   const int planes = two ? 2 : 1, passes = two ? 3 : 1;
   const int osz = out_mode == 0 ? 2 : 4;
   for (int k = 0; k < steps; ++k) {
@@ -496,10 +506,11 @@ hipError_t orthogonalize(int dtype, const void* g, int64_t ldg, int64_t stride_g
 
 }  // namespace atom
 
-// Tiles of a step's three products and ranges of k of the first (tests).
+// Tiles of a step's three products and ranges of k of the first, by the type of
+// the result (tests).
 extern "C" void atom_ns_choice(int dtype, int batch, int rows, int cols, int* out) {
   using namespace atom;
-  const Ws o = layout(dtype, batch, rows, cols);
+  const Ws o = layout(dtype == DT_F32, batch, rows, cols);
   const int passes = dtype == DT_F32 ? 3 : 1, lng = std::max(o.rp, o.cp);
   out[0] = tile_of(0, o.k, o.k, passes * lng / 32, batch);
   out[1] = tile_of(1, o.k, o.k, passes * o.k / 32, batch);

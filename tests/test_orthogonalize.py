@@ -403,3 +403,18 @@ def test_one_entry(dtype):
             off = (2.0 ** -21 * (len(coef) + 1) * 8 if dtype == "f32" or abs(x) < 0.01 or not coef else 2.0 ** -5) * abs(want)
             assert abs(got[20, 50].item() - want) <= off + 2.0 ** -149
             assert (got != 0).sum().item() == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,rows,cols", [(1, 33, 31), (2, 256, 256), (3, 100, 700), (1, 1030, 1000), (1, 3000, 128)])
+def test_fp32_results_of_bf16_gradients(batch, rows, cols):
+    """A result in fp32 is as accurate as of fp32 gradients: the bound is that of two planes of every factor."""
+    t = U.torch()
+    coef = [QUINTIC] * 5
+    g = t.stack([_matrix(rows, cols, "bf16", 80 + i) for i in range(batch)])
+    got = _run("bf16", g, coef, A.ATOM_EPI_STORE_F32)
+    _check("f32", got, g, coef)
+    # the same planes: the same bits
+    assert t.equal(got, _run("f32", g.float(), coef))
+    acc = _run("bf16", g, coef, A.ATOM_EPI_ACC_F32, 1.0, 1.0, start=0.0)
+    assert t.equal(acc, got)
