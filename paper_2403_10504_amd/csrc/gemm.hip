@@ -565,7 +565,8 @@ Choice choose(const GemmArgs& g, int esz, bool akc, bool bkc, int epi, double* u
   Choice best{0, 0, 1, false};
   double best_t = 0.0;
   auto consider = [&](const TileCfg& c, bool staged) {
-    if (c.bm == 256 && c.bn < 256 && !gemm_main_combo(akc, bkc, epi) && !gemm_loss_combo(akc, bkc, epi)) return;
+    if (c.bm == 256 && c.bn < 256 && !gemm_main_combo(akc, bkc, epi) &&
+        !(g.pl.kp ? gemm_planes_combo(akc, bkc, epi) : gemm_loss_combo(akc, bkc, epi))) return;
     const int64_t tiles = static_cast<int64_t>((g.M + c.bm - 1) / c.bm) * ((g.N + c.bn - 1) / c.bn);
     for (int want = 1; want <= (staged ? 1 : MAX_SPLITS); ++want) {
       const int per = (quads + want - 1) / want, splits = (quads + per - 1) / per;
@@ -775,7 +776,7 @@ hipError_t gemm(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi, hipSt
 hipError_t gemm_loss(const GemmArgs& g, int dtype, bool akc, bool bkc, int epi, hipStream_t s) {
   const bool planes = g.pl.kp > 0;
   const int esz = dtype == DT_BF16 || planes ? 2 : 4, e = 16 / esz;
-  if (planes ? !(epi == EPI_LSE || epi == EPI_DZ || epi == EPI_SCALE_F32 || epi == EPI_SCALE_ACC) || (bkc && !akc)
+  if (planes ? !gemm_planes_combo(akc, bkc, epi)
              : !(gemm_loss_combo(akc, bkc, epi) || (epi == EPI_STORE_F32 && akc && !bkc))) return hipErrorInvalidValue;
   // whole chunks in memory: leading dimensions, k of two k-contiguous operands
   // (each is read in full chunks), columns of a not k-contiguous B
@@ -866,4 +867,26 @@ extern "C" void atom_lse_cut(int dtype, int M, int N, int K, int64_t* out) {
   GemmArgs a = g;
   a.N = static_cast<int>(out[0]);
   out[1] = out[0] ? lse_entries(a, esz) : 0;
+}
+
+// The launches that gemm_loss makes of a product (tests): their number, and tile
+// rows and columns, ranges of k and length along the vocabulary of each.  dtype
+// 2: fp32 operands in three bf16 planes, K of one pass.
+extern "C" int atom_loss_launches(int dtype, int akc, int bkc, int epi, int M, int N, int K, uint64_t ws_bytes, int* out) {
+  using namespace atom;
+  GemmArgs g{};
+  g.M = M, g.N = N, g.K = K;
+  if (dtype == 2) g.pl.kp = (K + 31) / 32, g.pl.k = K, g.K = 6 * 32 * g.pl.kp;
+  float some;
+  g.ws = ws_bytes ? &some : nullptr;
+  g.ws_bytes = ws_bytes;
+  const int esz = dtype == DT_F32 ? 4 : 2, cut = first_range(g, esz, akc != 0, bkc != 0, epi);
+  int& len = epi == EPI_LSE || epi == EPI_DZ ? g.N : g.M;
+  const int lens[2] = {cut ? cut : len, cut ? len - cut : 0};
+  for (int i = 0; i < (cut ? 2 : 1); ++i) {
+    len = lens[i];
+    const Choice c = choose_loss(g, esz, akc != 0, bkc != 0, epi);
+    out[4 * i] = c.bm, out[4 * i + 1] = c.bn, out[4 * i + 2] = c.splits, out[4 * i + 3] = len;
+  }
+  return cut ? 2 : 1;
 }

@@ -107,6 +107,12 @@ constexpr bool gemm_loss_combo(bool akc, bool bkc, int epi) {
   return epi == EPI_SUM_SCALE && akc && !bkc;
 }
 
+// The same of fp32 operands in three bf16 planes: every result is fp32.
+constexpr bool gemm_planes_combo(bool akc, bool bkc, int epi) {
+  if (epi == EPI_LSE || epi == EPI_DZ) return akc && bkc;
+  return !bkc && (epi == EPI_SCALE_F32 || epi == EPI_SCALE_ACC);
+}
+
 // Tile configurations of the direct-load kernel (gemm_dl.h); 256x192 and
 // 256x128 exist for gemm_main_combo only.
 hipError_t gemm_dl_256(const GemmArgs& g, bool akc, bool bkc, int epi, hipStream_t s);

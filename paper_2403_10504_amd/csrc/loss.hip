@@ -417,3 +417,14 @@ hipError_t linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w,
 }
 
 }  // namespace atom
+
+// What the sizes are worked on as (tests): whether in three planes, rows of w at
+// a time (forward), columns of a piece and of the last one (backward), and the
+// bytes for ranges of k (backward).
+extern "C" void atom_linear_xent_plan(int dtype, int64_t rows, int V, int d, int piece, int64_t* out) {
+  using namespace atom;
+  out[0] = planes(dtype, rows, V, d, false), out[1] = out[0] ? plane_rows(V, d) : V;
+  const Pieces p = pieces_of(dtype, rows, V, d, piece);
+  out[2] = planes(dtype, rows, V, d, true), out[3] = p.width, out[4] = p.last;
+  out[5] = static_cast<int64_t>(split_bytes(rows, d));
+}

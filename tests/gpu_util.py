@@ -153,3 +153,31 @@ def lse_cut(dtype, rows, V, d):
     f.argtypes, f.restype = [ctypes.c_int] * 4 + [ctypes.c_void_p], None
     f(dt_code(dtype), rows, V, d, ctypes.addressof(out))
     return tuple(out)
+
+
+def loss_launches(dtype, akc, bkc, epi, M, N, K, ws_bytes=0):
+    """Launches of a product of the linear head's loss (`epi`: the library's internal epilogue), by its own rule: (tile
+    rows, tile columns, ranges of k, length along the vocabulary) each.  dtype "planes": fp32 in three bf16 planes."""
+    import ctypes
+
+    from paper_2403_10504_amd import atom as A
+
+    out = (ctypes.c_int * 8)()
+    f = A.lib().atom_loss_launches
+    f.argtypes, f.restype = [ctypes.c_int] * 7 + [ctypes.c_uint64, ctypes.c_void_p], ctypes.c_int
+    n = f(2 if dtype == "planes" else dt_code(dtype), akc, bkc, epi, M, N, K, ws_bytes, ctypes.addressof(out))
+    return [tuple(out[4 * i:4 * i + 4]) for i in range(n)]
+
+
+def xent_plan(dtype, rows, V, d, piece=0):
+    """How the loss of a linear head is worked on, by the library's own rule: forward in planes, rows of W at a time;
+    backward in planes, columns of a piece and of the last one, bytes for ranges of k."""
+    import ctypes
+
+    from paper_2403_10504_amd import atom as A
+
+    out = (ctypes.c_int64 * 6)()
+    f = A.lib().atom_linear_xent_plan
+    f.argtypes, f.restype = [ctypes.c_int, ctypes.c_int64] + [ctypes.c_int] * 3 + [ctypes.c_void_p], None
+    f(dt_code(dtype), rows, V, d, piece, ctypes.addressof(out))
+    return tuple(out)

@@ -530,3 +530,13 @@ def test_small_gradients_of_large_logits(dtype, rows, V, d):
     _, lse, _ = _fwd(dtype, x, w, tgt, d)
     dx, dw = _bwd(dtype, x, w, tgt, lse, d)
     assert dx.abs().max().item() <= V * 16 * 2e-28 and dw.abs().max().item() <= rows * 64 * 2e-28
+
+
+@pytest.mark.parametrize("rows,V,d,tile", [(1030, 8201, 516, (256, 192)), (1300, 40001, 260, (256, 128)),
+                                           (7688, 1000, 560, (256, 192))])
+def test_planes_dx_takes_every_tile(rows, V, d, tile):
+    """dx of fp32 operands in planes chooses among all five tiles for the first piece as for later ones (no GPU needed)."""
+    _, _, planes, width, last, ws = U.xent_plan("f32", rows, V, d)
+    assert planes
+    for epi in (SCALE_F32, SCALE_ACC):
+        assert U.loss_launches("planes", 1, 0, epi, rows, d, last if width == V else width, ws)[0][:2] == tile
