@@ -1,6 +1,7 @@
 """The linear head's loss and gradients of fp32 operands in three bf16 planes (x = h + m + l), six products of planes.
 
-A product of two numbers in planes keeps h h', h m', m h', m m', h l' and l h'; what is left out is below 2^-26 of it.
+A product of two numbers in planes keeps h h', h m', m h', m m', h l' and l h'; what is left out is at most 2^-24 of
+it (m is up to 2^-8, l up to 2^-17).
 Inputs in which every result is one such product show each of the six, at every tile that the library's rule takes:
 without one of the last three, the smallest, a result of random mantissas is 2^-18.5 off on average."""
 import pytest
@@ -9,8 +10,9 @@ from paper_2403_10504_amd import atom as A
 from tests import gpu_util as U
 from tests.test_linear_xent import DZ, LSE, SCALE_ACC, SCALE_F32, U32, _bwd, _case, _fwd
 
-# 6 roundings: three sums of a pass with what came before, two of the
-# accumulators' sets, one of the result; what is left out counts less than one
+# What is left out, up to 2^-24, and roundings: of the last pass with what came
+# before it, two of the accumulators' sets, one of the result (the passes before
+# round numbers of 2^-8 of theirs)
 SIX = 6 * U32
 
 # rows, V, d, piece: together they take every tile of every product, with k whole and in ranges
@@ -85,7 +87,7 @@ def test_single_products_show_each_pass():
     exact = a.double() * b.double()
     terms = [pa[i] * pb[j] for i, j in ((0, 0), (0, 1), (1, 0), (1, 1), (0, 2), (2, 0))]
     off = lambda z: ((z - exact).abs() / exact).max().item()  # noqa: E731
-    assert off(sum(terms)) <= U32 / 2
+    assert off(sum(terms)) <= U32
     for k in range(6):
         assert off(sum(terms) - terms[k]) > 4 * SIX
 
