@@ -184,19 +184,27 @@ __global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ g, int6
   }
 }
 
+// Threads a row (their logarithm) of the two kernels above, and partial sums of a
+// matrix: a few thousand workgroups over the batch, since each workgroup of the
+// second kernel sums all parts of its matrix.
+int row_threads(int cols) {
+  int lx = 0;
+  while (lx < 8 && 8 << lx < cols) ++lx;
+  return lx;
+}
+int norm_parts(int batch, int rows, int cols) {
+  const int at_once = 256 >> row_threads(cols);  // rows of a workgroup
+  return std::min(std::max(64, NORM_BLOCKS / batch), (rows + at_once - 1) / at_once);
+}
+
 template <typename T>
 void launch_pack(const void* g, int64_t ldg, int64_t stride, int batch, int rows, int cols, int rp, int cp,
                  double* part, const Steps& steps, int* exps, f16_t* hi, f16_t* lo, hipStream_t s) {
   const T* p = static_cast<const T*>(g);
   const int e = 16 / static_cast<int>(sizeof(T));
   const bool vec = reinterpret_cast<uintptr_t>(g) % 16 == 0 && ldg % e == 0 && stride % e == 0;
-  int lx = 0;
-  while (lx < 8 && 8 << lx < cols) ++lx;
-  const int64_t runs = (rows + (256 >> lx) - 1) / (256 >> lx);  // of rows a workgroup takes at once
+  const int lx = row_threads(cols), parts = norm_parts(batch, rows, cols);
   const int64_t pruns = (rp + (256 >> lx) - 1) / (256 >> lx);
-  // a few thousand workgroups over the batch: each of the second kernel's sums
-  // all parts of its matrix
-  const int parts = static_cast<int>(std::min<int64_t>(std::max(64, NORM_BLOCKS / batch), runs));
   const int64_t packs = std::min<int64_t>(std::max(64, 2048 / batch), pruns);
   const dim3 ngrid(parts, batch), pgrid(static_cast<unsigned>(packs), batch), block(256);
   const int64_t sx = static_cast<int64_t>(rp) * cp;
@@ -322,7 +330,7 @@ int ranges_of(int M, int ktiles, int batch) {
 
 // Workspace: partial sums, X (hi and lo, each twice: a step reads one and
 // writes the other; one plane's lo is read and written by the same lanes, so it
-// is there once), A, B.  n: bytes of a plane of X and of A, all matrices.
+// is there once), A, B, and the sums of the ranges of k.
 struct Ws {
   int rp, cp, k;  // padded lengths, the smaller of them
   int ranges;     // of k that A is the sum of
@@ -335,7 +343,7 @@ Ws layout(bool two, int batch, int rows, int cols) {
   const uint64_t x = up(2ull * batch * w.rp * w.cp), a = up(2ull * batch * w.k * w.k);
   uint64_t at = 0;
   auto take = [&](uint64_t n) { const uint64_t o = at; at += n; return o; };
-  w.part = take(up(8ull * batch * NORM_BLOCKS));
+  w.part = take(up(sizeof(double) * batch * norm_parts(batch, rows, cols)));
   w.exps = take(up(sizeof(int) * NS_EXPS * batch));
   w.x[0] = take(x);
   w.xl[0] = take(x);

@@ -418,3 +418,10 @@ def test_fp32_results_of_bf16_gradients(batch, rows, cols):
     assert t.equal(got, _run("f32", g.float(), coef))
     acc = _run("bf16", g, coef, A.ATOM_EPI_ACC_F32, 1.0, 1.0, start=0.0)
     assert t.equal(acc, got)
+
+
+def test_workspace_of_many_small_matrices():
+    """Partial sums of the norm take what is written: one per matrix of one row (no GPU needed)."""
+    n = 65535
+    # eight planes of 32 x 32, exponents of 64 steps, one partial sum, and the rounding of ten parts
+    assert A.atom_k_orthogonalize_ws_bytes(A.ATOM_F32, n, 1, 1) <= n * (8 * 2048 + 256 + 8) + 10 * 256
