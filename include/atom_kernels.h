@@ -138,15 +138,17 @@ int atom_k_linear_xent_fwd(int dtype, const void* x, int64_t ldx, const void* w,
  *   dw[v][c] = scale * sum_n dz[n][v] x[n][c]   ([V][lddw])
  * z is computed again, `piece` columns at a time (rounded up to a multiple of
  * 8, at most V; 0: the library's choice, dz of up to 512 MB and 2048 columns at
- * least), and dz of a piece goes through the
- * workspace in dtype (fewer columns take less of it and more time).  lse comes from the forward call; drow (NULL: 1) weighs
- * a token.  A token with a negative target or with drow 0 adds nothing,
- * whatever its row of x holds, and its row of dx is zero; one with a target of
- * V or more makes both gradients NaN.  dx or dw may be NULL (not wanted).
+ * least), and dz of a piece, drow in it, goes through the workspace in dtype
+ * (fewer columns take less of it and more time).  lse comes from the forward
+ * call; drow (NULL: 1) weighs a token (a factor of all tokens is more accurate as
+ * scale, which no bf16 dz rounds).  A token with a negative target or with drow 0
+ * adds nothing, whatever its row of x holds, and its row of dx is zero (of a
+ * finite w); one with a target of V or more makes both gradients NaN.  dx or dw
+ * may be NULL (not wanted).
  * dw_epi: ATOM_EPI_STORE (dw in dtype), ATOM_EPI_STORE_F32 or ATOM_EPI_ACC_F32
  * (dw fp32, += the gradient).  rows 0: dw is zeroed, or kept by
- * ATOM_EPI_ACC_F32, and no other pointer looked at.  dx and dw must not overlap the inputs.  Requirements as
- * above, for dx and lddx, dw and lddw as well. */
+ * ATOM_EPI_ACC_F32, and no other pointer looked at.  dx and dw must not overlap
+ * the inputs.  Requirements as above, for dx and lddx, dw and lddw as well. */
 uint64_t atom_k_linear_xent_bwd_ws_bytes(int dtype, int64_t rows, int V, int d, int piece);
 int atom_k_linear_xent_bwd(int dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const int32_t* tgt,
                            const float* lse, const float* drow, float scale, void* dx, int64_t lddx, void* dw,
