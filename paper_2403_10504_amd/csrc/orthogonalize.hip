@@ -102,18 +102,16 @@ __global__ void __launch_bounds__(256) norm_kernel(const T* __restrict__ g, int6
 }
 
 // Largest |a s + b s^3 + c s^5| of s in [0, top], from its extrema: a + 3 b x +
-// 5 c x^2 = 0, x = s^2.
+// 5 c x^2 = 0, x = s^2.  The root that -3 b and the discriminant's would cancel
+// in is the product of the roots over the other one (c may be 0 or next to it).
 __host__ __device__ inline double step_bound(double a, double b, double c, double top) {
   auto f = [=](double s) { return fabs(s * (a + s * s * (b + c * s * s))); };
   const double t = top * top, disc = 9 * b * b - 20 * a * c;
   double most = f(top);
-  if (c != 0.0 && disc >= 0.0) {
-    const double q = sqrt(disc), x0 = (-3 * b + q) / (10 * c), x1 = (-3 * b - q) / (10 * c);
+  if (disc >= 0.0) {
+    const double q = -0.5 * (3 * b + copysign(sqrt(disc), b)), x0 = q / (5 * c), x1 = a / q;
     if (x0 > 0.0 && x0 < t) most = fmax(most, f(sqrt(x0)));
     if (x1 > 0.0 && x1 < t) most = fmax(most, f(sqrt(x1)));
-  } else if (c == 0.0 && b != 0.0) {
-    const double x = -a / (3 * b);
-    if (x > 0.0 && x < t) most = fmax(most, f(sqrt(x)));
   }
   return most;
 }

@@ -425,3 +425,18 @@ def test_workspace_of_many_small_matrices():
     n = 65535
     # eight planes of 32 x 32, exponents of 64 steps, one partial sum, and the rounding of ten parts
     assert A.atom_k_orthogonalize_ws_bytes(A.ATOM_F32, n, 1, 1) <= n * (8 * 2048 + 256 + 8) + 10 * 256
+
+
+@pytest.mark.parametrize("c", [0.0, 1e-20, -1e-20, 1e-38, 1e-3])
+def test_refuses_an_extremum_inside(c):
+    """12 s - 12 s^3 is 4.6 at 0.58 and 0 at 1: beyond 4, also with a last coefficient next to zero (no GPU needed)."""
+    P = 1 << 20  # never read
+
+    def call(a):
+        A.atom_k_orthogonalize(A.ATOM_BF16, P, 64, 0, P, 64, 0, A.ATOM_EPI_STORE, 0.0, 1.0, 0, 64, 64, [(a, -a, c)], P,
+                               1 << 40)
+
+    with pytest.raises(A.AtomError) as e:
+        call(12.0)
+    assert e.value.status == A.ATOM_EINVAL
+    call(10.0)  # 3.85; no matrices
