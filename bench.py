@@ -42,8 +42,8 @@ HBM_PEAK_GBS = 8000.0
 # --copy-calibration 2147483648`, each scaled by what the counter reads for
 # the plain copy kernel of known size (profiles/gemm_wgrad_6.7b_hbm_traffic.md).
 # Valid only for the kernel sources it was measured on.
-WGRAD_TRAFFIC = {"sources_sha256": "b21c2b66e4276ad8c7020a55fb7828d04f85679f86ec7fce5e935b39eceb3882",
-                 "bytes_per_launch": 725817103}
+WGRAD_TRAFFIC = {"sources_sha256": "09b097d6e87e2f10724d1fe8ee9b6c5372ed476f1c99decadacd0ea00eca1fd8",
+                 "bytes_per_launch": 725825279}
 TRAFFIC_SOURCES = ("gemm.hip", "gemm_dl.h", "gemm_dl_256.hip", "common.h", "launch.h")
 
 
