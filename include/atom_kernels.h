@@ -93,6 +93,66 @@ int atom_k_attn_bwd(int dtype, const void* qkv, const void* o, const void* dout,
 int atom_k_attn_bwd_noalloc(int dtype, const void* qkv, const void* o, const void* dout, const float* lse,
                             void* dqkv, int B, int T, int H, int dh, void* stream);
 
+/* Rotary positions: pair i of the first `rot` elements of every head turns by
+ * the angle a_i = p * freq[i], p the row's position,
+ *   (u, w) -> mscale (u cos a - w sin a, u sin a + w cos a),
+ * and the rest of the head stays.  Pair i is elements (i, i + rot/2)
+ * (ATOM_ROPE_HALF) or (2i, 2i + 1) (ATOM_ROPE_PAIRS).
+ *
+ * atom_rope_freqs fills freq [rot/2] (a HOST array; the kernels read a copy of
+ * it on the device) with radians per position: base^(-2i/rot), for contexts
+ * beyond the trained one changed by `scaling`:
+ *   ATOM_ROPE_PLAIN   nothing;
+ *   ATOM_ROPE_LINEAR  all divided by factor;
+ *   ATOM_ROPE_BASE    base * factor^(rot/(rot-2)): the first stays, the last is
+ *                     divided by factor (rot 2: nothing);
+ *   ATOM_ROPE_PARTS   by the turns n = trained * freq / 2 pi of the trained length:
+ *                     those of n >= fast stay, those of n <= slow are divided by
+ *                     factor, between them (linear in n) a mean of both.
+ * ATOM_EINVAL: rot odd, below 2 or above 256, base or factor not finite and
+ * above 0, PARTS without 0 <= slow < fast and trained >= 1. */
+enum { ATOM_ROPE_HALF = 0, ATOM_ROPE_PAIRS = 1 };
+enum { ATOM_ROPE_PLAIN = 0, ATOM_ROPE_LINEAR = 1, ATOM_ROPE_BASE = 2, ATOM_ROPE_PARTS = 3 };
+int atom_rope_freqs(int rot, double base, int scaling, double factor, double trained, double slow, double fast,
+                    double* freq);
+
+/* The turn of `heads` heads of every row, head h at column h * dh of x [rows][ldx]
+ * and y [rows][ldy] (queries and keys of a fused qkv: heads = 2 H, ldx = 3 d).
+ * transposed: by -a, the gradient dx = mscale R^T dy of y = mscale R x.
+ * pos: device positions [rows], any int32; NULL: row % T (T >= 1; not read
+ * otherwise).  freq: device, [rot/2].  Angles are computed in 64 bits (at
+ * p freq = 10^9 they are off by 10^-7).  y may be x (with ldy = ldx), else they
+ * must not overlap.  Requirements: rows from 0 to 2^31 - 1; heads from 0 to 2^16;
+ * dh even, 2 to 256; rot even, 0 to dh (0: pos and freq are not read); ldx, ldy
+ * >= heads * dh; x and y aligned to their elements (to 16 bytes, with dh, rot
+ * and the leading dimensions multiples of 16, for the widest accesses). */
+int atom_k_rope(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const int32_t* pos, const double* freq,
+                float mscale, int layout, int transposed, int64_t rows, int T, int heads, int dh, int rot, void* stream);
+
+/* Norms of queries and keys, and the turn, in one pass over rows of Hq heads of
+ * queries, Hk of keys and Hv of values (a fused qkv: H each; one side alone: 0
+ * for the others), before atom_k_attn_fwd or atom_k_cross_attn_fwd:
+ *   u = g x / sqrt(mean(x^2) + eps) over a head's dh elements,  y = mscale R u,
+ * g = gq or gk [dh] in dtype, shared by the heads of a side (NULL: 1).  Heads of
+ * values are copied (nothing is done where y is x).  rot 0: the norms alone.
+ * Other arguments as for atom_k_rope; eps finite, above 0; Hq + Hk + Hv up to 2^16. */
+int atom_k_qknorm_rope_fwd(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const void* gq, const void* gk,
+                           float eps, const int32_t* pos, const double* freq, float mscale, int layout, int64_t rows,
+                           int T, int Hq, int Hk, int Hv, int dh, int rot, void* stream);
+
+/* Its gradients from dy and the x that went in: dx (the values' part of dy is
+ * copied; dx may be dy with the same leading dimension, else it overlaps neither
+ * dy nor x), and dgq, dgk (fp32 [dh], sums over rows and heads in a fixed order;
+ * NULL: not wanted; zeros where there are no rows or no heads of that side).
+ * ws: scratch of at least the bytes that the query returns (0 for sizes it
+ * refuses), 16-byte aligned; not needed, and may be NULL, without dgq and dgk.
+ * Calls that may overlap need scratch of their own. */
+uint64_t atom_k_qknorm_rope_bwd_ws_bytes(int64_t rows, int Hq, int Hk, int dh);
+int atom_k_qknorm_rope_bwd(int dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx, void* dx, int64_t lddx,
+                           const void* gq, const void* gk, float* dgq, float* dgk, float eps, const int32_t* pos,
+                           const double* freq, float mscale, int layout, int64_t rows, int T, int Hq, int Hk, int Hv,
+                           int dh, int rot, void* ws, uint64_t ws_bytes, void* stream);
+
 /* Scratch floats atom_k_colsum needs in `part`. */
 int64_t atom_k_colsum_part_floats(int64_t rows, int cols);
 

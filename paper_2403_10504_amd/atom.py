@@ -87,7 +87,7 @@ class AtomError(RuntimeError):
 
 _lib = None
 P = ctypes.c_void_p
-I32, I64, U64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64
+I32, I64, U64, F64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_double
 _SIGS = {
     "atom_version": (ctypes.c_char_p, []),
     "atom_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -130,6 +130,14 @@ _SIGS = {
     "atom_k_attn_fwd": (ctypes.c_int, [ctypes.c_int, P, P, P] + [ctypes.c_int] * 4 + [P]),
     "atom_k_attn_bwd": (ctypes.c_int, [ctypes.c_int, P, P, P, P, P, P] + [ctypes.c_int] * 4 + [P]),
     "atom_k_attn_bwd_noalloc": (ctypes.c_int, [ctypes.c_int, P, P, P, P, P] + [ctypes.c_int] * 4 + [P]),
+    "atom_rope_freqs": (ctypes.c_int, [ctypes.c_int, F64, ctypes.c_int] + [F64] * 4 + [P]),
+    "atom_k_rope": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, P, P, ctypes.c_float, ctypes.c_int, ctypes.c_int, I64]
+                    + [ctypes.c_int] * 4 + [P]),
+    "atom_k_qknorm_rope_fwd": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, P, P, ctypes.c_float, P, P, ctypes.c_float,
+                                              ctypes.c_int, I64] + [ctypes.c_int] * 6 + [P]),
+    "atom_k_qknorm_rope_bwd_ws_bytes": (U64, [I64] + [ctypes.c_int] * 3),
+    "atom_k_qknorm_rope_bwd": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, P, I64, P, P, P, P, ctypes.c_float, P, P,
+                                              ctypes.c_float, ctypes.c_int, I64] + [ctypes.c_int] * 6 + [P, U64, P]),
     "atom_k_colsum_part_floats": (I64, [I64, ctypes.c_int]),
     "atom_k_colsum": (ctypes.c_int, [ctypes.c_int, P, I64, ctypes.c_int, P, P, P]),
     "atom_k_xent": (ctypes.c_int, [ctypes.c_int, P, I64, P, P, I64, P, I64, ctypes.c_int, ctypes.c_float, P]),
@@ -476,6 +484,38 @@ ATOM_ATTN_NOALLOC_MAX_ROWS = 1 << 20
 
 def atom_k_attn_bwd_noalloc(dtype, qkv, o, dout, lse, dqkv, B, T, H, dh, stream=None):
     _kcall("atom_k_attn_bwd_noalloc", dtype, qkv, o, dout, lse, dqkv, B, T, H, dh, stream)
+
+
+ATOM_ROPE_HALF, ATOM_ROPE_PAIRS = 0, 1
+ATOM_ROPE_PLAIN, ATOM_ROPE_LINEAR, ATOM_ROPE_BASE, ATOM_ROPE_PARTS = range(4)
+
+
+def atom_rope_freqs(rot, base=10000.0, scaling=ATOM_ROPE_PLAIN, factor=1.0, trained=2048.0, slow=1.0, fast=32.0):
+    """Radians per position of each pair, a float64 array [rot/2] (on the host)."""
+    out = np.zeros(max(1, rot // 2), dtype=np.float64)
+    _check(lib().atom_rope_freqs(rot, base, scaling, factor, trained, slow, fast, out.ctypes.data_as(P)))
+    return out
+
+
+def atom_k_rope(dtype, x, ldx, y, ldy, pos, freq, mscale, layout, transposed, rows, T, heads, dh, rot, stream=None):
+    _kcall("atom_k_rope", dtype, x, ldx, y, ldy, pos, freq, mscale, layout, int(transposed), rows, T, heads, dh, rot,
+           stream)
+
+
+def atom_k_qknorm_rope_fwd(dtype, x, ldx, y, ldy, gq, gk, eps, pos, freq, mscale, layout, rows, T, Hq, Hk, Hv, dh, rot,
+                           stream=None):
+    _kcall("atom_k_qknorm_rope_fwd", dtype, x, ldx, y, ldy, gq, gk, eps, pos, freq, mscale, layout, rows, T, Hq, Hk, Hv,
+           dh, rot, stream)
+
+
+def atom_k_qknorm_rope_bwd_ws_bytes(rows, Hq, Hk, dh):
+    return lib().atom_k_qknorm_rope_bwd_ws_bytes(rows, Hq, Hk, dh)
+
+
+def atom_k_qknorm_rope_bwd(dtype, dy, lddy, x, ldx, dx, lddx, gq, gk, dgq, dgk, eps, pos, freq, mscale, layout, rows, T,
+                           Hq, Hk, Hv, dh, rot, ws, ws_bytes, stream=None):
+    _kcall("atom_k_qknorm_rope_bwd", dtype, dy, lddy, x, ldx, dx, lddx, gq, gk, dgq, dgk, eps, pos, freq, mscale, layout,
+           rows, T, Hq, Hk, Hv, dh, rot, ws, ws_bytes, stream)
 
 
 def atom_k_colsum_part_floats(rows, cols):

@@ -1,5 +1,6 @@
 // extern "C" wrappers of the kernel launchers (include/atom_kernels.h).
 #include <hip/hip_runtime.h>
+#include <math.h>
 
 #include "../../include/atom.h"
 #include "../../include/atom_kernels.h"
@@ -19,6 +20,20 @@ inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
 // rows of d elements, ld apart, in whole 16-byte chunks
 inline bool rows_ok(int dt, const void* p, int64_t ld, int d) {
   return p && !misaligned(p) && ld >= d && ld % (dt == ATOM_BF16 ? 8 : 4) == 0;
+}
+inline bool aligned_to(int dt, const void* p) { return reinterpret_cast<uintptr_t>(p) % (dt == ATOM_BF16 ? 2 : 4) == 0; }
+// rows, heads and turns of atom_k_rope and atom_k_qknorm_rope_*
+inline bool turn_ok(int dt, int layout, int64_t rows, int64_t heads, int dh, int rot, float mscale) {
+  return dt_ok(dt) && (layout == ATOM_ROPE_HALF || layout == ATOM_ROPE_PAIRS) && rows >= 0 && rows <= INT32_MAX &&
+         heads >= 0 && heads <= 1 << 16 && dh >= 2 && dh <= 256 && dh % 2 == 0 && rot >= 0 && rot <= dh && rot % 2 == 0 &&
+         isfinite(mscale);
+}
+inline bool heads_ok(int dt, const void* p, int64_t ld, int64_t heads, int dh) {
+  return p && aligned_to(dt, p) && ld >= heads * dh && ld <= INT64_MAX / 8 / INT32_MAX;
+}
+inline bool positions_ok(const int32_t* pos, const double* freq, int T, int rot) {
+  return rot == 0 || (freq && reinterpret_cast<uintptr_t>(freq) % 8 == 0 && reinterpret_cast<uintptr_t>(pos) % 4 == 0 &&
+                      (pos || T >= 1));
 }
 }  // namespace
 
@@ -81,6 +96,75 @@ int atom_k_attn_bwd(int dtype, const void* qkv, const void* o, const void* dout,
                     void* dqkv, int B, int T, int H, int dh, void* stream) {
   if (!dt_ok(dtype) || !qkv || !o || !dout || !lse || !delta || !dqkv) return ATOM_EINVAL;
   return st(attn_bwd(dtype, qkv, o, dout, lse, delta, dqkv, B, T, H, dh, S(stream)));
+}
+
+int atom_rope_freqs(int rot, double base, int scaling, double factor, double trained, double slow, double fast,
+                    double* freq) {
+  if (!freq || rot < 2 || rot > 256 || rot % 2 || !(base > 0) || !isfinite(base)) return ATOM_EINVAL;
+  if (scaling < ATOM_ROPE_PLAIN || scaling > ATOM_ROPE_PARTS) return ATOM_EINVAL;
+  if (scaling != ATOM_ROPE_PLAIN && (!(factor > 0) || !isfinite(factor))) return ATOM_EINVAL;
+  if (scaling == ATOM_ROPE_PARTS && !(slow >= 0 && slow < fast && isfinite(fast) && trained >= 1 && isfinite(trained)))
+    return ATOM_EINVAL;
+  if (scaling == ATOM_ROPE_BASE && rot > 2) base *= pow(factor, rot / (rot - 2.0));
+  for (int i = 0; i < rot / 2; ++i) {
+    double f = pow(base, -2.0 * i / rot);
+    if (scaling == ATOM_ROPE_LINEAR) f /= factor;
+    if (scaling == ATOM_ROPE_PARTS) {
+      const double keep = fmin(1.0, fmax(0.0, (trained * f / (2.0 * M_PI) - slow) / (fast - slow)));
+      f *= keep + (1.0 - keep) / factor;
+    }
+    freq[i] = f;
+  }
+  return ATOM_OK;
+}
+
+int atom_k_rope(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const int32_t* pos, const double* freq,
+                float mscale, int layout, int transposed, int64_t rows, int T, int heads, int dh, int rot, void* stream) {
+  if (!turn_ok(dtype, layout, rows, heads, dh, rot, mscale)) return ATOM_EINVAL;
+  if (rows == 0 || heads == 0) return ATOM_OK;
+  if (!heads_ok(dtype, x, ldx, heads, dh) || !heads_ok(dtype, y, ldy, heads, dh) || !positions_ok(pos, freq, T, rot))
+    return ATOM_EINVAL;
+  if (x == y && ldx != ldy) return ATOM_EINVAL;
+  return st(rope(dtype, x, ldx, y, ldy, pos, freq, mscale, layout, transposed != 0, rows, T, heads, dh, rot, S(stream)));
+}
+
+int atom_k_qknorm_rope_fwd(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const void* gq, const void* gk,
+                           float eps, const int32_t* pos, const double* freq, float mscale, int layout, int64_t rows,
+                           int T, int Hq, int Hk, int Hv, int dh, int rot, void* stream) {
+  if (Hq < 0 || Hk < 0 || Hv < 0 || !(eps > 0) || !isfinite(eps)) return ATOM_EINVAL;
+  const int64_t heads = static_cast<int64_t>(Hq) + Hk + Hv;
+  if (!turn_ok(dtype, layout, rows, heads, dh, rot, mscale)) return ATOM_EINVAL;
+  if (rows == 0 || heads == 0) return ATOM_OK;
+  if (!heads_ok(dtype, x, ldx, heads, dh) || !heads_ok(dtype, y, ldy, heads, dh) || !positions_ok(pos, freq, T, rot))
+    return ATOM_EINVAL;
+  if (!aligned_to(dtype, gq) || !aligned_to(dtype, gk) || (x == y && ldx != ldy)) return ATOM_EINVAL;
+  return st(qknorm_rope_fwd(dtype, x, ldx, y, ldy, gq, gk, eps, pos, freq, mscale, layout, rows, T, Hq, Hk, Hv, dh, rot,
+                            S(stream)));
+}
+
+uint64_t atom_k_qknorm_rope_bwd_ws_bytes(int64_t rows, int Hq, int Hk, int dh) {
+  return Hq >= 0 && Hk >= 0 && turn_ok(ATOM_BF16, ATOM_ROPE_HALF, rows, static_cast<int64_t>(Hq) + Hk, dh, 0, 1.f)
+             ? qknorm_rope_bwd_ws(dh)
+             : 0;
+}
+
+int atom_k_qknorm_rope_bwd(int dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx, void* dx, int64_t lddx,
+                           const void* gq, const void* gk, float* dgq, float* dgk, float eps, const int32_t* pos,
+                           const double* freq, float mscale, int layout, int64_t rows, int T, int Hq, int Hk, int Hv,
+                           int dh, int rot, void* ws, uint64_t ws_bytes, void* stream) {
+  if (Hq < 0 || Hk < 0 || Hv < 0 || !(eps > 0) || !isfinite(eps)) return ATOM_EINVAL;
+  const int64_t heads = static_cast<int64_t>(Hq) + Hk + Hv;
+  if (!turn_ok(dtype, layout, rows, heads, dh, rot, mscale)) return ATOM_EINVAL;
+  if (!aligned_to(ATOM_F32, dgq) || !aligned_to(ATOM_F32, dgk)) return ATOM_EINVAL;
+  if (rows > 0 && heads > 0) {
+    if (!heads_ok(dtype, x, ldx, heads, dh) || !heads_ok(dtype, dy, lddy, heads, dh) ||
+        !heads_ok(dtype, dx, lddx, heads, dh) || !positions_ok(pos, freq, T, rot))
+      return ATOM_EINVAL;
+    if (!aligned_to(dtype, gq) || !aligned_to(dtype, gk) || dx == x || (dx == dy && lddx != lddy)) return ATOM_EINVAL;
+    if ((dgq || dgk) && (!ws || misaligned(ws) || ws_bytes < qknorm_rope_bwd_ws(dh))) return ATOM_EINVAL;
+  }
+  return st(qknorm_rope_bwd(dtype, dy, lddy, x, ldx, dx, lddx, gq, gk, dgq, dgk, eps, pos, freq, mscale, layout, rows, T,
+                            Hq, Hk, Hv, dh, rot, static_cast<float*>(ws), S(stream)));
 }
 
 int64_t atom_k_colsum_part_floats(int64_t rows, int cols) { return colsum_blocks(rows) * cols; }

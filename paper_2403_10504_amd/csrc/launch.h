@@ -250,4 +250,17 @@ hipError_t attn_fwd(int dtype, const void* qkv, void* o, float* lse, int B, int 
 hipError_t attn_bwd(int dtype, const void* qkv, const void* o, const void* dout, const float* lse, float* delta,
                     void* dqkv, int B, int T, int H, int dh, hipStream_t s);
 
+// Rotary positions and the norms of queries and keys (atom_k_rope,
+// atom_k_qknorm_rope_*).  back: the transposed turn.
+hipError_t rope(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const int32_t* pos, const double* freq,
+                float mscale, int layout, bool back, int64_t rows, int T, int heads, int dh, int rot, hipStream_t s);
+hipError_t qknorm_rope_fwd(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const void* gq, const void* gk,
+                           float eps, const int32_t* pos, const double* freq, float mscale, int layout, int64_t rows,
+                           int T, int Hq, int Hk, int Hv, int dh, int rot, hipStream_t s);
+uint64_t qknorm_rope_bwd_ws(int dh);
+hipError_t qknorm_rope_bwd(int dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx, void* dx, int64_t lddx,
+                           const void* gq, const void* gk, float* dgq, float* dgk, float eps, const int32_t* pos,
+                           const double* freq, float mscale, int layout, int64_t rows, int T, int Hq, int Hk, int Hv,
+                           int dh, int rot, float* ws, hipStream_t s);
+
 }  // namespace atom

@@ -1,0 +1,426 @@
+// Rotary positions, and norms of queries and keys with the rotation in the same
+// pass (atom_k_rope, atom_k_qknorm_rope_fwd, _bwd).
+//
+// Pair i of a head at position p turns by a = p freq_i:
+//   (u, w) -> m (u cos a - w sin a, u sin a + w cos a);
+// the transposed turn (its gradient) has -a.  The norm is u = g x r with
+// r = 1/sqrt(mean x^2 + eps), in front of the turn.  With g' the gradient turned
+// back, its own gradient is
+//   dg = sum over rows and heads of g' x r,   dx = r (g' g - x r mean(g' g x r)).
+//
+// The kernels are bound by memory: each head is read once and written once
+// (the norm's backward: dy and x once, dx once; r is computed again rather than
+// kept, the whole head being in registers anyway).
+//
+// A lane holds V pairs of a head: in the half layout V elements at c V and V at
+// rot/2 + c V, in the pairs layout 2 V in a row; elements past rot in chunks of
+// 2 V, which do not turn.  So a pair never leaves its lane, P lanes (a power of
+// two) hold a head, and a wave 64 / P heads at a time.  A wave takes a whole
+// row, so the angles of its V pairs, and their sines, are computed once for all
+// of the row's heads; where rows are few a row's heads go to several waves.
+//
+// Angles are exact in 64 bits before they are reduced: p freq_i in fp32 is off
+// by a whole turn's part from p = 10^5 on (2^-24 of 10^5 radians: 0.006).
+#include <math.h>
+
+#include <algorithm>
+
+#include "../../include/atom.h"
+#include "../../include/atom_kernels.h"
+#include "common.h"
+#include "launch.h"
+
+namespace atom {
+namespace {
+
+constexpr int WAVES = 4;  // waves of a workgroup
+
+struct Args {
+  const void* x;
+  const void* dy;  // backward
+  void* y;         // y, or dx
+  int64_t ldx, lddy, ldy;
+  const void *gq, *gk;  // gains, null: 1
+  float* part;          // backward: [workgroups][2][dh] partial sums of the gains' gradients, null: not wanted
+  const int32_t* pos;   // null: row % T
+  const double* freq;
+  float mscale, eps;
+  int back;     // rope: the transposed turn
+  uint32_t rows, T;
+  int Hq, Hk, Hv;  // (rope: Hq alone)
+  int dh, rot;
+  int plog, per;  // log2 of P; groups of 64 / P heads that a workgroup takes of a row
+  int copy;       // the value heads are copied
+};
+
+enum { ROPE, NORM, NORM_BWD };
+
+// V elements, in one load of up to 16 bytes
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Vec {
+  T e[V];
+};
+
+// The two runs of V elements of chunk c, and the pair that each element is of.
+template <typename T, int V, bool PAIRS>
+struct Chunk {
+  float u[V], w[V];
+  ATOM_DEV void load(const T* p, int o0, int o1) {
+    const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(p + o0), b = *reinterpret_cast<const Vec<T, V>*>(p + o1);
+    set(a, b);
+  }
+  ATOM_DEV void set(const Vec<T, V>& a, const Vec<T, V>& b) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if constexpr (PAIRS) {
+        const int e = 2 * i;
+        u[i] = to_f<T>(e < V ? a.e[e % V] : b.e[e % V]);
+        w[i] = to_f<T>(e + 1 < V ? a.e[(e + 1) % V] : b.e[(e + 1) % V]);
+      } else {
+        u[i] = to_f<T>(a.e[i]);
+        w[i] = to_f<T>(b.e[i]);
+      }
+    }
+  }
+  ATOM_DEV void store(T* p, int o0, int o1) const {
+    Vec<T, V> a, b;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if constexpr (PAIRS) {
+        a.e[i] = from_f<T>(i % 2 ? w[i / 2] : u[i / 2]);
+        b.e[i] = from_f<T>((V + i) % 2 ? w[(V + i) / 2] : u[(V + i) / 2]);
+      } else {
+        a.e[i] = from_f<T>(u[i]);
+        b.e[i] = from_f<T>(w[i]);
+      }
+    }
+    *reinterpret_cast<Vec<T, V>*>(p + o0) = a;
+    *reinterpret_cast<Vec<T, V>*>(p + o1) = b;
+  }
+};
+
+// NC chunks of a lane (two for heads of more than 128 elements in single pairs).
+template <typename T, int V, int NC, bool PAIRS, int OP>
+__global__ void __launch_bounds__(64 * WAVES) rotary_kernel(const Args a) {
+  using C = Chunk<T, V, PAIRS>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int P = 1 << a.plog, HS = 64 >> a.plog;
+  const int slot = lane >> a.plog, lp = lane & (P - 1);
+  const int L = a.dh / (2 * V), rc = a.rot / (2 * V);
+  int o0[NC], o1[NC];
+  bool on[NC], turn[NC];
+#pragma unroll
+  for (int k = 0; k < NC; ++k) {
+    const int c = lp + 64 * k;
+    on[k] = c < L;
+    turn[k] = c < rc;
+    if (!turn[k] || PAIRS) o0[k] = 2 * V * c, o1[k] = o0[k] + V;
+    else o0[k] = V * c, o1[k] = a.rot / 2 + V * c;
+  }
+  const int gq = (a.Hq + HS - 1) / HS, gk = (a.Hk + HS - 1) / HS, gv = a.copy ? (a.Hv + HS - 1) / HS : 0;
+  const int g0 = blockIdx.y * a.per, g1 = min(g0 + a.per, gq + gk + gv);
+
+  C gain[NC];
+  float acc[2][NC][2 * V];  // of queries and of keys
+  if constexpr (OP == NORM_BWD) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) acc[s][k][i] = 0.f;
+  }
+  auto load_gain = [&](const void* g) {
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) gain[k].u[i] = gain[k].w[i] = 1.f;
+      if (g && on[k]) gain[k].load(static_cast<const T*>(g), o0[k], o1[k]);
+    }
+  };
+
+  for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * WAVES + wave; row < a.rows;
+       row += static_cast<uint64_t>(gridDim.x) * WAVES) {
+    float cs[NC][V], sn[NC][V];
+    if (a.rot) {
+      const double p = a.pos ? static_cast<double>(a.pos[row]) : static_cast<double>(static_cast<uint32_t>(row) % a.T);
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          cs[k][i] = 1.f;
+          sn[k][i] = 0.f;
+          if (!turn[k]) continue;
+          // half turns, reduced to [-1, 1] in 64 bits; then exact in fp32 to 2^-25
+          const double h = p * (a.freq[V * (lp + 64 * k) + i] * 0.31830988618379067154);
+          float s, c;
+          sincospif(static_cast<float>(h - 2.0 * rint(0.5 * h)), &s, &c);
+          cs[k][i] = c * a.mscale;
+          sn[k][i] = (OP == NORM_BWD || (OP == ROPE && a.back) ? -s : s) * a.mscale;
+        }
+    }
+    const T* x = static_cast<const T*>(a.x) + static_cast<int64_t>(row) * a.ldx;
+    const T* dy = OP == NORM_BWD ? static_cast<const T*>(a.dy) + static_cast<int64_t>(row) * a.lddy : x;
+    T* y = static_cast<T*>(a.y) + static_cast<int64_t>(row) * a.ldy;
+    auto rotate = [&](C (&v)[NC]) {
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+        if (turn[k]) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float u = v[k].u[i], w = v[k].w[i];
+            // one order of roundings, whatever the width of the accesses
+            v[k].u[i] = __builtin_fmaf(u, cs[k][i], -(w * sn[k][i]));
+            v[k].w[i] = __builtin_fmaf(u, sn[k][i], w * cs[k][i]);
+          }
+        }
+    };
+    // the sum of f over a head's elements
+    auto head_sum = [&](float s) {
+      for (int o = 1; o < P; o <<= 1) s += __shfl_xor(s, o, 64);
+      return s;
+    };
+    for (int g = g0; g < g1; ++g) {
+      const bool is_q = g < gq, is_v = g >= gq + gk;
+      const int h = (is_q ? g : is_v ? g - gq - gk : g - gq) * HS + slot;
+      const bool there = h < (is_q ? a.Hq : is_v ? a.Hv : a.Hk);
+      const int64_t at = static_cast<int64_t>(is_q ? h : is_v ? a.Hq + a.Hk + h : a.Hq + h) * a.dh;
+      if (is_v) {  // values: as they are
+        if (there) {
+#pragma unroll
+          for (int k = 0; k < NC; ++k)
+            if (on[k]) {
+              *reinterpret_cast<Vec<T, V>*>(y + at + o0[k]) = *reinterpret_cast<const Vec<T, V>*>(dy + at + o0[k]);
+              *reinterpret_cast<Vec<T, V>*>(y + at + o1[k]) = *reinterpret_cast<const Vec<T, V>*>(dy + at + o1[k]);
+            }
+        }
+        continue;
+      }
+      if (OP != ROPE && (g == g0 || g == gq)) load_gain(is_q ? a.gq : a.gk);
+      C v[NC];
+#pragma unroll
+      for (int k = 0; k < NC; ++k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[k].u[i] = v[k].w[i] = 0.f;
+        if (there && on[k]) v[k].load(x + at, o0[k], o1[k]);
+      }
+      if constexpr (OP == ROPE) {
+        rotate(v);
+      } else {
+        C d[NC];
+        if constexpr (OP == NORM_BWD) {
+#pragma unroll
+          for (int k = 0; k < NC; ++k) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) d[k].u[i] = d[k].w[i] = 0.f;
+            if (there && on[k]) d[k].load(dy + at, o0[k], o1[k]);
+          }
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) s += v[k].u[i] * v[k].u[i] + v[k].w[i] * v[k].w[i];
+        const float r = 1.f / sqrtf(head_sum(s) / a.dh + a.eps);
+        if constexpr (OP == NORM) {
+#pragma unroll
+          for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+              v[k].u[i] *= r * gain[k].u[i];
+              v[k].w[i] *= r * gain[k].w[i];
+            }
+          rotate(v);
+        } else {
+          rotate(d);
+          float m = 0.f;
+#pragma unroll
+          for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+              v[k].u[i] *= r;
+              v[k].w[i] *= r;
+              const float tu = d[k].u[i] * v[k].u[i], tw = d[k].w[i] * v[k].w[i];
+              if (is_q) acc[0][k][2 * i] += tu, acc[0][k][2 * i + 1] += tw;
+              else acc[1][k][2 * i] += tu, acc[1][k][2 * i + 1] += tw;
+              m += tu * gain[k].u[i] + tw * gain[k].w[i];
+            }
+          m = head_sum(m) / a.dh;
+#pragma unroll
+          for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+              v[k].u[i] = r * (d[k].u[i] * gain[k].u[i] - v[k].u[i] * m);
+              v[k].w[i] = r * (d[k].w[i] * gain[k].w[i] - v[k].w[i] * m);
+            }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+        if (there && on[k]) v[k].store(y + at, o0[k], o1[k]);
+    }
+  }
+
+  if constexpr (OP == NORM_BWD) {
+    if (!a.part) return;
+    // over the wave's slots, then over the waves, in this order
+    __shared__ float sums[WAVES][2][256];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) {
+          float v = acc[s][k][i];
+          for (int o = P; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+          // element i of the chunk: pair i / 2, first or second of it
+          const int e = PAIRS ? i : (i & 1) * V + (i >> 1);
+          if (slot == 0 && on[k]) sums[wave][s][(e < V ? o0[k] + e : o1[k] + e - V)] = v;
+        }
+    __syncthreads();
+    float* out = a.part + (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 2 * a.dh;
+    for (int t = threadIdx.x; t < 2 * a.dh; t += 64 * WAVES) {
+      const int s = t >= a.dh, e = t - s * a.dh;
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) v += sums[w][s][e];
+      out[t] = v;
+    }
+  }
+}
+
+// The grid: workgroups of four rows, and the parts of a row's heads.
+struct Shape {
+  int v, plog, per;
+  unsigned gx, gy;
+};
+
+// Pairs in a lane: as many as 16-byte accesses, the layout of the head and the
+// alignment of every buffer allow.
+int pairs_of(int dtype, int dh, int rot, uint64_t align) {
+  int v = dtype == DT_BF16 ? 8 : 4;
+  const int esz = dtype == DT_BF16 ? 2 : 4;
+  while (v > 1 && (dh % (2 * v) || rot % (2 * v) || align % (v * esz))) v /= 2;
+  return v;
+}
+
+// Rows that fill the card with a wave each; fewer are divided, a group of heads
+// each at the least.
+constexpr int64_t FULL_WAVES = 4096;
+constexpr int64_t MAX_PARTS = 64;
+// Workgroups of the backward at most: each leaves a partial sum of the gains.
+constexpr int64_t BWD_BLOCKS = 1024;
+
+Shape shape_of(int op, int64_t rows, int groups, int dh, int v, int plog) {
+  Shape s{v, plog, groups, 0, 1};
+  const int64_t wgs = (rows + WAVES - 1) / WAVES;
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({groups, FULL_WAVES / rows, MAX_PARTS}));
+  s.per = static_cast<int>((groups + parts - 1) / parts);
+  s.gy = static_cast<unsigned>((groups + s.per - 1) / s.per);
+  s.gx = static_cast<unsigned>(std::min<int64_t>(wgs, op == NORM_BWD ? std::max<int64_t>(1, BWD_BLOCKS / s.gy) : MAX_WORKGROUPS / s.gy - 1));
+  return s;
+}
+
+int plog_of(int dh, int v) {
+  const int l = dh / (2 * v);
+  int p = 0;
+  while (p < 6 && (1 << p) < l) ++p;
+  return p;
+}
+
+template <typename T, int V, int OP>
+void launch(const Args& a, bool pairs, const Shape& g, hipStream_t s) {
+  const dim3 grid(g.gx, g.gy), block(64 * WAVES);
+  if constexpr (V == 1) {
+    if (a.dh > 128) {
+      if (pairs) hipLaunchKernelGGL((rotary_kernel<T, V, 2, true, OP>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((rotary_kernel<T, V, 2, false, OP>), grid, block, 0, s, a);
+      return;
+    }
+  }
+  if (pairs) hipLaunchKernelGGL((rotary_kernel<T, V, 1, true, OP>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((rotary_kernel<T, V, 1, false, OP>), grid, block, 0, s, a);
+}
+
+template <int OP>
+hipError_t run(int dtype, Args& a, int layout, uint64_t align, hipStream_t s, unsigned* blocks) {
+  const int v = pairs_of(dtype, a.dh, a.rot, align);
+  a.plog = plog_of(a.dh, v);
+  const int HS = 64 >> a.plog;
+  const int groups = (a.Hq + HS - 1) / HS + (a.Hk + HS - 1) / HS + (a.copy ? (a.Hv + HS - 1) / HS : 0);
+  *blocks = 0;
+  if (a.rows == 0 || groups == 0) return hipSuccess;
+  const Shape g = shape_of(OP, a.rows, groups, a.dh, v, a.plog);
+  a.per = g.per;
+  *blocks = g.gx * g.gy;
+  const bool pairs = layout == ATOM_ROPE_PAIRS;
+  if (dtype == DT_BF16) {
+    if (v == 8) launch<bf16_t, 8, OP>(a, pairs, g, s);
+    else if (v == 4) launch<bf16_t, 4, OP>(a, pairs, g, s);
+    else if (v == 2) launch<bf16_t, 2, OP>(a, pairs, g, s);
+    else launch<bf16_t, 1, OP>(a, pairs, g, s);
+  } else {
+    if (v == 4) launch<float, 4, OP>(a, pairs, g, s);
+    else if (v == 2) launch<float, 2, OP>(a, pairs, g, s);
+    else launch<float, 1, OP>(a, pairs, g, s);
+  }
+  return hipGetLastError();
+}
+
+// Bits that an address, or a pitch in bytes, sets below 16.
+inline uint64_t low(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+
+uint64_t align_of(uint64_t bits) {
+  uint64_t al = 16;
+  while (al > 1 && (bits & (al - 1))) al /= 2;
+  return al;
+}
+
+}  // namespace
+
+hipError_t rope(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const int32_t* pos, const double* freq,
+                float mscale, int layout, bool back, int64_t rows, int T, int heads, int dh, int rot, hipStream_t s) {
+  Args a{};
+  a.x = x, a.y = y, a.ldx = ldx, a.ldy = ldy, a.pos = pos, a.freq = freq, a.mscale = mscale, a.back = back;
+  a.rows = static_cast<uint32_t>(rows), a.T = T, a.Hq = heads, a.dh = dh, a.rot = rot;
+  const uint64_t e = dtype == DT_BF16 ? 2 : 4;
+  unsigned blocks;
+  return run<ROPE>(dtype, a, layout, align_of(low(x) | low(y) | ldx * e | ldy * e), s, &blocks);
+}
+
+hipError_t qknorm_rope_fwd(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const void* gq, const void* gk,
+                           float eps, const int32_t* pos, const double* freq, float mscale, int layout, int64_t rows,
+                           int T, int Hq, int Hk, int Hv, int dh, int rot, hipStream_t s) {
+  Args a{};
+  a.x = x, a.y = y, a.ldx = ldx, a.ldy = ldy, a.gq = gq, a.gk = gk, a.eps = eps, a.pos = pos, a.freq = freq;
+  a.mscale = mscale, a.rows = static_cast<uint32_t>(rows), a.T = T, a.Hq = Hq, a.Hk = Hk, a.Hv = Hv, a.dh = dh, a.rot = rot;
+  a.copy = y != x;
+  const uint64_t e = dtype == DT_BF16 ? 2 : 4;
+  unsigned blocks;
+  return run<NORM>(dtype, a, layout, align_of(low(x) | low(y) | low(gq) | low(gk) | ldx * e | ldy * e), s, &blocks);
+}
+
+uint64_t qknorm_rope_bwd_ws(int dh) { return BWD_BLOCKS * 2 * dh * sizeof(float); }
+
+hipError_t qknorm_rope_bwd(int dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx, void* dx, int64_t lddx,
+                           const void* gq, const void* gk, float* dgq, float* dgk, float eps, const int32_t* pos,
+                           const double* freq, float mscale, int layout, int64_t rows, int T, int Hq, int Hk, int Hv,
+                           int dh, int rot, float* ws, hipStream_t s) {
+  Args a{};
+  a.x = x, a.dy = dy, a.y = dx, a.ldx = ldx, a.lddy = lddy, a.ldy = lddx, a.gq = gq, a.gk = gk, a.eps = eps;
+  a.pos = pos, a.freq = freq, a.mscale = mscale, a.rows = static_cast<uint32_t>(rows), a.T = T;
+  a.Hq = Hq, a.Hk = Hk, a.Hv = Hv, a.dh = dh, a.rot = rot;
+  a.copy = dx != dy;
+  a.part = dgq || dgk ? ws : nullptr;
+  const uint64_t e = dtype == DT_BF16 ? 2 : 4;
+  unsigned blocks;
+  hipError_t st = run<NORM_BWD>(dtype, a, layout,
+                                align_of(low(x) | low(dy) | low(dx) | low(gq) | low(gk) | ldx * e | lddy * e | lddx * e), s,
+                                &blocks);
+  if (st != hipSuccess || !(dgq || dgk)) return st;
+  // no parts: zeros
+  if (dgq && dgk) return sum_parts2(ws, blocks, 2 * dh, 2 * dh, DT_F32, dgq, dgk, dh, false, s);
+  return sum_parts(dgq || !ws ? ws : ws + dh, blocks, dh, 2 * dh, DT_F32, dgq ? dgq : dgk, false, s);
+}
+
+}  // namespace atom
