@@ -153,6 +153,55 @@ int atom_k_qknorm_rope_bwd(int dtype, const void* dy, int64_t lddy, const void* 
                            const double* freq, float mscale, int layout, int64_t rows, int T, int Hq, int Hk, int Hv,
                            int dh, int rot, void* ws, uint64_t ws_bytes, void* stream);
 
+/* Cross attention: the queries of B sequences on the keys and values of B others
+ * (an encoder's states), of other lengths; Hq heads of queries on Hk of keys and
+ * values, query head h on head h / (Hq / Hk).  For each sequence and head
+ *   z = scale q k^T,  lse = log sum_j exp z_j,  o = exp(z - lse) v.
+ * Every key of a sequence is visible to every query of it.  A row without keys
+ * (or with scores of -infinity alone) gives o 0 and lse -infinity.
+ *
+ * Rows: q and o [q_rows][Hq * dh], lse fp32 [q_rows][Hq], k and v [k_rows][Hk * dh],
+ * each with its leading dimension.  Padded: sequence b's queries are rows b * Tq
+ * on (q_start NULL), q_len[b] of them (NULL: Tq); packed: rows q_start[b] on,
+ * q_len[b] of them, at most Tq.  The same for keys with k_start, k_len and Tk.
+ * The four are device int32 [B]; a length is clamped to 0 .. T and to the rows
+ * that there are, and a start outside them makes the sequence empty.  Padding of a
+ * padded batch gets zeros (o, dq, dk, dv; lse -infinity); rows that no sequence of
+ * a packed one has stay as they are.  In the forward call sequences may share
+ * keys, in the backward call each key row is in one sequence at most; query rows
+ * in both. */
+typedef struct {
+  int32_t B, Tq, Tk, Hq, Hk, dh;
+  int64_t q_rows, k_rows;
+  const int32_t *q_start, *q_len, *k_start, *k_len;
+} atom_cross_shape;
+
+/* Forward; lse may be NULL (not wanted).  Requirements: dh 64 or 128, Hk >= 1
+ * divides Hq, B, Tq, Tk >= 0 (B or Tq 0: nothing is done), q_start with q_len only
+ * (k alike); without a start, q_rows >= B * Tq (k alike); scale finite, above 0;
+ * leading dimensions multiples of 8 (bf16) or 4 (fp32); tensors and ws 16-byte
+ * aligned; less than 2^26 pairs of query and head, and of key and head of keys, in
+ * padded lengths; Tq (Hq/Hk)^2 < 2^32, and less than 2^22 workgroups of 64 rows.
+ * o must not overlap the inputs.  ws: device scratch of at least the bytes
+ * that the query returns (0: none needed, or sizes refused); calls that may
+ * overlap need scratch of their own. */
+uint64_t atom_k_cross_attn_fwd_ws_bytes(int dtype, const atom_cross_shape* shape);
+int atom_k_cross_attn_fwd(int dtype, const atom_cross_shape* shape, const void* q, int64_t ldq, const void* k,
+                          int64_t ldk, const void* v, int64_t ldv, float scale, void* o, int64_t ldo, float* lse,
+                          void* ws, uint64_t ws_bytes, void* stream);
+
+/* Backward, from the forward's o and lse and the gradient dout of o, with the same
+ * shape and scale: with p = exp(z - lse) and D = sum_c dout o,
+ *   dv = p^T dout,  ds = p (dout v^T - D),  dq = scale ds k,  dk = scale ds^T q,
+ * dk and dv summed over the heads that share them, in a fixed order.  dq may be
+ * NULL (not wanted), or dk and dv both.  The gradients must not overlap the inputs
+ * or one another.  Requirements as above, for every tensor. */
+uint64_t atom_k_cross_attn_bwd_ws_bytes(int dtype, const atom_cross_shape* shape);
+int atom_k_cross_attn_bwd(int dtype, const atom_cross_shape* shape, const void* q, int64_t ldq, const void* k,
+                          int64_t ldk, const void* v, int64_t ldv, float scale, const void* o, int64_t ldo,
+                          const void* dout, int64_t lddo, const float* lse, void* dq, int64_t lddq, void* dk,
+                          int64_t lddk, void* dv, int64_t lddv, void* ws, uint64_t ws_bytes, void* stream);
+
 /* Scratch floats atom_k_colsum needs in `part`. */
 int64_t atom_k_colsum_part_floats(int64_t rows, int cols);
 

@@ -79,6 +79,13 @@ class atom_stats(ctypes.Structure):
                 ("opt_state_pinned", ctypes.c_int32)]
 
 
+class atom_cross_shape(ctypes.Structure):
+    """Sequences, heads and rows of atom_k_cross_attn_*; the last four are device pointers (int32 [B]) or None."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Tq", "Tk", "Hq", "Hk", "dh")] + [
+        (n, ctypes.c_int64) for n in ("q_rows", "k_rows")] + [
+        (n, ctypes.c_void_p) for n in ("q_start", "q_len", "k_start", "k_len")]
+
+
 class AtomError(RuntimeError):
     def __init__(self, status, msg=""):
         self.status = status
@@ -138,6 +145,11 @@ _SIGS = {
     "atom_k_qknorm_rope_bwd_ws_bytes": (U64, [I64] + [ctypes.c_int] * 3),
     "atom_k_qknorm_rope_bwd": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, P, I64, P, P, P, P, ctypes.c_float, P, P,
                                               ctypes.c_float, ctypes.c_int, I64] + [ctypes.c_int] * 6 + [P, U64, P]),
+    "atom_k_cross_attn_fwd_ws_bytes": (U64, [ctypes.c_int, P]),
+    "atom_k_cross_attn_fwd": (ctypes.c_int, [ctypes.c_int, P] + [P, I64] * 3 + [ctypes.c_float, P, I64, P, P, U64, P]),
+    "atom_k_cross_attn_bwd_ws_bytes": (U64, [ctypes.c_int, P]),
+    "atom_k_cross_attn_bwd": (ctypes.c_int, [ctypes.c_int, P] + [P, I64] * 3 + [ctypes.c_float] + [P, I64] * 2 + [P]
+                              + [P, I64] * 3 + [P, U64, P]),
     "atom_k_colsum_part_floats": (I64, [I64, ctypes.c_int]),
     "atom_k_colsum": (ctypes.c_int, [ctypes.c_int, P, I64, ctypes.c_int, P, P, P]),
     "atom_k_xent": (ctypes.c_int, [ctypes.c_int, P, I64, P, P, I64, P, I64, ctypes.c_int, ctypes.c_float, P]),
@@ -516,6 +528,24 @@ def atom_k_qknorm_rope_bwd(dtype, dy, lddy, x, ldx, dx, lddx, gq, gk, dgq, dgk, 
                            Hq, Hk, Hv, dh, rot, ws, ws_bytes, stream=None):
     _kcall("atom_k_qknorm_rope_bwd", dtype, dy, lddy, x, ldx, dx, lddx, gq, gk, dgq, dgk, eps, pos, freq, mscale, layout,
            rows, T, Hq, Hk, Hv, dh, rot, ws, ws_bytes, stream)
+
+
+def atom_k_cross_attn_fwd_ws_bytes(dtype, shape):
+    return lib().atom_k_cross_attn_fwd_ws_bytes(dtype, _ref(shape))
+
+
+def atom_k_cross_attn_fwd(dtype, shape, q, ldq, k, ldk, v, ldv, scale, o, ldo, lse, ws, ws_bytes, stream=None):
+    _kcall("atom_k_cross_attn_fwd", dtype, _ref(shape), q, ldq, k, ldk, v, ldv, scale, o, ldo, lse, ws, ws_bytes, stream)
+
+
+def atom_k_cross_attn_bwd_ws_bytes(dtype, shape):
+    return lib().atom_k_cross_attn_bwd_ws_bytes(dtype, _ref(shape))
+
+
+def atom_k_cross_attn_bwd(dtype, shape, q, ldq, k, ldk, v, ldv, scale, o, ldo, dout, lddo, lse, dq, lddq, dk, lddk, dv,
+                          lddv, ws, ws_bytes, stream=None):
+    _kcall("atom_k_cross_attn_bwd", dtype, _ref(shape), q, ldq, k, ldk, v, ldv, scale, o, ldo, dout, lddo, lse, dq, lddq,
+           dk, lddk, dv, lddv, ws, ws_bytes, stream)
 
 
 def atom_k_colsum_part_floats(rows, cols):

@@ -27,7 +27,8 @@ HIP_SOURCES = ["gemm.hip", "gemm_dl_256.hip", "gemm_dl_192.hip", "gemm_dl_256x12
                "gemm_loss_f32.hip", "loss.hip",
                "gemm_planes_256.hip", "gemm_planes_192.hip", "gemm_planes_256x128.hip", "gemm_planes_128.hip", "gemm_planes_64.hip",
                "gemm_ns_256.hip", "gemm_ns_192.hip", "gemm_ns_128.hip", "gemm_ns_64.hip", "orthogonalize.hip",
-               "attention.hip", "attention_f32.hip", "rotary.hip", "rowops.hip", "runtime.cpp", "nodes.cpp", "schedule.cpp",
+               "attention.hip", "attention_f32.hip", "rotary.hip", "cross_attention.hip", "cross_attention_f32.hip",
+               "rowops.hip", "runtime.cpp", "nodes.cpp", "schedule.cpp",
                "host_accum.cpp", "transfer.cpp", "capi_kernels.cpp"]
 # per-source optimisation level (see attention_f32.hip)
 OPT = {"attention_f32.hip": "-O1"}

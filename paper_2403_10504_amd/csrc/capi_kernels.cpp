@@ -35,6 +35,27 @@ inline bool positions_ok(const int32_t* pos, const double* freq, int T, int rot)
   return rot == 0 || (freq && reinterpret_cast<uintptr_t>(freq) % 8 == 0 && reinterpret_cast<uintptr_t>(pos) % 4 == 0 &&
                       (pos || T >= 1));
 }
+inline bool cross_ok(int dt, const atom_cross_shape* s) {
+  return dt_ok(dt) && s && cross_attn_ok(dt, s->B, s->Tq, s->Tk, s->Hq, s->Hk, s->dh);
+}
+// starts come with lengths; without them the rows hold the padded batch
+inline bool side_ok(const int32_t* start, const int32_t* len, int64_t rows, int64_t B, int64_t T) {
+  if (reinterpret_cast<uintptr_t>(start) % 4 || reinterpret_cast<uintptr_t>(len) % 4 || rows < 0) return false;
+  return start ? len != nullptr && rows <= INT32_MAX : rows >= B * T;
+}
+inline bool cross_rows_ok(int dt, const void* p, int64_t ld, int64_t heads, int dh) {
+  return p && !misaligned(p) && ld >= heads * dh && ld % (dt == ATOM_BF16 ? 8 : 4) == 0 && ld <= INT64_MAX / 8 / INT32_MAX;
+}
+inline CrossArgs cross_args(const atom_cross_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                            const void* v, int64_t ldv, float scale) {
+  CrossArgs a{};
+  a.q = q, a.k = k, a.v = v, a.ldq = ldq, a.ldk = ldk, a.ldv = ldv, a.scale = scale;
+  a.B = s->B, a.Tq = s->Tq, a.Tk = s->Tk, a.Hq = s->Hq, a.Hk = s->Hk, a.G = s->Hq / s->Hk;
+  a.gmul = static_cast<uint32_t>(((1ull << 32) + a.G - 1) / a.G);
+  a.q_rows = s->q_rows, a.k_rows = s->k_rows;
+  a.q_start = s->q_start, a.q_len = s->q_len, a.k_start = s->k_start, a.k_len = s->k_len;
+  return a;
+}
 }  // namespace
 
 extern "C" {
@@ -165,6 +186,61 @@ int atom_k_qknorm_rope_bwd(int dtype, const void* dy, int64_t lddy, const void* 
   }
   return st(qknorm_rope_bwd(dtype, dy, lddy, x, ldx, dx, lddx, gq, gk, dgq, dgk, eps, pos, freq, mscale, layout, rows, T,
                             Hq, Hk, Hv, dh, rot, static_cast<float*>(ws), S(stream)));
+}
+
+uint64_t atom_k_cross_attn_fwd_ws_bytes(int dtype, const atom_cross_shape* shape) {
+  return cross_ok(dtype, shape) ? cross_attn_fwd_ws(dtype, shape->B, shape->Tq, shape->Tk, shape->Hq, shape->Hk, shape->dh)
+                                : 0;
+}
+
+int atom_k_cross_attn_fwd(int dtype, const atom_cross_shape* shape, const void* q, int64_t ldq, const void* k,
+                          int64_t ldk, const void* v, int64_t ldv, float scale, void* o, int64_t ldo, float* lse,
+                          void* ws, uint64_t ws_bytes, void* stream) {
+  if (!cross_ok(dtype, shape) || !(scale > 0) || !isfinite(scale)) return ATOM_EINVAL;
+  const atom_cross_shape& c = *shape;
+  if (!side_ok(c.q_start, c.q_len, c.q_rows, c.B, c.Tq) || !side_ok(c.k_start, c.k_len, c.k_rows, c.B, c.Tk))
+    return ATOM_EINVAL;
+  if (c.B == 0 || c.Tq == 0) return ATOM_OK;
+  if (!cross_rows_ok(dtype, q, ldq, c.Hq, c.dh) || !cross_rows_ok(dtype, o, ldo, c.Hq, c.dh)) return ATOM_EINVAL;
+  if (c.Tk > 0 && (!cross_rows_ok(dtype, k, ldk, c.Hk, c.dh) || !cross_rows_ok(dtype, v, ldv, c.Hk, c.dh)))
+    return ATOM_EINVAL;
+  const uint64_t need = cross_attn_fwd_ws(dtype, c.B, c.Tq, c.Tk, c.Hq, c.Hk, c.dh);
+  if (!aligned_to(ATOM_F32, lse) || (need && (!ws || misaligned(ws) || ws_bytes < need))) return ATOM_EINVAL;
+  CrossArgs a = cross_args(shape, q, ldq, k, ldk, v, ldv, scale);
+  a.o = o, a.ldo = ldo, a.lse = lse;
+  return st(cross_attn_fwd(dtype, a, c.dh, ws, S(stream)));
+}
+
+uint64_t atom_k_cross_attn_bwd_ws_bytes(int dtype, const atom_cross_shape* shape) {
+  return cross_ok(dtype, shape) ? cross_attn_bwd_ws(dtype, shape->B, shape->Tq, shape->Tk, shape->Hq, shape->Hk, shape->dh)
+                                : 0;
+}
+
+int atom_k_cross_attn_bwd(int dtype, const atom_cross_shape* shape, const void* q, int64_t ldq, const void* k,
+                          int64_t ldk, const void* v, int64_t ldv, float scale, const void* o, int64_t ldo,
+                          const void* dout, int64_t lddo, const float* lse, void* dq, int64_t lddq, void* dk,
+                          int64_t lddk, void* dv, int64_t lddv, void* ws, uint64_t ws_bytes, void* stream) {
+  if (!cross_ok(dtype, shape) || !(scale > 0) || !isfinite(scale)) return ATOM_EINVAL;
+  const atom_cross_shape& c = *shape;
+  if (!side_ok(c.q_start, c.q_len, c.q_rows, c.B, c.Tq) || !side_ok(c.k_start, c.k_len, c.k_rows, c.B, c.Tk))
+    return ATOM_EINVAL;
+  if ((dk == nullptr) != (dv == nullptr)) return ATOM_EINVAL;
+  if (c.B == 0 || (c.Tq == 0 && c.Tk == 0) || (!dq && !dk)) return ATOM_OK;
+  if (c.Tq > 0) {
+    if (!cross_rows_ok(dtype, q, ldq, c.Hq, c.dh) || !cross_rows_ok(dtype, o, ldo, c.Hq, c.dh) ||
+        !cross_rows_ok(dtype, dout, lddo, c.Hq, c.dh) || !lse || !aligned_to(ATOM_F32, lse))
+      return ATOM_EINVAL;
+    if (dq && !cross_rows_ok(dtype, dq, lddq, c.Hq, c.dh)) return ATOM_EINVAL;
+    if (!ws || misaligned(ws) || ws_bytes < cross_attn_bwd_ws(dtype, c.B, c.Tq, c.Tk, c.Hq, c.Hk, c.dh)) return ATOM_EINVAL;
+  }
+  if (c.Tk > 0) {
+    if (!cross_rows_ok(dtype, k, ldk, c.Hk, c.dh) || !cross_rows_ok(dtype, v, ldv, c.Hk, c.dh)) return ATOM_EINVAL;
+    if (dk && (!cross_rows_ok(dtype, dk, lddk, c.Hk, c.dh) || !cross_rows_ok(dtype, dv, lddv, c.Hk, c.dh))) return ATOM_EINVAL;
+  }
+  CrossArgs a = cross_args(shape, q, ldq, k, ldk, v, ldv, scale);
+  a.o = const_cast<void*>(o), a.ldo = ldo, a.dout = dout, a.lddo = lddo, a.lse = const_cast<float*>(lse);
+  a.dq = dq, a.lddq = lddq, a.dk = dk, a.lddk = lddk, a.dv = dv, a.lddv = lddv;
+  return st(cross_attn_bwd(dtype, a, c.dh, ws, S(stream)));
 }
 
 int64_t atom_k_colsum_part_floats(int64_t rows, int cols) { return colsum_blocks(rows) * cols; }

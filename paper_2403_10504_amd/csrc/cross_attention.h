@@ -1,0 +1,103 @@
+// What the cross-attention kernels (cross_attention.hip, bf16;
+// cross_attention_f32.hip) and their launcher share: the arguments, a
+// sequence's rows, the mapping of workgroups, and the kernels that join ranges.
+//
+// A sequence's queries of the G heads that share a head of keys are packed into
+// one list of rows, p = t G + g: one token of many heads still fills the rows of
+// a matrix instruction, and the shared keys are read once for all of them.
+#pragma once
+
+#include "attention_kernels.h"
+
+namespace atom {
+
+namespace cross {
+
+// A sequence's rows: the first, and how many.  Lengths and starts are clamped
+// to the buffer, so no value of them leads out of it.
+struct Seq {
+  int64_t row0;
+  int n;
+};
+ATOM_DEV Seq seq(const int32_t* start, const int32_t* len, int T, int64_t rows, int b) {
+  int n = len ? min(max(len[b], 0), T) : T;
+  if (!start) return Seq{static_cast<int64_t>(b) * T, n};
+  const int64_t r = start[b];
+  if (r < 0 || r >= rows) return Seq{0, 0};
+  return Seq{r, static_cast<int>(min(static_cast<int64_t>(n), rows - r))};
+}
+
+// Work item of a workgroup: the hardware hands consecutive ids to the eight XCDs
+// in turn; each XCD takes a run of consecutive items, so that the blocks of one
+// sequence and head, which read the same keys, share an L2.  Ids past the items
+// (the grid is a multiple of eight) are negative.
+ATOM_DEV int item_of(int n_items) {
+  const int per = (n_items + 7) >> 3, id = blockIdx.x;
+  const int i = (id & 7) * per + (id >> 3);
+  return (id >> 3) < per && i < n_items ? i : -1;
+}
+
+// Token and head (of the group) of packed row p.
+struct Row {
+  int t, g;
+};
+ATOM_DEV Row row_of(const CrossArgs& a, int p) {
+  if (a.G == 1) return Row{p, 0};
+  const int t = static_cast<int>(__umulhi(static_cast<uint32_t>(p), a.gmul));
+  return Row{t, p - t * a.G};
+}
+
+// Offset of packed row p of head group hk in a tensor of leading dimension ld.
+template <int DH>
+ATOM_DEV int64_t at(const CrossArgs& a, const Seq& s, int hk, int p, int64_t ld) {
+  const Row r = row_of(a, p);
+  return (s.row0 + r.t) * ld + static_cast<int64_t>(hk * a.G + r.g) * DH;
+}
+
+// log-sum-exp in base 2 for the backward's exponents: a row that has none (no
+// finite score) gets +infinity, and so no weight anywhere.
+ATOM_DEV float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * attn::LOG2E; }
+
+// Where the running maximum starts: below every finite score, and finite, so
+// that a score of -infinity weighs 0 against it.
+constexpr float NO_MAX = -3e38f;
+
+// A row's output from the sums of its ranges, in range order: 64 lanes a row.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) cross_join_kernel(const CrossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t P = static_cast<int64_t>(a.Tq) * a.G, n = P * a.B * a.Hk;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (r >= n) return;
+  const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh / a.Hk, hk = bh % a.Hk;
+  const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b);
+  const bool on = p < qs.n * a.G;
+  if (!on && a.q_start) return;
+  constexpr int E = DH / 64;
+  float m = NO_MAX, l = 0.f, o[E] = {};
+  if (on) {
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.ml[2 * (s * n + r)]);
+    for (int s = 0; s < a.splits; ++s) {
+      const float f = attn::ex2(a.ml[2 * (s * n + r)] - m);
+      l += f * a.ml[2 * (s * n + r) + 1];
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += f * a.part[(s * n + r) * DH + E * lane + e];
+    }
+  }
+  const int64_t lo = at<DH>(a, qs, hk, p, a.ldo) + E * lane;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < E; ++e) static_cast<T*>(a.o)[lo + e] = from_f<T>(o[e] * inv);
+  if (a.lse && lane == 0) {
+    const Row w = row_of(a, p);
+    a.lse[(qs.row0 + w.t) * a.Hq + hk * a.G + w.g] = l == 0.f ? -INFINITY : (m + log2f(l)) * attn::LN2;
+  }
+}
+
+}  // namespace cross
+
+hipError_t cross_fwd_f32(const CrossArgs& a, int dh, hipStream_t s);
+hipError_t cross_dq_f32(const CrossArgs& a, int dh, hipStream_t s);
+hipError_t cross_dkdv_f32(const CrossArgs& a, int dh, hipStream_t s);
+
+}  // namespace atom

@@ -1,0 +1,859 @@
+// Cross attention (atom_k_cross_attn_fwd, _bwd): queries of one sequence on the
+// keys and values of another, of another length, heads of keys shared by groups
+// of query heads.  bf16 kernels, and the launchers of both types.
+//
+//   z = scale q k^T;  lse = log sum exp z;  o = exp(z - lse) v
+//   D = sum do o;  p = exp(z - lse);  ds = p (do v^T - D)
+//   dv = p^T do;  dq = scale ds k;  dk = scale ds^T q
+//
+// The tiles are those of the causal attention (attention_kernels.h): a wave owns
+// 16 rows or two times 16, key (or query) tiles of 64 rows go straight from
+// memory to LDS, two stages; the scores stay in registers, S^T = K Q^T feeding
+// the second product's operand; every output has one owner, so no atomics.  p and
+// ds are rounded to bf16 for the second products (the operands' type: half a step
+// of 2^-8 in each term, in random directions); sums and statistics are fp32.
+#include "cross_attention.h"
+
+#include "../../include/atom.h"
+#include "../../include/atom_kernels.h"
+
+namespace atom {
+namespace cross {
+
+using namespace attn;
+
+// Fragment of packed row p of a head group (zeros behind the last).
+template <int DH>
+ATOM_DEV void frag_row(Frag<bf16_t>& f, const CrossArgs& a, const bf16_t* base, const Seq& s, int hk, int p, int P,
+                       int64_t ld, int col) {
+  if (p < P) frag_load(f, base + at<DH>(a, s, hk, p, ld) + col);
+  else frag_zero(f);
+}
+
+// The tiles of a range.
+struct Range {
+  int t0, t1;
+};
+ATOM_DEV Range range_of(int n_rows, int splits, int s) {
+  const int n = (n_rows + BT - 1) / BT, per = (n + splits - 1) / splits;
+  return Range{min(s * per, n), min(s * per + per, n)};
+}
+
+// ------------------------------------------------------------------ forward
+template <int DH, int GR, int NW, int WPS, bool SPLIT>
+__global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs a) {
+  constexpr int NT = 64 * NW;
+  using F = FwdDL<DH, NT>;
+  constexpr int NS = DH / 32, NCT = DH / 16, BQ = NW * 16 * GR, RB = DH * 2;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * F::STAGE];
+
+  const int BH = a.B * a.Hk;
+  const int item = item_of(a.n_x * BH * a.splits);
+  if (item < 0) return;
+  const int x = item % a.n_x, split = SPLIT ? item / a.n_x % a.splits : 0, bh = item / (a.n_x * a.splits);
+  const int b = bh / a.Hk, hk = bh % a.Hk;
+  const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
+  const int P = qs.n * a.G, n_keys = ks.n;
+  const int q0 = x * BQ;
+  if (q0 >= P && (SPLIT || a.q_start)) return;
+
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lg = lane >> 4;
+  const int qw = q0 + w * 16 * GR;
+  const float sc = a.scale * LOG2E;
+  const bf16_t* qb = static_cast<const bf16_t*>(a.q);
+  const bf16_t* kb = static_cast<const bf16_t*>(a.k) + ks.row0 * a.ldk + hk * DH;
+  const bf16_t* vb = static_cast<const bf16_t*>(a.v) + ks.row0 * a.ldv + hk * DH;
+
+  Frag<bf16_t> qf[GR][NS];
+#pragma unroll
+  for (int g = 0; g < GR; ++g)
+#pragma unroll
+    for (int s = 0; s < NS; ++s) frag_row<DH>(qf[g][s], a, qb, qs, hk, qw + g * 16 + lr, P, a.ldq, 32 * s + 8 * lg);
+
+  f32x4_t acc_o[GR][NCT];
+  float m_i[GR], l_i[GR];
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    m_i[g] = NO_MAX;
+    l_i[g] = 0.f;
+#pragma unroll
+    for (int c = 0; c < NCT; ++c) acc_o[g][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // chunk q * NT + tid of a tile (row, slot); the last, partial tile reads its
+  // last key again (whose scores are masked)
+  const bf16_t* ksrc[F::LPT];
+  const bf16_t* vsrc[F::LPT];
+#pragma unroll
+  for (int q = 0; q < F::LPT; ++q) {
+    const int id = q * NT + tid, row = id / F::CPR, slot = id % F::CPR;
+    ksrc[q] = kb + static_cast<int64_t>(row) * a.ldk + (slot ^ F::kswz(row)) * 8;
+    vsrc[q] = vb + static_cast<int64_t>(row) * a.ldv + (slot ^ F::vswz(row)) * 8;
+  }
+  auto load_tile = [&](int st, int j0) {
+    const uint32_t kl = lds_offset(lds + st * F::STAGE), vl = kl + F::TILE;
+    const bool whole = j0 + BT <= n_keys;
+#pragma unroll
+    for (int q = 0; q < F::LPT; ++q) {
+      const uint32_t lo = __builtin_amdgcn_readfirstlane((q * NT + w * 64) * 16);
+      if (whole) {
+        lds_dma16(ksrc[q] + static_cast<int64_t>(j0) * a.ldk, kl + lo);
+        lds_dma16(vsrc[q] + static_cast<int64_t>(j0) * a.ldv, vl + lo);
+      } else {
+        const int id = q * NT + tid, row = id / F::CPR, slot = id % F::CPR;
+        const int64_t gr = min(j0 + row, n_keys - 1);
+        lds_dma16(kb + gr * a.ldk + (slot ^ F::kswz(row)) * 8, kl + lo);
+        lds_dma16(vb + gr * a.ldv + (slot ^ F::vswz(row)) * 8, vl + lo);
+      }
+    }
+  };
+  auto kfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int jt, int s) {
+    const int row = jt * 16 + lr;
+    f.v = *reinterpret_cast<const uint4*>(st + row * RB + ((4 * s + lg) ^ F::kswz(row)) * 16);
+  };
+  auto vfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int s2, int c) {
+    const int chunk = 2 * c + ((lr & 3) >> 1);
+    const int r0 = 32 * s2 + 4 * lg + (lr >> 2), r1 = r0 + 16;
+    const uint2 lo = ds_read_tr8(st + r0 * RB + (chunk ^ F::vswz(r0)) * 16 + 8 * (lr & 1));
+    const uint2 hi = ds_read_tr8(st + r1 * RB + (chunk ^ F::vswz(r1)) * 16 + 8 * (lr & 1));
+    f.v = make_uint4(lo.x, lo.y, hi.x, hi.y);
+  };
+
+  const Range rg = q0 < P ? range_of(n_keys, a.splits, split) : Range{0, 0};
+  if (rg.t0 < rg.t1) load_tile(0, rg.t0 * BT);
+  for (int kt = rg.t0; kt < rg.t1; ++kt) {
+    const int j0 = kt * BT, cur = (kt - rg.t0) & 1;
+    // tile kt has landed for every wave, and every wave is done with the stage before
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    asm volatile("s_barrier" ::: "memory");
+    if (kt + 1 < rg.t1) load_tile(cur ^ 1, j0 + BT);
+    if (qw >= P) continue;
+    const uint8_t* kst = lds + cur * F::STAGE;
+    const uint8_t* vst = kst + F::TILE;
+    float p[GR][4][4];
+    float mloc[GR];
+#pragma unroll
+    for (int g = 0; g < GR; ++g) mloc[g] = -INFINITY;
+    auto score_tile = [&](auto MASK_) {
+      constexpr bool MASK = decltype(MASK_)::value;
+      Frag<bf16_t> kf[2][NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) kfrag(kf[0][s], kst, 0, s);
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt) {
+        if (jt + 1 < 4) {
+#pragma unroll
+          for (int s = 0; s < NS; ++s) kfrag(kf[(jt + 1) & 1][s], kst, jt + 1, s);
+        }
+        f32x4_t z[GR];
+#pragma unroll
+        for (int g = 0; g < GR; ++g) z[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+          for (int g = 0; g < GR; ++g) mfma16(z[g], kf[jt & 1][s], qf[g][s]);
+#pragma unroll
+        for (int g = 0; g < GR; ++g)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float v = z[g][r];
+            if constexpr (MASK) v = j0 + jt * 16 + 4 * lg + r < n_keys ? v : -INFINITY;
+            p[g][jt][r] = v;
+            mloc[g] = fmaxf(mloc[g], v);
+          }
+      }
+    };
+    if (j0 + BT > n_keys) score_tile(std::true_type{});
+    else score_tile(std::false_type{});
+    Frag<bf16_t> vf[2];
+    vfrag(vf[0], vst, 0, 0);
+#pragma unroll
+    for (int g = 0; g < GR; ++g) {
+      const float mx = rows4_max(mloc[g]) * sc;
+      if (__builtin_amdgcn_ballot_w64(mx > m_i[g] + RESCALE_LOG2) != 0) {
+        const float m_new = fmaxf(m_i[g], mx);
+        const float alpha = ex2(m_i[g] - m_new);
+        l_i[g] *= alpha;
+        m_i[g] = m_new;
+#pragma unroll
+        for (int c = 0; c < NCT; ++c) acc_o[g][c] *= alpha;
+      }
+      float lsum = 0.f;
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          p[g][jt][r] = ex2(__builtin_fmaf(p[g][jt][r], sc, -m_i[g]));
+          lsum += p[g][jt][r];
+        }
+      l_i[g] += lsum;
+    }
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      Frag<bf16_t> pf[GR];
+#pragma unroll
+      for (int g = 0; g < GR; ++g) frag_from_pair(pf[g], p[g], s2);
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) {
+        const int n = s2 * NCT + c;
+        if (n + 1 < 2 * NCT) vfrag(vf[(n + 1) & 1], vst, (n + 1) / NCT, (n + 1) % NCT);
+#pragma unroll
+        for (int g = 0; g < GR; ++g) mfma16(acc_o[g][c], vf[n & 1], pf[g]);
+      }
+    }
+  }
+
+  // padded queries of a padded batch get zeros (P up to Tq G)
+  const int p_end = a.q_start ? P : a.Tq * a.G;
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    const int pi = qw + g * 16 + lr;
+    const float l_tot = rows4_sum(l_i[g]);
+    if (SPLIT) {
+      if (pi >= P) continue;
+      const int64_t n = static_cast<int64_t>(a.Tq) * a.G, r = (static_cast<int64_t>(split) * BH + bh) * n + pi;
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) {
+        float v[4] = {acc_o[g][c][0], acc_o[g][c][1], acc_o[g][c][2], acc_o[g][c][3]};
+        store_row4<float>(a.part + r * DH + c * 16 + 4 * lg, v);
+      }
+      if (lg == 0) a.ml[2 * r] = m_i[g], a.ml[2 * r + 1] = l_tot;
+      continue;
+    }
+    if (pi >= p_end) continue;
+    const bool none = l_tot == 0.f || pi >= P;  // no keys, or padding: zeros
+    const float inv = 1.f / l_tot;
+    const Row rw = row_of(a, pi);
+    bf16_t* orow = static_cast<bf16_t*>(a.o) + (qs.row0 + rw.t) * a.ldo + static_cast<int64_t>(hk * a.G + rw.g) * DH;
+#pragma unroll
+    for (int c = 0; c < NCT; ++c) {
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = none ? 0.f : acc_o[g][c][r] * inv;
+      store_row4<bf16_t>(orow + c * 16 + 4 * lg, v);
+    }
+    if (lg == 0 && a.lse)
+      a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g] = none ? -INFINITY : (m_i[g] + log2f(l_tot)) * LN2;
+  }
+}
+
+// ------------------------------------------------------------ backward: dQ
+// Also D of every row, which the dK/dV kernel reads (a.dq null: D alone).
+template <int DH, int NW, int SUB, bool SPLIT>
+__global__ void __launch_bounds__(64 * NW, DH == 64 ? 4 : 2) cross_dq_kernel(const CrossArgs a) {
+  using F = FwdDL<DH>;
+  constexpr int NS = DH / 32, NCT = DH / 16, BQ = NW * 16, NT = 64 * NW, RB = DH * 2;
+  constexpr int LPT = F::TILE / (NT * 16);
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * SUB * F::STAGE];
+
+  const int BH = a.B * a.Hk;
+  const int item = item_of(a.n_x * BH * a.splits);
+  if (item < 0) return;
+  const int x = item % a.n_x, split = SPLIT ? item / a.n_x % a.splits : 0, bh = item / (a.n_x * a.splits);
+  const int b = bh / a.Hk, hk = bh % a.Hk;
+  const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
+  const int P = qs.n * a.G, n_keys = ks.n;
+  const int q0 = x * BQ;
+  if (q0 >= P && (SPLIT || a.q_start)) return;
+  const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
+
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lg = lane >> 4;
+  const int qw = q0 + w * 16, pi = qw + lr;
+  const float sc = a.scale * LOG2E;
+  const bf16_t* kb = static_cast<const bf16_t*>(a.k) + ks.row0 * a.ldk + hk * DH;
+  const bf16_t* vb = static_cast<const bf16_t*>(a.v) + ks.row0 * a.ldv + hk * DH;
+
+  Frag<bf16_t> qf[NS], of[NS];
+  float lse_i = INFINITY;
+  if (pi < P) {
+    const Row rw = row_of(a, pi);
+    lse_i = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
+  }
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    frag_row<DH>(qf[s], a, static_cast<const bf16_t*>(a.q), qs, hk, pi, P, a.ldq, 32 * s + 8 * lg);
+    frag_row<DH>(of[s], a, static_cast<const bf16_t*>(a.dout), qs, hk, pi, P, a.lddo, 32 * s + 8 * lg);
+  }
+  f32x4_t acc[NCT];
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  auto load_tile = [&](int st, int j0) {
+    const uint32_t kl = lds_offset(lds + st * F::STAGE), vl = kl + F::TILE;
+#pragma unroll
+    for (int q = 0; q < LPT; ++q) {
+      const int id = q * NT + tid, row = id / F::CPR, slot = id % F::CPR;
+      const int64_t gr = min(j0 + row, n_keys - 1);
+      const uint32_t lo = __builtin_amdgcn_readfirstlane((q * NT + w * 64) * 16);
+      lds_dma16(kb + gr * a.ldk + (slot ^ dsw<DH>(row)) * 8, kl + lo);
+      lds_dma16(vb + gr * a.ldv + (slot ^ F::kswz(row)) * 8, vl + lo);
+    }
+  };
+  auto rowfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int jt, int s, bool dual) {
+    const int row = jt * 16 + lr, chunk = 4 * s + lg;
+    f.v = *reinterpret_cast<const uint4*>(st + row * RB + (chunk ^ (dual ? dsw<DH>(row) : F::kswz(row))) * 16);
+  };
+  auto trfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int s2, int c) {
+    const int chunk = 2 * c + ((lr & 3) >> 1);
+    const int r0 = 32 * s2 + 4 * lg + (lr >> 2), r1 = r0 + 16;
+    const uint2 lo = ds_read_tr8(st + r0 * RB + (chunk ^ dsw<DH>(r0)) * 16 + 8 * (lr & 1));
+    const uint2 hi = ds_read_tr8(st + r1 * RB + (chunk ^ dsw<DH>(r1)) * 16 + 8 * (lr & 1));
+    f.v = make_uint4(lo.x, lo.y, hi.x, hi.y);
+  };
+
+  const Range rg = q0 < P && a.dq ? range_of(n_keys, a.splits, split) : Range{0, 0};
+  auto load_stage = [&](int st, int kt) {
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
+      if (kt + u < rg.t1) load_tile(st * SUB + u, (kt + u) * BT);
+  };
+  load_stage(0, rg.t0);
+  float del_i;
+  {
+    Frag<bf16_t> f[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) frag_row<DH>(f[s], a, static_cast<const bf16_t*>(a.o), qs, hk, pi, P, a.ldo, 32 * s + 8 * lg);
+    del_i = row_dot<NS>(f, of);
+    if (lg == 0 && pi < P && split == 0) a.delta[bh * n_p + pi] = del_i;
+  }
+  if (!a.dq) return;
+  for (int ks0 = rg.t0; ks0 < rg.t1; ks0 += SUB) {
+    const int cur = ((ks0 - rg.t0) / SUB) & 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    asm volatile("s_barrier" ::: "memory");
+    if (ks0 + SUB < rg.t1) load_stage(cur ^ 1, ks0 + SUB);
+    if (qw >= P) continue;
+#pragma unroll 1
+    for (int u = 0; u < SUB; ++u) {
+      const int kt = ks0 + u, j0 = kt * BT;
+      if (kt >= rg.t1) break;
+      const uint8_t* kst = lds + (cur * SUB + u) * F::STAGE;
+      const uint8_t* vst = kst + F::TILE;
+      float ds[4][4];
+      auto score_tile = [&](auto MASK_) {
+        constexpr bool MASK = decltype(MASK_)::value;
+        Frag<bf16_t> kf[2][NS], vf[2][NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          rowfrag(kf[0][s], kst, 0, s, true);
+          rowfrag(vf[0][s], vst, 0, s, false);
+        }
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+          if (jt + 1 < 4) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+              rowfrag(kf[(jt + 1) & 1][s], kst, jt + 1, s, true);
+              rowfrag(vf[(jt + 1) & 1][s], vst, jt + 1, s, false);
+            }
+          }
+          f32x4_t sa = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < NS; ++s) {
+            mfma16(sa, kf[jt & 1][s], qf[s]);  // S^T[j][i]: lane holds one query, keys 4lg + r
+            mfma16(dp, vf[jt & 1][s], of[s]);  // dP^T[j][i]
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float pv = ex2(__builtin_fmaf(sa[r], sc, -lse_i));
+            float d = pv * (dp[r] - del_i);
+            if constexpr (MASK) d = j0 + jt * 16 + 4 * lg + r < n_keys ? d : 0.f;
+            ds[jt][r] = d;
+          }
+        }
+      };
+      if (j0 + BT > n_keys) score_tile(std::true_type{});
+      else score_tile(std::false_type{});
+      Frag<bf16_t> kt2[2];
+      trfrag(kt2[0], kst, 0, 0);
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        Frag<bf16_t> dsf;
+        frag_from_pair(dsf, ds, s2);
+#pragma unroll
+        for (int c = 0; c < NCT; ++c) {
+          const int n = s2 * NCT + c;
+          if (n + 1 < 2 * NCT) trfrag(kt2[(n + 1) & 1], kst, (n + 1) / NCT, (n + 1) % NCT);
+          mfma16(acc[c], kt2[n & 1], dsf);  // dQ^T[c][i]
+        }
+      }
+    }
+  }
+
+  if (SPLIT) {
+    if (pi < P) {
+      float* row = a.part + ((static_cast<int64_t>(split) * BH + bh) * n_p + pi) * DH;
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) {
+        float v[4] = {acc[c][0], acc[c][1], acc[c][2], acc[c][3]};
+        store_row4<float>(row + c * 16 + 4 * lg, v);
+      }
+    }
+    return;
+  }
+  if (pi < (a.q_start ? P : n_p)) {
+    bf16_t* row = static_cast<bf16_t*>(a.dq) + at<DH>(a, qs, hk, pi, a.lddq);
+#pragma unroll
+    for (int c = 0; c < NCT; ++c) {
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = pi < P ? acc[c][r] * a.scale : 0.f;  // (padding: zeros)
+      store_row4<bf16_t>(row + c * 16 + 4 * lg, v);
+    }
+  }
+}
+
+// -------------------------------------------------------- backward: dK, dV
+template <int DH, int W, int SUB, bool SPLIT>
+__global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(const CrossArgs a) {
+  using F = FwdDL<DH>;
+  constexpr int NS = DH / 32, NCT = DH / 16, NT = 64 * W, RB = DH * 2, BKEYS = 16 * W;
+  constexpr int LPT = F::TILE / (NT * 16);
+  constexpr int STAGE = dkdv_stage<DH>();
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * SUB * STAGE];
+
+  const int BH = a.B * a.Hk;
+  const int item = item_of(a.n_x * BH * a.splits);
+  if (item < 0) return;
+  const int x = item % a.n_x, split = SPLIT ? item / a.n_x % a.splits : 0, bh = item / (a.n_x * a.splits);
+  const int b = bh / a.Hk, hk = bh % a.Hk;
+  const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
+  const int P = qs.n * a.G, n_keys = ks.n;
+  const int k0 = x * BKEYS;
+  if (k0 >= n_keys && (SPLIT || a.k_start)) return;
+  const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
+
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lg = lane >> 4;
+  const int kw = k0 + w * 16, kj = kw + lr;
+  const float sc = a.scale * LOG2E;
+  const bf16_t* qb = static_cast<const bf16_t*>(a.q);
+  const bf16_t* ob = static_cast<const bf16_t*>(a.dout);
+  const bf16_t* kb = static_cast<const bf16_t*>(a.k) + ks.row0 * a.ldk + hk * DH;
+  const bf16_t* vb = static_cast<const bf16_t*>(a.v) + ks.row0 * a.ldv + hk * DH;
+
+  Frag<bf16_t> kf[NS], vf[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    frag_global(kf[s], kb, a.ldk, kj, n_keys, 32 * s + 8 * lg);
+    frag_global(vf[s], vb, a.ldv, kj, n_keys, 32 * s + 8 * lg);
+  }
+  f32x4_t acc_dk[NCT], acc_dv[NCT];
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) {
+    acc_dk[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    acc_dv[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  auto load_tile = [&](int st, int i0) {
+    const uint32_t ql = lds_offset(lds + st * STAGE), ol = ql + F::TILE;
+#pragma unroll
+    for (int q = 0; q < LPT; ++q) {
+      const int id = q * NT + tid, row = id / F::CPR, slot = id % F::CPR;
+      const Row rw = row_of(a, min(i0 + row, P - 1));
+      const int64_t col = static_cast<int64_t>(hk * a.G + rw.g) * DH + (slot ^ dsw<DH>(row)) * 8;
+      const uint32_t lo = __builtin_amdgcn_readfirstlane((q * NT + w * 64) * 16);
+      lds_dma16(qb + (qs.row0 + rw.t) * a.ldq + col, ql + lo);
+      lds_dma16(ob + (qs.row0 + rw.t) * a.lddo + col, ol + lo);
+    }
+  };
+  // LSE and D of a stage's rows go through registers; rows past the end get
+  // LSE = +inf, so their P is 0
+  float pre_lse = 0.f, pre_del = 0.f;
+  auto read_rows = [&](int i0) {
+    if (tid < SUB * BT) {
+      const int i = i0 + tid;
+      pre_lse = INFINITY;
+      pre_del = 0.f;
+      if (i < P) {
+        const Row rw = row_of(a, i);
+        pre_lse = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
+        pre_del = a.delta[bh * n_p + i];
+      }
+    }
+  };
+  auto store_rows = [&](int st) {
+    if (tid < SUB * BT) {
+      float* rows = reinterpret_cast<float*>(lds + (st * SUB + tid / BT) * STAGE + 2 * F::TILE);
+      rows[tid % BT] = pre_lse;
+      rows[BT + tid % BT] = pre_del;
+    }
+  };
+  auto rowfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int it, int s) {
+    const int row = it * 16 + lr, chunk = 4 * s + lg;
+    f.v = *reinterpret_cast<const uint4*>(st + row * RB + (chunk ^ dsw<DH>(row)) * 16);
+  };
+  auto trfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int s2, int c) {
+    const int chunk = 2 * c + ((lr & 3) >> 1);
+    const int r0 = 32 * s2 + 4 * lg + (lr >> 2), r1 = r0 + 16;
+    const uint2 lo = ds_read_tr8(st + r0 * RB + (chunk ^ dsw<DH>(r0)) * 16 + 8 * (lr & 1));
+    const uint2 hi = ds_read_tr8(st + r1 * RB + (chunk ^ dsw<DH>(r1)) * 16 + 8 * (lr & 1));
+    f.v = make_uint4(lo.x, lo.y, hi.x, hi.y);
+  };
+
+  const Range rg = k0 < n_keys ? range_of(P, a.splits, split) : Range{0, 0};
+  auto load_stage = [&](int st, int qt) {
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
+      if (qt + u < rg.t1) load_tile(st * SUB + u, (qt + u) * BT);
+  };
+  if (rg.t0 < rg.t1) {
+    load_stage(0, rg.t0);
+    read_rows(rg.t0 * BT);
+    store_rows(0);
+  }
+  for (int qs0 = rg.t0; qs0 < rg.t1; qs0 += SUB) {
+    const int cur = ((qs0 - rg.t0) / SUB) & 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    asm volatile("s_barrier" ::: "memory");
+    const bool more = qs0 + SUB < rg.t1;
+    if (more) {
+      load_stage(cur ^ 1, qs0 + SUB);
+      read_rows((qs0 + SUB) * BT);
+    }
+#pragma unroll 1
+    for (int u = 0; u < SUB; ++u) {
+      if (qs0 + u >= rg.t1 || kw >= n_keys) break;
+      const uint8_t* qst = lds + (cur * SUB + u) * STAGE;
+      const uint8_t* ost = qst + F::TILE;
+      const float* lse_s = reinterpret_cast<const float*>(qst + 2 * F::TILE);
+      const float* del_s = lse_s + BT;
+      float p[4][4], ds[4][4];
+      // keys past the end need no mask: their columns are never stored, and
+      // their fragments are zeros
+      if constexpr (DH == 128) {
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          Frag<bf16_t> qf[NS], of[NS];
+#pragma unroll
+          for (int s = 0; s < NS; ++s) {
+            rowfrag(qf[s], qst, it, s);
+            rowfrag(of[s], ost, it, s);
+          }
+          f32x4_t sa = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < NS; ++s) {
+            mfma16(sa, qf[s], kf[s]);  // S[i][j]: lane holds key kj, queries 4lg + r
+            mfma16(dp, of[s], vf[s]);  // dP[i][j]
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int il = it * 16 + 4 * lg + r;
+            p[it][r] = ex2(__builtin_fmaf(sa[r], sc, -lse_s[il]));
+            ds[it][r] = p[it][r] * (dp[r] - del_s[il]);
+          }
+          // LDS reads stay in their 16-query step, else all are hoisted and spill
+          __builtin_amdgcn_sched_barrier(0x000A);
+        }
+      } else {
+        Frag<bf16_t> qf[2][NS], of[2][NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          rowfrag(qf[0][s], qst, 0, s);
+          rowfrag(of[0][s], ost, 0, s);
+        }
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          if (it + 1 < 4) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+              rowfrag(qf[(it + 1) & 1][s], qst, it + 1, s);
+              rowfrag(of[(it + 1) & 1][s], ost, it + 1, s);
+            }
+          }
+          f32x4_t sa = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < NS; ++s) {
+            mfma16(sa, qf[it & 1][s], kf[s]);
+            mfma16(dp, of[it & 1][s], vf[s]);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int il = it * 16 + 4 * lg + r;
+            p[it][r] = ex2(__builtin_fmaf(sa[r], sc, -lse_s[il]));
+            ds[it][r] = p[it][r] * (dp[r] - del_s[il]);
+          }
+        }
+      }
+      Frag<bf16_t> ot2[2], qt2[2];
+      trfrag(ot2[0], ost, 0, 0);
+      trfrag(qt2[0], qst, 0, 0);
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        Frag<bf16_t> pf, dsf;
+        frag_from_pair(pf, p, s2);
+        frag_from_pair(dsf, ds, s2);
+#pragma unroll
+        for (int c = 0; c < NCT; ++c) {
+          const int n = s2 * NCT + c;
+          if (n + 1 < 2 * NCT) {
+            trfrag(ot2[(n + 1) & 1], ost, (n + 1) / NCT, (n + 1) % NCT);
+            trfrag(qt2[(n + 1) & 1], qst, (n + 1) / NCT, (n + 1) % NCT);
+          }
+          mfma16(acc_dv[c], ot2[n & 1], pf);   // dV^T[c][j]
+          mfma16(acc_dk[c], qt2[n & 1], dsf);  // dK^T[c][j]
+        }
+      }
+    }
+    if (more) store_rows(cur ^ 1);
+  }
+
+  if (kj >= (SPLIT || a.k_start ? n_keys : a.Tk)) return;
+  const int64_t r = SPLIT ? (static_cast<int64_t>(split) * BH + bh) * a.Tk + kj : ks.row0 + kj;
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) {
+    float vk[4], vv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      vk[i] = kj < n_keys ? acc_dk[c][i] * a.scale : 0.f;  // (padding: zeros)
+      vv[i] = kj < n_keys ? acc_dv[c][i] : 0.f;
+    }
+    if (SPLIT) {
+      store_row4<float>(a.part + r * DH + c * 16 + 4 * lg, vk);
+      store_row4<float>(a.part2 + r * DH + c * 16 + 4 * lg, vv);
+    } else {
+      store_row4<bf16_t>(static_cast<bf16_t*>(a.dk) + r * a.lddk + hk * DH + c * 16 + 4 * lg, vk);
+      store_row4<bf16_t>(static_cast<bf16_t*>(a.dv) + r * a.lddv + hk * DH + c * 16 + 4 * lg, vv);
+    }
+  }
+}
+
+}  // namespace cross
+
+namespace {
+
+using namespace cross;
+
+// The shape of each launch: blocks of rows, ranges, and the workspace.
+struct Plan {
+  bool small;     // blocks of 64 rows instead of 128
+  int n_x, splits;
+};
+
+constexpr int64_t CUS = 256;
+
+// Blocks of `big` rows where they fill the card, of 64 where not; with few of
+// those too, the other side in ranges of at least two tiles.
+Plan plan_of(int64_t rows, int64_t heads, int64_t other, int big) {
+  Plan p{};
+  const int64_t n_big = (rows + big - 1) / big * heads;
+  p.small = n_big < CUS;
+  const int64_t blk = p.small ? 64 : big;
+  p.n_x = static_cast<int>((rows + blk - 1) / blk);
+  const int64_t n = p.n_x * heads, tiles = (other + attn::BT - 1) / attn::BT;
+  p.splits = 1;
+  if (n > 0 && n < CUS) p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(2 * CUS / n, tiles / 2)));
+  return p;
+}
+
+Plan fwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G) {
+  return plan_of(static_cast<int64_t>(Tq) * G, static_cast<int64_t>(B) * Hk, Tk, dtype == DT_BF16 ? 128 : 64);
+}
+// (their workgroups are not made smaller)
+Plan bwd_plan(int dtype, int64_t rows, int64_t heads, int64_t other) {
+  Plan p{};
+  const int blk = dtype == DT_BF16 ? 128 : 64;
+  p.n_x = static_cast<int>((rows + blk - 1) / blk);
+  const int64_t n = p.n_x * heads, tiles = (other + attn::BT - 1) / attn::BT;
+  p.splits = 1;
+  if (n > 0 && n < CUS) p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(CUS / n, tiles / 2)));
+  return p;
+}
+
+unsigned grid_of(const CrossArgs& a) {
+  const int64_t n = static_cast<int64_t>(a.n_x) * a.splits * a.B * a.Hk;
+  return static_cast<unsigned>((n + 7) / 8 * 8);
+}
+
+// Sums of ranges, in range order, to dq (packed rows, times the scale).
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) cross_sum_dq_kernel(const CrossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t P = static_cast<int64_t>(a.Tq) * a.G, n = P * a.B * a.Hk;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (r >= n) return;
+  const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh / a.Hk, hk = bh % a.Hk;
+  const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b);
+  const bool on = p < qs.n * a.G;
+  if (!on && a.q_start) return;
+  constexpr int E = DH / 64;
+  float v[E] = {};
+  for (int s = 0; s < a.splits && on; ++s)
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] += a.part[(s * n + r) * DH + E * lane + e];
+  const int64_t lo = at<DH>(a, qs, hk, p, a.lddq) + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; ++e) static_cast<T*>(a.dq)[lo + e] = from_f<T>(v[e] * a.scale);
+}
+
+// The same to dk and dv (which hold the scale).
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) cross_sum_dkdv_kernel(const CrossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t n = static_cast<int64_t>(a.Tk) * a.B * a.Hk;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (r >= n) return;
+  const int bh = static_cast<int>(r / a.Tk), j = static_cast<int>(r % a.Tk), b = bh / a.Hk, hk = bh % a.Hk;
+  const Seq ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
+  const bool on = j < ks.n;
+  if (!on && a.k_start) return;
+  constexpr int E = DH / 64;
+  float vk[E] = {}, vv[E] = {};
+  for (int s = 0; s < a.splits && on; ++s)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      vk[e] += a.part[(s * n + r) * DH + E * lane + e];
+      vv[e] += a.part2[(s * n + r) * DH + E * lane + e];
+    }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    static_cast<T*>(a.dk)[(ks.row0 + j) * a.lddk + hk * DH + E * lane + e] = from_f<T>(vk[e]);
+    static_cast<T*>(a.dv)[(ks.row0 + j) * a.lddv + hk * DH + E * lane + e] = from_f<T>(vv[e]);
+  }
+}
+
+template <int DH>
+void fwd_bf16(const CrossArgs& a, bool small, hipStream_t s) {
+  const dim3 grid(grid_of(a));
+  if (a.splits > 1) {
+    if (small) hipLaunchKernelGGL((cross_fwd_kernel<DH, 1, 4, 2, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((cross_fwd_kernel<DH, DH == 64 ? 2 : 1, DH == 64 ? 4 : 8, 4, true>), grid, dim3(DH == 64 ? 256 : 512), 0, s, a);
+  } else {
+    if (small) hipLaunchKernelGGL((cross_fwd_kernel<DH, 1, 4, 2, false>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((cross_fwd_kernel<DH, DH == 64 ? 2 : 1, DH == 64 ? 4 : 8, 4, false>), grid, dim3(DH == 64 ? 256 : 512), 0, s, a);
+  }
+}
+
+template <int DH>
+void dq_bf16(const CrossArgs& a, hipStream_t s) {
+  if (a.splits > 1) hipLaunchKernelGGL((cross_dq_kernel<DH, 8, 2, true>), dim3(grid_of(a)), dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((cross_dq_kernel<DH, 8, 2, false>), dim3(grid_of(a)), dim3(512), 0, s, a);
+}
+
+template <int DH>
+void dkdv_bf16(const CrossArgs& a, hipStream_t s) {
+  if (a.splits > 1) hipLaunchKernelGGL((cross_dkdv_kernel<DH, 8, 2, true>), dim3(grid_of(a)), dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((cross_dkdv_kernel<DH, 8, 2, false>), dim3(grid_of(a)), dim3(512), 0, s, a);
+}
+
+unsigned rows_grid(int64_t rows) { return static_cast<unsigned>((rows + 3) / 4); }
+
+template <typename T>
+void join(const CrossArgs& a, int dh, hipStream_t s) {
+  const dim3 grid(rows_grid(static_cast<int64_t>(a.Tq) * a.G * a.B * a.Hk));
+  if (dh == 64) hipLaunchKernelGGL((cross_join_kernel<T, 64>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((cross_join_kernel<T, 128>), grid, dim3(256), 0, s, a);
+}
+
+template <typename T>
+void sum_dq(const CrossArgs& a, int dh, hipStream_t s) {
+  const dim3 grid(rows_grid(static_cast<int64_t>(a.Tq) * a.G * a.B * a.Hk));
+  if (dh == 64) hipLaunchKernelGGL((cross_sum_dq_kernel<T, 64>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((cross_sum_dq_kernel<T, 128>), grid, dim3(256), 0, s, a);
+}
+
+template <typename T>
+void sum_dkdv(const CrossArgs& a, int dh, hipStream_t s) {
+  const dim3 grid(rows_grid(static_cast<int64_t>(a.Tk) * a.B * a.Hk));
+  if (dh == 64) hipLaunchKernelGGL((cross_sum_dkdv_kernel<T, 64>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((cross_sum_dkdv_kernel<T, 128>), grid, dim3(256), 0, s, a);
+}
+
+// Floats of a ws, in whole 16-byte pieces.
+uint64_t up4(uint64_t n) { return (n + 3) / 4 * 4; }
+
+// Workgroups of a launch: below half of what a dispatch counts (512 threads each).
+bool fits(const Plan& p, int64_t heads) { return static_cast<int64_t>(p.n_x) * p.splits * heads < MAX_WORKGROUPS / 2 - 8; }
+
+}  // namespace
+
+bool cross_attn_ok(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
+  if (B < 0 || Tq < 0 || Tk < 0 || Hq < 1 || Hk < 1 || Hq % Hk || (dh != 64 && dh != 128)) return false;
+  const int64_t G = Hq / Hk, heads = static_cast<int64_t>(B) * Hk;
+  if (G > 1 << 15 || Tq * G > (1ll << 32) / G - 1 || Tq * G >= 1ll << 30 || Tk >= 1 << 30) return false;
+  if (heads >= 1 << 30) return false;
+  // rows of the launches that join ranges, four a workgroup
+  if (heads * Tq * G >= MAX_WORKGROUPS * 4 - 4 || heads * Tk >= MAX_WORKGROUPS * 4 - 4) return false;
+  return fits(fwd_plan(dtype, B, Tq, Tk, Hk, G), heads) && fits(bwd_plan(dtype, Tq * G, heads, Tk), heads) &&
+         fits(bwd_plan(dtype, Tk, heads, Tq * G), heads);
+}
+
+uint64_t cross_attn_fwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
+  const Plan p = fwd_plan(dtype, B, Tq, Tk, Hk, Hq / Hk);
+  if (p.splits == 1) return 0;
+  const uint64_t rows = static_cast<uint64_t>(p.splits) * B * Hq * Tq;
+  return 4 * (rows * dh + up4(2 * rows));
+}
+
+uint64_t cross_attn_bwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
+  const int64_t rows = static_cast<int64_t>(Hq / Hk) * Tq, heads = static_cast<int64_t>(B) * Hk;
+  const Plan q = bwd_plan(dtype, rows, heads, Tk), k = bwd_plan(dtype, Tk, heads, rows);
+  const uint64_t nq = q.splits > 1 ? static_cast<uint64_t>(q.splits) * rows * heads * dh : 0;
+  const uint64_t nk = k.splits > 1 ? 2ull * k.splits * Tk * heads * dh : 0;
+  return 4 * (up4(rows * heads) + std::max(nq, nk));
+}
+
+hipError_t cross_attn_fwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t s) {
+  const Plan p = fwd_plan(dtype, a.B, a.Tq, a.Tk, a.Hk, a.G);
+  a.n_x = p.n_x, a.splits = p.splits;
+  if (a.splits > 1) {
+    a.part = static_cast<float*>(ws);
+    a.ml = a.part + static_cast<uint64_t>(p.splits) * a.B * a.Hq * a.Tq * dh;
+  }
+  hipError_t e;
+  if (dtype == DT_BF16) {
+    if (dh == 64) fwd_bf16<64>(a, p.small, s);
+    else fwd_bf16<128>(a, p.small, s);
+    e = hipGetLastError();
+  } else {
+    e = cross_fwd_f32(a, dh, s);
+  }
+  if (e != hipSuccess || a.splits == 1) return e;
+  if (dtype == DT_BF16) join<bf16_t>(a, dh, s);
+  else join<float>(a, dh, s);
+  return hipGetLastError();
+}
+
+hipError_t cross_attn_bwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t s) {
+  const int64_t rows = static_cast<int64_t>(a.G) * a.Tq, heads = static_cast<int64_t>(a.B) * a.Hk;
+  a.delta = static_cast<float*>(ws);
+  float* part = a.delta + up4(rows * heads);
+  const Plan q = bwd_plan(dtype, rows, heads, a.Tk), k = bwd_plan(dtype, a.Tk, heads, rows);
+  hipError_t e = hipSuccess;
+  // dQ first: it computes D
+  if (rows > 0) {
+    a.n_x = q.n_x, a.splits = a.dq ? q.splits : 1, a.part = part;
+    if (dtype == DT_BF16) {
+      if (dh == 64) dq_bf16<64>(a, s);
+      else dq_bf16<128>(a, s);
+      e = hipGetLastError();
+    } else {
+      e = cross_dq_f32(a, dh, s);
+    }
+    if (e == hipSuccess && a.splits > 1) {
+      if (dtype == DT_BF16) sum_dq<bf16_t>(a, dh, s);
+      else sum_dq<float>(a, dh, s);
+      e = hipGetLastError();
+    }
+  }
+  if (e != hipSuccess || !a.dk || a.Tk == 0) return e;
+  a.n_x = k.n_x, a.splits = k.splits, a.part = part, a.part2 = part + static_cast<uint64_t>(k.splits) * a.Tk * heads * dh;
+  if (dtype == DT_BF16) {
+    if (dh == 64) dkdv_bf16<64>(a, s);
+    else dkdv_bf16<128>(a, s);
+    e = hipGetLastError();
+  } else {
+    e = cross_dkdv_f32(a, dh, s);
+  }
+  if (e != hipSuccess || a.splits == 1) return e;
+  if (dtype == DT_BF16) sum_dkdv<bf16_t>(a, dh, s);
+  else sum_dkdv<float>(a, dh, s);
+  return hipGetLastError();
+}
+
+}  // namespace atom

@@ -1,0 +1,428 @@
+// Cross attention in fp32 (validation mode): the tiles of cross_attention.hip on
+// fp32 matrix instructions.  Workgroups of four waves, 16 rows each; tiles of 64
+// rows in their natural layout, through registers into padded LDS, two stages.
+// A transposed operand is read by elements: a fragment's eight matrix
+// instructions take 256 cycles, its eight LDS reads 16.
+#include "cross_attention.h"
+
+namespace atom {
+namespace cross {
+
+using namespace attn;
+
+template <int DH>
+struct Tile {
+  static constexpr int RP = DH + 4;            // pitch of a row
+  static constexpr int N = BT * DH / 4 / 256;  // 16-byte chunks of a thread
+  float4 r[N];
+  // rows r0 .. of the list that `addr` maps to addresses; behind the last (n
+  // of them, at least one) the last again
+  template <typename F>
+  ATOM_DEV void load(F addr, int r0, int n, int tid) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int id = i * 256 + tid;
+      r[i] = *reinterpret_cast<const float4*>(addr(min(r0 + id / (DH / 4), n - 1)) + id % (DH / 4) * 4);
+    }
+  }
+  ATOM_DEV void store(float* s, int tid) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int id = i * 256 + tid;
+      *reinterpret_cast<float4*>(s + id / (DH / 4) * RP + id % (DH / 4) * 4) = r[i];
+    }
+  }
+  // rows of 32 columns from 32 s on, and column c of the rows that frag_from_pair
+  // gives eight elements
+  static ATOM_DEV void row(Frag<float>& f, const float* s, int r, int col) { frag_load(f, s + r * RP + col); }
+  static ATOM_DEV void col(Frag<float>& f, const float* s, int c, int s2, int lg) {
+    const float* p = s + (32 * s2 + 4 * lg) * RP + c;
+    f.lo = make_float4(p[0], p[RP], p[2 * RP], p[3 * RP]);
+    p += 16 * RP;
+    f.hi = make_float4(p[0], p[RP], p[2 * RP], p[3 * RP]);
+  }
+};
+
+struct Item {
+  int x, split, bh, b, hk;
+  bool on;
+};
+ATOM_DEV Item item(const CrossArgs& a) {
+  const int i = item_of(a.n_x * a.B * a.Hk * a.splits);
+  if (i < 0) return Item{0, 0, 0, 0, 0, false};
+  const int bh = i / (a.n_x * a.splits);
+  return Item{i % a.n_x, i / a.n_x % a.splits, bh, bh / a.Hk, bh % a.Hk, true};
+}
+
+ATOM_DEV void range_of(int n_rows, int splits, int s, int* t0, int* t1) {
+  const int n = (n_rows + BT - 1) / BT, per = (n + splits - 1) / splits;
+  *t0 = min(s * per, n);
+  *t1 = min(s * per + per, n);
+}
+
+template <int DH>
+__global__ void __launch_bounds__(256) cross_fwd_f32_kernel(const CrossArgs a) {
+  using L = Tile<DH>;
+  constexpr int NS = DH / 32, NCT = DH / 16;
+  __shared__ __attribute__((aligned(16))) float Ks[BT * L::RP], Vs[BT * L::RP];
+  const Item it = item(a);
+  if (!it.on) return;
+  const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, it.b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, it.b);
+  const int P = qs.n * a.G, q0 = it.x * 64, hk = it.hk;
+  if (q0 >= P && (a.splits > 1 || a.q_start)) return;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 15, lg = lane >> 4;
+  const int pi = q0 + w * 16 + lr;
+  const float sc = a.scale * LOG2E;
+  const float* kb = static_cast<const float*>(a.k) + ks.row0 * a.ldk + hk * DH;
+  const float* vb = static_cast<const float*>(a.v) + ks.row0 * a.ldv + hk * DH;
+  auto k_at = [&](int j) { return kb + j * a.ldk; };
+  auto v_at = [&](int j) { return vb + j * a.ldv; };
+
+  Frag<float> qf[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    if (pi < P) frag_load(qf[s], static_cast<const float*>(a.q) + at<DH>(a, qs, hk, pi, a.ldq) + 32 * s + 8 * lg);
+    else frag_zero(qf[s]);
+  }
+  f32x4_t acc[NCT];
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m = NO_MAX, l = 0.f;
+
+  int t0 = 0, t1 = 0;
+  if (q0 < P) range_of(ks.n, a.splits, it.split, &t0, &t1);
+  L lk, lv;
+  if (t0 < t1) {
+    lk.load(k_at, t0 * BT, ks.n, tid);
+    lv.load(v_at, t0 * BT, ks.n, tid);
+  }
+  for (int kt = t0; kt < t1; ++kt) {
+    __syncthreads();
+    lk.store(Ks, tid);
+    lv.store(Vs, tid);
+    __syncthreads();
+    if (kt + 1 < t1) {
+      lk.load(k_at, (kt + 1) * BT, ks.n, tid);
+      lv.load(v_at, (kt + 1) * BT, ks.n, tid);
+    }
+    float p[4][4], mx = -INFINITY;
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt) {
+      f32x4_t z = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        Frag<float> kf;
+        L::row(kf, Ks, jt * 16 + lr, 32 * s + 8 * lg);
+        mfma16(z, kf, qf[s]);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[jt][r] = kt * BT + jt * 16 + 4 * lg + r < ks.n ? z[r] : -INFINITY;
+        mx = fmaxf(mx, p[jt][r]);
+      }
+    }
+    const float m_new = fmaxf(m, rows4_max(mx) * sc), alpha = ex2(m - m_new);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int c = 0; c < NCT; ++c) acc[c] *= alpha;
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[jt][r] = ex2(__builtin_fmaf(p[jt][r], sc, -m));
+        l += p[jt][r];
+      }
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      Frag<float> pf;
+      frag_from_pair(pf, p, s2);
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) {
+        Frag<float> vf;
+        L::col(vf, Vs, c * 16 + lr, s2, lg);
+        mfma16(acc[c], vf, pf);
+      }
+    }
+  }
+
+  const float l_tot = rows4_sum(l);
+  const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
+  if (a.splits > 1) {
+    if (pi >= P) return;
+    const int64_t r = (static_cast<int64_t>(it.split) * a.B * a.Hk + it.bh) * n_p + pi;
+#pragma unroll
+    for (int c = 0; c < NCT; ++c) {
+      float v[4] = {acc[c][0], acc[c][1], acc[c][2], acc[c][3]};
+      store_row4<float>(a.part + r * DH + c * 16 + 4 * lg, v);
+    }
+    if (lg == 0) a.ml[2 * r] = m, a.ml[2 * r + 1] = l_tot;
+    return;
+  }
+  if (pi >= (a.q_start ? P : n_p)) return;
+  const bool none = l_tot == 0.f || pi >= P;  // no keys, or padding: zeros
+  const float inv = 1.f / l_tot;
+  float* orow = static_cast<float*>(a.o) + at<DH>(a, qs, hk, pi, a.ldo);
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) {
+    float v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = none ? 0.f : acc[c][r] * inv;
+    store_row4<float>(orow + c * 16 + 4 * lg, v);
+  }
+  if (lg == 0 && a.lse) {
+    const Row rw = row_of(a, pi);
+    a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g] = none ? -INFINITY : (m + log2f(l_tot)) * LN2;
+  }
+}
+
+// dQ, and D of every row (a.dq null: D alone).
+template <int DH>
+__global__ void __launch_bounds__(256) cross_dq_f32_kernel(const CrossArgs a) {
+  using L = Tile<DH>;
+  constexpr int NS = DH / 32, NCT = DH / 16;
+  __shared__ __attribute__((aligned(16))) float Ks[BT * L::RP], Vs[BT * L::RP];
+  const Item it = item(a);
+  if (!it.on) return;
+  const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, it.b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, it.b);
+  const int P = qs.n * a.G, q0 = it.x * 64, hk = it.hk;
+  if (q0 >= P && (a.splits > 1 || a.q_start)) return;
+  const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 15, lg = lane >> 4;
+  const int pi = q0 + w * 16 + lr;
+  const float sc = a.scale * LOG2E;
+  const float* kb = static_cast<const float*>(a.k) + ks.row0 * a.ldk + hk * DH;
+  const float* vb = static_cast<const float*>(a.v) + ks.row0 * a.ldv + hk * DH;
+  auto k_at = [&](int j) { return kb + j * a.ldk; };
+  auto v_at = [&](int j) { return vb + j * a.ldv; };
+
+  Frag<float> qf[NS], of[NS];
+  float lse_i = INFINITY, del = 0.f;
+  if (pi < P) {
+    const Row rw = row_of(a, pi);
+    lse_i = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
+  }
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    frag_zero(qf[s]);
+    frag_zero(of[s]);
+    if (pi < P) {
+      Frag<float> f;
+      frag_load(qf[s], static_cast<const float*>(a.q) + at<DH>(a, qs, hk, pi, a.ldq) + 32 * s + 8 * lg);
+      frag_load(of[s], static_cast<const float*>(a.dout) + at<DH>(a, qs, hk, pi, a.lddo) + 32 * s + 8 * lg);
+      frag_load(f, static_cast<const float*>(a.o) + at<DH>(a, qs, hk, pi, a.ldo) + 32 * s + 8 * lg);
+      del += f.lo.x * of[s].lo.x + f.lo.y * of[s].lo.y + f.lo.z * of[s].lo.z + f.lo.w * of[s].lo.w;
+      del += f.hi.x * of[s].hi.x + f.hi.y * of[s].hi.y + f.hi.z * of[s].hi.z + f.hi.w * of[s].hi.w;
+    }
+  }
+  del = rows4_sum(del);
+  if (lg == 0 && pi < P && it.split == 0) a.delta[it.bh * n_p + pi] = del;
+  if (!a.dq) return;
+  f32x4_t acc[NCT];
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  int t0 = 0, t1 = 0;
+  if (q0 < P) range_of(ks.n, a.splits, it.split, &t0, &t1);
+  L lk, lv;
+  if (t0 < t1) {
+    lk.load(k_at, t0 * BT, ks.n, tid);
+    lv.load(v_at, t0 * BT, ks.n, tid);
+  }
+  for (int kt = t0; kt < t1; ++kt) {
+    __syncthreads();
+    lk.store(Ks, tid);
+    lv.store(Vs, tid);
+    __syncthreads();
+    if (kt + 1 < t1) {
+      lk.load(k_at, (kt + 1) * BT, ks.n, tid);
+      lv.load(v_at, (kt + 1) * BT, ks.n, tid);
+    }
+    float ds[4][4];
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt) {
+      f32x4_t z = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        Frag<float> kf, vf;
+        L::row(kf, Ks, jt * 16 + lr, 32 * s + 8 * lg);
+        L::row(vf, Vs, jt * 16 + lr, 32 * s + 8 * lg);
+        mfma16(z, kf, qf[s]);
+        mfma16(dp, vf, of[s]);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        ds[jt][r] = kt * BT + jt * 16 + 4 * lg + r < ks.n ? ex2(__builtin_fmaf(z[r], sc, -lse_i)) * (dp[r] - del) : 0.f;
+    }
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      Frag<float> df;
+      frag_from_pair(df, ds, s2);
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) {
+        Frag<float> kf;
+        L::col(kf, Ks, c * 16 + lr, s2, lg);
+        mfma16(acc[c], kf, df);
+      }
+    }
+  }
+  float* row;
+  float f = a.scale;
+  if (a.splits > 1) {
+    if (pi >= P) return;
+    row = a.part + ((static_cast<int64_t>(it.split) * a.B * a.Hk + it.bh) * n_p + pi) * DH;
+    f = 1.f;
+  } else {
+    if (pi >= (a.q_start ? P : n_p)) return;
+    row = static_cast<float*>(a.dq) + at<DH>(a, qs, hk, pi, a.lddq);
+  }
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) {
+    float v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = pi < P ? acc[c][r] * f : 0.f;  // (padding: zeros)
+    store_row4<float>(row + c * 16 + 4 * lg, v);
+  }
+}
+
+template <int DH>
+__global__ void __launch_bounds__(256) cross_dkdv_f32_kernel(const CrossArgs a) {
+  using L = Tile<DH>;
+  constexpr int NS = DH / 32, NCT = DH / 16;
+  __shared__ __attribute__((aligned(16))) float Qs[BT * L::RP], Os[BT * L::RP];
+  __shared__ float lse_s[BT], del_s[BT];
+  const Item it = item(a);
+  if (!it.on) return;
+  const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, it.b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, it.b);
+  const int P = qs.n * a.G, k0 = it.x * 64, hk = it.hk;
+  if (k0 >= ks.n && (a.splits > 1 || a.k_start)) return;
+  const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 15, lg = lane >> 4;
+  const int kj = k0 + w * 16 + lr;
+  const float sc = a.scale * LOG2E;
+  auto q_at = [&](int p) { return static_cast<const float*>(a.q) + at<DH>(a, qs, hk, p, a.ldq); };
+  auto o_at = [&](int p) { return static_cast<const float*>(a.dout) + at<DH>(a, qs, hk, p, a.lddo); };
+
+  Frag<float> kf[NS], vf[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    frag_zero(kf[s]);
+    frag_zero(vf[s]);
+    if (kj < ks.n) {
+      frag_load(kf[s], static_cast<const float*>(a.k) + (ks.row0 + kj) * a.ldk + hk * DH + 32 * s + 8 * lg);
+      frag_load(vf[s], static_cast<const float*>(a.v) + (ks.row0 + kj) * a.ldv + hk * DH + 32 * s + 8 * lg);
+    }
+  }
+  f32x4_t acc_k[NCT], acc_v[NCT];
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) acc_k[c] = acc_v[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  int t0 = 0, t1 = 0;
+  if (k0 < ks.n) range_of(P, a.splits, it.split, &t0, &t1);
+  L lq, lo;
+  float pre_lse = 0.f, pre_del = 0.f;
+  auto fetch = [&](int t) {
+    lq.load(q_at, t * BT, P, tid);
+    lo.load(o_at, t * BT, P, tid);
+    if (tid < BT) {
+      const int i = t * BT + tid;
+      pre_lse = INFINITY;
+      pre_del = 0.f;
+      if (i < P) {
+        const Row rw = row_of(a, i);
+        pre_lse = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
+        pre_del = a.delta[it.bh * n_p + i];
+      }
+    }
+  };
+  if (t0 < t1) fetch(t0);
+  for (int t = t0; t < t1; ++t) {
+    __syncthreads();
+    lq.store(Qs, tid);
+    lo.store(Os, tid);
+    if (tid < BT) lse_s[tid] = pre_lse, del_s[tid] = pre_del;
+    __syncthreads();
+    if (t + 1 < t1) fetch(t + 1);
+    float p[4][4], ds[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f32x4_t z = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        Frag<float> qf, of;
+        L::row(qf, Qs, i * 16 + lr, 32 * s + 8 * lg);
+        L::row(of, Os, i * 16 + lr, 32 * s + 8 * lg);
+        mfma16(z, qf, kf[s]);
+        mfma16(dp, of, vf[s]);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int il = i * 16 + 4 * lg + r;
+        p[i][r] = ex2(__builtin_fmaf(z[r], sc, -lse_s[il]));
+        ds[i][r] = p[i][r] * (dp[r] - del_s[il]);
+      }
+    }
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      Frag<float> pf, df;
+      frag_from_pair(pf, p, s2);
+      frag_from_pair(df, ds, s2);
+#pragma unroll
+      for (int c = 0; c < NCT; ++c) {
+        Frag<float> of, qf;
+        L::col(of, Os, c * 16 + lr, s2, lg);
+        L::col(qf, Qs, c * 16 + lr, s2, lg);
+        mfma16(acc_v[c], of, pf);
+        mfma16(acc_k[c], qf, df);
+      }
+    }
+  }
+  float *rk, *rv;
+  if (a.splits > 1) {
+    if (kj >= ks.n) return;
+    const int64_t r = (static_cast<int64_t>(it.split) * a.B * a.Hk + it.bh) * a.Tk + kj;
+    rk = a.part + r * DH;
+    rv = a.part2 + r * DH;
+  } else {
+    if (kj >= (a.k_start ? ks.n : a.Tk)) return;
+    rk = static_cast<float*>(a.dk) + (ks.row0 + kj) * a.lddk + hk * DH;
+    rv = static_cast<float*>(a.dv) + (ks.row0 + kj) * a.lddv + hk * DH;
+  }
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) {
+    float vk[4], vv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      vk[i] = kj < ks.n ? acc_k[c][i] * a.scale : 0.f;  // (padding: zeros)
+      vv[i] = kj < ks.n ? acc_v[c][i] : 0.f;
+    }
+    store_row4<float>(rk + c * 16 + 4 * lg, vk);
+    store_row4<float>(rv + c * 16 + 4 * lg, vv);
+  }
+}
+
+}  // namespace cross
+
+namespace {
+dim3 grid_of(const CrossArgs& a) {
+  return dim3(static_cast<unsigned>((static_cast<int64_t>(a.n_x) * a.splits * a.B * a.Hk + 7) / 8 * 8));
+}
+}  // namespace
+
+hipError_t cross_fwd_f32(const CrossArgs& a, int dh, hipStream_t s) {
+  if (dh == 64) hipLaunchKernelGGL(cross::cross_fwd_f32_kernel<64>, grid_of(a), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cross::cross_fwd_f32_kernel<128>, grid_of(a), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t cross_dq_f32(const CrossArgs& a, int dh, hipStream_t s) {
+  if (dh == 64) hipLaunchKernelGGL(cross::cross_dq_f32_kernel<64>, grid_of(a), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cross::cross_dq_f32_kernel<128>, grid_of(a), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t cross_dkdv_f32(const CrossArgs& a, int dh, hipStream_t s) {
+  if (dh == 64) hipLaunchKernelGGL(cross::cross_dkdv_f32_kernel<64>, grid_of(a), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cross::cross_dkdv_f32_kernel<128>, grid_of(a), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace atom

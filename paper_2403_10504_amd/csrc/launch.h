@@ -250,6 +250,29 @@ hipError_t attn_fwd(int dtype, const void* qkv, void* o, float* lse, int B, int 
 hipError_t attn_bwd(int dtype, const void* qkv, const void* o, const void* dout, const float* lse, float* delta,
                     void* dqkv, int B, int T, int H, int dh, hipStream_t s);
 
+// Cross attention (atom_k_cross_attn_*).  The launchers fill the fields from n_x on.
+struct CrossArgs {
+  const void *q, *k, *v, *dout;
+  void *o, *dq, *dk, *dv;
+  float *lse, *delta;  // [row][Hq]; [B * Hk][Tq G] of the workspace
+  int64_t ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv;
+  int64_t q_rows, k_rows;
+  const int32_t *q_start, *q_len, *k_start, *k_len;
+  int B, Tq, Tk, Hq, Hk, G;
+  uint32_t gmul;  // ceil(2^32 / G): p / G is the high word of p gmul
+  float scale;
+  int n_x, splits;  // blocks of rows of a sequence and head, ranges of its other side
+  float *part, *part2;  // ranges' sums: [splits][B * Hk][rows][dh] (dK and dV: two)
+  float* ml;            // forward: the ranges' maxima and sums, [splits][B * Hk][Tq G][2]
+};
+
+// Whether the sizes are taken, by the forward and the backward alike.
+bool cross_attn_ok(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh);
+uint64_t cross_attn_fwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh);
+hipError_t cross_attn_fwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t s);
+uint64_t cross_attn_bwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh);
+hipError_t cross_attn_bwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t s);
+
 // Rotary positions and the norms of queries and keys (atom_k_rope,
 // atom_k_qknorm_rope_*).  back: the transposed turn.
 hipError_t rope(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const int32_t* pos, const double* freq,

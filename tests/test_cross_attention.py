@@ -1,0 +1,545 @@
+"""Cross attention (atom_k_cross_attn_*) against its formulas in 64 bits.
+
+Bounds, u = 2^-24, of absolute sums of the terms that a result adds:
+  z      a product of dh terms: dh u of sum |q||k|, times the scale, and its rounding;
+  p      exp in base 2 of z - max or z - lse: the error of z, 4 u (|z| + |max|) for the exponent's sum and product,
+         2^-21 for the function; relative
+  o      twice p's (above and below the bar), n u for sums of n keys; bf16 rounds p to half a step, 2^-8
+  D, dp  dh u of their terms' absolute sums
+  ds     p (p's error |dp - D| + D's and dp's), 2 u; bf16 rounds it: 2^-8
+  dq, dk, dv  what their factors p and ds are off, and n u for their sums
+and every result's own rounding: half a step of its type."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_2403_10504_amd import atom as A
+from tests import gpu_util as U
+
+u = 2.0 ** -24
+HALF = {"bf16": 2.0 ** -8, "f32": u}
+FILL = 77.0
+
+
+def _type(dtype):
+    t = U.torch()
+    return t.bfloat16 if dtype == "bf16" else t.float32
+
+
+class Case:
+    """Inputs with NaN in every row that no sequence has, and the sequences' rows."""
+
+    def __init__(self, dtype, B, Tq, Tk, Hq, Hk, dh, rows="full", seed=0, pad=0, q_len=None, k_len=None, size=1.5):
+        t = U.torch()
+        g = t.Generator(device="cuda").manual_seed(seed)
+        r = np.random.default_rng(seed)
+        self.__dict__.update(dtype=dtype, B=B, Tq=Tq, Tk=Tk, Hq=Hq, Hk=Hk, dh=dh, rows=rows)
+        self.scale = float(np.float32(dh ** -0.5))
+
+        def side(T, given, lo):
+            if rows == "full":
+                n = [T] * B
+            else:
+                n = list(given) if given is not None else [T] + [int(v) for v in r.integers(lo, T + 1, B - 1)]
+            if rows != "packed":
+                return n, [b * T for b in range(B)], B * T
+            start = [3]
+            for v in n[:-1]:
+                start.append(start[-1] + v + 2)
+            return n, start, start[-1] + n[-1] + 4
+
+        self.qn, self.qs, self.nq = side(Tq, q_len, 0)
+        self.kn, self.ks, self.nk = side(Tk, k_len, 0)
+        i32 = lambda v: t.tensor(v, device="cuda", dtype=t.int32)  # noqa: E731
+        self.idx = dict(q_start=i32(self.qs), q_len=i32(self.qn), k_start=i32(self.ks), k_len=i32(self.kn))
+
+        def rows_of(n, H, starts, lens, scale):
+            x = t.full((n + 1, H * dh + pad), float("nan"), device="cuda", dtype=_type(dtype))
+            for s, m in zip(starts, lens):
+                x[s:s + m, :H * dh] = t.randn(m, H * dh, device="cuda", generator=g) * scale
+            return x
+
+        self.q = rows_of(self.nq, Hq, self.qs, self.qn, size)
+        self.k = rows_of(self.nk, Hk, self.ks, self.kn, 1.0)
+        self.v = rows_of(self.nk, Hk, self.ks, self.kn, 1.0)
+        self.dout = rows_of(self.nq, Hq, self.qs, self.qn, 0.1)
+        self.pad = pad
+        ptr = {k: v.data_ptr() for k, v in self.idx.items()}
+        if rows != "packed":
+            ptr.update(q_start=None, k_start=None)
+        if rows == "full":
+            ptr.update(q_len=None, k_len=None)
+        self.shape = A.atom_cross_shape(B, Tq, Tk, Hq, Hk, dh, self.nq, self.nk, **ptr)
+
+    def empty(self, like):
+        return U.torch().full_like(like, FILL)
+
+    def ws(self, query):
+        t = U.torch()
+        n = query(U.dt_code(self.dtype), self.shape)
+        return t.full((n + 64,), 0xA5, device="cuda", dtype=t.uint8), n
+
+    def fwd(self, o, lse, stream=None, ws=None):
+        buf, n = ws or self.ws(A.atom_k_cross_attn_fwd_ws_bytes)
+        A.atom_k_cross_attn_fwd(U.dt_code(self.dtype), self.shape, self.q.data_ptr(), self.q.stride(0), self.k.data_ptr(),
+                                self.k.stride(0), self.v.data_ptr(), self.v.stride(0), self.scale, o.data_ptr(), o.stride(0),
+                                None if lse is None else lse.data_ptr(), buf.data_ptr(), n, stream)
+        assert (buf[n:] == 0xA5).all() if stream is None else True
+
+    def bwd(self, o, lse, dq, dk, dv, stream=None, ws=None):
+        buf, n = ws or self.ws(A.atom_k_cross_attn_bwd_ws_bytes)
+        p = lambda x: (None, 0) if x is None else (x.data_ptr(), x.stride(0))  # noqa: E731
+        A.atom_k_cross_attn_bwd(U.dt_code(self.dtype), self.shape, *p(self.q), *p(self.k), *p(self.v), self.scale, *p(o),
+                                *p(self.dout), lse.data_ptr(), *p(dq), *p(dk), *p(dv), buf.data_ptr(), n, stream)
+        assert (buf[n:] == 0xA5).all() if stream is None else True
+
+    def sequences(self):
+        """Per sequence: rows of queries and keys, and q, k, v, dout in 64 bits as [H][n][dh], k and v repeated."""
+        G = self.Hq // self.Hk
+        for b in range(self.B):
+            qr, kr = slice(self.qs[b], self.qs[b] + self.qn[b]), slice(self.ks[b], self.ks[b] + self.kn[b])
+
+            def heads(x, r, H, share):
+                y = x[r, :H * self.dh].double().view(-1, H, self.dh).transpose(0, 1).contiguous()
+                return y.repeat_interleave(share, 0)
+
+            yield (qr, kr, heads(self.q, qr, self.Hq, 1), heads(self.k, kr, self.Hk, G), heads(self.v, kr, self.Hk, G),
+                   heads(self.dout, qr, self.Hq, 1))
+
+    def covered(self, n, starts, lens):
+        t = U.torch()
+        on = t.zeros(n + 1, device="cuda", dtype=t.bool)
+        for s, m in zip(starts, lens):
+            on[s:s + m] = True
+        return on
+
+    def outside(self, x, side, width):
+        """What no sequence has stays, or is zeros in a padded batch; columns and the row behind the end stay."""
+        n, starts, lens = (self.nq, self.qs, self.qn) if side == "q" else (self.nk, self.ks, self.kn)
+        on = self.covered(n, starts, lens)
+        on[n] = False
+        rest = x[~on][:, :width]
+        keep = FILL
+        if self.rows != "packed":
+            assert bool((rest[:-1] == 0).all())
+            rest = rest[-1:]
+        assert bool((rest == keep).all()) and bool((x[:, width:] == keep).all())
+
+
+def _scores(c, q, k):
+    """z and its error's bound, [H][nq][nk]."""
+    z = c.scale * (q @ k.transpose(1, 2).contiguous())
+    terms = c.scale * (q.abs() @ k.abs().transpose(1, 2).contiguous())
+    return z, (c.dh + 4) * u * terms
+
+
+def _within(got, ref, bound, dtype):
+    slack = (got.double() - ref).abs() - (bound + (ref.abs() + bound) * HALF[dtype] + 2.0 ** -126)
+    assert bool(U.torch().isfinite(got.double()).all())
+    if slack.numel():
+        assert slack.max().item() <= 0.0, slack.max().item()
+
+
+def _flat(x):
+    return x.transpose(0, 1).flatten(1)
+
+
+def _check_fwd(c, o, lse):
+    t = U.torch()
+    for qr, kr, q, k, v, _ in c.sequences():
+        if k.shape[1] == 0:
+            assert bool((o[qr, :c.Hq * c.dh] == 0).all()) and (lse is None or bool((lse[qr] == -math.inf).all()))
+            continue
+        z, ez = _scores(c, q, k)
+        m = z.max(2, keepdim=True).values
+        p = t.exp(z - m)
+        s = p.sum(2, keepdim=True)
+        e = (ez + 4 * u * (z.abs() + m.abs()) + 2.0 ** -21).max(2, keepdim=True).values
+        n = k.shape[1]
+        absv = (p / s) @ v.abs()
+        bound = (2 * e + (n + 64) * u + (2.0 ** -8 if c.dtype == "bf16" else 0.0)) * absv
+        _within(o[qr, :c.Hq * c.dh], _flat((p / s) @ v), _flat(bound), c.dtype)
+        if lse is not None:
+            ref = (m + t.log(s)).squeeze(2)
+            _within(lse[qr], ref.T, (e.squeeze(2) + (n + 64) * u + 4 * u * ref.abs()).T, "f32")
+    if o.shape[0] == c.nq + 1:
+        c.outside(o, "q", c.Hq * c.dh)
+
+
+# B, Tq, Tk, Hq, Hk, dh, rows, pad
+SHAPES = [
+    (1, 1, 1, 1, 1, 64, "full", 0), (1, 1, 1, 1, 1, 128, "full", 0), (2, 1, 77, 4, 4, 128, "padded", 8),
+    (3, 1, 300, 8, 1, 64, "packed", 0), (2, 5, 64, 6, 2, 128, "full", 8), (1, 64, 63, 3, 3, 64, "full", 16),
+    (1, 65, 65, 2, 2, 128, "full", 0), (5, 33, 130, 5, 5, 64, "padded", 0), (4, 130, 129, 6, 2, 128, "packed", 8),
+    (4, 129, 1000, 4, 4, 64, "padded", 0), (1, 3, 4100, 4, 2, 128, "full", 0), (2, 500, 17, 40, 5, 64, "packed", 0),
+    (9, 200, 200, 16, 16, 128, "padded", 0), (12, 150, 90, 24, 24, 64, "packed", 8), (1, 700, 3, 1, 1, 128, "full", 0),
+    (2, 1024, 260, 16, 4, 64, "full", 0), (2, 300, 700, 40, 40, 128, "full", 0)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh,rows,pad", SHAPES)
+def test_forward(dtype, B, Tq, Tk, Hq, Hk, dh, rows, pad):
+    t = U.torch()
+    c = Case(dtype, B, Tq, Tk, Hq, Hk, dh, rows, seed=B * 7 + Tq + Tk, pad=pad)
+    o, lse = c.empty(c.q), t.full((c.nq + 1, Hq), FILL, device="cuda")
+    c.fwd(o, lse)
+    _check_fwd(c, o, lse)
+    on = c.covered(c.nq, c.qs, c.qn)[:c.nq]
+    assert bool((lse[:c.nq][~on] == (FILL if rows == "packed" else -math.inf)).all()) and bool((lse[c.nq] == FILL).all())
+    # without lse; again: the same bits
+    o2 = c.empty(c.q)
+    c.fwd(o2, None)
+    assert t.equal(o, o2)
+
+
+def _gradients(c, o, lse):
+    """Per sequence (qr, kr, dq, dk, dv and their bounds) from the given o and lse."""
+    t = U.torch()
+    r = 2.0 ** -8 if c.dtype == "bf16" else 0.0
+    G = c.Hq // c.Hk
+    for qr, kr, q, k, v, do in c.sequences():
+        nq, nk = q.shape[1], k.shape[1]
+        oo = o[qr, :c.Hq * c.dh].double().view(nq, c.Hq, c.dh).transpose(0, 1)
+        l = lse[qr].double().T.unsqueeze(2)
+        z, ez = _scores(c, q, k)
+        p = t.exp(z - l) if nk else z
+        ep = p * (ez + 4 * u * (z.abs() + l.abs()) + 2.0 ** -21) if nk else z
+        vt = v.transpose(1, 2).contiguous()
+        D = (do * oo).sum(2, keepdim=True)
+        eD = (c.dh + 4) * u * (do * oo).abs().sum(2, keepdim=True)
+        dp, edp = do @ vt, (c.dh + 4) * u * (do.abs() @ vt.abs())
+        ds = p * (dp - D)
+        eds = ep * (dp - D).abs() + p * (eD + edp + 2 * u * (dp - D).abs())
+        wds, wp = eds + r * (ds.abs() + eds), ep + r * (p + ep)
+        tr = lambda x: x.transpose(1, 2).contiguous()  # noqa: E731
+        sq, sk = (nk + 64) * u, (nq * G + 64) * u
+        dq, eq = c.scale * (ds @ k), c.scale * ((wds + sq * ds.abs()) @ k.abs())
+        dk, ek = c.scale * (tr(ds) @ q), c.scale * (tr(wds + sk * ds.abs()) @ q.abs())
+        dv, ev = tr(p) @ do, tr(wp + sk * p) @ do.abs()
+        fold = lambda x: _flat(x.view(c.Hk, G, nk, c.dh).sum(1))  # noqa: E731
+        yield qr, kr, (_flat(dq), _flat(eq)), (fold(dk), fold(ek)), (fold(dv), fold(ev))
+
+
+def _reference_fwd(c):
+    """o and lse in 64 bits, rounded to their types; NaN where no sequence is."""
+    t = U.torch()
+    o, lse = t.full_like(c.q, float("nan")), t.full((c.nq + 1, c.Hq), float("nan"), device="cuda")
+    for qr, kr, q, k, v, _ in c.sequences():
+        if k.shape[1] == 0:
+            o[qr, :c.Hq * c.dh], lse[qr] = 0.0, -math.inf
+            continue
+        z, _ = _scores(c, q, k)
+        o[qr, :c.Hq * c.dh] = _flat(t.softmax(z, 2) @ v).to(o.dtype)
+        lse[qr] = t.logsumexp(z, 2).T.float()
+    return o, lse
+
+
+def _check_bwd(c, o, lse, dq, dk, dv):
+    for qr, kr, q, k, v in _gradients(c, o, lse):
+        if dq is not None:
+            _within(dq[qr, :c.Hq * c.dh], *q, c.dtype)
+        if dk is not None:
+            _within(dk[kr, :c.Hk * c.dh], *k, c.dtype)
+            _within(dv[kr, :c.Hk * c.dh], *v, c.dtype)
+    if dq is not None:
+        c.outside(dq, "q", c.Hq * c.dh)
+    if dk is not None:
+        c.outside(dk, "k", c.Hk * c.dh)
+        c.outside(dv, "k", c.Hk * c.dh)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh,rows,pad", SHAPES)
+def test_backward(dtype, B, Tq, Tk, Hq, Hk, dh, rows, pad):
+    t = U.torch()
+    c = Case(dtype, B, Tq, Tk, Hq, Hk, dh, rows, seed=B * 11 + Tq + Tk, pad=pad)
+    o, lse = _reference_fwd(c)
+    dq, dk, dv = c.empty(c.q), c.empty(c.k), c.empty(c.v)
+    c.bwd(o, lse, dq, dk, dv)
+    _check_bwd(c, o, lse, dq, dk, dv)
+    # one side alone: the same bits
+    q2, k2, v2 = c.empty(c.q), c.empty(c.k), c.empty(c.v)
+    c.bwd(o, lse, q2, None, None)
+    c.bwd(o, lse, None, k2, v2)
+    assert t.equal(q2, dq) and t.equal(k2, dk) and t.equal(v2, dv)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", ["padded", "packed"])
+@pytest.mark.parametrize("q_len,k_len", [([0, 9, 40], [50, 0, 1]), ([40, 0, 0], [0, 0, 50]), ([0, 0, 0], [5, 6, 7]),
+                                         ([1, 40, 17], [0, 0, 0])])
+def test_empty_sequences(dtype, rows, q_len, k_len):
+    t = U.torch()
+    c = Case(dtype, 3, 40, 50, 4, 2, 64, rows, seed=5, q_len=q_len, k_len=k_len)
+    o, lse = c.empty(c.q), t.full((c.nq + 1, 4), FILL, device="cuda")
+    c.fwd(o, lse)
+    _check_fwd(c, o, lse)
+    dq, dk, dv = c.empty(c.q), c.empty(c.k), c.empty(c.v)
+    c.bwd(o, lse, dq, dk, dv)
+    for b in range(3):
+        qr, kr = slice(c.qs[b], c.qs[b] + c.qn[b]), slice(c.ks[b], c.ks[b] + c.kn[b])
+        if c.kn[b] == 0:
+            assert bool((dq[qr] == 0).all())
+        if c.qn[b] == 0:
+            assert bool((dk[kr] == 0).all()) and bool((dv[kr] == 0).all())
+    for x, s in ((dq, "q"), (dk, "k"), (dv, "k")):
+        c.outside(x, s, x.shape[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_queries_or_keys(dtype):
+    """Lengths of zero by the shape: nothing to do, or zeros."""
+    t = U.torch()
+    c = Case(dtype, 2, 30, 20, 2, 2, 64, seed=6)
+    o, lse = c.empty(c.q), t.full((c.nq + 1, 2), FILL, device="cuda")
+    c.shape.Tk = 0
+    c.fwd(o, lse)
+    assert bool((o[:c.nq] == 0).all()) and bool((lse[:c.nq] == -math.inf).all())
+    dq = c.empty(c.q)
+    c.bwd(o, lse, dq, None, None)
+    assert bool((dq[:c.nq] == 0).all())
+    c.shape.Tk, c.shape.Tq = 20, 0
+    dk, dv, o2 = c.empty(c.k), c.empty(c.v), c.empty(c.q)
+    c.fwd(o2, None)
+    c.bwd(o, lse, None, dk, dv)
+    assert bool((o2 == FILL).all()) and bool((dk[:c.nk] == 0).all()) and bool((dv[:c.nk] == 0).all())
+    c.shape.B = 0
+    c.fwd(o2, None)
+    assert bool((o2 == FILL).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lengths_and_starts_are_clamped(dtype):
+    """Starts outside the rows make a sequence empty, lengths are cut to T and to the rows that there are."""
+    t = U.torch()
+    c = Case(dtype, 4, 20, 30, 2, 1, 64, "packed", seed=7, q_len=[20, 20, 20, 20], k_len=[30, 30, 30, 30])
+    good_o, good_lse = c.empty(c.q), t.full((c.nq + 1, 2), FILL, device="cuda")
+    c.fwd(good_o, good_lse)
+    for bad in (-1, -2 ** 31, c.nk, c.nk + 1, 2 ** 31 - 1):
+        c.idx["k_start"].copy_(t.tensor(c.ks, dtype=t.int32))
+        c.idx["k_start"][1] = bad
+        o, lse = c.empty(c.q), t.full((c.nq + 1, 2), FILL, device="cuda")
+        c.fwd(o, lse)
+        r = slice(c.qs[1], c.qs[1] + 20)
+        assert bool((o[r] == 0).all()) and bool((lse[r] == -math.inf).all())
+        o[r], lse[r] = good_o[r], good_lse[r]
+        assert t.equal(o, good_o) and t.equal(lse, good_lse)
+    c.idx["k_start"].copy_(t.tensor(c.ks, dtype=t.int32))
+    c.idx["k_len"].copy_(t.tensor([30, 31, 2 ** 31 - 1, 30], dtype=t.int32))
+    o, lse = c.empty(c.q), t.full((c.nq + 1, 2), FILL, device="cuda")
+    c.fwd(o, lse)
+    assert t.equal(o, good_o) and t.equal(lse, good_lse)
+    # a sequence of queries that would run over the end
+    c.shape.q_rows = c.qs[3] + 5
+    o = c.empty(c.q)
+    c.fwd(o, None)
+    assert bool((o[c.qs[3] + 5:] == FILL).all()) and t.equal(o[:c.qs[3] + 5], good_o[:c.qs[3] + 5])
+    c.idx["q_len"][:] = -5
+    o = c.empty(c.q)
+    c.fwd(o, None)
+    assert bool((o == FILL).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sequences_that_share_keys(dtype):
+    """Several continuations of one encoder sequence read its states once each, from the same rows."""
+    t = U.torch()
+    c = Case(dtype, 3, 1, 200, 4, 2, 128, "packed", seed=8, q_len=[1, 1, 1], k_len=[200, 200, 200])
+    c.ks = [c.ks[0]] * 3
+    c.idx["k_start"].fill_(c.ks[0])
+    o, lse = c.empty(c.q), t.full((c.nq + 1, 4), FILL, device="cuda")
+    c.fwd(o, lse)
+    _check_fwd(c, o, lse)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_and_infinite_scores(dtype):
+    t = U.torch()
+    # scores of +-2000: one key has all the weight, and lse is its score
+    c = Case(dtype, 1, 40, 130, 2, 2, 64, seed=9, size=400.0)
+    o, lse = c.empty(c.q), t.empty(c.nq + 1, 2, device="cuda").fill_(FILL)
+    c.fwd(o, lse)
+    for qr, kr, q, k, v, _ in c.sequences():
+        z, ez = _scores(c, q, k)
+        ref = t.logsumexp(z, 2)
+        assert ((lse[qr].double().T - ref).abs() <= ez.max(2).values + 8 * u * z.abs().max(2).values + 1e-4).all()
+    # keys at -infinity weigh nothing, in the first tile of 64 and alone; keys of NaN spoil every row of theirs
+    c = Case(dtype, 2, 20, 130, 2, 2, 64, seed=10)
+    c.q[:, :] = c.q.abs()
+    c.k[0:70, :64] = -math.inf  # sequence 0, head 0
+    o, lse = c.empty(c.q), t.empty(c.nq + 1, 2, device="cuda").fill_(FILL)
+    c.fwd(o, lse)
+    d = Case(dtype, 2, 20, 130, 2, 2, 64, seed=10)
+    d.q[:, :] = d.q.abs()
+    short = Case(dtype, 2, 20, 60, 2, 2, 64, seed=10)
+    short.q, short.k, short.v = d.q, t.cat([d.k[70:130], d.k[130:190]]), t.cat([d.v[70:130], d.v[130:190]])
+    o2, lse2 = c.empty(c.q), t.empty(c.nq + 1, 2, device="cuda").fill_(FILL)
+    short.fwd(o2, lse2)
+    tol = 2.0 ** -6 if dtype == "bf16" else 2.0 ** -17  # the same terms in other tiles: p's roundings, twice
+    assert (o[:20, :64].float() - o2[:20, :64].float()).abs().max() <= tol * 4
+    assert (lse[:20, 0] - lse2[:20, 0]).abs().max() <= 2.0 ** -18 * lse2[:20, 0].abs().max()
+    c.k[0:130, :64] = -math.inf
+    c.k[130 + 100, 64 + 3] = float("nan")
+    c.fwd(o, lse)
+    assert bool((o[:20, :64] == 0).all()) and bool((lse[:20, 0] == -math.inf).all())
+    assert bool(o[20:40, 64:].isnan().all()) and bool(o[20:40, :64].isfinite().all()) and bool(o[:20, 64:].isfinite().all())
+    dq, dk, dv = c.empty(c.q), c.empty(c.k), c.empty(c.v)
+    c.bwd(o, lse, dq, dk, dv)
+    assert bool((dv[:130, :64] == 0).all())  # no weight: no gradient
+    assert bool(dv[:130, 64:].isfinite().all()) and bool(dv[130:260, :64].isfinite().all())
+
+
+@pytest.mark.gpu
+def test_gradient_against_differences():
+    """<grad, e> against the central difference of <dout, o> along e, o in 64 bits (errors h^2 and 2^-52 / h), on fp32
+    gradients (2^-18 of the terms, by the bounds of the file's head at these sizes)."""
+    t = U.torch()
+    c = Case("f32", 2, 7, 9, 4, 2, 64, "padded", seed=12, k_len=[9, 4], q_len=[7, 5])
+    o, lse = _reference_fwd(c)
+    dq, dk, dv = c.empty(c.q), c.empty(c.k), c.empty(c.v)
+    c.bwd(o, lse, dq, dk, dv)
+
+    def value(**move):
+        total = 0.0
+        for b, (qr, kr, q, k, v, do) in enumerate(c.sequences()):
+            G = c.Hq // c.Hk
+
+            def add(x, name, r, H, share):
+                if name not in move:
+                    return x
+                e = move[name][r].view(-1, H, c.dh).transpose(0, 1)
+                return x + e.repeat_interleave(share, 0)
+
+            q, k, v = add(q, "q", qr, c.Hq, 1), add(k, "k", kr, c.Hk, G), add(v, "v", kr, c.Hk, G)
+            total += (t.softmax(c.scale * (q @ k.transpose(1, 2).contiguous()), 2) @ v * do).sum().item()
+        return total
+
+    h = 1e-4
+    g = t.Generator(device="cuda").manual_seed(1)
+    for name, grad, H in (("q", dq, c.Hq), ("k", dk, c.Hk), ("v", dv, c.Hk)):
+        e = t.randn(grad.shape[0], H * c.dh, device="cuda", generator=g, dtype=t.float64)
+        e[c.covered(*((c.nq, c.qs, c.qn) if name == "q" else (c.nk, c.ks, c.kn))).logical_not()] = 0.0
+        diff = (value(**{name: h * e}) - value(**{name: -h * e})) / (2 * h)
+        terms = grad.double() * e
+        assert abs(diff - terms.sum().item()) <= terms.abs().sum().item() * (2.0 ** -16 + 1e-6)
+
+
+@pytest.mark.gpu
+def test_streams_graphs_and_repeats():
+    """Two streams at once, and captured calls replayed on new inputs and lengths, give the bits of each alone."""
+    t = U.torch()
+    cases = [Case("bf16", 2, 3, 900, 8, 2, 128, "padded", seed=20), Case("bf16", 3, 140, 90, 4, 4, 64, "packed", seed=21)]
+
+    def buffers(c):
+        return dict(o=c.empty(c.q), lse=t.full((c.nq + 1, c.Hq), FILL, device="cuda"), dq=c.empty(c.q), dk=c.empty(c.k),
+                    dv=c.empty(c.v), fws=c.ws(A.atom_k_cross_attn_fwd_ws_bytes), bws=c.ws(A.atom_k_cross_attn_bwd_ws_bytes))
+
+    def both(c, b, stream):
+        c.fwd(b["o"], b["lse"], stream, b["fws"])
+        c.bwd(b["o"], b["lse"], b["dq"], b["dk"], b["dv"], stream, b["bws"])
+
+    same = lambda a, b: all(t.equal(a[k], b[k]) for k in ("o", "lse", "dq", "dk", "dv"))  # noqa: E731
+    alone, at_once = [buffers(c) for c in cases], [buffers(c) for c in cases]
+    for c, b in zip(cases, alone):
+        both(c, b, None)
+    t.cuda.synchronize()
+    streams = [t.cuda.Stream(), t.cuda.Stream()]
+    for _ in range(3):
+        for c, b, s in zip(cases, at_once, streams):
+            both(c, b, s.cuda_stream)
+    t.cuda.synchronize()
+    assert all(same(a, b) for a, b in zip(alone, at_once))
+    for c in cases:
+        g, s, b, eager = t.cuda.CUDAGraph(), t.cuda.Stream(), buffers(c), buffers(c)
+        s.wait_stream(t.cuda.current_stream())
+        with t.cuda.graph(g, stream=s):
+            both(c, b, t.cuda.current_stream().cuda_stream)
+        for i in range(3):
+            c.q.mul_(-0.5)
+            c.idx["k_len"].sub_(c.idx["k_len"] // 3)  # (the rows behind hold finite values)
+            for x in (b, eager):
+                for k in ("o", "dq", "dk", "dv", "lse"):
+                    x[k].fill_(FILL)
+            both(c, eager, None)
+            g.replay()
+            t.cuda.synchronize()
+            assert same(eager, b)
+
+
+@pytest.mark.gpu
+def test_far_rows():
+    """Offsets beyond 32 bits: rows of keys and values 2^22 elements apart, the last ones behind 2^32."""
+    t = U.torch()
+    near = Case("bf16", 1, 70, 1100, 2, 1, 64, seed=30)
+    ld = 1 << 22
+    far = Case("bf16", 1, 70, 1100, 2, 1, 64, seed=30)
+    buf = t.empty(1100 * ld, device="cuda", dtype=t.bfloat16).view(1100, ld)
+    buf[:, :64], buf[:, 64:128] = near.k[:1100], near.v[:1100]
+    far.k, far.v = buf, buf[:, 64:]
+    out = []
+    for c in (near, far):
+        o, lse = c.empty(c.q), t.full((c.nq + 1, 2), FILL, device="cuda")
+        c.fwd(o, lse)
+        dq = c.empty(c.q)
+        dk, dv = (c.empty(c.k), c.empty(c.v)) if c is near else (buf[:, 128:], buf[:, 192:])
+        c.bwd(o, lse, dq, dk, dv)
+        out.append((o, lse, dq, dk[:1100, :64].clone(), dv[:1100, :64].clone()))
+    assert all(t.equal(a, b) for a, b in zip(*out))
+
+
+def _refused(fn, *args):
+    with pytest.raises(A.AtomError) as e:
+        fn(*args)
+    assert e.value.status == A.ATOM_EINVAL
+
+
+SHAPE = dict(B=2, Tq=8, Tk=16, Hq=4, Hk=2, dh=64, q_rows=16, k_rows=32, q_start=None, q_len=None, k_start=None, k_len=None)
+BAD_SHAPES = [dict(B=-1), dict(Tq=-1), dict(Tk=-1), dict(Hq=0), dict(Hk=0), dict(Hk=3), dict(Hq=-4), dict(dh=96), dict(dh=32),
+              dict(q_rows=15), dict(k_rows=31), dict(q_rows=-1), dict(q_start=4096), dict(k_start=4096),
+              dict(q_start=4096, q_len=4096, q_rows=1 << 31), dict(q_len=4098), dict(k_start=4096, k_len=4097),
+              dict(B=1 << 16, Tq=1 << 16), dict(B=1 << 20, Hq=64, Hk=64), dict(Tq=1 << 30), dict(Tk=1 << 30),
+              dict(Hq=1 << 16, Hk=1), dict(Hq=8192, Hk=1, Tq=64, q_rows=128)]
+
+
+@pytest.mark.parametrize("dtype", [A.ATOM_BF16, A.ATOM_F32])
+def test_refusals(dtype):
+    """Each argument out of its range alone, on the host (no pointer is looked at)."""
+    good = A.atom_cross_shape(**SHAPE)
+    nf, nb = A.atom_k_cross_attn_fwd_ws_bytes(dtype, good), A.atom_k_cross_attn_bwd_ws_bytes(dtype, good)
+    assert nb > 0
+    fwd = dict(dtype=dtype, shape=good, q=4096, ldq=256, k=4096, ldk=128, v=4096, ldv=128, scale=0.125, o=8192, ldo=256,
+               lse=4096, ws=4096, ws_bytes=nf)
+    bwd = dict(dtype=dtype, shape=good, q=4096, ldq=256, k=4096, ldk=128, v=4096, ldv=128, scale=0.125, o=4096, ldo=256,
+               dout=4096, lddo=256, lse=4096, dq=8192, lddq=256, dk=12288, lddk=128, dv=16384, lddv=128, ws=4096, ws_bytes=nb)
+    for call, args in ((A.atom_k_cross_attn_fwd, fwd), (A.atom_k_cross_attn_bwd, bwd)):
+        for change in BAD_SHAPES:
+            _refused(call, *{**args, "shape": A.atom_cross_shape(**{**SHAPE, **change})}.values())
+        for k, v in args.items():
+            if k in ("dtype", "shape", "scale", "ws", "ws_bytes", "lse"):
+                continue
+            bad = [v - 1, v - 4, 1 << 40] if k.startswith("ld") else [None, v + 8]
+            if (k in ("dq", "dk", "dv")) and call is A.atom_k_cross_attn_bwd:
+                bad = [v + 8] if k == "dq" else bad
+            for b in bad:
+                _refused(call, *{**args, k: b}.values())
+        for k, v in [("dtype", 2), ("scale", 0.0), ("scale", -1.0), ("scale", math.nan), ("scale", math.inf), ("lse", 4098)]:
+            _refused(call, *{**args, k: v}.values())
+    for k, v in [("ws", None), ("ws", 4104), ("ws_bytes", nb - 1), ("lse", None)]:
+        _refused(A.atom_k_cross_attn_bwd, *{**bwd, k: v}.values())
+    # few rows, long keys: ranges, and their workspace
+    long_ = A.atom_cross_shape(**{**SHAPE, "Tk": 4096, "k_rows": 8192})
+    n = A.atom_k_cross_attn_fwd_ws_bytes(dtype, long_)
+    assert n > 0
+    for k, v in [("ws", None), ("ws", 4104), ("ws_bytes", n - 1)]:
+        _refused(A.atom_k_cross_attn_fwd, *{**fwd, "shape": long_, "ws_bytes": n, k: v}.values())
+    for change in BAD_SHAPES[:9] + BAD_SHAPES[17:]:
+        s = A.atom_cross_shape(**{**SHAPE, **change})
+        assert A.atom_k_cross_attn_fwd_ws_bytes(dtype, s) == 0 and A.atom_k_cross_attn_bwd_ws_bytes(dtype, s) == 0
