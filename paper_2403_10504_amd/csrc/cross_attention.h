@@ -29,7 +29,9 @@ ATOM_DEV Seq seq(const int32_t* start, const int32_t* len, int T, int64_t rows, 
 
 // Work item of a workgroup: the hardware hands consecutive ids to the eight XCDs
 // in turn; each XCD takes a run of consecutive items, so that the blocks of one
-// sequence and head, which read the same keys, share an L2.  Ids past the items
+// sequence and head, which read the same keys, share an L2.  Heads are outside,
+// sequences inside (bh = head B + sequence), so that every XCD has some of the
+// long and some of the short sequences.  Ids past the items
 // (the grid is a multiple of eight) are negative.
 ATOM_DEV int item_of(int n_items) {
   const int per = (n_items + 7) >> 3, id = blockIdx.x;
@@ -69,7 +71,7 @@ __global__ void __launch_bounds__(256) cross_join_kernel(const CrossArgs a) {
   const int64_t P = static_cast<int64_t>(a.Tq) * a.G, n = P * a.B * a.Hk;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (r >= n) return;
-  const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh / a.Hk, hk = bh % a.Hk;
+  const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh % a.B, hk = bh / a.B;
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b);
   const bool on = p < qs.n * a.G;
   if (!on && a.q_start) return;

@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
   const int item = item_of(a.n_x * BH * a.splits);
   if (item < 0) return;
   const int x = item % a.n_x, split = SPLIT ? item / a.n_x % a.splits : 0, bh = item / (a.n_x * a.splits);
-  const int b = bh / a.Hk, hk = bh % a.Hk;
+  const int b = bh % a.B, hk = bh / a.B;  // (see item_of)
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
   const int P = qs.n * a.G, n_keys = ks.n;
   const int q0 = x * BQ;
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(64 * NW, DH == 64 ? 4 : 2) cross_dq_kernel(con
   const int item = item_of(a.n_x * BH * a.splits);
   if (item < 0) return;
   const int x = item % a.n_x, split = SPLIT ? item / a.n_x % a.splits : 0, bh = item / (a.n_x * a.splits);
-  const int b = bh / a.Hk, hk = bh % a.Hk;
+  const int b = bh % a.B, hk = bh / a.B;  // (see item_of)
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
   const int P = qs.n * a.G, n_keys = ks.n;
   const int q0 = x * BQ;
@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(co
   const int item = item_of(a.n_x * BH * a.splits);
   if (item < 0) return;
   const int x = item % a.n_x, split = SPLIT ? item / a.n_x % a.splits : 0, bh = item / (a.n_x * a.splits);
-  const int b = bh / a.Hk, hk = bh % a.Hk;
+  const int b = bh % a.B, hk = bh / a.B;  // (see item_of)
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
   const int P = qs.n * a.G, n_keys = ks.n;
   const int k0 = x * BKEYS;
@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(256) cross_sum_dq_kernel(const CrossArgs a) {
   const int64_t P = static_cast<int64_t>(a.Tq) * a.G, n = P * a.B * a.Hk;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (r >= n) return;
-  const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh / a.Hk, hk = bh % a.Hk;
+  const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh % a.B, hk = bh / a.B;
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b);
   const bool on = p < qs.n * a.G;
   if (!on && a.q_start) return;
@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(256) cross_sum_dkdv_kernel(const CrossArgs a) 
   const int64_t n = static_cast<int64_t>(a.Tk) * a.B * a.Hk;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (r >= n) return;
-  const int bh = static_cast<int>(r / a.Tk), j = static_cast<int>(r % a.Tk), b = bh / a.Hk, hk = bh % a.Hk;
+  const int bh = static_cast<int>(r / a.Tk), j = static_cast<int>(r % a.Tk), b = bh % a.B, hk = bh / a.B;
   const Seq ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
   const bool on = j < ks.n;
   if (!on && a.k_start) return;

@@ -51,7 +51,7 @@ ATOM_DEV Item item(const CrossArgs& a) {
   const int i = item_of(a.n_x * a.B * a.Hk * a.splits);
   if (i < 0) return Item{0, 0, 0, 0, 0, false};
   const int bh = i / (a.n_x * a.splits);
-  return Item{i % a.n_x, i / a.n_x % a.splits, bh, bh / a.Hk, bh % a.Hk, true};
+  return Item{i % a.n_x, i / a.n_x % a.splits, bh, bh % a.B, bh / a.B, true};
 }
 
 ATOM_DEV void range_of(int n_rows, int splits, int s, int* t0, int* t1) {

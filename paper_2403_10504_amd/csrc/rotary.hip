@@ -61,52 +61,82 @@ struct alignas(sizeof(T) * V) Vec {
   T e[V];
 };
 
-// The two runs of V elements of chunk c, and the pair that each element is of.
-template <typename T, int V, bool PAIRS>
-struct Chunk {
-  float u[V], w[V];
+// A lane's two runs of V elements of a head, as they are in memory.
+template <typename T, int V>
+struct Raw {
+  Vec<T, V> a, b;
   ATOM_DEV void load(const T* p, int o0, int o1) {
-    const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(p + o0), b = *reinterpret_cast<const Vec<T, V>*>(p + o1);
-    set(a, b);
-  }
-  ATOM_DEV void set(const Vec<T, V>& a, const Vec<T, V>& b) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if constexpr (PAIRS) {
-        const int e = 2 * i;
-        u[i] = to_f<T>(e < V ? a.e[e % V] : b.e[e % V]);
-        w[i] = to_f<T>(e + 1 < V ? a.e[(e + 1) % V] : b.e[(e + 1) % V]);
-      } else {
-        u[i] = to_f<T>(a.e[i]);
-        w[i] = to_f<T>(b.e[i]);
-      }
-    }
+    a = *reinterpret_cast<const Vec<T, V>*>(p + o0);
+    b = *reinterpret_cast<const Vec<T, V>*>(p + o1);
   }
   ATOM_DEV void store(T* p, int o0, int o1) const {
-    Vec<T, V> a, b;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if constexpr (PAIRS) {
-        a.e[i] = from_f<T>(i % 2 ? w[i / 2] : u[i / 2]);
-        b.e[i] = from_f<T>((V + i) % 2 ? w[(V + i) / 2] : u[(V + i) / 2]);
-      } else {
-        a.e[i] = from_f<T>(u[i]);
-        b.e[i] = from_f<T>(w[i]);
-      }
-    }
     *reinterpret_cast<Vec<T, V>*>(p + o0) = a;
     *reinterpret_cast<Vec<T, V>*>(p + o1) = b;
   }
 };
 
+// The same as pairs (u, w).
+template <typename T, int V, bool PAIRS>
+struct Chunk {
+  float u[V], w[V];
+  ATOM_DEV void set(const Raw<T, V>& r) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if constexpr (PAIRS) {
+        const int e = 2 * i;
+        u[i] = to_f<T>(e < V ? r.a.e[e % V] : r.b.e[e % V]);
+        w[i] = to_f<T>(e + 1 < V ? r.a.e[(e + 1) % V] : r.b.e[(e + 1) % V]);
+      } else {
+        u[i] = to_f<T>(r.a.e[i]);
+        w[i] = to_f<T>(r.b.e[i]);
+      }
+    }
+  }
+  ATOM_DEV Raw<T, V> get() const {
+    Raw<T, V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if constexpr (PAIRS) {
+        r.a.e[i] = from_f<T>(i % 2 ? w[i / 2] : u[i / 2]);
+        r.b.e[i] = from_f<T>((V + i) % 2 ? w[(V + i) / 2] : u[(V + i) / 2]);
+      } else {
+        r.a.e[i] = from_f<T>(u[i]);
+        r.b.e[i] = from_f<T>(w[i]);
+      }
+    }
+    return r;
+  }
+};
+
+// v of another lane of the row of 16, by data-parallel-primitive control word.
+template <int CTRL>
+ATOM_DEV float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// The sum over P neighbouring lanes, in all of them: pairs, quads (quad_perm),
+// then halves and rows of equal values, mirrored, then rows against each other.
+ATOM_DEV float sum_inside(float v, int P) {
+  float a, b;
+  if (P > 1) v += dpp<0xB1>(v);
+  if (P > 2) v += dpp<0x4E>(v);
+  if (P > 4) v += dpp<0x141>(v);
+  if (P > 8) v += dpp<0x140>(v);
+  if (P > 16) pair16(v, a, b), v = a + b;
+  if (P > 32) pair32(v, a, b), v = a + b;
+  return v;
+}
+
 // NC chunks of a lane (two for heads of more than 128 elements in single pairs).
 template <typename T, int V, int NC, bool PAIRS, int OP>
 __global__ void __launch_bounds__(64 * WAVES) rotary_kernel(const Args a) {
   using C = Chunk<T, V, PAIRS>;
+  using R = Raw<T, V>;
+  __shared__ float2 turns[WAVES][128];  // cosine and sine of a row's pairs, times mscale
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int P = 1 << a.plog, HS = 64 >> a.plog;
   const int slot = lane >> a.plog, lp = lane & (P - 1);
   const int L = a.dh / (2 * V), rc = a.rot / (2 * V);
+  const float inv_dh = 1.f / a.dh;
   int o0[NC], o1[NC];
   bool on[NC], turn[NC];
 #pragma unroll
@@ -135,33 +165,75 @@ __global__ void __launch_bounds__(64 * WAVES) rotary_kernel(const Args a) {
     for (int k = 0; k < NC; ++k) {
 #pragma unroll
       for (int i = 0; i < V; ++i) gain[k].u[i] = gain[k].w[i] = 1.f;
-      if (g && on[k]) gain[k].load(static_cast<const T*>(g), o0[k], o1[k]);
+      if (g && on[k]) {
+        R r;
+        r.load(static_cast<const T*>(g), o0[k], o1[k]);
+        gain[k].set(r);
+      }
     }
+  };
+  // group g: its side, and the lane's head
+  struct Head {
+    bool is_q, is_v, there;
+    int64_t at;
+  };
+  auto head_of = [&](int g) {
+    Head h;
+    h.is_q = g < gq, h.is_v = g >= gq + gk;
+    const int i = (h.is_q ? g : h.is_v ? g - gq - gk : g - gq) * HS + slot;
+    h.there = i < (h.is_q ? a.Hq : h.is_v ? a.Hv : a.Hk);
+    h.at = static_cast<int64_t>(h.is_q ? i : h.is_v ? a.Hq + a.Hk + i : a.Hq + i) * a.dh;
+    return h;
   };
 
   for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * WAVES + wave; row < a.rows;
        row += static_cast<uint64_t>(gridDim.x) * WAVES) {
-    float cs[NC][V], sn[NC][V];
-    if (a.rot) {
-      const double p = a.pos ? static_cast<double>(a.pos[row]) : static_cast<double>(static_cast<uint32_t>(row) % a.T);
-#pragma unroll
-      for (int k = 0; k < NC; ++k)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          cs[k][i] = 1.f;
-          sn[k][i] = 0.f;
-          if (!turn[k]) continue;
-          // half turns, reduced to [-1, 1] in 64 bits; then exact in fp32 to 2^-25
-          const double h = p * (a.freq[V * (lp + 64 * k) + i] * 0.31830988618379067154);
-          float s, c;
-          sincospif(static_cast<float>(h - 2.0 * rint(0.5 * h)), &s, &c);
-          cs[k][i] = c * a.mscale;
-          sn[k][i] = (OP == NORM_BWD || (OP == ROPE && a.back) ? -s : s) * a.mscale;
-        }
-    }
     const T* x = static_cast<const T*>(a.x) + static_cast<int64_t>(row) * a.ldx;
     const T* dy = OP == NORM_BWD ? static_cast<const T*>(a.dy) + static_cast<int64_t>(row) * a.lddy : x;
     T* y = static_cast<T*>(a.y) + static_cast<int64_t>(row) * a.ldy;
+    // the next group's loads are in flight while one is worked on, the first
+    // one's while the angles are computed
+    R rx[NC], rd[NC];
+    auto fetch = [&](const Head& h) {
+#pragma unroll
+      for (int k = 0; k < NC; ++k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) rx[k].a.e[i] = rx[k].b.e[i] = rd[k].a.e[i] = rd[k].b.e[i] = 0;
+        if (h.there && on[k]) {
+          if (OP == NORM_BWD) rd[k].load(dy + h.at, o0[k], o1[k]);
+          if (OP != NORM_BWD || !h.is_v) rx[k].load(x + h.at, o0[k], o1[k]);
+        }
+      }
+    };
+    Head h = head_of(g0);
+    fetch(h);
+    float cs[NC][V], sn[NC][V];
+    if (a.rot) {
+      // each lane one pair in 64 (they are the same in every head), passed on
+      // through LDS inside the wave
+      const double p = a.pos ? static_cast<double>(a.pos[row]) : static_cast<double>(static_cast<uint32_t>(row) % a.T);
+      for (int i = lane; i < a.rot / 2; i += 64) {
+        // half turns, reduced to [-1, 1] in 64 bits; then exact in fp32 to 2^-25
+        const double t = p * (a.freq[i] * 0.31830988618379067154);
+        float s, c;
+        sincospif(static_cast<float>(t - 2.0 * rint(0.5 * t)), &s, &c);
+        turns[wave][i] = make_float2(c * a.mscale, (OP == NORM_BWD || (OP == ROPE && a.back) ? -s : s) * a.mscale);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+        if (turn[k]) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float2 t = turns[wave][V * (lp + 64 * k) + i];
+            cs[k][i] = t.x;
+            sn[k][i] = t.y;
+          }
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
     auto rotate = [&](C (&v)[NC]) {
 #pragma unroll
       for (int k = 0; k < NC; ++k)
@@ -175,53 +247,34 @@ __global__ void __launch_bounds__(64 * WAVES) rotary_kernel(const Args a) {
           }
         }
     };
-    // the sum of f over a head's elements
-    auto head_sum = [&](float s) {
-      for (int o = 1; o < P; o <<= 1) s += __shfl_xor(s, o, 64);
-      return s;
-    };
     for (int g = g0; g < g1; ++g) {
-      const bool is_q = g < gq, is_v = g >= gq + gk;
-      const int h = (is_q ? g : is_v ? g - gq - gk : g - gq) * HS + slot;
-      const bool there = h < (is_q ? a.Hq : is_v ? a.Hv : a.Hk);
-      const int64_t at = static_cast<int64_t>(is_q ? h : is_v ? a.Hq + a.Hk + h : a.Hq + h) * a.dh;
-      if (is_v) {  // values: as they are
-        if (there) {
+      const Head cur = h;
+      R cx[NC], cd[NC];
 #pragma unroll
-          for (int k = 0; k < NC; ++k)
-            if (on[k]) {
-              *reinterpret_cast<Vec<T, V>*>(y + at + o0[k]) = *reinterpret_cast<const Vec<T, V>*>(dy + at + o0[k]);
-              *reinterpret_cast<Vec<T, V>*>(y + at + o1[k]) = *reinterpret_cast<const Vec<T, V>*>(dy + at + o1[k]);
-            }
-        }
+      for (int k = 0; k < NC; ++k) cx[k] = rx[k], cd[k] = rd[k];
+      if (g + 1 < g1) {
+        h = head_of(g + 1);
+        fetch(h);
+      }
+      if (cur.is_v) {  // values: as they are
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+          if (cur.there && on[k]) (OP == NORM_BWD ? cd[k] : cx[k]).store(y + cur.at, o0[k], o1[k]);
         continue;
       }
-      if (OP != ROPE && (g == g0 || g == gq)) load_gain(is_q ? a.gq : a.gk);
+      if (OP != ROPE && (g == g0 || g == gq)) load_gain(cur.is_q ? a.gq : a.gk);
       C v[NC];
 #pragma unroll
-      for (int k = 0; k < NC; ++k) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[k].u[i] = v[k].w[i] = 0.f;
-        if (there && on[k]) v[k].load(x + at, o0[k], o1[k]);
-      }
+      for (int k = 0; k < NC; ++k) v[k].set(cx[k]);
       if constexpr (OP == ROPE) {
         rotate(v);
       } else {
-        C d[NC];
-        if constexpr (OP == NORM_BWD) {
-#pragma unroll
-          for (int k = 0; k < NC; ++k) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) d[k].u[i] = d[k].w[i] = 0.f;
-            if (there && on[k]) d[k].load(dy + at, o0[k], o1[k]);
-          }
-        }
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < NC; ++k)
 #pragma unroll
           for (int i = 0; i < V; ++i) s += v[k].u[i] * v[k].u[i] + v[k].w[i] * v[k].w[i];
-        const float r = 1.f / sqrtf(head_sum(s) / a.dh + a.eps);
+        const float r = __builtin_amdgcn_rsqf(sum_inside(s, P) * inv_dh + a.eps);
         if constexpr (OP == NORM) {
 #pragma unroll
           for (int k = 0; k < NC; ++k)
@@ -232,6 +285,9 @@ __global__ void __launch_bounds__(64 * WAVES) rotary_kernel(const Args a) {
             }
           rotate(v);
         } else {
+          C d[NC];
+#pragma unroll
+          for (int k = 0; k < NC; ++k) d[k].set(cd[k]);
           rotate(d);
           float m = 0.f;
 #pragma unroll
@@ -241,11 +297,11 @@ __global__ void __launch_bounds__(64 * WAVES) rotary_kernel(const Args a) {
               v[k].u[i] *= r;
               v[k].w[i] *= r;
               const float tu = d[k].u[i] * v[k].u[i], tw = d[k].w[i] * v[k].w[i];
-              if (is_q) acc[0][k][2 * i] += tu, acc[0][k][2 * i + 1] += tw;
+              if (cur.is_q) acc[0][k][2 * i] += tu, acc[0][k][2 * i + 1] += tw;
               else acc[1][k][2 * i] += tu, acc[1][k][2 * i + 1] += tw;
               m += tu * gain[k].u[i] + tw * gain[k].w[i];
             }
-          m = head_sum(m) / a.dh;
+          m = sum_inside(m, P) * inv_dh;
 #pragma unroll
           for (int k = 0; k < NC; ++k)
 #pragma unroll
@@ -257,26 +313,50 @@ __global__ void __launch_bounds__(64 * WAVES) rotary_kernel(const Args a) {
       }
 #pragma unroll
       for (int k = 0; k < NC; ++k)
-        if (there && on[k]) v[k].store(y + at, o0[k], o1[k]);
+        if (cur.there && on[k]) v[k].get().store(y + cur.at, o0[k], o1[k]);
     }
   }
 
   if constexpr (OP == NORM_BWD) {
     if (!a.part) return;
-    // over the wave's slots, then over the waves, in this order
+    // over the wave's slots (lanes P apart), then over the waves, in this order
+    auto each = [&](auto f) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+#pragma unroll
+          for (int i = 0; i < 2 * V; ++i) acc[s][k][i] = f(acc[s][k][i]);
+    };
+    if (P <= 1) each([](float v) { return v + dpp<0x121>(v); });  // (rotations of a row of 16)
+    if (P <= 2) each([](float v) { return v + dpp<0x122>(v); });
+    if (P <= 4) each([](float v) { return v + dpp<0x124>(v); });
+    if (P <= 8) each([](float v) { return v + dpp<0x128>(v); });
+    if (P <= 16)
+      each([](float v) {
+        float p, q;
+        pair16(v, p, q);
+        return p + q;
+      });
+    if (P <= 32)
+      each([](float v) {
+        float p, q;
+        pair32(v, p, q);
+        return p + q;
+      });
     __shared__ float sums[WAVES][2][256];
+    if (slot == 0) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int k = 0; k < NC; ++k)
+        for (int k = 0; k < NC; ++k)
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) {
-          float v = acc[s][k][i];
-          for (int o = P; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-          // element i of the chunk: pair i / 2, first or second of it
-          const int e = PAIRS ? i : (i & 1) * V + (i >> 1);
-          if (slot == 0 && on[k]) sums[wave][s][(e < V ? o0[k] + e : o1[k] + e - V)] = v;
-        }
+          for (int i = 0; i < 2 * V; ++i) {
+            // element i of the chunk: pair i / 2, first or second of it
+            const int e = PAIRS ? i : (i & 1) * V + (i >> 1);
+            if (on[k]) sums[wave][s][(e < V ? o0[k] + e : o1[k] + e - V)] = acc[s][k][i];
+          }
+    }
     __syncthreads();
     float* out = a.part + (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 2 * a.dh;
     for (int t = threadIdx.x; t < 2 * a.dh; t += 64 * WAVES) {
@@ -287,6 +367,28 @@ __global__ void __launch_bounds__(64 * WAVES) rotary_kernel(const Args a) {
       out[t] = v;
     }
   }
+}
+
+// dgq and dgk (null: not wanted) from the workgroups' sums [n][2][dh]: 16 columns
+// of a workgroup, part slice, slice + 64, ... to each of 64 slices, then the
+// slices in order.
+__global__ void __launch_bounds__(1024) gain_sum_kernel(const float* __restrict__ part, int n, int dh, float* dgq,
+                                                        float* dgk) {
+  __shared__ float sh[64][16];
+  const int cl = threadIdx.x & 15, sl = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
+  float s = 0.f;
+  if (c < 2 * dh) {
+#pragma unroll 8
+    for (int p = sl; p < n; p += 64) s += part[static_cast<int64_t>(p) * 2 * dh + c];
+  }
+  sh[sl][cl] = s;
+  __syncthreads();
+  for (int half = 32; half; half >>= 1) {
+    if (sl < half) sh[sl][cl] += sh[sl + half][cl];
+    __syncthreads();
+  }
+  float* out = c < dh ? dgq : dgk;
+  if (sl == 0 && c < 2 * dh && out) out[c < dh ? c : c - dh] = sh[0][cl];
 }
 
 // The grid: workgroups of four rows, and the parts of a row's heads.
@@ -418,9 +520,9 @@ hipError_t qknorm_rope_bwd(int dtype, const void* dy, int64_t lddy, const void* 
                                 align_of(low(x) | low(dy) | low(dx) | low(gq) | low(gk) | ldx * e | lddy * e | lddx * e), s,
                                 &blocks);
   if (st != hipSuccess || !(dgq || dgk)) return st;
-  // no parts: zeros
-  if (dgq && dgk) return sum_parts2(ws, blocks, 2 * dh, 2 * dh, DT_F32, dgq, dgk, dh, false, s);
-  return sum_parts(dgq || !ws ? ws : ws + dh, blocks, dh, 2 * dh, DT_F32, dgq ? dgq : dgk, false, s);
+  // (no parts: zeros)
+  hipLaunchKernelGGL(gain_sum_kernel, dim3((2 * dh + 15) / 16), dim3(1024), 0, s, ws, static_cast<int>(blocks), dh, dgq, dgk);
+  return hipGetLastError();
 }
 
 }  // namespace atom
