@@ -40,12 +40,26 @@ ATOM_DEV Range range_of(int n_rows, int splits, int s) {
 }
 
 // ------------------------------------------------------------------ forward
+// A tile's scores are computed one tile ahead: the matrix instructions of
+// S(t+1) = K Q^T stand between the exponentials of P(t), which need nothing of
+// them, so that both units work in one wave.  K is staged one tile ahead of V.
+//
+// Loads are by a tile's base (scalar) and the lane's 32-bit offset in it.
+ATOM_DEV void lds_dma16_at(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0"
+               :
+               : "s"(base), "v"(off), "s"(lds)
+               : "memory", "m0");
+}
+
 template <int DH, int GR, int NW, int WPS, bool SPLIT>
 __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs a) {
   constexpr int NT = 64 * NW;
   using F = FwdDL<DH, NT>;
   constexpr int NS = DH / 32, NCT = DH / 16, BQ = NW * 16 * GR, RB = DH * 2;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * F::STAGE];
+  constexpr int ROWS = NT / F::CPR;  // rows of a tile that the workgroup loads at once
+  static_assert(ROWS % 16 == 0, "swizzles repeat from load to load");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * F::TILE];  // K, K, V, V
 
   const int BH = a.B * a.Hk;
   const int item = item_of(a.n_x * BH * a.splits);
@@ -65,6 +79,35 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
   const bf16_t* kb = static_cast<const bf16_t*>(a.k) + ks.row0 * a.ldk + hk * DH;
   const bf16_t* vb = static_cast<const bf16_t*>(a.v) + ks.row0 * a.ldv + hk * DH;
 
+  // Row and chunk of a thread's loads; the last, partial tile reads its last
+  // key again (whose scores are masked).
+  const int lrow = tid / F::CPR, slot = tid % F::CPR;
+  const uint32_t k_col = (slot ^ F::kswz(lrow)) * 16, v_col = (slot ^ F::vswz(lrow)) * 16;
+  auto load_tile = [&](const bf16_t* base, int64_t ld, uint32_t col, int at_lds, int j0) {
+    const bf16_t* tile = base + j0 * ld;
+    const uint32_t pitch = static_cast<uint32_t>(ld) * 2, dst = lds_offset(lds + at_lds) + w * 1024;
+    const bool whole = j0 + BT <= n_keys;
+#pragma unroll
+    for (int q = 0; q < F::LPT; ++q) {
+      const int row = whole ? lrow + q * ROWS : min(lrow + q * ROWS, n_keys - 1 - j0);
+      lds_dma16_at(tile, row * pitch + col, __builtin_amdgcn_readfirstlane(dst + q * NT * 16));
+    }
+  };
+  auto load_k = [&](int kt) { load_tile(kb, a.ldk, k_col, (kt & 1) * F::TILE, kt * BT); };
+  auto load_v = [&](int kt) { load_tile(vb, a.ldv, v_col, (2 + (kt & 1)) * F::TILE, kt * BT); };
+  // every load has landed, for every wave, and every wave is done with the stages before
+  auto fence = [&] {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    asm volatile("s_barrier" ::: "memory");
+  };
+
+  const Range rg = q0 < P ? range_of(n_keys, a.splits, split) : Range{0, 0};
+  if (rg.t0 < rg.t1) {
+    load_k(rg.t0);
+    load_v(rg.t0);
+  }
+
   Frag<bf16_t> qf[GR][NS];
 #pragma unroll
   for (int g = 0; g < GR; ++g)
@@ -72,7 +115,7 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
     for (int s = 0; s < NS; ++s) frag_row<DH>(qf[g][s], a, qb, qs, hk, qw + g * 16 + lr, P, a.ldq, 32 * s + 8 * lg);
 
   f32x4_t acc_o[GR][NCT];
-  float m_i[GR], l_i[GR];
+  float m_i[GR], l_i[GR], mloc[GR];
 #pragma unroll
   for (int g = 0; g < GR; ++g) {
     m_i[g] = NO_MAX;
@@ -80,98 +123,76 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
 #pragma unroll
     for (int c = 0; c < NCT; ++c) acc_o[g][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-
-  // chunk q * NT + tid of a tile (row, slot); the last, partial tile reads its
-  // last key again (whose scores are masked)
-  const bf16_t* ksrc[F::LPT];
-  const bf16_t* vsrc[F::LPT];
-#pragma unroll
-  for (int q = 0; q < F::LPT; ++q) {
-    const int id = q * NT + tid, row = id / F::CPR, slot = id % F::CPR;
-    ksrc[q] = kb + static_cast<int64_t>(row) * a.ldk + (slot ^ F::kswz(row)) * 8;
-    vsrc[q] = vb + static_cast<int64_t>(row) * a.ldv + (slot ^ F::vswz(row)) * 8;
-  }
-  auto load_tile = [&](int st, int j0) {
-    const uint32_t kl = lds_offset(lds + st * F::STAGE), vl = kl + F::TILE;
-    const bool whole = j0 + BT <= n_keys;
-#pragma unroll
-    for (int q = 0; q < F::LPT; ++q) {
-      const uint32_t lo = __builtin_amdgcn_readfirstlane((q * NT + w * 64) * 16);
-      if (whole) {
-        lds_dma16(ksrc[q] + static_cast<int64_t>(j0) * a.ldk, kl + lo);
-        lds_dma16(vsrc[q] + static_cast<int64_t>(j0) * a.ldv, vl + lo);
-      } else {
-        const int id = q * NT + tid, row = id / F::CPR, slot = id % F::CPR;
-        const int64_t gr = min(j0 + row, n_keys - 1);
-        lds_dma16(kb + gr * a.ldk + (slot ^ F::kswz(row)) * 8, kl + lo);
-        lds_dma16(vb + gr * a.ldv + (slot ^ F::vswz(row)) * 8, vl + lo);
-      }
-    }
-  };
   auto kfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int jt, int s) {
     const int row = jt * 16 + lr;
     f.v = *reinterpret_cast<const uint4*>(st + row * RB + ((4 * s + lg) ^ F::kswz(row)) * 16);
   };
   auto vfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int s2, int c) {
+    // keys 32 s2 + 4 lg + 0..3 and 32 s2 + 16 + 4 lg + 0..3, the order of the
+    // P fragment built from two 16-key tiles
     const int chunk = 2 * c + ((lr & 3) >> 1);
     const int r0 = 32 * s2 + 4 * lg + (lr >> 2), r1 = r0 + 16;
     const uint2 lo = ds_read_tr8(st + r0 * RB + (chunk ^ F::vswz(r0)) * 16 + 8 * (lr & 1));
     const uint2 hi = ds_read_tr8(st + r1 * RB + (chunk ^ F::vswz(r1)) * 16 + 8 * (lr & 1));
     f.v = make_uint4(lo.x, lo.y, hi.x, hi.y);
   };
-
-  const Range rg = q0 < P ? range_of(n_keys, a.splits, split) : Range{0, 0};
-  if (rg.t0 < rg.t1) load_tile(0, rg.t0 * BT);
-  for (int kt = rg.t0; kt < rg.t1; ++kt) {
-    const int j0 = kt * BT, cur = (kt - rg.t0) & 1;
-    // tile kt has landed for every wave, and every wave is done with the stage before
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-    asm volatile("s_barrier" ::: "memory");
-    if (kt + 1 < rg.t1) load_tile(cur ^ 1, j0 + BT);
-    if (qw >= P) continue;
-    const uint8_t* kst = lds + cur * F::STAGE;
-    const uint8_t* vst = kst + F::TILE;
-    float p[GR][4][4];
-    float mloc[GR];
+  // z = raw scores of tile kt, `between` standing between the matrix
+  // instructions of its four parts
+  auto scores = [&](float (&z)[GR][4][4], int kt, auto between) {
+    const uint8_t* st = lds + (kt & 1) * F::TILE;
+    Frag<bf16_t> kf[2][NS];
 #pragma unroll
-    for (int g = 0; g < GR; ++g) mloc[g] = -INFINITY;
-    auto score_tile = [&](auto MASK_) {
-      constexpr bool MASK = decltype(MASK_)::value;
-      Frag<bf16_t> kf[2][NS];
+    for (int s = 0; s < NS; ++s) kfrag(kf[0][s], st, 0, s);
 #pragma unroll
-      for (int s = 0; s < NS; ++s) kfrag(kf[0][s], kst, 0, s);
+    for (int jt = 0; jt < 4; ++jt) {
+      if (jt + 1 < 4) {
 #pragma unroll
-      for (int jt = 0; jt < 4; ++jt) {
-        if (jt + 1 < 4) {
+        for (int s = 0; s < NS; ++s) kfrag(kf[(jt + 1) & 1][s], st, jt + 1, s);
+      }
+      f32x4_t c[GR];
 #pragma unroll
-          for (int s = 0; s < NS; ++s) kfrag(kf[(jt + 1) & 1][s], kst, jt + 1, s);
-        }
-        f32x4_t z[GR];
+      for (int g = 0; g < GR; ++g) c[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int g = 0; g < GR; ++g) z[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int s = 0; s < NS; ++s)
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
+        for (int g = 0; g < GR; ++g) mfma16(c[g], kf[jt & 1][s], qf[g][s]);
+      between(jt);
 #pragma unroll
-          for (int g = 0; g < GR; ++g) mfma16(z[g], kf[jt & 1][s], qf[g][s]);
+      for (int g = 0; g < GR; ++g)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[g][jt][r] = c[g][r];
+    }
+  };
+  // a tile's scores behind the last key: -infinity
+  auto mask = [&](float (&z)[GR][4][4], int kt) {
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int g = 0; g < GR; ++g)
+          z[g][jt][r] = kt * BT + jt * 16 + 4 * lg + r < n_keys ? z[g][jt][r] : -INFINITY;
+  };
+  auto maxima = [&](const float (&z)[GR][4][4]) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float v = z[g][r];
-            if constexpr (MASK) v = j0 + jt * 16 + 4 * lg + r < n_keys ? v : -INFINITY;
-            p[g][jt][r] = v;
-            mloc[g] = fmaxf(mloc[g], v);
-          }
-      }
-    };
-    if (j0 + BT > n_keys) score_tile(std::true_type{});
-    else score_tile(std::false_type{});
-    Frag<bf16_t> vf[2];
-    vfrag(vf[0], vst, 0, 0);
+    for (int g = 0; g < GR; ++g) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, z[g][jt][r]);
+      mloc[g] = m;
+    }
+  };
+  // One tile: its exponentials and its part of O, and the scores of the next
+  // (NEXT 0: none; 1: a whole one; 2: the last).  Without branches from the
+  // first score on, so that the compiler's order is the one asked for.
+  auto step = [&](auto NEXT_, float (&z)[GR][4][4], float (&next)[GR][4][4], int kt) {
+    constexpr int NEXT = decltype(NEXT_)::value;
 #pragma unroll
     for (int g = 0; g < GR; ++g) {
       const float mx = rows4_max(mloc[g]) * sc;
+      // the reference is raised only where a score is beyond it by 2^8
       if (__builtin_amdgcn_ballot_w64(mx > m_i[g] + RESCALE_LOG2) != 0) {
         const float m_new = fmaxf(m_i[g], mx);
         const float alpha = ex2(m_i[g] - m_new);
@@ -180,29 +201,82 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
 #pragma unroll
         for (int c = 0; c < NCT; ++c) acc_o[g][c] *= alpha;
       }
-      float lsum = 0.f;
+    }
+    fence();
+    if (NEXT && kt + 2 < rg.t1) load_k(kt + 2);
+    if (NEXT) load_v(kt + 1);
+    auto exps = [&](int jt) {
 #pragma unroll
-      for (int jt = 0; jt < 4; ++jt)
+      for (int g = 0; g < GR; ++g)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          p[g][jt][r] = ex2(__builtin_fmaf(p[g][jt][r], sc, -m_i[g]));
-          lsum += p[g][jt][r];
+          z[g][jt][r] = ex2(__builtin_fmaf(z[g][jt][r], sc, -m_i[g]));
+          l_i[g] += z[g][jt][r];
         }
-      l_i[g] += lsum;
+    };
+    if constexpr (NEXT != 0) {
+      scores(next, kt + 1, exps);
+    } else {
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt) exps(jt);
+    }
+    const uint8_t* vst = lds + (2 + (kt & 1)) * F::TILE;
+    constexpr int AHEAD = 4;  // fragments of V in flight
+    Frag<bf16_t> vf[AHEAD];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) vfrag(vf[n], vst, n / NCT, n % NCT);
+    if constexpr (NEXT == 2) {
+      if (kt * BT + 2 * BT > n_keys) mask(next, kt + 1);
     }
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2) {
       Frag<bf16_t> pf[GR];
 #pragma unroll
-      for (int g = 0; g < GR; ++g) frag_from_pair(pf[g], p[g], s2);
+      for (int g = 0; g < GR; ++g) frag_from_pair(pf[g], z[g], s2);
 #pragma unroll
       for (int c = 0; c < NCT; ++c) {
         const int n = s2 * NCT + c;
-        if (n + 1 < 2 * NCT) vfrag(vf[(n + 1) & 1], vst, (n + 1) / NCT, (n + 1) % NCT);
 #pragma unroll
-        for (int g = 0; g < GR; ++g) mfma16(acc_o[g][c], vf[n & 1], pf[g]);
+        for (int g = 0; g < GR; ++g) mfma16(acc_o[g][c], vf[n % AHEAD], pf[g]);
+        if (n + AHEAD < 2 * NCT) vfrag(vf[n % AHEAD], vst, (n + AHEAD) / NCT, (n + AHEAD) % NCT);
       }
     }
+    if constexpr (NEXT != 0) maxima(next);
+  };
+  if (rg.t0 < rg.t1) {
+    float z0[GR][4][4], z1[GR][4][4];
+    using None = std::integral_constant<int, 0>;
+    using Whole = std::integral_constant<int, 1>;
+    using Last = std::integral_constant<int, 2>;
+    fence();
+    if (rg.t0 + 1 < rg.t1) load_k(rg.t0 + 1);
+    scores(z0, rg.t0, [](int) {});
+    if (rg.t0 * BT + BT > n_keys) mask(z0, rg.t0);
+    maxima(z0);
+    int kt = rg.t0;
+    for (; kt + 3 < rg.t1; kt += 2) {
+      step(Whole{}, z0, z1, kt);
+      step(Whole{}, z1, z0, kt + 1);
+    }
+    // one to three tiles
+    auto move = [&] {
+#pragma unroll
+      for (int g = 0; g < GR; ++g)
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) z0[g][jt][r] = z1[g][jt][r];
+      ++kt;
+    };
+    if (kt + 2 < rg.t1) {
+      step(Whole{}, z0, z1, kt);
+      move();
+    }
+    if (kt + 1 < rg.t1) {
+      step(Last{}, z0, z1, kt);
+      move();
+    }
+    step(None{}, z0, z1, kt);
   }
 
   // padded queries of a padded batch get zeros (P up to Tq G)
@@ -651,8 +725,16 @@ Plan plan_of(int64_t rows, int64_t heads, int64_t other, int big) {
   return p;
 }
 
-Plan fwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G) {
-  return plan_of(static_cast<int64_t>(Tq) * G, static_cast<int64_t>(B) * Hk, Tk, dtype == DT_BF16 ? 128 : 64);
+// The forward's larger workgroups: groups of 16 rows a wave, waves, waves on a SIMD.
+template <int DH>
+struct FwdBig {
+  static constexpr int GR = 2, NW = DH == 64 ? 4 : 8, WPS = 2;
+  static constexpr int ROWS = 16 * GR * NW;
+};
+
+Plan fwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
+  return plan_of(static_cast<int64_t>(Tq) * G, static_cast<int64_t>(B) * Hk, Tk,
+                 dtype != DT_BF16 ? 64 : dh == 64 ? FwdBig<64>::ROWS : FwdBig<128>::ROWS);
 }
 // (their workgroups are not made smaller)
 Plan bwd_plan(int dtype, int64_t rows, int64_t heads, int64_t other) {
@@ -719,13 +801,14 @@ __global__ void __launch_bounds__(256) cross_sum_dkdv_kernel(const CrossArgs a) 
 
 template <int DH>
 void fwd_bf16(const CrossArgs& a, bool small, hipStream_t s) {
-  const dim3 grid(grid_of(a));
+  using C = FwdBig<DH>;
+  const dim3 grid(grid_of(a)), big(64 * C::NW), four(256);
   if (a.splits > 1) {
-    if (small) hipLaunchKernelGGL((cross_fwd_kernel<DH, 1, 4, 2, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((cross_fwd_kernel<DH, DH == 64 ? 2 : 1, DH == 64 ? 4 : 8, 4, true>), grid, dim3(DH == 64 ? 256 : 512), 0, s, a);
+    if (small) hipLaunchKernelGGL((cross_fwd_kernel<DH, 1, 4, 2, true>), grid, four, 0, s, a);
+    else hipLaunchKernelGGL((cross_fwd_kernel<DH, C::GR, C::NW, C::WPS, true>), grid, big, 0, s, a);
   } else {
-    if (small) hipLaunchKernelGGL((cross_fwd_kernel<DH, 1, 4, 2, false>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((cross_fwd_kernel<DH, DH == 64 ? 2 : 1, DH == 64 ? 4 : 8, 4, false>), grid, dim3(DH == 64 ? 256 : 512), 0, s, a);
+    if (small) hipLaunchKernelGGL((cross_fwd_kernel<DH, 1, 4, 2, false>), grid, four, 0, s, a);
+    else hipLaunchKernelGGL((cross_fwd_kernel<DH, C::GR, C::NW, C::WPS, false>), grid, big, 0, s, a);
   }
 }
 
@@ -779,12 +862,12 @@ bool cross_attn_ok(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
   if (heads >= 1 << 30) return false;
   // rows of the launches that join ranges, four a workgroup
   if (heads * Tq * G >= MAX_WORKGROUPS * 4 - 4 || heads * Tk >= MAX_WORKGROUPS * 4 - 4) return false;
-  return fits(fwd_plan(dtype, B, Tq, Tk, Hk, G), heads) && fits(bwd_plan(dtype, Tq * G, heads, Tk), heads) &&
+  return fits(fwd_plan(dtype, B, Tq, Tk, Hk, G, dh), heads) && fits(bwd_plan(dtype, Tq * G, heads, Tk), heads) &&
          fits(bwd_plan(dtype, Tk, heads, Tq * G), heads);
 }
 
 uint64_t cross_attn_fwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
-  const Plan p = fwd_plan(dtype, B, Tq, Tk, Hk, Hq / Hk);
+  const Plan p = fwd_plan(dtype, B, Tq, Tk, Hk, Hq / Hk, dh);
   if (p.splits == 1) return 0;
   const uint64_t rows = static_cast<uint64_t>(p.splits) * B * Hq * Tq;
   return 4 * (rows * dh + up4(2 * rows));
@@ -799,7 +882,7 @@ uint64_t cross_attn_bwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int
 }
 
 hipError_t cross_attn_fwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t s) {
-  const Plan p = fwd_plan(dtype, a.B, a.Tq, a.Tk, a.Hk, a.G);
+  const Plan p = fwd_plan(dtype, a.B, a.Tq, a.Tk, a.Hk, a.G, dh);
   a.n_x = p.n_x, a.splits = p.splits;
   if (a.splits > 1) {
     a.part = static_cast<float*>(ws);
