@@ -231,7 +231,8 @@ int atom_k_cross_attn_bwd(int dtype, const atom_cross_shape* shape, const void* 
         !cross_rows_ok(dtype, dout, lddo, c.Hq, c.dh) || !lse || !aligned_to(ATOM_F32, lse))
       return ATOM_EINVAL;
     if (dq && !cross_rows_ok(dtype, dq, lddq, c.Hq, c.dh)) return ATOM_EINVAL;
-    if (!ws || misaligned(ws) || ws_bytes < cross_attn_bwd_ws(dtype, c.B, c.Tq, c.Tk, c.Hq, c.Hk, c.dh)) return ATOM_EINVAL;
+    const uint64_t need = cross_attn_bwd_ws(dtype, c.B, c.Tq, c.Tk, c.Hq, c.Hk, c.dh);
+    if (need && (!ws || misaligned(ws) || ws_bytes < need)) return ATOM_EINVAL;
   }
   if (c.Tk > 0) {
     if (!cross_rows_ok(dtype, k, ldk, c.Hk, c.dh) || !cross_rows_ok(dtype, v, ldv, c.Hk, c.dh)) return ATOM_EINVAL;

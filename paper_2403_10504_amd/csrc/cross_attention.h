@@ -33,8 +33,8 @@ ATOM_DEV Seq seq(const int32_t* start, const int32_t* len, int T, int64_t rows, 
 // sequences inside (bh = head B + sequence), so that every XCD has some of the
 // long and some of the short sequences.  Ids past the items
 // (the grid is a multiple of eight) are negative.
-ATOM_DEV int item_of(int n_items) {
-  const int per = (n_items + 7) >> 3, id = blockIdx.x;
+ATOM_DEV int item_of(int n_items, int id) {
+  const int per = (n_items + 7) >> 3;
   const int i = (id & 7) * per + (id >> 3);
   return (id >> 3) < per && i < n_items ? i : -1;
 }
@@ -59,6 +59,9 @@ ATOM_DEV int64_t at(const CrossArgs& a, const Seq& s, int hk, int p, int64_t ld)
 // log-sum-exp in base 2 for the backward's exponents: a row that has none (no
 // finite score) gets +infinity, and so no weight anywhere.
 ATOM_DEV float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * attn::LOG2E; }
+
+// Queries whose D fits beside the stages of a small backward's workgroup.
+constexpr int SMALL_ROWS = 2048;
 
 // Where the running maximum starts: below every finite score, and finite, so
 // that a score of -infinity weighs 0 against it.
@@ -99,7 +102,6 @@ __global__ void __launch_bounds__(256) cross_join_kernel(const CrossArgs a) {
 }  // namespace cross
 
 hipError_t cross_fwd_f32(const CrossArgs& a, int dh, hipStream_t s);
-hipError_t cross_dq_f32(const CrossArgs& a, int dh, hipStream_t s);
-hipError_t cross_dkdv_f32(const CrossArgs& a, int dh, hipStream_t s);
+hipError_t cross_bwd_f32(const CrossArgs& a, int dh, bool small, hipStream_t s);
 
 }  // namespace atom

@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
   __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * F::TILE];  // K, K, V, V
 
   const int BH = a.B * a.Hk;
-  const int item = item_of(a.n_x * BH * a.splits);
+  const int item = item_of(a.n_x * BH * a.splits, blockIdx.x);
   if (item < 0) return;
   const int x = item % a.n_x, split = SPLIT ? item / a.n_x % a.splits : 0, bh = item / (a.n_x * a.splits);
   const int b = bh % a.B, hk = bh / a.B;  // (see item_of)
@@ -314,23 +314,21 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
 }
 
 // ------------------------------------------------------------ backward: dQ
-// Also D of every row, which the dK/dV kernel reads (a.dq null: D alone).
-template <int DH, int NW, int SUB, bool SPLIT>
-__global__ void __launch_bounds__(64 * NW, DH == 64 ? 4 : 2) cross_dq_kernel(const CrossArgs a) {
+// Also D of every row, for a dK/dV kernel that reads it (a.dq null: D alone).
+template <int DH, int NW, int SUB>
+ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
   using F = FwdDL<DH>;
   constexpr int NS = DH / 32, NCT = DH / 16, BQ = NW * 16, NT = 64 * NW, RB = DH * 2;
   constexpr int LPT = F::TILE / (NT * 16);
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * SUB * F::STAGE];
 
   const int BH = a.B * a.Hk;
-  const int item = item_of(a.n_x * BH * a.splits);
-  if (item < 0) return;
-  const int x = item % a.n_x, split = SPLIT ? item / a.n_x % a.splits : 0, bh = item / (a.n_x * a.splits);
+  const bool ranges = a.splits > 1;
+  const int x = item % a.n_x, split = item / a.n_x % a.splits, bh = item / (a.n_x * a.splits);
   const int b = bh % a.B, hk = bh / a.B;  // (see item_of)
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
   const int P = qs.n * a.G, n_keys = ks.n;
   const int q0 = x * BQ;
-  if (q0 >= P && (SPLIT || a.q_start)) return;
+  if (q0 >= P && (ranges || a.q_start)) return;
   const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
 
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -391,7 +389,7 @@ __global__ void __launch_bounds__(64 * NW, DH == 64 ? 4 : 2) cross_dq_kernel(con
 #pragma unroll
     for (int s = 0; s < NS; ++s) frag_row<DH>(f[s], a, static_cast<const bf16_t*>(a.o), qs, hk, pi, P, a.ldo, 32 * s + 8 * lg);
     del_i = row_dot<NS>(f, of);
-    if (lg == 0 && pi < P && split == 0) a.delta[bh * n_p + pi] = del_i;
+    if (a.delta && lg == 0 && pi < P && split == 0) a.delta[bh * n_p + pi] = del_i;
   }
   if (!a.dq) return;
   for (int ks0 = rg.t0; ks0 < rg.t1; ks0 += SUB) {
@@ -458,7 +456,7 @@ __global__ void __launch_bounds__(64 * NW, DH == 64 ? 4 : 2) cross_dq_kernel(con
     }
   }
 
-  if (SPLIT) {
+  if (ranges) {
     if (pi < P) {
       float* row = a.part + ((static_cast<int64_t>(split) * BH + bh) * n_p + pi) * DH;
 #pragma unroll
@@ -482,23 +480,23 @@ __global__ void __launch_bounds__(64 * NW, DH == 64 ? 4 : 2) cross_dq_kernel(con
 }
 
 // -------------------------------------------------------- backward: dK, dV
-template <int DH, int W, int SUB, bool SPLIT>
-__global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(const CrossArgs a) {
+// OWN_D: D of the range's queries is computed here, from O and dO, into d_own
+// (LDS); otherwise it is read from a.delta.
+template <int DH, int W, int SUB, bool OWN_D>
+ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item) {
   using F = FwdDL<DH>;
   constexpr int NS = DH / 32, NCT = DH / 16, NT = 64 * W, RB = DH * 2, BKEYS = 16 * W;
   constexpr int LPT = F::TILE / (NT * 16);
   constexpr int STAGE = dkdv_stage<DH>();
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * SUB * STAGE];
 
   const int BH = a.B * a.Hk;
-  const int item = item_of(a.n_x * BH * a.splits);
-  if (item < 0) return;
-  const int x = item % a.n_x, split = SPLIT ? item / a.n_x % a.splits : 0, bh = item / (a.n_x * a.splits);
+  const bool ranges = a.k_splits > 1;
+  const int x = item % a.k_x, split = item / a.k_x % a.k_splits, bh = item / (a.k_x * a.k_splits);
   const int b = bh % a.B, hk = bh / a.B;  // (see item_of)
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
   const int P = qs.n * a.G, n_keys = ks.n;
   const int k0 = x * BKEYS;
-  if (k0 >= n_keys && (SPLIT || a.k_start)) return;
+  if (k0 >= n_keys && (ranges || a.k_start)) return;
   const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
 
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -546,7 +544,7 @@ __global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(co
       if (i < P) {
         const Row rw = row_of(a, i);
         pre_lse = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
-        pre_del = a.delta[bh * n_p + i];
+        if constexpr (!OWN_D) pre_del = a.delta[bh * n_p + i];
       }
     }
   };
@@ -554,7 +552,7 @@ __global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(co
     if (tid < SUB * BT) {
       float* rows = reinterpret_cast<float*>(lds + (st * SUB + tid / BT) * STAGE + 2 * F::TILE);
       rows[tid % BT] = pre_lse;
-      rows[BT + tid % BT] = pre_del;
+      if constexpr (!OWN_D) rows[BT + tid % BT] = pre_del;
     }
   };
   auto rowfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int it, int s) {
@@ -569,7 +567,7 @@ __global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(co
     f.v = make_uint4(lo.x, lo.y, hi.x, hi.y);
   };
 
-  const Range rg = k0 < n_keys ? range_of(P, a.splits, split) : Range{0, 0};
+  const Range rg = k0 < n_keys ? range_of(P, a.k_splits, split) : Range{0, 0};
   auto load_stage = [&](int st, int qt) {
 #pragma unroll
     for (int u = 0; u < SUB; ++u)
@@ -579,6 +577,28 @@ __global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(co
     load_stage(0, rg.t0);
     read_rows(rg.t0 * BT);
     store_rows(0);
+  }
+  if constexpr (OWN_D) {
+    // 16 queries a wave and step, FLY steps' loads in flight; rows past the end
+    // are zeros.  The loop's first barrier makes d_own visible.
+    constexpr int FLY = 2;
+    for (int r0 = rg.t0 * BT; r0 < rg.t1 * BT; r0 += 16 * W * FLY) {
+      Frag<bf16_t> fo[FLY][NS], fd[FLY][NS];
+#pragma unroll
+      for (int f = 0; f < FLY; ++f)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          const int r = r0 + 16 * (f * W + w) + lr;
+          frag_row<DH>(fo[f][s], a, static_cast<const bf16_t*>(a.o), qs, hk, r, P, a.ldo, 32 * s + 8 * lg);
+          frag_row<DH>(fd[f][s], a, ob, qs, hk, r, P, a.lddo, 32 * s + 8 * lg);
+        }
+#pragma unroll
+      for (int f = 0; f < FLY; ++f) {
+        const int r = r0 + 16 * (f * W + w) + lr;
+        const float v = row_dot<NS>(fo[f], fd[f]);
+        if (lg == 0 && r < rg.t1 * BT) d_own[r - rg.t0 * BT] = v;
+      }
+    }
   }
   for (int qs0 = rg.t0; qs0 < rg.t1; qs0 += SUB) {
     const int cur = ((qs0 - rg.t0) / SUB) & 1;
@@ -596,7 +616,7 @@ __global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(co
       const uint8_t* qst = lds + (cur * SUB + u) * STAGE;
       const uint8_t* ost = qst + F::TILE;
       const float* lse_s = reinterpret_cast<const float*>(qst + 2 * F::TILE);
-      const float* del_s = lse_s + BT;
+      const float* del_s = OWN_D ? d_own + (qs0 + u - rg.t0) * BT : lse_s + BT;
       float p[4][4], ds[4][4];
       // keys past the end need no mask: their columns are never stored, and
       // their fragments are zeros
@@ -677,8 +697,8 @@ __global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(co
     if (more) store_rows(cur ^ 1);
   }
 
-  if (kj >= (SPLIT || a.k_start ? n_keys : a.Tk)) return;
-  const int64_t r = SPLIT ? (static_cast<int64_t>(split) * BH + bh) * a.Tk + kj : ks.row0 + kj;
+  if (kj >= (ranges || a.k_start ? n_keys : a.Tk)) return;
+  const int64_t r = ranges ? (static_cast<int64_t>(split) * BH + bh) * a.Tk + kj : ks.row0 + kj;
 #pragma unroll
   for (int c = 0; c < NCT; ++c) {
     float vk[4], vv[4];
@@ -687,14 +707,46 @@ __global__ void __launch_bounds__(64 * W, DH == 64 ? 4 : 2) cross_dkdv_kernel(co
       vk[i] = kj < n_keys ? acc_dk[c][i] * a.scale : 0.f;  // (padding: zeros)
       vv[i] = kj < n_keys ? acc_dv[c][i] : 0.f;
     }
-    if (SPLIT) {
-      store_row4<float>(a.part + r * DH + c * 16 + 4 * lg, vk);
-      store_row4<float>(a.part2 + r * DH + c * 16 + 4 * lg, vv);
+    if (ranges) {
+      store_row4<float>(a.part_k + r * DH + c * 16 + 4 * lg, vk);
+      store_row4<float>(a.part_v + r * DH + c * 16 + 4 * lg, vv);
     } else {
       store_row4<bf16_t>(static_cast<bf16_t*>(a.dk) + r * a.lddk + hk * DH + c * 16 + 4 * lg, vk);
       store_row4<bf16_t>(static_cast<bf16_t*>(a.dv) + r * a.lddv + hk * DH + c * 16 + 4 * lg, vv);
     }
   }
+}
+
+// Large problems: a launch each, workgroups of 128 rows, two tiles a barrier.
+template <int DH>
+__global__ void __launch_bounds__(512, DH == 64 ? 4 : 2) cross_dq_kernel(const CrossArgs a) {
+  constexpr int SUB = 2;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * SUB * FwdDL<DH>::STAGE];
+  const int item = item_of(a.n_x * a.B * a.Hk * a.splits, blockIdx.x);
+  if (item >= 0) dq_body<DH, 8, SUB>(lds, a, item);
+}
+template <int DH>
+__global__ void __launch_bounds__(512, DH == 64 ? 4 : 2) cross_dkdv_kernel(const CrossArgs a) {
+  constexpr int SUB = 2;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * SUB * dkdv_stage<DH>()];
+  const int item = item_of(a.k_x * a.B * a.Hk * a.k_splits, blockIdx.x);
+  if (item >= 0) dkdv_body<DH, 8, SUB, false>(lds, nullptr, a, item);
+}
+
+// Small ones: both in one launch, workgroups of 64 rows, D computed on both
+// sides, so that neither waits for the other and twice as many CUs have work.
+template <int DH>
+__global__ void __launch_bounds__(256, DH == 64 ? 3 : 2) cross_bwd_small_kernel(const CrossArgs a) {
+  constexpr int STAGES = 2 * dkdv_stage<DH>();
+  static_assert(dkdv_stage<DH>() >= FwdDL<DH>::STAGE, "stages");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES + SMALL_ROWS * 4];
+// the first part of the grid dK and dV, the rest dQ: every XCD has both
+  const int n_k = a.dk ? a.k_x * a.B * a.Hk * a.k_splits : 0, n_q = a.dq ? a.n_x * a.B * a.Hk * a.splits : 0;
+  const int k_end = (n_k + 7) & ~7, id = blockIdx.x;
+  const int item = id < k_end ? item_of(n_k, id) : item_of(n_q, id - k_end);
+  if (item < 0) return;
+  if (id < k_end) dkdv_body<DH, 4, 1, true>(lds, reinterpret_cast<float*>(lds + STAGES), a, item);
+  else dq_body<DH, 4, 1>(lds, a, item);
 }
 
 }  // namespace cross
@@ -710,18 +762,27 @@ struct Plan {
 };
 
 constexpr int64_t CUS = 256;
+// Tiles of 64 x 64 for each of two workgroups a CU, of both sides, up to which
+// the backward is one launch.
+constexpr int64_t SMALL_TILES_64 = 12, SMALL_TILES_128 = 8;
+// Tiles that ranges have to save a workgroup.
+constexpr int64_t RANGE_GAIN = 2;
 
 // Blocks of `big` rows where they fill the card, of 64 where not; with few of
-// those too, the other side in ranges of at least two tiles.
+// those too, the other side in ranges.  One block of rows for each sequence and
+// head is a call that reads its keys for little work (single tokens): it takes
+// more ranges, so that many loads are in flight and long sequences do not wait
+// for one workgroup.
+constexpr int64_t TOKEN_WGS = 1024, TOKEN_TILES = 8;
 Plan plan_of(int64_t rows, int64_t heads, int64_t other, int big) {
   Plan p{};
   const int64_t n_big = (rows + big - 1) / big * heads;
-  p.small = n_big < CUS;
+  p.small = n_big < CUS || rows <= 64;
   const int64_t blk = p.small ? 64 : big;
   p.n_x = static_cast<int>((rows + blk - 1) / blk);
   const int64_t n = p.n_x * heads, tiles = (other + attn::BT - 1) / attn::BT;
-  p.splits = 1;
-  if (n > 0 && n < CUS) p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(2 * CUS / n, tiles / 2)));
+  const int64_t want = rows <= 64 ? TOKEN_WGS : n < CUS ? 2 * CUS : 0, least = rows <= 64 ? TOKEN_TILES : 2;
+  p.splits = n > 0 ? static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want / n, tiles / least))) : 1;
   return p;
 }
 
@@ -736,61 +797,78 @@ Plan fwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
   return plan_of(static_cast<int64_t>(Tq) * G, static_cast<int64_t>(B) * Hk, Tk,
                  dtype != DT_BF16 ? 64 : dh == 64 ? FwdBig<64>::ROWS : FwdBig<128>::ROWS);
 }
-// (their workgroups are not made smaller)
-Plan bwd_plan(int dtype, int64_t rows, int64_t heads, int64_t other) {
-  Plan p{};
-  const int blk = dtype == DT_BF16 ? 128 : 64;
-  p.n_x = static_cast<int>((rows + blk - 1) / blk);
-  const int64_t n = p.n_x * heads, tiles = (other + attn::BT - 1) / attn::BT;
-  p.splits = 1;
-  if (n > 0 && n < CUS) p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(CUS / n, tiles / 2)));
+// The backward's two sides: q (blocks of queries, ranges of keys) and k.
+struct BwdPlan {
+  bool small;
+  Plan q, k;
+};
+// Ranges of a side: none where they would not shorten a workgroup's tiles from
+// `all` to the `fair` share by more than the launch that joins them costs.
+int ranges_of(int64_t all, int64_t fair, int64_t least) {
+  const int64_t per = std::max(fair, least);
+  return static_cast<int>(all > per + RANGE_GAIN ? (all + per - 1) / per : 1);
+}
+BwdPlan bwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
+  const int64_t heads = static_cast<int64_t>(B) * Hk, rows = static_cast<int64_t>(Tq) * G;
+  const int64_t tq = (rows + attn::BT - 1) / attn::BT, tk = (Tk + attn::BT - 1) / attn::BT;
+  BwdPlan p{};
+  const int64_t fair = (2 * tq * tk * heads + 2 * CUS - 1) / (2 * CUS);
+  p.small = fair <= (dh == 64 ? SMALL_TILES_64 : SMALL_TILES_128);
+  const int blk = p.small || dtype != DT_BF16 ? 64 : 128;
+  p.q.n_x = static_cast<int>((rows + blk - 1) / blk);
+  p.k.n_x = static_cast<int>((Tk + blk - 1) / blk);
+  if (p.small) {
+    // both sides share two workgroups a CU
+    p.q.splits = ranges_of(tk, fair, 2);
+    // (and D of a range of queries has to fit the LDS)
+    p.k.splits = std::max(ranges_of(tq, fair, 2), static_cast<int>((tq + SMALL_ROWS / attn::BT - 1) / (SMALL_ROWS / attn::BT)));
+  } else {
+    p.q.splits = ranges_of(tk, (p.q.n_x * heads * tk + CUS - 1) / CUS, 4);
+    p.k.splits = ranges_of(tq, (p.k.n_x * heads * tq + CUS - 1) / CUS, 4);
+  }
+  p.q.splits = std::max(1, p.q.splits), p.k.splits = std::max(1, p.k.splits);
   return p;
 }
 
-unsigned grid_of(const CrossArgs& a) {
-  const int64_t n = static_cast<int64_t>(a.n_x) * a.splits * a.B * a.Hk;
-  return static_cast<unsigned>((n + 7) / 8 * 8);
+// Grids are multiples of eight (see item_of).
+unsigned grid_of(const CrossArgs& a, int64_t x, int64_t splits) {
+  return static_cast<unsigned>((x * splits * a.B * a.Hk + 7) / 8 * 8);
 }
 
-// Sums of ranges, in range order, to dq (packed rows, times the scale).
+// Sums of the ranges, in range order, to dq (packed rows, times the scale) and
+// to dk and dv (which hold it): 64 lanes a row, a side that has none left out.
 template <typename T, int DH>
-__global__ void __launch_bounds__(256) cross_sum_dq_kernel(const CrossArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t P = static_cast<int64_t>(a.Tq) * a.G, n = P * a.B * a.Hk;
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (r >= n) return;
-  const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh % a.B, hk = bh / a.B;
-  const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b);
-  const bool on = p < qs.n * a.G;
-  if (!on && a.q_start) return;
+__global__ void __launch_bounds__(256) cross_sum_kernel(const CrossArgs a, int64_t n_q, int64_t n_k) {
   constexpr int E = DH / 64;
-  float v[E] = {};
-  for (int s = 0; s < a.splits && on; ++s)
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] += a.part[(s * n + r) * DH + E * lane + e];
-  const int64_t lo = at<DH>(a, qs, hk, p, a.lddq) + E * lane;
-#pragma unroll
-  for (int e = 0; e < E; ++e) static_cast<T*>(a.dq)[lo + e] = from_f<T>(v[e] * a.scale);
-}
-
-// The same to dk and dv (which hold the scale).
-template <typename T, int DH>
-__global__ void __launch_bounds__(256) cross_sum_dkdv_kernel(const CrossArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t n = static_cast<int64_t>(a.Tk) * a.B * a.Hk;
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (r >= n) return;
+  int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (r < n_q) {
+    const int64_t P = static_cast<int64_t>(a.Tq) * a.G;
+    const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh % a.B, hk = bh / a.B;
+    const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b);
+    const bool on = p < qs.n * a.G;
+    if (!on && a.q_start) return;
+    float v[E] = {};
+    for (int s = 0; s < a.splits && on; ++s)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] += a.part[(s * n_q + r) * DH + E * lane + e];
+    const int64_t lo = at<DH>(a, qs, hk, p, a.lddq) + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) static_cast<T*>(a.dq)[lo + e] = from_f<T>(v[e] * a.scale);
+    return;
+  }
+  r -= n_q;
+  if (r >= n_k) return;
   const int bh = static_cast<int>(r / a.Tk), j = static_cast<int>(r % a.Tk), b = bh % a.B, hk = bh / a.B;
   const Seq ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
   const bool on = j < ks.n;
   if (!on && a.k_start) return;
-  constexpr int E = DH / 64;
   float vk[E] = {}, vv[E] = {};
-  for (int s = 0; s < a.splits && on; ++s)
+  for (int s = 0; s < a.k_splits && on; ++s)
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      vk[e] += a.part[(s * n + r) * DH + E * lane + e];
-      vv[e] += a.part2[(s * n + r) * DH + E * lane + e];
+      vk[e] += a.part_k[(s * n_k + r) * DH + E * lane + e];
+      vv[e] += a.part_v[(s * n_k + r) * DH + E * lane + e];
     }
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -802,7 +880,7 @@ __global__ void __launch_bounds__(256) cross_sum_dkdv_kernel(const CrossArgs a) 
 template <int DH>
 void fwd_bf16(const CrossArgs& a, bool small, hipStream_t s) {
   using C = FwdBig<DH>;
-  const dim3 grid(grid_of(a)), big(64 * C::NW), four(256);
+  const dim3 grid(grid_of(a, a.n_x, a.splits)), big(64 * C::NW), four(256);
   if (a.splits > 1) {
     if (small) hipLaunchKernelGGL((cross_fwd_kernel<DH, 1, 4, 2, true>), grid, four, 0, s, a);
     else hipLaunchKernelGGL((cross_fwd_kernel<DH, C::GR, C::NW, C::WPS, true>), grid, big, 0, s, a);
@@ -812,46 +890,44 @@ void fwd_bf16(const CrossArgs& a, bool small, hipStream_t s) {
   }
 }
 
-template <int DH>
-void dq_bf16(const CrossArgs& a, hipStream_t s) {
-  if (a.splits > 1) hipLaunchKernelGGL((cross_dq_kernel<DH, 8, 2, true>), dim3(grid_of(a)), dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((cross_dq_kernel<DH, 8, 2, false>), dim3(grid_of(a)), dim3(512), 0, s, a);
-}
-
-template <int DH>
-void dkdv_bf16(const CrossArgs& a, hipStream_t s) {
-  if (a.splits > 1) hipLaunchKernelGGL((cross_dkdv_kernel<DH, 8, 2, true>), dim3(grid_of(a)), dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((cross_dkdv_kernel<DH, 8, 2, false>), dim3(grid_of(a)), dim3(512), 0, s, a);
-}
-
 unsigned rows_grid(int64_t rows) { return static_cast<unsigned>((rows + 3) / 4); }
 
 template <typename T>
-void join(const CrossArgs& a, int dh, hipStream_t s) {
+hipError_t join(const CrossArgs& a, int dh, hipStream_t s) {
   const dim3 grid(rows_grid(static_cast<int64_t>(a.Tq) * a.G * a.B * a.Hk));
   if (dh == 64) hipLaunchKernelGGL((cross_join_kernel<T, 64>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((cross_join_kernel<T, 128>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int DH>
+hipError_t bwd_bf16(const CrossArgs& a, bool small, hipStream_t s) {
+  const unsigned nq = a.dq || a.delta ? grid_of(a, a.n_x, a.splits) : 0, nk = a.dk ? grid_of(a, a.k_x, a.k_splits) : 0;
+  if (small) {
+    if (nq + nk) hipLaunchKernelGGL(cross_bwd_small_kernel<DH>, dim3(nq + nk), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  // dQ first: it computes D
+  if (nq) hipLaunchKernelGGL(cross_dq_kernel<DH>, dim3(nq), dim3(512), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !nk) return e;
+  hipLaunchKernelGGL(cross_dkdv_kernel<DH>, dim3(nk), dim3(512), 0, s, a);
+  return hipGetLastError();
 }
 
 template <typename T>
-void sum_dq(const CrossArgs& a, int dh, hipStream_t s) {
-  const dim3 grid(rows_grid(static_cast<int64_t>(a.Tq) * a.G * a.B * a.Hk));
-  if (dh == 64) hipLaunchKernelGGL((cross_sum_dq_kernel<T, 64>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((cross_sum_dq_kernel<T, 128>), grid, dim3(256), 0, s, a);
-}
-
-template <typename T>
-void sum_dkdv(const CrossArgs& a, int dh, hipStream_t s) {
-  const dim3 grid(rows_grid(static_cast<int64_t>(a.Tk) * a.B * a.Hk));
-  if (dh == 64) hipLaunchKernelGGL((cross_sum_dkdv_kernel<T, 64>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((cross_sum_dkdv_kernel<T, 128>), grid, dim3(256), 0, s, a);
+hipError_t sum(const CrossArgs& a, int dh, hipStream_t s) {
+  const int64_t heads = static_cast<int64_t>(a.B) * a.Hk;
+  const int64_t n_q = a.dq && a.splits > 1 ? a.Tq * heads * a.G : 0, n_k = a.dk && a.k_splits > 1 ? a.Tk * heads : 0;
+  if (n_q + n_k == 0) return hipSuccess;
+  const dim3 grid(rows_grid(n_q + n_k));
+  if (dh == 64) hipLaunchKernelGGL((cross_sum_kernel<T, 64>), grid, dim3(256), 0, s, a, n_q, n_k);
+  else hipLaunchKernelGGL((cross_sum_kernel<T, 128>), grid, dim3(256), 0, s, a, n_q, n_k);
+  return hipGetLastError();
 }
 
 // Floats of a ws, in whole 16-byte pieces.
 uint64_t up4(uint64_t n) { return (n + 3) / 4 * 4; }
-
-// Workgroups of a launch: below half of what a dispatch counts (512 threads each).
-bool fits(const Plan& p, int64_t heads) { return static_cast<int64_t>(p.n_x) * p.splits * heads < MAX_WORKGROUPS / 2 - 8; }
 
 }  // namespace
 
@@ -861,9 +937,12 @@ bool cross_attn_ok(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
   if (G > 1 << 15 || Tq * G > (1ll << 32) / G - 1 || Tq * G >= 1ll << 30 || Tk >= 1 << 30) return false;
   if (heads >= 1 << 30) return false;
   // rows of the launches that join ranges, four a workgroup
-  if (heads * Tq * G >= MAX_WORKGROUPS * 4 - 4 || heads * Tk >= MAX_WORKGROUPS * 4 - 4) return false;
-  return fits(fwd_plan(dtype, B, Tq, Tk, Hk, G, dh), heads) && fits(bwd_plan(dtype, Tq * G, heads, Tk), heads) &&
-         fits(bwd_plan(dtype, Tk, heads, Tq * G), heads);
+  if (heads * (Tq * G + Tk) >= MAX_WORKGROUPS * 4 - 4) return false;
+  const BwdPlan p = bwd_plan(dtype, B, Tq, Tk, Hk, G, dh);
+  const int64_t n_q = static_cast<int64_t>(p.q.n_x) * p.q.splits, n_k = static_cast<int64_t>(p.k.n_x) * p.k.splits;
+  const Plan f = fwd_plan(dtype, B, Tq, Tk, Hk, G, dh);
+  // below half of what a dispatch counts (512 threads each)
+  return (n_q + n_k) * heads < MAX_WORKGROUPS / 2 - 16 && static_cast<int64_t>(f.n_x) * f.splits * heads < MAX_WORKGROUPS / 2 - 16;
 }
 
 uint64_t cross_attn_fwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
@@ -873,12 +952,22 @@ uint64_t cross_attn_fwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int
   return 4 * (rows * dh + up4(2 * rows));
 }
 
+// Floats of the backward's workspace: D (large problems), then the ranges' sums.
+struct BwdSpace {
+  uint64_t delta, q, k;
+};
+static BwdSpace bwd_space(const BwdPlan& p, int64_t rows_q, int64_t rows_k, int dh) {
+  BwdSpace s{};
+  s.delta = p.small ? 0 : up4(rows_q);
+  s.q = p.q.splits > 1 ? static_cast<uint64_t>(p.q.splits) * rows_q * dh : 0;
+  s.k = p.k.splits > 1 ? static_cast<uint64_t>(p.k.splits) * rows_k * dh : 0;
+  return s;
+}
+
 uint64_t cross_attn_bwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
-  const int64_t rows = static_cast<int64_t>(Hq / Hk) * Tq, heads = static_cast<int64_t>(B) * Hk;
-  const Plan q = bwd_plan(dtype, rows, heads, Tk), k = bwd_plan(dtype, Tk, heads, rows);
-  const uint64_t nq = q.splits > 1 ? static_cast<uint64_t>(q.splits) * rows * heads * dh : 0;
-  const uint64_t nk = k.splits > 1 ? 2ull * k.splits * Tk * heads * dh : 0;
-  return 4 * (up4(rows * heads) + std::max(nq, nk));
+  const BwdSpace w = bwd_space(bwd_plan(dtype, B, Tq, Tk, Hk, Hq / Hk, dh), static_cast<int64_t>(Hq) * B * Tq,
+                               static_cast<int64_t>(B) * Hk * Tk, dh);
+  return 4 * (w.delta + w.q + 2 * w.k);
 }
 
 hipError_t cross_attn_fwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t s) {
@@ -897,46 +986,24 @@ hipError_t cross_attn_fwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t
     e = cross_fwd_f32(a, dh, s);
   }
   if (e != hipSuccess || a.splits == 1) return e;
-  if (dtype == DT_BF16) join<bf16_t>(a, dh, s);
-  else join<float>(a, dh, s);
-  return hipGetLastError();
+  return dtype == DT_BF16 ? join<bf16_t>(a, dh, s) : join<float>(a, dh, s);
 }
 
 hipError_t cross_attn_bwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t s) {
-  const int64_t rows = static_cast<int64_t>(a.G) * a.Tq, heads = static_cast<int64_t>(a.B) * a.Hk;
-  a.delta = static_cast<float*>(ws);
-  float* part = a.delta + up4(rows * heads);
-  const Plan q = bwd_plan(dtype, rows, heads, a.Tk), k = bwd_plan(dtype, a.Tk, heads, rows);
-  hipError_t e = hipSuccess;
-  // dQ first: it computes D
-  if (rows > 0) {
-    a.n_x = q.n_x, a.splits = a.dq ? q.splits : 1, a.part = part;
-    if (dtype == DT_BF16) {
-      if (dh == 64) dq_bf16<64>(a, s);
-      else dq_bf16<128>(a, s);
-      e = hipGetLastError();
-    } else {
-      e = cross_dq_f32(a, dh, s);
-    }
-    if (e == hipSuccess && a.splits > 1) {
-      if (dtype == DT_BF16) sum_dq<bf16_t>(a, dh, s);
-      else sum_dq<float>(a, dh, s);
-      e = hipGetLastError();
-    }
-  }
-  if (e != hipSuccess || !a.dk || a.Tk == 0) return e;
-  a.n_x = k.n_x, a.splits = k.splits, a.part = part, a.part2 = part + static_cast<uint64_t>(k.splits) * a.Tk * heads * dh;
-  if (dtype == DT_BF16) {
-    if (dh == 64) dkdv_bf16<64>(a, s);
-    else dkdv_bf16<128>(a, s);
-    e = hipGetLastError();
-  } else {
-    e = cross_dkdv_f32(a, dh, s);
-  }
-  if (e != hipSuccess || a.splits == 1) return e;
-  if (dtype == DT_BF16) sum_dkdv<bf16_t>(a, dh, s);
-  else sum_dkdv<float>(a, dh, s);
-  return hipGetLastError();
+  const BwdPlan p = bwd_plan(dtype, a.B, a.Tq, a.Tk, a.Hk, a.G, dh);
+  const BwdSpace w = bwd_space(p, static_cast<int64_t>(a.Hq) * a.B * a.Tq, static_cast<int64_t>(a.B) * a.Hk * a.Tk, dh);
+  float* f = static_cast<float*>(ws);
+  a.delta = p.small ? nullptr : f;
+  a.part = f + w.delta, a.part_k = a.part + w.q, a.part_v = a.part_k + w.k;
+  a.n_x = p.q.n_x, a.splits = a.dq ? p.q.splits : 1;
+  a.k_x = p.k.n_x, a.k_splits = p.k.splits;
+  if (a.Tq == 0) a.dq = nullptr, a.delta = nullptr;
+  if (a.Tk == 0) a.dk = a.dv = nullptr;
+  hipError_t e;
+  if (dtype != DT_BF16) e = cross_bwd_f32(a, dh, p.small, s);
+  else e = dh == 64 ? bwd_bf16<64>(a, p.small, s) : bwd_bf16<128>(a, p.small, s);
+  if (e != hipSuccess) return e;
+  return dtype == DT_BF16 ? sum<bf16_t>(a, dh, s) : sum<float>(a, dh, s);
 }
 
 }  // namespace atom

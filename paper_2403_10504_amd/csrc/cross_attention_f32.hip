@@ -45,13 +45,10 @@ struct Tile {
 
 struct Item {
   int x, split, bh, b, hk;
-  bool on;
 };
-ATOM_DEV Item item(const CrossArgs& a) {
-  const int i = item_of(a.n_x * a.B * a.Hk * a.splits);
-  if (i < 0) return Item{0, 0, 0, 0, 0, false};
-  const int bh = i / (a.n_x * a.splits);
-  return Item{i % a.n_x, i / a.n_x % a.splits, bh, bh % a.B, bh / a.B, true};
+ATOM_DEV Item item(const CrossArgs& a, int i, int n_x, int splits) {
+  const int bh = i / (n_x * splits);
+  return Item{i % n_x, i / n_x % splits, bh, bh % a.B, bh / a.B};
 }
 
 ATOM_DEV void range_of(int n_rows, int splits, int s, int* t0, int* t1) {
@@ -65,8 +62,9 @@ __global__ void __launch_bounds__(256) cross_fwd_f32_kernel(const CrossArgs a) {
   using L = Tile<DH>;
   constexpr int NS = DH / 32, NCT = DH / 16;
   __shared__ __attribute__((aligned(16))) float Ks[BT * L::RP], Vs[BT * L::RP];
-  const Item it = item(a);
-  if (!it.on) return;
+  const int id = item_of(a.n_x * a.B * a.Hk * a.splits, blockIdx.x);
+  if (id < 0) return;
+  const Item it = item(a, id, a.n_x, a.splits);
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, it.b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, it.b);
   const int P = qs.n * a.G, q0 = it.x * 64, hk = it.hk;
   if (q0 >= P && (a.splits > 1 || a.q_start)) return;
@@ -178,12 +176,10 @@ __global__ void __launch_bounds__(256) cross_fwd_f32_kernel(const CrossArgs a) {
 
 // dQ, and D of every row (a.dq null: D alone).
 template <int DH>
-__global__ void __launch_bounds__(256) cross_dq_f32_kernel(const CrossArgs a) {
+ATOM_DEV void dq_f32(float* Ks, float* Vs, const CrossArgs& a, int id) {
   using L = Tile<DH>;
   constexpr int NS = DH / 32, NCT = DH / 16;
-  __shared__ __attribute__((aligned(16))) float Ks[BT * L::RP], Vs[BT * L::RP];
-  const Item it = item(a);
-  if (!it.on) return;
+  const Item it = item(a, id, a.n_x, a.splits);
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, it.b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, it.b);
   const int P = qs.n * a.G, q0 = it.x * 64, hk = it.hk;
   if (q0 >= P && (a.splits > 1 || a.q_start)) return;
@@ -216,7 +212,7 @@ __global__ void __launch_bounds__(256) cross_dq_f32_kernel(const CrossArgs a) {
     }
   }
   del = rows4_sum(del);
-  if (lg == 0 && pi < P && it.split == 0) a.delta[it.bh * n_p + pi] = del;
+  if (a.delta && lg == 0 && pi < P && it.split == 0) a.delta[it.bh * n_p + pi] = del;
   if (!a.dq) return;
   f32x4_t acc[NCT];
 #pragma unroll
@@ -285,17 +281,15 @@ __global__ void __launch_bounds__(256) cross_dq_f32_kernel(const CrossArgs a) {
   }
 }
 
-template <int DH>
-__global__ void __launch_bounds__(256) cross_dkdv_f32_kernel(const CrossArgs a) {
+// OWN_D: D of the range's queries is computed here into d_own (LDS).
+template <int DH, bool OWN_D>
+ATOM_DEV void dkdv_f32(float* Qs, float* Os, float* lse_s, float* del_s, float* d_own, const CrossArgs& a, int id) {
   using L = Tile<DH>;
   constexpr int NS = DH / 32, NCT = DH / 16;
-  __shared__ __attribute__((aligned(16))) float Qs[BT * L::RP], Os[BT * L::RP];
-  __shared__ float lse_s[BT], del_s[BT];
-  const Item it = item(a);
-  if (!it.on) return;
+  const Item it = item(a, id, a.k_x, a.k_splits);
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, it.b), ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, it.b);
   const int P = qs.n * a.G, k0 = it.x * 64, hk = it.hk;
-  if (k0 >= ks.n && (a.splits > 1 || a.k_start)) return;
+  if (k0 >= ks.n && (a.k_splits > 1 || a.k_start)) return;
   const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 15, lg = lane >> 4;
   const int kj = k0 + w * 16 + lr;
@@ -318,7 +312,7 @@ __global__ void __launch_bounds__(256) cross_dkdv_f32_kernel(const CrossArgs a) 
   for (int c = 0; c < NCT; ++c) acc_k[c] = acc_v[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   int t0 = 0, t1 = 0;
-  if (k0 < ks.n) range_of(P, a.splits, it.split, &t0, &t1);
+  if (k0 < ks.n) range_of(P, a.k_splits, it.split, &t0, &t1);
   L lq, lo;
   float pre_lse = 0.f, pre_del = 0.f;
   auto fetch = [&](int t) {
@@ -331,16 +325,36 @@ __global__ void __launch_bounds__(256) cross_dkdv_f32_kernel(const CrossArgs a) 
       if (i < P) {
         const Row rw = row_of(a, i);
         pre_lse = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
-        pre_del = a.delta[it.bh * n_p + i];
+        if constexpr (!OWN_D) pre_del = a.delta[it.bh * n_p + i];
       }
     }
   };
   if (t0 < t1) fetch(t0);
+  if constexpr (OWN_D) {  // (the loop's first barrier makes it visible)
+    for (int r0 = t0 * BT; r0 < t1 * BT; r0 += 64) {
+      const int r = r0 + w * 16 + lr;
+      float v = 0.f;
+      if (r < P) {
+        const float* po = static_cast<const float*>(a.o) + at<DH>(a, qs, hk, r, a.ldo);
+        const float* pd = o_at(r);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          Frag<float> f, g;
+          frag_load(f, po + 32 * s + 8 * lg);
+          frag_load(g, pd + 32 * s + 8 * lg);
+          v += f.lo.x * g.lo.x + f.lo.y * g.lo.y + f.lo.z * g.lo.z + f.lo.w * g.lo.w;
+          v += f.hi.x * g.hi.x + f.hi.y * g.hi.y + f.hi.z * g.hi.z + f.hi.w * g.hi.w;
+        }
+      }
+      v = rows4_sum(v);
+      if (lg == 0) d_own[r - t0 * BT] = v;
+    }
+  }
   for (int t = t0; t < t1; ++t) {
     __syncthreads();
     lq.store(Qs, tid);
     lo.store(Os, tid);
-    if (tid < BT) lse_s[tid] = pre_lse, del_s[tid] = pre_del;
+    if (tid < BT) lse_s[tid] = pre_lse, del_s[tid] = OWN_D ? d_own[(t - t0) * BT + tid] : pre_del;
     __syncthreads();
     if (t + 1 < t1) fetch(t + 1);
     float p[4][4], ds[4][4];
@@ -378,11 +392,11 @@ __global__ void __launch_bounds__(256) cross_dkdv_f32_kernel(const CrossArgs a) 
     }
   }
   float *rk, *rv;
-  if (a.splits > 1) {
+  if (a.k_splits > 1) {
     if (kj >= ks.n) return;
     const int64_t r = (static_cast<int64_t>(it.split) * a.B * a.Hk + it.bh) * a.Tk + kj;
-    rk = a.part + r * DH;
-    rv = a.part2 + r * DH;
+    rk = a.part_k + r * DH;
+    rv = a.part_v + r * DH;
   } else {
     if (kj >= (a.k_start ? ks.n : a.Tk)) return;
     rk = static_cast<float*>(a.dk) + (ks.row0 + kj) * a.lddk + hk * DH;
@@ -401,28 +415,62 @@ __global__ void __launch_bounds__(256) cross_dkdv_f32_kernel(const CrossArgs a) 
   }
 }
 
+template <int DH>
+__global__ void __launch_bounds__(256) cross_dq_f32_kernel(const CrossArgs a) {
+  __shared__ __attribute__((aligned(16))) float tiles[2][BT * Tile<DH>::RP];
+  const int id = item_of(a.n_x * a.B * a.Hk * a.splits, blockIdx.x);
+  if (id >= 0) dq_f32<DH>(tiles[0], tiles[1], a, id);
+}
+template <int DH>
+__global__ void __launch_bounds__(256) cross_dkdv_f32_kernel(const CrossArgs a) {
+  __shared__ __attribute__((aligned(16))) float tiles[2][BT * Tile<DH>::RP];
+  __shared__ float rows[2][BT];
+  const int id = item_of(a.k_x * a.B * a.Hk * a.k_splits, blockIdx.x);
+  if (id >= 0) dkdv_f32<DH, false>(tiles[0], tiles[1], rows[0], rows[1], nullptr, a, id);
+}
+// Small problems: both in one launch (see cross_bwd_small_kernel).
+template <int DH>
+__global__ void __launch_bounds__(256) cross_bwd_small_f32_kernel(const CrossArgs a) {
+  __shared__ __attribute__((aligned(16))) float tiles[2][BT * Tile<DH>::RP];
+  __shared__ float rows[2][BT], d_own[SMALL_ROWS];
+const int n_k = a.dk ? a.k_x * a.B * a.Hk * a.k_splits : 0, n_q = a.dq ? a.n_x * a.B * a.Hk * a.splits : 0;
+  const int k_end = (n_k + 7) & ~7, id = blockIdx.x;
+  const int i = id < k_end ? item_of(n_k, id) : item_of(n_q, id - k_end);
+  if (i < 0) return;
+  if (id < k_end) dkdv_f32<DH, true>(tiles[0], tiles[1], rows[0], rows[1], d_own, a, i);
+  else dq_f32<DH>(tiles[0], tiles[1], a, i);
+}
+
 }  // namespace cross
 
 namespace {
-dim3 grid_of(const CrossArgs& a) {
-  return dim3(static_cast<unsigned>((static_cast<int64_t>(a.n_x) * a.splits * a.B * a.Hk + 7) / 8 * 8));
+unsigned grid_of(const CrossArgs& a, int64_t x, int64_t splits) {
+  return static_cast<unsigned>((x * splits * a.B * a.Hk + 7) / 8 * 8);
+}
+
+template <int DH>
+hipError_t bwd(const CrossArgs& a, bool small, hipStream_t s) {
+  const unsigned nq = a.dq || a.delta ? grid_of(a, a.n_x, a.splits) : 0, nk = a.dk ? grid_of(a, a.k_x, a.k_splits) : 0;
+  if (small) {
+    if (nq + nk) hipLaunchKernelGGL(cross::cross_bwd_small_f32_kernel<DH>, dim3(nq + nk), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  if (nq) hipLaunchKernelGGL(cross::cross_dq_f32_kernel<DH>, dim3(nq), dim3(256), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !nk) return e;
+  hipLaunchKernelGGL(cross::cross_dkdv_f32_kernel<DH>, dim3(nk), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 }  // namespace
 
 hipError_t cross_fwd_f32(const CrossArgs& a, int dh, hipStream_t s) {
-  if (dh == 64) hipLaunchKernelGGL(cross::cross_fwd_f32_kernel<64>, grid_of(a), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(cross::cross_fwd_f32_kernel<128>, grid_of(a), dim3(256), 0, s, a);
+  const dim3 grid(grid_of(a, a.n_x, a.splits));
+  if (dh == 64) hipLaunchKernelGGL(cross::cross_fwd_f32_kernel<64>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cross::cross_fwd_f32_kernel<128>, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
-hipError_t cross_dq_f32(const CrossArgs& a, int dh, hipStream_t s) {
-  if (dh == 64) hipLaunchKernelGGL(cross::cross_dq_f32_kernel<64>, grid_of(a), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(cross::cross_dq_f32_kernel<128>, grid_of(a), dim3(256), 0, s, a);
-  return hipGetLastError();
-}
-hipError_t cross_dkdv_f32(const CrossArgs& a, int dh, hipStream_t s) {
-  if (dh == 64) hipLaunchKernelGGL(cross::cross_dkdv_f32_kernel<64>, grid_of(a), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(cross::cross_dkdv_f32_kernel<128>, grid_of(a), dim3(256), 0, s, a);
-  return hipGetLastError();
+hipError_t cross_bwd_f32(const CrossArgs& a, int dh, bool small, hipStream_t s) {
+  return dh == 64 ? bwd<64>(a, small, s) : bwd<128>(a, small, s);
 }
 
 }  // namespace atom

@@ -261,9 +261,10 @@ struct CrossArgs {
   int B, Tq, Tk, Hq, Hk, G;
   uint32_t gmul;  // ceil(2^32 / G): p / G is the high word of p gmul
   float scale;
-  int n_x, splits;  // blocks of rows of a sequence and head, ranges of its other side
-  float *part, *part2;  // ranges' sums: [splits][B * Hk][rows][dh] (dK and dV: two)
-  float* ml;            // forward: the ranges' maxima and sums, [splits][B * Hk][Tq G][2]
+  int n_x, splits;    // blocks of queries of a sequence and head group, ranges of its keys
+  int k_x, k_splits;  // backward: blocks of keys, ranges of queries
+  float *part, *part_k, *part_v;  // the ranges' sums of O or dQ, of dK and dV: [splits][B * Hk][rows][dh]
+  float* ml;                      // forward: the ranges' maxima and sums, [splits][B * Hk][Tq G][2]
 };
 
 // Whether the sizes are taken, by the forward and the backward alike.
