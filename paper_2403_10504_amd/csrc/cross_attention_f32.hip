@@ -14,7 +14,7 @@ template <int DH>
 struct Tile {
   static constexpr int RP = DH + 4;            // pitch of a row
   static constexpr int N = BT * DH / 4 / 256;  // 16-byte chunks of a thread
-  float4 r[N];
+  f32x4_t r[N];
   // rows r0 .. of the list that `addr` maps to addresses; behind the last (n
   // of them, at least one) the last again
   template <typename F>
@@ -22,14 +22,14 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int id = i * 256 + tid;
-      r[i] = *reinterpret_cast<const float4*>(addr(min(r0 + id / (DH / 4), n - 1)) + id % (DH / 4) * 4);
+      r[i] = *reinterpret_cast<const f32x4_t*>(addr(min(r0 + id / (DH / 4), n - 1)) + id % (DH / 4) * 4);
     }
   }
   ATOM_DEV void store(float* s, int tid) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int id = i * 256 + tid;
-      *reinterpret_cast<float4*>(s + id / (DH / 4) * RP + id % (DH / 4) * 4) = r[i];
+      *reinterpret_cast<f32x4_t*>(s + id / (DH / 4) * RP + id % (DH / 4) * 4) = r[i];
     }
   }
   // rows of 32 columns from 32 s on, and column c of the rows that frag_from_pair
@@ -57,10 +57,15 @@ ATOM_DEV void range_of(int n_rows, int splits, int s, int* t0, int* t1) {
   *t1 = min(s * per + per, n);
 }
 
-template <int DH>
-__global__ void __launch_bounds__(256) cross_fwd_f32_kernel(const CrossArgs a) {
+// FEW: at most 16 rows (single tokens), which all four waves share, each taking
+// 16 of a tile's 64 keys; their sums meet at the end (8 x 2000 keys, 16 heads of
+// 128: 153 us with one wave at work, see the launcher).
+template <int DH, bool FEW>
+__global__ void __launch_bounds__(256, 2) cross_fwd_f32_kernel(const CrossArgs a) {
   using L = Tile<DH>;
+  static_assert(!FEW || 3 * 64 * (DH / 4 + 2) <= BT * L::RP, "the waves' sums in a tile's place");
   constexpr int NS = DH / 32, NCT = DH / 16;
+  constexpr int JT = FEW ? 1 : 4;  // 16-key parts of a tile that a wave takes
   __shared__ __attribute__((aligned(16))) float Ks[BT * L::RP], Vs[BT * L::RP];
   const int id = item_of(a.n_x * a.B * a.Hk * a.splits, blockIdx.x);
   if (id < 0) return;
@@ -69,7 +74,7 @@ __global__ void __launch_bounds__(256) cross_fwd_f32_kernel(const CrossArgs a) {
   const int P = qs.n * a.G, q0 = it.x * 64, hk = it.hk;
   if (q0 >= P && (a.splits > 1 || a.q_start)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 15, lg = lane >> 4;
-  const int pi = q0 + w * 16 + lr;
+  const int pi = q0 + (FEW ? 0 : w * 16) + lr, j_w = FEW ? w * 16 : 0;
   const float sc = a.scale * LOG2E;
   const float* kb = static_cast<const float*>(a.k) + ks.row0 * a.ldk + hk * DH;
   const float* vb = static_cast<const float*>(a.v) + ks.row0 * a.ldv + hk * DH;
@@ -103,19 +108,19 @@ __global__ void __launch_bounds__(256) cross_fwd_f32_kernel(const CrossArgs a) {
       lk.load(k_at, (kt + 1) * BT, ks.n, tid);
       lv.load(v_at, (kt + 1) * BT, ks.n, tid);
     }
-    float p[4][4], mx = -INFINITY;
+    float p[JT][4], mx = -INFINITY;
 #pragma unroll
-    for (int jt = 0; jt < 4; ++jt) {
+    for (int jt = 0; jt < JT; ++jt) {
       f32x4_t z = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         Frag<float> kf;
-        L::row(kf, Ks, jt * 16 + lr, 32 * s + 8 * lg);
+        L::row(kf, Ks, j_w + jt * 16 + lr, 32 * s + 8 * lg);
         mfma16(z, kf, qf[s]);
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[jt][r] = kt * BT + jt * 16 + 4 * lg + r < ks.n ? z[r] : -INFINITY;
+        p[jt][r] = kt * BT + j_w + jt * 16 + 4 * lg + r < ks.n ? z[r] : -INFINITY;
         mx = fmaxf(mx, p[jt][r]);
       }
     }
@@ -125,26 +130,62 @@ __global__ void __launch_bounds__(256) cross_fwd_f32_kernel(const CrossArgs a) {
 #pragma unroll
     for (int c = 0; c < NCT; ++c) acc[c] *= alpha;
 #pragma unroll
-    for (int jt = 0; jt < 4; ++jt)
+    for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         p[jt][r] = ex2(__builtin_fmaf(p[jt][r], sc, -m));
         l += p[jt][r];
       }
+    if constexpr (FEW) {
+      const float* vp = Vs + (j_w + 4 * lg) * L::RP + lr;
 #pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2) {
-      Frag<float> pf;
-      frag_from_pair(pf, p, s2);
+      for (int c = 0; c < NCT; ++c)
 #pragma unroll
-      for (int c = 0; c < NCT; ++c) {
-        Frag<float> vf;
-        L::col(vf, Vs, c * 16 + lr, s2, lg);
-        mfma16(acc[c], vf, pf);
+        for (int r = 0; r < 4; ++r)
+          acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vp[r * L::RP + c * 16], p[0][r], acc[c], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        Frag<float> pf;
+        frag_from_pair(pf, p, s2);
+#pragma unroll
+        for (int c = 0; c < NCT; ++c) {
+          Frag<float> vf;
+          L::col(vf, Vs, c * 16 + lr, s2, lg);
+          mfma16(acc[c], vf, pf);
+        }
       }
     }
   }
 
-  const float l_tot = rows4_sum(l);
+  float l_tot = rows4_sum(l);
+  if constexpr (FEW) {
+    // the waves' sums, brought to the largest maximum, in wave order
+    float* sums = Ks;
+    __syncthreads();
+    if (w) {
+      float* mine = sums + ((w - 1) * 64 + lane) * (4 * NCT + 2);
+#pragma unroll
+      for (int c = 0; c < NCT; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mine[4 * c + r] = acc[c][r];
+      mine[4 * NCT] = m;
+      mine[4 * NCT + 1] = l_tot;
+    }
+    __syncthreads();
+    if (w) return;
+#pragma unroll
+    for (int v = 0; v < 3; ++v) {
+      const float* o = sums + (v * 64 + lane) * (4 * NCT + 2);
+      const float m1 = fmaxf(m, o[4 * NCT]), f0 = ex2(m - m1), f1 = ex2(o[4 * NCT] - m1);
+      m = m1;
+      l_tot = l_tot * f0 + o[4 * NCT + 1] * f1;
+#pragma unroll
+      for (int c = 0; c < NCT; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[c][r] = acc[c][r] * f0 + o[4 * c + r] * f1;
+    }
+  }
   const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
   if (a.splits > 1) {
     if (pi >= P) return;
@@ -416,13 +457,13 @@ ATOM_DEV void dkdv_f32(float* Qs, float* Os, float* lse_s, float* del_s, float* 
 }
 
 template <int DH>
-__global__ void __launch_bounds__(256) cross_dq_f32_kernel(const CrossArgs a) {
+__global__ void __launch_bounds__(256, 2) cross_dq_f32_kernel(const CrossArgs a) {
   __shared__ __attribute__((aligned(16))) float tiles[2][BT * Tile<DH>::RP];
   const int id = item_of(a.n_x * a.B * a.Hk * a.splits, blockIdx.x);
   if (id >= 0) dq_f32<DH>(tiles[0], tiles[1], a, id);
 }
 template <int DH>
-__global__ void __launch_bounds__(256) cross_dkdv_f32_kernel(const CrossArgs a) {
+__global__ void __launch_bounds__(256, 2) cross_dkdv_f32_kernel(const CrossArgs a) {
   __shared__ __attribute__((aligned(16))) float tiles[2][BT * Tile<DH>::RP];
   __shared__ float rows[2][BT];
   const int id = item_of(a.k_x * a.B * a.Hk * a.k_splits, blockIdx.x);
@@ -430,7 +471,7 @@ __global__ void __launch_bounds__(256) cross_dkdv_f32_kernel(const CrossArgs a) 
 }
 // Small problems: both in one launch (see cross_bwd_small_kernel).
 template <int DH>
-__global__ void __launch_bounds__(256) cross_bwd_small_f32_kernel(const CrossArgs a) {
+__global__ void __launch_bounds__(256, 2) cross_bwd_small_f32_kernel(const CrossArgs a) {
   __shared__ __attribute__((aligned(16))) float tiles[2][BT * Tile<DH>::RP];
   __shared__ float rows[2][BT], d_own[SMALL_ROWS];
 const int n_k = a.dk ? a.k_x * a.B * a.Hk * a.k_splits : 0, n_q = a.dq ? a.n_x * a.B * a.Hk * a.splits : 0;
@@ -465,8 +506,14 @@ hipError_t bwd(const CrossArgs& a, bool small, hipStream_t s) {
 
 hipError_t cross_fwd_f32(const CrossArgs& a, int dh, hipStream_t s) {
   const dim3 grid(grid_of(a, a.n_x, a.splits));
-  if (dh == 64) hipLaunchKernelGGL(cross::cross_fwd_f32_kernel<64>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(cross::cross_fwd_f32_kernel<128>, grid, dim3(256), 0, s, a);
+  const bool few = static_cast<int64_t>(a.Tq) * a.G <= 16;
+  if (dh == 64) {
+    if (few) hipLaunchKernelGGL((cross::cross_fwd_f32_kernel<64, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((cross::cross_fwd_f32_kernel<64, false>), grid, dim3(256), 0, s, a);
+  } else {
+    if (few) hipLaunchKernelGGL((cross::cross_fwd_f32_kernel<128, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((cross::cross_fwd_f32_kernel<128, false>), grid, dim3(256), 0, s, a);
+  }
   return hipGetLastError();
 }
 hipError_t cross_bwd_f32(const CrossArgs& a, int dh, bool small, hipStream_t s) {
