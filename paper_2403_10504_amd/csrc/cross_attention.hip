@@ -315,10 +315,10 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
 
 // ------------------------------------------------------------ backward: dQ
 // Also D of every row, for a dK/dV kernel that reads it (a.dq null: D alone).
-template <int DH, int NW, int SUB>
+template <int DH, int GR, int NW, int SUB>
 ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
   using F = FwdDL<DH>;
-  constexpr int NS = DH / 32, NCT = DH / 16, BQ = NW * 16, NT = 64 * NW, RB = DH * 2;
+  constexpr int NS = DH / 32, NCT = DH / 16, BQ = NW * 16 * GR, NT = 64 * NW, RB = DH * 2;
   constexpr int LPT = F::TILE / (NT * 16);
 
   const int BH = a.B * a.Hk;
@@ -333,25 +333,10 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
 
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lg = lane >> 4;
-  const int qw = q0 + w * 16, pi = qw + lr;
+  const int qw = q0 + w * 16 * GR;
   const float sc = a.scale * LOG2E;
   const bf16_t* kb = static_cast<const bf16_t*>(a.k) + ks.row0 * a.ldk + hk * DH;
   const bf16_t* vb = static_cast<const bf16_t*>(a.v) + ks.row0 * a.ldv + hk * DH;
-
-  Frag<bf16_t> qf[NS], of[NS];
-  float lse_i = INFINITY;
-  if (pi < P) {
-    const Row rw = row_of(a, pi);
-    lse_i = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
-  }
-#pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    frag_row<DH>(qf[s], a, static_cast<const bf16_t*>(a.q), qs, hk, pi, P, a.ldq, 32 * s + 8 * lg);
-    frag_row<DH>(of[s], a, static_cast<const bf16_t*>(a.dout), qs, hk, pi, P, a.lddo, 32 * s + 8 * lg);
-  }
-  f32x4_t acc[NCT];
-#pragma unroll
-  for (int c = 0; c < NCT; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   auto load_tile = [&](int st, int j0) {
     const uint32_t kl = lds_offset(lds + st * F::STAGE), vl = kl + F::TILE;
@@ -364,6 +349,38 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
       lds_dma16(vb + gr * a.ldv + (slot ^ F::kswz(row)) * 8, vl + lo);
     }
   };
+  const Range rg = q0 < P && a.dq ? range_of(n_keys, a.splits, split) : Range{0, 0};
+  auto load_stage = [&](int st, int kt) {
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
+      if (kt + u < rg.t1) load_tile(st * SUB + u, (kt + u) * BT);
+  };
+  load_stage(0, rg.t0);
+
+  Frag<bf16_t> qf[GR][NS], of[GR][NS];
+  float lse_i[GR], del_i[GR];
+  f32x4_t acc[GR][NCT];
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    const int pi = qw + g * 16 + lr;
+    lse_i[g] = INFINITY;
+    if (pi < P) {
+      const Row rw = row_of(a, pi);
+      lse_i[g] = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
+    }
+    Frag<bf16_t> f[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      frag_row<DH>(qf[g][s], a, static_cast<const bf16_t*>(a.q), qs, hk, pi, P, a.ldq, 32 * s + 8 * lg);
+      frag_row<DH>(of[g][s], a, static_cast<const bf16_t*>(a.dout), qs, hk, pi, P, a.lddo, 32 * s + 8 * lg);
+      frag_row<DH>(f[s], a, static_cast<const bf16_t*>(a.o), qs, hk, pi, P, a.ldo, 32 * s + 8 * lg);
+    }
+    del_i[g] = row_dot<NS>(f, of[g]);
+    if (a.delta && lg == 0 && pi < P && split == 0) a.delta[bh * n_p + pi] = del_i[g];
+#pragma unroll
+    for (int c = 0; c < NCT; ++c) acc[g][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  if (!a.dq) return;
   auto rowfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int jt, int s, bool dual) {
     const int row = jt * 16 + lr, chunk = 4 * s + lg;
     f.v = *reinterpret_cast<const uint4*>(st + row * RB + (chunk ^ (dual ? dsw<DH>(row) : F::kswz(row))) * 16);
@@ -375,23 +392,6 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
     const uint2 hi = ds_read_tr8(st + r1 * RB + (chunk ^ dsw<DH>(r1)) * 16 + 8 * (lr & 1));
     f.v = make_uint4(lo.x, lo.y, hi.x, hi.y);
   };
-
-  const Range rg = q0 < P && a.dq ? range_of(n_keys, a.splits, split) : Range{0, 0};
-  auto load_stage = [&](int st, int kt) {
-#pragma unroll
-    for (int u = 0; u < SUB; ++u)
-      if (kt + u < rg.t1) load_tile(st * SUB + u, (kt + u) * BT);
-  };
-  load_stage(0, rg.t0);
-  float del_i;
-  {
-    Frag<bf16_t> f[NS];
-#pragma unroll
-    for (int s = 0; s < NS; ++s) frag_row<DH>(f[s], a, static_cast<const bf16_t*>(a.o), qs, hk, pi, P, a.ldo, 32 * s + 8 * lg);
-    del_i = row_dot<NS>(f, of);
-    if (a.delta && lg == 0 && pi < P && split == 0) a.delta[bh * n_p + pi] = del_i;
-  }
-  if (!a.dq) return;
   for (int ks0 = rg.t0; ks0 < rg.t1; ks0 += SUB) {
     const int cur = ((ks0 - rg.t0) / SUB) & 1;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -405,7 +405,7 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
       if (kt >= rg.t1) break;
       const uint8_t* kst = lds + (cur * SUB + u) * F::STAGE;
       const uint8_t* vst = kst + F::TILE;
-      float ds[4][4];
+      float ds[GR][4][4];
       auto score_tile = [&](auto MASK_) {
         constexpr bool MASK = decltype(MASK_)::value;
         Frag<bf16_t> kf[2][NS], vf[2][NS];
@@ -423,57 +423,69 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
               rowfrag(vf[(jt + 1) & 1][s], vst, jt + 1, s, false);
             }
           }
-          f32x4_t sa = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          f32x4_t sa[GR], dp[GR];
 #pragma unroll
-          for (int s = 0; s < NS; ++s) {
-            mfma16(sa, kf[jt & 1][s], qf[s]);  // S^T[j][i]: lane holds one query, keys 4lg + r
-            mfma16(dp, vf[jt & 1][s], of[s]);  // dP^T[j][i]
-          }
+          for (int g = 0; g < GR; ++g) sa[g] = dp[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float pv = ex2(__builtin_fmaf(sa[r], sc, -lse_i));
-            float d = pv * (dp[r] - del_i);
-            if constexpr (MASK) d = j0 + jt * 16 + 4 * lg + r < n_keys ? d : 0.f;
-            ds[jt][r] = d;
-          }
+          for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int g = 0; g < GR; ++g) {
+              mfma16(sa[g], kf[jt & 1][s], qf[g][s]);  // S^T[j][i]: lane holds one query, keys 4lg + r
+              mfma16(dp[g], vf[jt & 1][s], of[g][s]);  // dP^T[j][i]
+            }
+#pragma unroll
+          for (int g = 0; g < GR; ++g)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float pv = ex2(__builtin_fmaf(sa[g][r], sc, -lse_i[g]));
+              float d = pv * (dp[g][r] - del_i[g]);
+              if constexpr (MASK) d = j0 + jt * 16 + 4 * lg + r < n_keys ? d : 0.f;
+              ds[g][jt][r] = d;
+            }
         }
       };
       if (j0 + BT > n_keys) score_tile(std::true_type{});
       else score_tile(std::false_type{});
-      Frag<bf16_t> kt2[2];
-      trfrag(kt2[0], kst, 0, 0);
+      constexpr int AHEAD = 2;
+      Frag<bf16_t> kt2[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) trfrag(kt2[n], kst, n / NCT, n % NCT);
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
-        Frag<bf16_t> dsf;
-        frag_from_pair(dsf, ds, s2);
+        Frag<bf16_t> dsf[GR];
+#pragma unroll
+        for (int g = 0; g < GR; ++g) frag_from_pair(dsf[g], ds[g], s2);
 #pragma unroll
         for (int c = 0; c < NCT; ++c) {
           const int n = s2 * NCT + c;
-          if (n + 1 < 2 * NCT) trfrag(kt2[(n + 1) & 1], kst, (n + 1) / NCT, (n + 1) % NCT);
-          mfma16(acc[c], kt2[n & 1], dsf);  // dQ^T[c][i]
+#pragma unroll
+          for (int g = 0; g < GR; ++g) mfma16(acc[g][c], kt2[n % AHEAD], dsf[g]);  // dQ^T[c][i]
+          if (n + AHEAD < 2 * NCT) trfrag(kt2[n % AHEAD], kst, (n + AHEAD) / NCT, (n + AHEAD) % NCT);
         }
       }
     }
   }
 
-  if (ranges) {
-    if (pi < P) {
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    const int pi = qw + g * 16 + lr;
+    if (ranges) {
+      if (pi >= P) continue;
       float* row = a.part + ((static_cast<int64_t>(split) * BH + bh) * n_p + pi) * DH;
 #pragma unroll
       for (int c = 0; c < NCT; ++c) {
-        float v[4] = {acc[c][0], acc[c][1], acc[c][2], acc[c][3]};
+        float v[4] = {acc[g][c][0], acc[g][c][1], acc[g][c][2], acc[g][c][3]};
         store_row4<float>(row + c * 16 + 4 * lg, v);
       }
+      continue;
     }
-    return;
-  }
-  if (pi < (a.q_start ? P : n_p)) {
+    if (pi >= (a.q_start ? P : n_p)) continue;
     bf16_t* row = static_cast<bf16_t*>(a.dq) + at<DH>(a, qs, hk, pi, a.lddq);
 #pragma unroll
     for (int c = 0; c < NCT; ++c) {
       float v[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = pi < P ? acc[c][r] * a.scale : 0.f;  // (padding: zeros)
+      for (int r = 0; r < 4; ++r) v[r] = pi < P ? acc[g][c][r] * a.scale : 0.f;  // (padding: zeros)
       store_row4<bf16_t>(row + c * 16 + 4 * lg, v);
     }
   }
@@ -717,13 +729,21 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
   }
 }
 
+// Groups of 16 queries a wave, waves, waves on a SIMD, and tiles a barrier, of
+// the dQ kernel's larger workgroups.
+template <int DH>
+struct DqBig {
+  static constexpr int GR = 2, NW = 4, WPS = 2, SUB = 1;
+  static constexpr int ROWS = 16 * GR * NW;
+};
+
 // Large problems: a launch each, workgroups of 128 rows, two tiles a barrier.
 template <int DH>
-__global__ void __launch_bounds__(512, DH == 64 ? 4 : 2) cross_dq_kernel(const CrossArgs a) {
-  constexpr int SUB = 2;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * SUB * FwdDL<DH>::STAGE];
+__global__ void __launch_bounds__(64 * DqBig<DH>::NW, DqBig<DH>::WPS) cross_dq_kernel(const CrossArgs a) {
+  using C = DqBig<DH>;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * C::SUB * FwdDL<DH>::STAGE];
   const int item = item_of(a.n_x * a.B * a.Hk * a.splits, blockIdx.x);
-  if (item >= 0) dq_body<DH, 8, SUB>(lds, a, item);
+  if (item >= 0) dq_body<DH, C::GR, C::NW, C::SUB>(lds, a, item);
 }
 template <int DH>
 __global__ void __launch_bounds__(512, DH == 64 ? 4 : 2) cross_dkdv_kernel(const CrossArgs a) {
@@ -746,7 +766,7 @@ __global__ void __launch_bounds__(256, DH == 64 ? 3 : 2) cross_bwd_small_kernel(
   const int item = id < k_end ? item_of(n_k, id) : item_of(n_q, id - k_end);
   if (item < 0) return;
   if (id < k_end) dkdv_body<DH, 4, 1, true>(lds, reinterpret_cast<float*>(lds + STAGES), a, item);
-  else dq_body<DH, 4, 1>(lds, a, item);
+  else dq_body<DH, 1, 4, 1>(lds, a, item);
 }
 
 }  // namespace cross
@@ -814,8 +834,8 @@ BwdPlan bwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
   BwdPlan p{};
   const int64_t fair = (2 * tq * tk * heads + 2 * CUS - 1) / (2 * CUS);
   p.small = fair <= (dh == 64 ? SMALL_TILES_64 : SMALL_TILES_128);
-  const int blk = p.small || dtype != DT_BF16 ? 64 : 128;
-  p.q.n_x = static_cast<int>((rows + blk - 1) / blk);
+  const int blk = p.small || dtype != DT_BF16 ? 64 : 128, blk_q = blk == 64 ? 64 : dh == 64 ? DqBig<64>::ROWS : DqBig<128>::ROWS;
+  p.q.n_x = static_cast<int>((rows + blk_q - 1) / blk_q);
   p.k.n_x = static_cast<int>((Tk + blk - 1) / blk);
   if (p.small) {
     // both sides share two workgroups a CU
@@ -908,7 +928,7 @@ hipError_t bwd_bf16(const CrossArgs& a, bool small, hipStream_t s) {
     return hipGetLastError();
   }
   // dQ first: it computes D
-  if (nq) hipLaunchKernelGGL(cross_dq_kernel<DH>, dim3(nq), dim3(512), 0, s, a);
+  if (nq) hipLaunchKernelGGL(cross_dq_kernel<DH>, dim3(nq), dim3(64 * DqBig<DH>::NW), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !nk) return e;
   hipLaunchKernelGGL(cross_dkdv_kernel<DH>, dim3(nk), dim3(512), 0, s, a);
