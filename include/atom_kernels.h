@@ -179,8 +179,8 @@ typedef struct {
 /* Forward; lse may be NULL (not wanted).  Requirements: dh 64 or 128, Hk >= 1
  * divides Hq, B, Tq, Tk >= 0 (B or Tq 0: nothing is done), q_start with q_len only
  * (k alike); without a start, q_rows >= B * Tq (k alike); scale finite, above 0;
- * leading dimensions multiples of 8 (bf16) or 4 (fp32); tensors and ws 16-byte
- * aligned; less than 2^26 pairs of query and head, and of key and head of keys, in
+ * leading dimensions multiples of 8 (bf16) or 4 (fp32), below 2^24; tensors and ws
+ * 16-byte aligned; less than 2^26 pairs of query and head, and of key and head of keys, in
  * padded lengths; Tq (Hq/Hk)^2 < 2^32, and less than 2^22 workgroups of 64 rows.
  * o must not overlap the inputs.  ws: device scratch of at least the bytes
  * that the query returns (0: none needed, or sizes refused); calls that may

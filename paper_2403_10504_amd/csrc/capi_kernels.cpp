@@ -44,7 +44,7 @@ inline bool side_ok(const int32_t* start, const int32_t* len, int64_t rows, int6
   return start ? len != nullptr && rows <= INT32_MAX : rows >= B * T;
 }
 inline bool cross_rows_ok(int dt, const void* p, int64_t ld, int64_t heads, int dh) {
-  return p && !misaligned(p) && ld >= heads * dh && ld % (dt == ATOM_BF16 ? 8 : 4) == 0 && ld <= INT64_MAX / 8 / INT32_MAX;
+  return p && !misaligned(p) && ld >= heads * dh && ld % (dt == ATOM_BF16 ? 8 : 4) == 0 && ld < 1 << 24;
 }
 inline CrossArgs cross_args(const atom_cross_shape* s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                             const void* v, int64_t ldv, float scale) {

@@ -30,6 +30,15 @@ ATOM_DEV void frag_row(Frag<bf16_t>& f, const CrossArgs& a, const bf16_t* base, 
   else frag_zero(f);
 }
 
+// Direct loads by a tile's base (scalar) and the lane's 32-bit offset in it
+// (leading dimensions below 2^24: 64 rows stay within 2^32 bytes).
+ATOM_DEV void lds_dma16_at(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0"
+               :
+               : "s"(base), "v"(off), "s"(lds)
+               : "memory", "m0");
+}
+
 // The tiles of a range.
 struct Range {
   int t0, t1;
@@ -43,15 +52,6 @@ ATOM_DEV Range range_of(int n_rows, int splits, int s) {
 // A tile's scores are computed one tile ahead: the matrix instructions of
 // S(t+1) = K Q^T stand between the exponentials of P(t), which need nothing of
 // them, so that both units work in one wave.  K is staged one tile ahead of V.
-//
-// Loads are by a tile's base (scalar) and the lane's 32-bit offset in it.
-ATOM_DEV void lds_dma16_at(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0"
-               :
-               : "s"(base), "v"(off), "s"(lds)
-               : "memory", "m0");
-}
-
 template <int DH, int GR, int NW, int WPS, bool SPLIT>
 __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs a) {
   constexpr int NT = 64 * NW;
@@ -319,7 +319,8 @@ template <int DH, int GR, int NW, int SUB>
 ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
   using F = FwdDL<DH>;
   constexpr int NS = DH / 32, NCT = DH / 16, BQ = NW * 16 * GR, NT = 64 * NW, RB = DH * 2;
-  constexpr int LPT = F::TILE / (NT * 16);
+  constexpr int LPT = F::TILE / (NT * 16), ROWS = NT / F::CPR;
+  static_assert(ROWS % 16 == 0, "swizzles repeat from load to load");
 
   const int BH = a.B * a.Hk;
   const bool ranges = a.splits > 1;
@@ -338,15 +339,17 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
   const bf16_t* kb = static_cast<const bf16_t*>(a.k) + ks.row0 * a.ldk + hk * DH;
   const bf16_t* vb = static_cast<const bf16_t*>(a.v) + ks.row0 * a.ldv + hk * DH;
 
+  const int lrow = tid / F::CPR, slot = tid % F::CPR;
+  const uint32_t k_col = (slot ^ dsw<DH>(lrow)) * 16, v_col = (slot ^ F::kswz(lrow)) * 16;
   auto load_tile = [&](int st, int j0) {
-    const uint32_t kl = lds_offset(lds + st * F::STAGE), vl = kl + F::TILE;
+    const uint32_t dst = lds_offset(lds + st * F::STAGE) + w * 1024;
+    const bf16_t *kt = kb + j0 * a.ldk, *vt = vb + j0 * a.ldv;
+    const uint32_t kp = static_cast<uint32_t>(a.ldk) * 2, vp = static_cast<uint32_t>(a.ldv) * 2;
 #pragma unroll
     for (int q = 0; q < LPT; ++q) {
-      const int id = q * NT + tid, row = id / F::CPR, slot = id % F::CPR;
-      const int64_t gr = min(j0 + row, n_keys - 1);
-      const uint32_t lo = __builtin_amdgcn_readfirstlane((q * NT + w * 64) * 16);
-      lds_dma16(kb + gr * a.ldk + (slot ^ dsw<DH>(row)) * 8, kl + lo);
-      lds_dma16(vb + gr * a.ldv + (slot ^ F::kswz(row)) * 8, vl + lo);
+      const uint32_t row = min(lrow + q * ROWS, n_keys - 1 - j0);
+      lds_dma16_at(kt, row * kp + k_col, __builtin_amdgcn_readfirstlane(dst + q * NT * 16));
+      lds_dma16_at(vt, row * vp + v_col, __builtin_amdgcn_readfirstlane(dst + F::TILE + q * NT * 16));
     }
   };
   const Range rg = q0 < P && a.dq ? range_of(n_keys, a.splits, split) : Range{0, 0};
@@ -498,7 +501,8 @@ template <int DH, int W, int SUB, bool OWN_D>
 ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item) {
   using F = FwdDL<DH>;
   constexpr int NS = DH / 32, NCT = DH / 16, NT = 64 * W, RB = DH * 2, BKEYS = 16 * W;
-  constexpr int LPT = F::TILE / (NT * 16);
+  constexpr int LPT = F::TILE / (NT * 16), ROWS = NT / F::CPR;
+  static_assert(ROWS % 16 == 0, "swizzles repeat from load to load");
   constexpr int STAGE = dkdv_stage<DH>();
 
   const int BH = a.B * a.Hk;
@@ -533,16 +537,18 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
     acc_dv[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
+  const int lrow = tid / F::CPR;
+  const uint32_t col = ((tid % F::CPR) ^ dsw<DH>(lrow)) * 16;
   auto load_tile = [&](int st, int i0) {
-    const uint32_t ql = lds_offset(lds + st * STAGE), ol = ql + F::TILE;
+    const uint32_t dst = lds_offset(lds + st * STAGE) + w * 1024;
+    const int t0 = row_of(a, i0).t;  // the tile's first token: its rows are less than 2^32 bytes on
+    const bf16_t *qt = qb + (qs.row0 + t0) * a.ldq, *ot = ob + (qs.row0 + t0) * a.lddo;
 #pragma unroll
     for (int q = 0; q < LPT; ++q) {
-      const int id = q * NT + tid, row = id / F::CPR, slot = id % F::CPR;
-      const Row rw = row_of(a, min(i0 + row, P - 1));
-      const int64_t col = static_cast<int64_t>(hk * a.G + rw.g) * DH + (slot ^ dsw<DH>(row)) * 8;
-      const uint32_t lo = __builtin_amdgcn_readfirstlane((q * NT + w * 64) * 16);
-      lds_dma16(qb + (qs.row0 + rw.t) * a.ldq + col, ql + lo);
-      lds_dma16(ob + (qs.row0 + rw.t) * a.lddo + col, ol + lo);
+      const Row rw = row_of(a, min(i0 + lrow + q * ROWS, P - 1));
+      const uint32_t c = static_cast<uint32_t>(hk * a.G + rw.g) * (DH * 2) + col, t = rw.t - t0;
+      lds_dma16_at(qt, t * (static_cast<uint32_t>(a.ldq) * 2) + c, __builtin_amdgcn_readfirstlane(dst + q * NT * 16));
+      lds_dma16_at(ot, t * (static_cast<uint32_t>(a.lddo) * 2) + c, __builtin_amdgcn_readfirstlane(dst + F::TILE + q * NT * 16));
     }
   };
   // LSE and D of a stage's rows go through registers; rows past the end get
@@ -733,7 +739,7 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
 // the dQ kernel's larger workgroups.
 template <int DH>
 struct DqBig {
-  static constexpr int GR = 2, NW = 4, WPS = 2, SUB = 1;
+  static constexpr int GR = 2, NW = DH == 64 ? 4 : 8, WPS = 2, SUB = 1;
   static constexpr int ROWS = 16 * GR * NW;
 };
 

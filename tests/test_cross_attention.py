@@ -524,7 +524,7 @@ def test_refusals(dtype):
         for k, v in args.items():
             if k in ("dtype", "shape", "scale", "ws", "ws_bytes", "lse"):
                 continue
-            bad = [v - 1, v - 4, 1 << 40] if k.startswith("ld") else [None, v + 8]
+            bad = [v - 1, v - 4, 1 << 24, 1 << 40] if k.startswith("ld") else [None, v + 8]
             if (k in ("dq", "dk", "dv")) and call is A.atom_k_cross_attn_bwd:
                 bad = [v + 8] if k == "dq" else bad
             for b in bad:
