@@ -122,9 +122,10 @@ int atom_rope_freqs(int rot, double base, int scaling, double factor, double tra
  * pos: device positions [rows], any int32; NULL: row % T (T >= 1; not read
  * otherwise).  freq: device, [rot/2].  Angles are computed in 64 bits (at
  * p freq = 10^9 they are off by 10^-7).  y may be x (with ldy = ldx), else they
- * must not overlap.  Requirements: rows from 0 to 2^31 - 1; heads from 0 to 2^16;
- * dh even, 2 to 256; rot even, 0 to dh (0: pos and freq are not read); ldx, ldy
- * >= heads * dh; x and y aligned to their elements (to 16 bytes, with dh, rot
+ * must not overlap.  Requirements: rows from 0 to 2^31 - 1; heads from 0 to 2^16
+ * (rows or heads 0: nothing is done, and no pointer looked at); dh even, 2 to 256;
+ * rot even, 0 to dh (0: pos and freq are not read); mscale finite; ldx, ldy >=
+ * heads * dh, up to 2^29; x and y aligned to their elements (to 16 bytes, with dh, rot
  * and the leading dimensions multiples of 16, for the widest accesses). */
 int atom_k_rope(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const int32_t* pos, const double* freq,
                 float mscale, int layout, int transposed, int64_t rows, int T, int heads, int dh, int rot, void* stream);
@@ -135,7 +136,8 @@ int atom_k_rope(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, con
  *   u = g x / sqrt(mean(x^2) + eps) over a head's dh elements,  y = mscale R u,
  * g = gq or gk [dh] in dtype, shared by the heads of a side (NULL: 1).  Heads of
  * values are copied (nothing is done where y is x).  rot 0: the norms alone.
- * Other arguments as for atom_k_rope; eps finite, above 0; Hq + Hk + Hv up to 2^16. */
+ * Other arguments as for atom_k_rope; eps a normal number above 0; Hq + Hk + Hv up
+ * to 2^16.  The squares of a head's elements and their sum are fp32. */
 int atom_k_qknorm_rope_fwd(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const void* gq, const void* gk,
                            float eps, const int32_t* pos, const double* freq, float mscale, int layout, int64_t rows,
                            int T, int Hq, int Hk, int Hv, int dh, int rot, void* stream);

@@ -1,4 +1,5 @@
 // extern "C" wrappers of the kernel launchers (include/atom_kernels.h).
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -152,7 +153,7 @@ int atom_k_rope(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, con
 int atom_k_qknorm_rope_fwd(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, const void* gq, const void* gk,
                            float eps, const int32_t* pos, const double* freq, float mscale, int layout, int64_t rows,
                            int T, int Hq, int Hk, int Hv, int dh, int rot, void* stream) {
-  if (Hq < 0 || Hk < 0 || Hv < 0 || !(eps > 0) || !isfinite(eps)) return ATOM_EINVAL;
+  if (Hq < 0 || Hk < 0 || Hv < 0 || !(eps >= FLT_MIN) || !isfinite(eps)) return ATOM_EINVAL;
   const int64_t heads = static_cast<int64_t>(Hq) + Hk + Hv;
   if (!turn_ok(dtype, layout, rows, heads, dh, rot, mscale)) return ATOM_EINVAL;
   if (rows == 0 || heads == 0) return ATOM_OK;
@@ -173,7 +174,7 @@ int atom_k_qknorm_rope_bwd(int dtype, const void* dy, int64_t lddy, const void* 
                            const void* gq, const void* gk, float* dgq, float* dgk, float eps, const int32_t* pos,
                            const double* freq, float mscale, int layout, int64_t rows, int T, int Hq, int Hk, int Hv,
                            int dh, int rot, void* ws, uint64_t ws_bytes, void* stream) {
-  if (Hq < 0 || Hk < 0 || Hv < 0 || !(eps > 0) || !isfinite(eps)) return ATOM_EINVAL;
+  if (Hq < 0 || Hk < 0 || Hv < 0 || !(eps >= FLT_MIN) || !isfinite(eps)) return ATOM_EINVAL;
   const int64_t heads = static_cast<int64_t>(Hq) + Hk + Hv;
   if (!turn_ok(dtype, layout, rows, heads, dh, rot, mscale)) return ATOM_EINVAL;
   if (!aligned_to(ATOM_F32, dgq) || !aligned_to(ATOM_F32, dgk)) return ATOM_EINVAL;

@@ -7,6 +7,8 @@ python -m paper_2403_10504_amd.kernel_bench layernorm [iters]
 python -m paper_2403_10504_amd.kernel_bench xent [iters]
 python -m paper_2403_10504_amd.kernel_bench linear_xent [iters]
 python -m paper_2403_10504_amd.kernel_bench orthogonalize [iters]
+python -m paper_2403_10504_amd.kernel_bench rotary [iters]
+python -m paper_2403_10504_amd.kernel_bench cross_attention [iters]
 
 attention: causal attention at the 6.7B shape (B 2, T 2048, 32 heads of 128),
 GPT-3 Small's (B 8, 12 heads of 64) and 13B's (B 1, 40 heads of 128); the
@@ -19,7 +21,10 @@ layernorm: the LayerNorm backward (accumulate, bf16 copy, both partial sums)
 and forward (bf16 output, row statistics) at the four GPT-3 widths.
 linear_xent: the head's loss without logits, and its gradients, at the four
 GPT-3 widths; orthogonalize: five Newton-Schulz steps of the weight matrices of
-a block at those widths.  One line per measurement; times from HIP events.
+a block at those widths.  rotary: the turn of queries and keys, and their norms
+with the turn and its gradients, on a block's fused qkv at those widths;
+cross_attention: the same batches' queries on encoder states of half the length,
+and one token of each sequence.  One line per measurement; times from HIP events.
 """
 from __future__ import annotations
 
@@ -199,6 +204,54 @@ def orthogonalize(iters=10):
               f"workspace {n / 1e6:.0f} MB", flush=True)
 
 
+def rotary(iters=50):
+    """Positions, and norms with positions, of a block's queries and keys (GPT-3 widths, their token counts)."""
+    for B, T, H, dh in ((8, 2048, 12, 64), (4, 2048, 16, 128), (2, 2048, 32, 128), (1, 2048, 40, 128)):
+        n, w = B * T, 3 * H * dh
+        x = torch.randn(n, w, device="cuda").to(torch.bfloat16)
+        dy = (torch.randn(n, w, device="cuda") * 1e-3).to(torch.bfloat16)
+        y, dg = torch.empty_like(x), torch.empty(2, dh, device="cuda")
+        g = torch.ones(dh, device="cuda").to(torch.bfloat16)
+        freq = torch.from_numpy(A.atom_rope_freqs(dh)).cuda()
+        ws = torch.empty(A.atom_k_qknorm_rope_bwd_ws_bytes(n, H, H, dh), device="cuda", dtype=torch.uint8)
+        tail = (1e-6, None, freq.data_ptr(), 1.0, A.ATOM_ROPE_HALF, n, T, H, H, H, dh, dh)
+        turn = lambda: A.atom_k_rope(1, x.data_ptr(), w, y.data_ptr(), w, None, freq.data_ptr(), 1.0,  # noqa: E731
+                                     A.ATOM_ROPE_HALF, 0, n, T, 2 * H, dh, dh)
+        fwd = lambda: A.atom_k_qknorm_rope_fwd(1, x.data_ptr(), w, y.data_ptr(), w, g.data_ptr(),  # noqa: E731
+                                               g.data_ptr(), *tail)
+        bwd = lambda: A.atom_k_qknorm_rope_bwd(1, dy.data_ptr(), w, x.data_ptr(), w, y.data_ptr(), w,  # noqa: E731
+                                               g.data_ptr(), g.data_ptr(), dg[0].data_ptr(), dg[1].data_ptr(), *tail,
+                                               ws.data_ptr(), ws.numel())
+        for name, fn, parts in (("turn", turn, 4), ("norms and turn", fwd, 6), ("their gradients", bwd, 8)):
+            us = _time(fn, iters)
+            print(f"rotary {name} rows={n} H={H} dh={dh}: {us:.1f} us, {2 * parts * n * H * dh / us / 1e3:.0f} GB/s "
+                  f"algorithmic", flush=True)
+
+
+def cross_attention(iters=20):
+    """Queries on encoder states of half their length, forward and gradients, and one token a sequence."""
+    for B, T, H, dh in ((8, 2048, 12, 64), (4, 2048, 16, 128), (2, 2048, 32, 128), (1, 2048, 40, 128)):
+        d, Tk = H * dh, T // 2
+        rnd = lambda n, s: (torch.randn(n, d, device="cuda") * s).to(torch.bfloat16)  # noqa: E731
+        k, v = rnd(B * Tk, 1.0), rnd(B * Tk, 1.0)
+        for Tq in (T, 1):
+            q, dout = rnd(B * Tq, 1.0), rnd(B * Tq, 1e-3)
+            o, dq, dk, dv = (torch.empty_like(t) for t in (q, q, k, v))
+            lse = torch.empty(B * Tq, H, device="cuda")
+            shape = A.atom_cross_shape(B, Tq, Tk, H, H, dh, B * Tq, B * Tk)
+            ws = torch.empty(max(16, A.atom_k_cross_attn_fwd_ws_bytes(1, shape),
+                                 A.atom_k_cross_attn_bwd_ws_bytes(1, shape)), device="cuda", dtype=torch.uint8)
+            ins = (1, shape, q.data_ptr(), d, k.data_ptr(), d, v.data_ptr(), d, dh ** -0.5, o.data_ptr(), d)
+            fwd = lambda: A.atom_k_cross_attn_fwd(*ins, lse.data_ptr(), ws.data_ptr(), ws.numel())  # noqa: E731
+            bwd = lambda: A.atom_k_cross_attn_bwd(*ins, dout.data_ptr(), d, lse.data_ptr(), dq.data_ptr(),  # noqa: E731
+                                                  d, dk.data_ptr(), d, dv.data_ptr(), d, ws.data_ptr(), ws.numel())
+            for name, fn, mult in (("fwd", fwd, 4),) + ((("bwd", bwd, 10),) if Tq > 1 else ()):
+                us = _time(fn, iters)
+                print(f"cross attention {name} B={B} Tq={Tq} Tk={Tk} H={H} dh={dh}: {us:.1f} us, "
+                      f"{mult * B * H * Tq * Tk * dh / us / 1e6:.0f} TFLOP/s (algorithmic), "
+                      f"{4 * B * (Tq + Tk) * d / us / 1e3:.0f} GB/s", flush=True)
+
+
 def main(argv):
     if not torch.cuda.is_available():
         raise SystemExit("kernel_bench needs a GPU")
@@ -215,6 +268,10 @@ def main(argv):
         linear_xent(int(argv[2]) if len(argv) > 2 else 10)
     elif what == "orthogonalize":
         orthogonalize(int(argv[2]) if len(argv) > 2 else 10)
+    elif what == "rotary":
+        rotary(int(argv[2]) if len(argv) > 2 else 50)
+    elif what == "cross_attention":
+        cross_attention(int(argv[2]) if len(argv) > 2 else 20)
     elif what == "layernorm":
         layernorm(int(argv[2]) if len(argv) > 2 else 50)
     else:

@@ -412,7 +412,7 @@ def test_refusals():
     _refused(A.atom_k_rope, *{**rope, "y": 4096, "ldy": 1024}.values())
     norm = dict(dtype=1, x=4096, ldx=1536, y=8192, ldy=1536, gq=4096, gk=4096, eps=1e-6, pos=None, freq=4096, mscale=1.0,
                 layout=0, rows=4, T=4, Hq=4, Hk=4, Hv=4, dh=128, rot=128)
-    for k, v in [("dtype", 7), ("x", None), ("y", None), ("ldx", 1535), ("ldy", 1535), ("gq", 4097), ("gk", 4097), ("eps", 0.0),
+    for k, v in [("dtype", 7), ("x", None), ("y", None), ("ldx", 1535), ("ldy", 1535), ("gq", 4097), ("gk", 4097), ("eps", 0.0), ("eps", 1e-39),
                  ("eps", -1.0), ("eps", math.nan), ("eps", math.inf), ("freq", None), ("T", 0), ("Hq", -1), ("Hk", -1),
                  ("Hv", -1), ("Hv", 1 << 16), ("dh", 1), ("rot", 200)]:
         _refused(A.atom_k_qknorm_rope_fwd, *{**norm, k: v}.values())
