@@ -56,9 +56,10 @@ ATOM_DEV int64_t at(const CrossArgs& a, const Seq& s, int hk, int p, int64_t ld)
   return (s.row0 + r.t) * ld + static_cast<int64_t>(hk * a.G + r.g) * DH;
 }
 
-// log-sum-exp in base 2 for the backward's exponents: a row that has none (no
+// log-sum-exp for the backward's exponents (in base 2): a row that has none (no
 // finite score) gets +infinity, and so no weight anywhere.
-ATOM_DEV float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * attn::LOG2E; }
+ATOM_DEV float lse_of(float lse) { return lse == -INFINITY ? INFINITY : lse; }
+ATOM_DEV float lse2_of(float lse) { return lse_of(lse) * attn::LOG2E; }
 
 // Queries whose D fits beside the stages of a small backward's workgroup.
 constexpr int SMALL_ROWS = 2048;
@@ -66,6 +67,15 @@ constexpr int SMALL_ROWS = 2048;
 // Where the running maximum starts: below every finite score, and finite, so
 // that a score of -infinity weighs 0 against it.
 constexpr float NO_MAX = -3e38f;
+
+// e^t for t <= 0 to an fp32 rounding or two: the part of t log2(e) that fp32 cuts
+// off goes into the result (with it cut, p is off by |t| 2^-24: at lse 8, 1e-6).
+// The fp32 kernels keep maxima and lse in natural units.
+ATOM_DEV float exp_near(float t) {
+  const float h = t * attn::LOG2E, r = __builtin_fmaf(t, attn::LOG2E, -h) + t * 1.92596299e-8f;
+  const float p = attn::ex2(h);
+  return t < -104.f ? 0.f : __builtin_fmaf(p, r * attn::LN2, p);
+}
 
 // A row's output from the sums of its ranges, in range order: 64 lanes a row.
 template <typename T, int DH>
@@ -79,11 +89,12 @@ __global__ void __launch_bounds__(256) cross_join_kernel(const CrossArgs a) {
   const bool on = p < qs.n * a.G;
   if (!on && a.q_start) return;
   constexpr int E = DH / 64;
+  constexpr bool NATURAL = sizeof(T) == 4;  // the maxima's units
   float m = NO_MAX, l = 0.f, o[E] = {};
   if (on) {
     for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.ml[2 * (s * n + r)]);
     for (int s = 0; s < a.splits; ++s) {
-      const float f = attn::ex2(a.ml[2 * (s * n + r)] - m);
+      const float t = a.ml[2 * (s * n + r)] - m, f = NATURAL ? exp_near(t) : attn::ex2(t);
       l += f * a.ml[2 * (s * n + r) + 1];
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] += f * a.part[(s * n + r) * DH + E * lane + e];
@@ -95,7 +106,7 @@ __global__ void __launch_bounds__(256) cross_join_kernel(const CrossArgs a) {
   for (int e = 0; e < E; ++e) static_cast<T*>(a.o)[lo + e] = from_f<T>(o[e] * inv);
   if (a.lse && lane == 0) {
     const Row w = row_of(a, p);
-    a.lse[(qs.row0 + w.t) * a.Hq + hk * a.G + w.g] = l == 0.f ? -INFINITY : (m + log2f(l)) * attn::LN2;
+    a.lse[(qs.row0 + w.t) * a.Hq + hk * a.G + w.g] = l == 0.f ? -INFINITY : NATURAL ? m + logf(l) : (m + log2f(l)) * attn::LN2;
   }
 }
 

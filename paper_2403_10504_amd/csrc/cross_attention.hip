@@ -279,13 +279,11 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
     step(None{}, z0, z1, kt);
   }
 
-  // padded queries of a padded batch get zeros (P up to Tq G)
-  const int p_end = a.q_start ? P : a.Tq * a.G;
+  if constexpr (SPLIT) {
 #pragma unroll
-  for (int g = 0; g < GR; ++g) {
-    const int pi = qw + g * 16 + lr;
-    const float l_tot = rows4_sum(l_i[g]);
-    if (SPLIT) {
+    for (int g = 0; g < GR; ++g) {
+      const int pi = qw + g * 16 + lr;
+      const float l_tot = rows4_sum(l_i[g]);
       if (pi >= P) continue;
       const int64_t n = static_cast<int64_t>(a.Tq) * a.G, r = (static_cast<int64_t>(split) * BH + bh) * n + pi;
 #pragma unroll
@@ -294,22 +292,43 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
         store_row4<float>(a.part + r * DH + c * 16 + 4 * lg, v);
       }
       if (lg == 0) a.ml[2 * r] = m_i[g], a.ml[2 * r + 1] = l_tot;
-      continue;
     }
-    if (pi >= p_end) continue;
+    return;
+  }
+  // Results go out through LDS (a wave's rows in the stages, which every wave is
+  // done with), so that a store covers whole rows instead of 32 bytes of each.
+  constexpr int WROWS = 16 * GR;
+  static_assert(NW * WROWS * RB <= 4 * F::TILE, "results in the stages' place");
+  uint8_t* mine = lds + w * WROWS * RB;
+  fence();
+  // padded queries of a padded batch get zeros (P up to Tq G)
+  const int p_end = a.q_start ? P : a.Tq * a.G;
+#pragma unroll
+  for (int g = 0; g < GR; ++g) {
+    const int row = g * 16 + lr, pi = qw + row;
+    const float l_tot = rows4_sum(l_i[g]);
     const bool none = l_tot == 0.f || pi >= P;  // no keys, or padding: zeros
     const float inv = 1.f / l_tot;
-    const Row rw = row_of(a, pi);
-    bf16_t* orow = static_cast<bf16_t*>(a.o) + (qs.row0 + rw.t) * a.ldo + static_cast<int64_t>(hk * a.G + rw.g) * DH;
 #pragma unroll
     for (int c = 0; c < NCT; ++c) {
       float v[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) v[r] = none ? 0.f : acc_o[g][c][r] * inv;
-      store_row4<bf16_t>(orow + c * 16 + 4 * lg, v);
+      const int chunk = (2 * c + (lg >> 1)) ^ (row & (F::CPR - 1));
+      store_row4<bf16_t>(reinterpret_cast<bf16_t*>(mine + row * RB + chunk * 16 + 8 * (lg & 1)), v);
     }
-    if (lg == 0 && a.lse)
+    if (lg == 0 && a.lse && pi < p_end) {
+      const Row rw = row_of(a, pi);
       a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g] = none ? -INFINITY : (m_i[g] + log2f(l_tot)) * LN2;
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < WROWS * F::CPR / 64; ++i) {
+    const int row = i * (64 / F::CPR) + lane / F::CPR, chunk = lane % F::CPR, pi = qw + row;
+    const uint4 v = *reinterpret_cast<const uint4*>(mine + row * RB + (chunk ^ (row & (F::CPR - 1))) * 16);
+    if (pi < p_end) *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.o) + at<DH>(a, qs, hk, pi, a.ldo) + chunk * 8) = v;
   }
 }
 

@@ -43,6 +43,15 @@ struct Tile {
   }
 };
 
+// Scores are sums of DH terms; each of two accumulators takes half of them, so
+// that fewer roundings meet the large partial sums (an instruction rounds after
+// each of its four products), and the instructions' chains are half as long.
+struct Halves {
+  f32x4_t x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  ATOM_DEV void add(int s, const Frag<float>& a, const Frag<float>& b) { mfma16(x[s & 1], a, b); }
+  ATOM_DEV f32x4_t sum() const { return x[0] + x[1]; }
+};
+
 struct Item {
   int x, split, bh, b, hk;
 };
@@ -75,7 +84,6 @@ __global__ void __launch_bounds__(256, 2) cross_fwd_f32_kernel(const CrossArgs a
   if (q0 >= P && (a.splits > 1 || a.q_start)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 15, lg = lane >> 4;
   const int pi = q0 + (FEW ? 0 : w * 16) + lr, j_w = FEW ? w * 16 : 0;
-  const float sc = a.scale * LOG2E;
   const float* kb = static_cast<const float*>(a.k) + ks.row0 * a.ldk + hk * DH;
   const float* vb = static_cast<const float*>(a.v) + ks.row0 * a.ldv + hk * DH;
   auto k_at = [&](int j) { return kb + j * a.ldk; };
@@ -111,20 +119,21 @@ __global__ void __launch_bounds__(256, 2) cross_fwd_f32_kernel(const CrossArgs a
     float p[JT][4], mx = -INFINITY;
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt) {
-      f32x4_t z = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      Halves zh;
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         Frag<float> kf;
         L::row(kf, Ks, j_w + jt * 16 + lr, 32 * s + 8 * lg);
-        mfma16(z, kf, qf[s]);
+        zh.add(s, kf, qf[s]);
       }
+      const f32x4_t z = zh.sum();
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         p[jt][r] = kt * BT + j_w + jt * 16 + 4 * lg + r < ks.n ? z[r] : -INFINITY;
         mx = fmaxf(mx, p[jt][r]);
       }
     }
-    const float m_new = fmaxf(m, rows4_max(mx) * sc), alpha = ex2(m - m_new);
+    const float m_new = fmaxf(m, rows4_max(mx) * a.scale), alpha = exp_near(m - m_new);
     m = m_new;
     l *= alpha;
 #pragma unroll
@@ -133,7 +142,7 @@ __global__ void __launch_bounds__(256, 2) cross_fwd_f32_kernel(const CrossArgs a
     for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[jt][r] = ex2(__builtin_fmaf(p[jt][r], sc, -m));
+        p[jt][r] = exp_near(__builtin_fmaf(p[jt][r], a.scale, -m));
         l += p[jt][r];
       }
     if constexpr (FEW) {
@@ -177,7 +186,7 @@ __global__ void __launch_bounds__(256, 2) cross_fwd_f32_kernel(const CrossArgs a
 #pragma unroll
     for (int v = 0; v < 3; ++v) {
       const float* o = sums + (v * 64 + lane) * (4 * NCT + 2);
-      const float m1 = fmaxf(m, o[4 * NCT]), f0 = ex2(m - m1), f1 = ex2(o[4 * NCT] - m1);
+      const float m1 = fmaxf(m, o[4 * NCT]), f0 = exp_near(m - m1), f1 = exp_near(o[4 * NCT] - m1);
       m = m1;
       l_tot = l_tot * f0 + o[4 * NCT + 1] * f1;
 #pragma unroll
@@ -211,7 +220,7 @@ __global__ void __launch_bounds__(256, 2) cross_fwd_f32_kernel(const CrossArgs a
   }
   if (lg == 0 && a.lse) {
     const Row rw = row_of(a, pi);
-    a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g] = none ? -INFINITY : (m + log2f(l_tot)) * LN2;
+    a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g] = none ? -INFINITY : m + logf(l_tot);
   }
 }
 
@@ -227,7 +236,6 @@ ATOM_DEV void dq_f32(float* Ks, float* Vs, const CrossArgs& a, int id) {
   const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 15, lg = lane >> 4;
   const int pi = q0 + w * 16 + lr;
-  const float sc = a.scale * LOG2E;
   const float* kb = static_cast<const float*>(a.k) + ks.row0 * a.ldk + hk * DH;
   const float* vb = static_cast<const float*>(a.v) + ks.row0 * a.ldv + hk * DH;
   auto k_at = [&](int j) { return kb + j * a.ldk; };
@@ -237,7 +245,7 @@ ATOM_DEV void dq_f32(float* Ks, float* Vs, const CrossArgs& a, int id) {
   float lse_i = INFINITY, del = 0.f;
   if (pi < P) {
     const Row rw = row_of(a, pi);
-    lse_i = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
+    lse_i = lse_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
   }
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
@@ -278,18 +286,19 @@ ATOM_DEV void dq_f32(float* Ks, float* Vs, const CrossArgs& a, int id) {
     float ds[4][4];
 #pragma unroll
     for (int jt = 0; jt < 4; ++jt) {
-      f32x4_t z = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      Halves zh, dh;
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         Frag<float> kf, vf;
         L::row(kf, Ks, jt * 16 + lr, 32 * s + 8 * lg);
         L::row(vf, Vs, jt * 16 + lr, 32 * s + 8 * lg);
-        mfma16(z, kf, qf[s]);
-        mfma16(dp, vf, of[s]);
+        zh.add(s, kf, qf[s]);
+        dh.add(s, vf, of[s]);
       }
+      const f32x4_t z = zh.sum(), dp = dh.sum();
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        ds[jt][r] = kt * BT + jt * 16 + 4 * lg + r < ks.n ? ex2(__builtin_fmaf(z[r], sc, -lse_i)) * (dp[r] - del) : 0.f;
+        ds[jt][r] = kt * BT + jt * 16 + 4 * lg + r < ks.n ? exp_near(__builtin_fmaf(z[r], a.scale, -lse_i)) * (dp[r] - del) : 0.f;
     }
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2) {
@@ -334,7 +343,6 @@ ATOM_DEV void dkdv_f32(float* Qs, float* Os, float* lse_s, float* del_s, float* 
   const int64_t n_p = static_cast<int64_t>(a.Tq) * a.G;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 15, lg = lane >> 4;
   const int kj = k0 + w * 16 + lr;
-  const float sc = a.scale * LOG2E;
   auto q_at = [&](int p) { return static_cast<const float*>(a.q) + at<DH>(a, qs, hk, p, a.ldq); };
   auto o_at = [&](int p) { return static_cast<const float*>(a.dout) + at<DH>(a, qs, hk, p, a.lddo); };
 
@@ -365,7 +373,7 @@ ATOM_DEV void dkdv_f32(float* Qs, float* Os, float* lse_s, float* del_s, float* 
       pre_del = 0.f;
       if (i < P) {
         const Row rw = row_of(a, i);
-        pre_lse = lse2_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
+        pre_lse = lse_of(a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g]);
         if constexpr (!OWN_D) pre_del = a.delta[it.bh * n_p + i];
       }
     }
@@ -398,27 +406,31 @@ ATOM_DEV void dkdv_f32(float* Qs, float* Os, float* lse_s, float* del_s, float* 
     if (tid < BT) lse_s[tid] = pre_lse, del_s[tid] = OWN_D ? d_own[(t - t0) * BT + tid] : pre_del;
     __syncthreads();
     if (t + 1 < t1) fetch(t + 1);
-    float p[4][4], ds[4][4];
+    const int steps = (P - t * BT + 15) / 16;  // of 16 queries; the rest of a last tile is left out
+    float p[4][4] = {}, ds[4][4] = {};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      f32x4_t z = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (i >= steps) continue;
+      Halves zh, dh;
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         Frag<float> qf, of;
         L::row(qf, Qs, i * 16 + lr, 32 * s + 8 * lg);
         L::row(of, Os, i * 16 + lr, 32 * s + 8 * lg);
-        mfma16(z, qf, kf[s]);
-        mfma16(dp, of, vf[s]);
+        zh.add(s, qf, kf[s]);
+        dh.add(s, of, vf[s]);
       }
+      const f32x4_t z = zh.sum(), dp = dh.sum();
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int il = i * 16 + 4 * lg + r;
-        p[i][r] = ex2(__builtin_fmaf(z[r], sc, -lse_s[il]));
+        p[i][r] = exp_near(__builtin_fmaf(z[r], a.scale, -lse_s[il]));
         ds[i][r] = p[i][r] * (dp[r] - del_s[il]);
       }
     }
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2) {
+      if (2 * s2 >= steps) continue;
       Frag<float> pf, df;
       frag_from_pair(pf, p, s2);
       frag_from_pair(df, ds, s2);
