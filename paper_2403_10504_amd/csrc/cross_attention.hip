@@ -30,6 +30,11 @@ ATOM_DEV void frag_row(Frag<bf16_t>& f, const CrossArgs& a, const bf16_t* base, 
   else frag_zero(f);
 }
 
+// Makes the compiler wait for a fragment's load here: it places its waits at the
+// first use, and one inside a tile loop, which it cannot count past the direct
+// loads that it does not see, is a wait for all of them in every tile.
+ATOM_DEV void settle(Frag<bf16_t>& f) { asm volatile("" : "+v"(f.v.x), "+v"(f.v.y), "+v"(f.v.z), "+v"(f.v.w)); }
+
 // Direct loads by a tile's base (scalar) and the lane's 32-bit offset in it
 // (leading dimensions below 2^24: 64 rows stay within 2^32 bytes).
 ATOM_DEV void lds_dma16_at(const void* base, uint32_t off, uint32_t lds) {
@@ -249,6 +254,10 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
     using Whole = std::integral_constant<int, 1>;
     using Last = std::integral_constant<int, 2>;
     fence();
+#pragma unroll
+    for (int g = 0; g < GR; ++g)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) settle(qf[g][s]);
     if (rg.t0 + 1 < rg.t1) load_k(rg.t0 + 1);
     scores(z0, rg.t0, [](int) {});
     if (rg.t0 * BT + BT > n_keys) mask(z0, rg.t0);
@@ -397,11 +406,15 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
       frag_row<DH>(of[g][s], a, static_cast<const bf16_t*>(a.dout), qs, hk, pi, P, a.lddo, 32 * s + 8 * lg);
       frag_row<DH>(f[s], a, static_cast<const bf16_t*>(a.o), qs, hk, pi, P, a.ldo, 32 * s + 8 * lg);
     }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) settle(qf[g][s]);
     del_i[g] = row_dot<NS>(f, of[g]);
     if (a.delta && lg == 0 && pi < P && split == 0) a.delta[bh * n_p + pi] = del_i[g];
 #pragma unroll
     for (int c = 0; c < NCT; ++c) acc[g][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
+#pragma unroll
+  for (int g = 0; g < GR; ++g) asm volatile("" : "+v"(lse_i[g]), "+v"(del_i[g]));
   if (!a.dq) return;
   auto rowfrag = [&](Frag<bf16_t>& f, const uint8_t* st, int jt, int s, bool dual) {
     const int row = jt * 16 + lr, chunk = 4 * s + lg;
@@ -637,6 +650,11 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
       }
     }
   }
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    settle(kf[s]);
+    settle(vf[s]);
+  }
   for (int qs0 = rg.t0; qs0 < rg.t1; qs0 += SUB) {
     const int cur = ((qs0 - rg.t0) / SUB) & 1;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -655,65 +673,45 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
       const float* lse_s = reinterpret_cast<const float*>(qst + 2 * F::TILE);
       const float* del_s = OWN_D ? d_own + (qs0 + u - rg.t0) * BT : lse_s + BT;
       float p[4][4], ds[4][4];
-      // keys past the end need no mask: their columns are never stored, and
-      // their fragments are zeros
-      if constexpr (DH == 128) {
-#pragma unroll
-        for (int it = 0; it < 4; ++it) {
-          Frag<bf16_t> qf[NS], of[NS];
-#pragma unroll
-          for (int s = 0; s < NS; ++s) {
-            rowfrag(qf[s], qst, it, s);
-            rowfrag(of[s], ost, it, s);
-          }
-          f32x4_t sa = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int s = 0; s < NS; ++s) {
-            mfma16(sa, qf[s], kf[s]);  // S[i][j]: lane holds key kj, queries 4lg + r
-            mfma16(dp, of[s], vf[s]);  // dP[i][j]
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int il = it * 16 + 4 * lg + r;
-            p[it][r] = ex2(__builtin_fmaf(sa[r], sc, -lse_s[il]));
-            ds[it][r] = p[it][r] * (dp[r] - del_s[il]);
-          }
-          // LDS reads stay in their 16-query step, else all are hoisted and spill
-          __builtin_amdgcn_sched_barrier(0x000A);
-        }
-      } else {
-        Frag<bf16_t> qf[2][NS], of[2][NS];
+      // Keys past the end need no mask: their columns are never stored, and
+      // their fragments are zeros.  Each step's LDS reads stand before the
+      // exponentials of the step before, and stay there (hoisted, they spill).
+      Frag<bf16_t> qf[NS], of[NS];
+      auto read = [&](int it) {
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          rowfrag(qf[0][s], qst, 0, s);
-          rowfrag(of[0][s], ost, 0, s);
+          rowfrag(qf[s], qst, it, s);
+          rowfrag(of[s], ost, it, s);
         }
+      };
+      constexpr int AHEAD = 2;
+      Frag<bf16_t> ot2[AHEAD], qt2[AHEAD];
+      read(0);
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-          if (it + 1 < 4) {
+      for (int it = 0; it < 4; ++it) {
+        f32x4_t sa = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-              rowfrag(qf[(it + 1) & 1][s], qst, it + 1, s);
-              rowfrag(of[(it + 1) & 1][s], ost, it + 1, s);
-            }
+        for (int s = 0; s < NS; ++s) {
+          mfma16(sa, qf[s], kf[s]);  // S[i][j]: lane holds key kj, queries 4lg + r
+          mfma16(dp, of[s], vf[s]);  // dP[i][j]
+        }
+        if (it + 1 < 4) {
+          read(it + 1);
+        } else {
+#pragma unroll
+          for (int n = 0; n < AHEAD; ++n) {
+            trfrag(ot2[n], ost, 0, n);
+            trfrag(qt2[n], qst, 0, n);
           }
-          f32x4_t sa = f32x4_t{0.f, 0.f, 0.f, 0.f}, dp = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        __builtin_amdgcn_sched_barrier(0x000A);
 #pragma unroll
-          for (int s = 0; s < NS; ++s) {
-            mfma16(sa, qf[it & 1][s], kf[s]);
-            mfma16(dp, of[it & 1][s], vf[s]);
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int il = it * 16 + 4 * lg + r;
-            p[it][r] = ex2(__builtin_fmaf(sa[r], sc, -lse_s[il]));
-            ds[it][r] = p[it][r] * (dp[r] - del_s[il]);
-          }
+        for (int r = 0; r < 4; ++r) {
+          const int il = it * 16 + 4 * lg + r;
+          p[it][r] = ex2(__builtin_fmaf(sa[r], sc, -lse_s[il]));
+          ds[it][r] = p[it][r] * (dp[r] - del_s[il]);
         }
       }
-      Frag<bf16_t> ot2[2], qt2[2];
-      trfrag(ot2[0], ost, 0, 0);
-      trfrag(qt2[0], qst, 0, 0);
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
         Frag<bf16_t> pf, dsf;
@@ -722,12 +720,12 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
 #pragma unroll
         for (int c = 0; c < NCT; ++c) {
           const int n = s2 * NCT + c;
-          if (n + 1 < 2 * NCT) {
-            trfrag(ot2[(n + 1) & 1], ost, (n + 1) / NCT, (n + 1) % NCT);
-            trfrag(qt2[(n + 1) & 1], qst, (n + 1) / NCT, (n + 1) % NCT);
+          mfma16(acc_dv[c], ot2[n % AHEAD], pf);   // dV^T[c][j]
+          mfma16(acc_dk[c], qt2[n % AHEAD], dsf);  // dK^T[c][j]
+          if (n + AHEAD < 2 * NCT) {
+            trfrag(ot2[n % AHEAD], ost, (n + AHEAD) / NCT, (n + AHEAD) % NCT);
+            trfrag(qt2[n % AHEAD], qst, (n + AHEAD) / NCT, (n + AHEAD) % NCT);
           }
-          mfma16(acc_dv[c], ot2[n & 1], pf);   // dV^T[c][j]
-          mfma16(acc_dk[c], qt2[n & 1], dsf);  // dK^T[c][j]
         }
       }
     }
@@ -754,21 +752,13 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
   }
 }
 
-// Groups of 16 queries a wave, waves, waves on a SIMD, and tiles a barrier, of
-// the dQ kernel's larger workgroups.
-template <int DH>
-struct DqBig {
-  static constexpr int GR = 2, NW = DH == 64 ? 4 : 8, WPS = 2, SUB = 1;
-  static constexpr int ROWS = 16 * GR * NW;
-};
-
-// Large problems: a launch each, workgroups of 128 rows, two tiles a barrier.
-template <int DH>
-__global__ void __launch_bounds__(64 * DqBig<DH>::NW, DqBig<DH>::WPS) cross_dq_kernel(const CrossArgs a) {
-  using C = DqBig<DH>;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * C::SUB * FwdDL<DH>::STAGE];
+// Large problems: a launch each.  dQ in workgroups of NW waves of 32 queries, dK
+// and dV of eight waves of 16 keys, two tiles a barrier.
+template <int DH, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) cross_dq_kernel(const CrossArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * FwdDL<DH>::STAGE];
   const int item = item_of(a.n_x * a.B * a.Hk * a.splits, blockIdx.x);
-  if (item >= 0) dq_body<DH, C::GR, C::NW, C::SUB>(lds, a, item);
+  if (item >= 0) dq_body<DH, 2, NW, 1>(lds, a, item);
 }
 template <int DH>
 __global__ void __launch_bounds__(512, DH == 64 ? 4 : 2) cross_dkdv_kernel(const CrossArgs a) {
@@ -802,11 +792,14 @@ using namespace cross;
 
 // The shape of each launch: blocks of rows, ranges, and the workspace.
 struct Plan {
-  bool small;     // blocks of 64 rows instead of 128
+  int blk;  // rows of a workgroup: 64, 128 or 256
   int n_x, splits;
 };
 
 constexpr int64_t CUS = 256;
+// A workgroup's time alone on its CU, of the time beside another, and what the
+// smaller workgroups cost in full rounds.
+constexpr double ALONE = 0.6, SHARE = 1.05;
 // Tiles of 64 x 64 for each of two workgroups a CU, of both sides, up to which
 // the backward is one launch.
 constexpr int64_t SMALL_TILES_64 = 12, SMALL_TILES_128 = 8;
@@ -819,28 +812,30 @@ constexpr int64_t RANGE_GAIN = 2;
 // more ranges, so that many loads are in flight and long sequences do not wait
 // for one workgroup.
 constexpr int64_t TOKEN_WGS = 1024, TOKEN_TILES = 8;
-Plan plan_of(int64_t rows, int64_t heads, int64_t other, int big) {
+// Rounds of workgroups that a launch of n takes where `each` share a CU; a last
+// round that leaves every CU at most one of two is shorter.
+double rounds(int64_t n, int each) {
+  const int64_t slots = CUS * each, rem = n % slots;
+  return static_cast<double>(n / slots) + (rem == 0 ? 0.0 : each == 2 && rem <= CUS ? ALONE : 1.0);
+}
+// Of workgroups of 256 rows, one a CU, and of 128, two: the one whose rounds take
+// less, of which both take the same but for SHARE.
+int rows_of(int64_t rows, int64_t heads) {
+  const double big = rounds((rows + 255) / 256 * heads, 1), mid = SHARE * rounds((rows + 127) / 128 * heads, 2);
+  return mid < big ? 128 : 256;
+}
+Plan plan_of(int64_t rows, int64_t heads, int64_t other, bool most64, int dh) {
   Plan p{};
-  const int64_t n_big = (rows + big - 1) / big * heads;
-  p.small = n_big < CUS || rows <= 64;
-  const int64_t blk = p.small ? 64 : big;
-  p.n_x = static_cast<int>((rows + blk - 1) / blk);
+  p.blk = most64 || rows <= 64 || (rows + 127) / 128 * heads < CUS ? 64 : dh == 64 ? 128 : rows_of(rows, heads);
+  p.n_x = static_cast<int>((rows + p.blk - 1) / p.blk);
   const int64_t n = p.n_x * heads, tiles = (other + attn::BT - 1) / attn::BT;
   const int64_t want = rows <= 64 ? TOKEN_WGS : n < CUS ? 2 * CUS : 0, least = rows <= 64 ? TOKEN_TILES : 2;
   p.splits = n > 0 ? static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want / n, tiles / least))) : 1;
   return p;
 }
 
-// The forward's larger workgroups: groups of 16 rows a wave, waves, waves on a SIMD.
-template <int DH>
-struct FwdBig {
-  static constexpr int GR = 2, NW = DH == 64 ? 4 : 8, WPS = 2;
-  static constexpr int ROWS = 16 * GR * NW;
-};
-
 Plan fwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
-  return plan_of(static_cast<int64_t>(Tq) * G, static_cast<int64_t>(B) * Hk, Tk,
-                 dtype != DT_BF16 ? 64 : dh == 64 ? FwdBig<64>::ROWS : FwdBig<128>::ROWS);
+  return plan_of(static_cast<int64_t>(Tq) * G, static_cast<int64_t>(B) * Hk, Tk, dtype != DT_BF16, dh);
 }
 // The backward's two sides: q (blocks of queries, ranges of keys) and k.
 struct BwdPlan {
@@ -859,9 +854,11 @@ BwdPlan bwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
   BwdPlan p{};
   const int64_t fair = (2 * tq * tk * heads + 2 * CUS - 1) / (2 * CUS);
   p.small = fair <= (dh == 64 ? SMALL_TILES_64 : SMALL_TILES_128);
-  const int blk = p.small || dtype != DT_BF16 ? 64 : 128, blk_q = blk == 64 ? 64 : dh == 64 ? DqBig<64>::ROWS : DqBig<128>::ROWS;
-  p.q.n_x = static_cast<int>((rows + blk_q - 1) / blk_q);
-  p.k.n_x = static_cast<int>((Tk + blk - 1) / blk);
+  const bool most64 = p.small || dtype != DT_BF16;
+  p.q.blk = most64 ? 64 : dh == 64 ? 128 : rows_of(rows, heads);
+  p.k.blk = most64 ? 64 : 128;
+  p.q.n_x = static_cast<int>((rows + p.q.blk - 1) / p.q.blk);
+  p.k.n_x = static_cast<int>((Tk + p.k.blk - 1) / p.k.blk);
   if (p.small) {
     // both sides share two workgroups a CU
     p.q.splits = ranges_of(tk, fair, 2);
@@ -922,17 +919,22 @@ __global__ void __launch_bounds__(256) cross_sum_kernel(const CrossArgs a, int64
   }
 }
 
-template <int DH>
-void fwd_bf16(const CrossArgs& a, bool small, hipStream_t s) {
-  using C = FwdBig<DH>;
-  const dim3 grid(grid_of(a, a.n_x, a.splits)), big(64 * C::NW), four(256);
-  if (a.splits > 1) {
-    if (small) hipLaunchKernelGGL((cross_fwd_kernel<DH, 1, 4, 2, true>), grid, four, 0, s, a);
-    else hipLaunchKernelGGL((cross_fwd_kernel<DH, C::GR, C::NW, C::WPS, true>), grid, big, 0, s, a);
+template <int DH, int GR, int NW>
+void fwd_launch(const CrossArgs& a, hipStream_t s) {
+  const dim3 grid(grid_of(a, a.n_x, a.splits)), block(64 * NW);
+  if (a.splits > 1) hipLaunchKernelGGL((cross_fwd_kernel<DH, GR, NW, 2, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((cross_fwd_kernel<DH, GR, NW, 2, false>), grid, block, 0, s, a);
+}
+hipError_t fwd_bf16(const CrossArgs& a, int blk, int dh, hipStream_t s) {
+  if (dh == 64) {
+    if (blk == 64) fwd_launch<64, 1, 4>(a, s);
+    else fwd_launch<64, 2, 4>(a, s);
   } else {
-    if (small) hipLaunchKernelGGL((cross_fwd_kernel<DH, 1, 4, 2, false>), grid, four, 0, s, a);
-    else hipLaunchKernelGGL((cross_fwd_kernel<DH, C::GR, C::NW, C::WPS, false>), grid, big, 0, s, a);
+    if (blk == 64) fwd_launch<128, 1, 4>(a, s);
+    else if (blk == 128) fwd_launch<128, 2, 4>(a, s);
+    else fwd_launch<128, 2, 8>(a, s);
   }
+  return hipGetLastError();
 }
 
 unsigned rows_grid(int64_t rows) { return static_cast<unsigned>((rows + 3) / 4); }
@@ -946,17 +948,22 @@ hipError_t join(const CrossArgs& a, int dh, hipStream_t s) {
 }
 
 template <int DH>
-hipError_t bwd_bf16(const CrossArgs& a, bool small, hipStream_t s) {
+hipError_t bwd_bf16(const CrossArgs& a, const BwdPlan& p, hipStream_t s) {
   const unsigned nq = a.dq || a.delta ? grid_of(a, a.n_x, a.splits) : 0, nk = a.dk ? grid_of(a, a.k_x, a.k_splits) : 0;
-  if (small) {
+  if (p.small) {
     if (nq + nk) hipLaunchKernelGGL(cross_bwd_small_kernel<DH>, dim3(nq + nk), dim3(256), 0, s, a);
     return hipGetLastError();
   }
   // dQ first: it computes D
-  if (nq) hipLaunchKernelGGL(cross_dq_kernel<DH>, dim3(nq), dim3(64 * DqBig<DH>::NW), 0, s, a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !nk) return e;
-  hipLaunchKernelGGL(cross_dkdv_kernel<DH>, dim3(nk), dim3(512), 0, s, a);
+  if (nq) {
+    if constexpr (DH == 128) {
+      if (p.q.blk == 256) hipLaunchKernelGGL((cross_dq_kernel<DH, 8>), dim3(nq), dim3(512), 0, s, a);
+    }
+    if (p.q.blk == 128) hipLaunchKernelGGL((cross_dq_kernel<DH, 4>), dim3(nq), dim3(256), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (nk) hipLaunchKernelGGL(cross_dkdv_kernel<DH>, dim3(nk), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 
@@ -1024,9 +1031,7 @@ hipError_t cross_attn_fwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t
   }
   hipError_t e;
   if (dtype == DT_BF16) {
-    if (dh == 64) fwd_bf16<64>(a, p.small, s);
-    else fwd_bf16<128>(a, p.small, s);
-    e = hipGetLastError();
+    e = fwd_bf16(a, p.blk, dh, s);
   } else {
     e = cross_fwd_f32(a, dh, s);
   }
@@ -1046,7 +1051,7 @@ hipError_t cross_attn_bwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t
   if (a.Tk == 0) a.dk = a.dv = nullptr;
   hipError_t e;
   if (dtype != DT_BF16) e = cross_bwd_f32(a, dh, p.small, s);
-  else e = dh == 64 ? bwd_bf16<64>(a, p.small, s) : bwd_bf16<128>(a, p.small, s);
+  else e = dh == 64 ? bwd_bf16<64>(a, p, s) : bwd_bf16<128>(a, p, s);
   if (e != hipSuccess) return e;
   return dtype == DT_BF16 ? sum<bf16_t>(a, dh, s) : sum<float>(a, dh, s);
 }

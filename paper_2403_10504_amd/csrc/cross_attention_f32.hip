@@ -406,11 +406,9 @@ ATOM_DEV void dkdv_f32(float* Qs, float* Os, float* lse_s, float* del_s, float* 
     if (tid < BT) lse_s[tid] = pre_lse, del_s[tid] = OWN_D ? d_own[(t - t0) * BT + tid] : pre_del;
     __syncthreads();
     if (t + 1 < t1) fetch(t + 1);
-    const int steps = (P - t * BT + 15) / 16;  // of 16 queries; the rest of a last tile is left out
-    float p[4][4] = {}, ds[4][4] = {};
+    float p[4][4], ds[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (i >= steps) continue;
       Halves zh, dh;
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
@@ -430,7 +428,6 @@ ATOM_DEV void dkdv_f32(float* Qs, float* Os, float* lse_s, float* del_s, float* 
     }
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2) {
-      if (2 * s2 >= steps) continue;
       Frag<float> pf, df;
       frag_from_pair(pf, p, s2);
       frag_from_pair(df, ds, s2);
