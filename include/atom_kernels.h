@@ -14,7 +14,9 @@
  * are chosen by them (a product by M, N, K, epilogue and workspace; a head's
  * attention beyond 256 rows by the number of heads in the call; a row's
  * LayerNorm gradient at 2048 < d <= 4096 by the number of rows; column sums by
- * the number of rows).  Rows of different calls are equal to rounding only.
+ * the number of rows; cross attention by its whole shape; gradients of norms by
+ * the number of rows and heads, and a head's sums by the alignment of its
+ * buffers).  Rows of different calls are equal to rounding only.
  */
 #ifndef ATOM_KERNELS_H
 #define ATOM_KERNELS_H

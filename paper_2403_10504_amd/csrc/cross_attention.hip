@@ -12,6 +12,13 @@
 // the second product's operand; every output has one owner, so no atomics.  p and
 // ds are rounded to bf16 for the second products (the operands' type: half a step
 // of 2^-8 in each term, in random directions); sums and statistics are fp32.
+//
+// What bounds it: long sequences the vector unit and the matrix cores, which
+// share a SIMD's issue slots (2 x 2048 queries, 4096 keys, 32 heads of 128: 259 us,
+// 1.06 PFLOP/s, matrix cores busy 48 %; a library product here 1.43); short ones
+// the bytes of q and o and the start of a workgroup (8 x 2048 queries on 48 to 500
+// keys, 12 heads of 64: 31 us, of which 15 remain with 64 keys); single tokens the
+// keys' bytes (8 x 1 on 261 to 2048 keys, 40 heads of 128: 51 us, 4.5 TB/s).
 #include "cross_attention.h"
 
 #include "../../include/atom.h"
@@ -57,6 +64,11 @@ ATOM_DEV Range range_of(int n_rows, int splits, int s) {
 // A tile's scores are computed one tile ahead: the matrix instructions of
 // S(t+1) = K Q^T stand between the exponentials of P(t), which need nothing of
 // them, so that both units work in one wave.  K is staged one tile ahead of V.
+// (2 x 2048 x 4096, 32 heads of 128: 16 rows a wave, one tile after the other 311
+// us, 32 rows 308 to 310; ahead 275 in 256-row workgroups, 289 in 128-row ones, 360
+// with 16 rows a wave; without branches between the score and the second product 260
+// and 275.  Orders asked for by scheduling groups: 266 to 270; two score tiles' sums
+// side by side, 3 to 6 fragments of V ahead: within 2 us.)
 template <int DH, int GR, int NW, int WPS, bool SPLIT>
 __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs a) {
   constexpr int NT = 64 * NW;
@@ -343,6 +355,9 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
 
 // ------------------------------------------------------------ backward: dQ
 // Also D of every row, for a dK/dV kernel that reads it (a.dq null: D alone).
+// 32 queries a wave in large problems, which halves the LDS reads of K and V (2 x
+// 2048 x 1500, 32 heads of 128: 203 us with 16, 155 with 32: 0.98 PFLOP/s of its
+// three products).
 template <int DH, int GR, int NW, int SUB>
 ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
   using F = FwdDL<DH>;
@@ -529,6 +544,12 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
 // -------------------------------------------------------- backward: dK, dV
 // OWN_D: D of the range's queries is computed here, from O and dO, into d_own
 // (LDS); otherwise it is read from a.delta.
+// Two waves a SIMD, which the accumulators of dK and dV and the fragments of K and V
+// leave room for, do not hide all of the LDS reads and exponentials (2 x 2048 x 1500,
+// 32 heads of 128: 219 us, 0.92 PFLOP/s of its four products, matrix cores busy 37 %,
+// LDS 41 %).  Slower there: 32 keys a wave at one wave a SIMD (250), row fragments
+// of two steps held (233), the second products beside the next step's scores (235),
+// workgroups of four waves (246), three or four fragments ahead (224).
 template <int DH, int W, int SUB, bool OWN_D>
 ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item) {
   using F = FwdDL<DH>;
@@ -769,13 +790,15 @@ __global__ void __launch_bounds__(512, DH == 64 ? 4 : 2) cross_dkdv_kernel(const
 }
 
 // Small ones: both in one launch, workgroups of 64 rows, D computed on both
-// sides, so that neither waits for the other and twice as many CUs have work.
+// sides, so that neither waits for the other and twice as many CUs have work
+// (packed 333, 255 and 270 queries of 16 heads on 200, 39 and 108 keys of 4 heads of
+// 128: 34.8 us in two launches, 27 in one).
 template <int DH>
 __global__ void __launch_bounds__(256, DH == 64 ? 3 : 2) cross_bwd_small_kernel(const CrossArgs a) {
   constexpr int STAGES = 2 * dkdv_stage<DH>();
   static_assert(dkdv_stage<DH>() >= FwdDL<DH>::STAGE, "stages");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES + SMALL_ROWS * 4];
-// the first part of the grid dK and dV, the rest dQ: every XCD has both
+  // the first part of the grid dK and dV, the rest dQ: every XCD has both
   const int n_k = a.dk ? a.k_x * a.B * a.Hk * a.k_splits : 0, n_q = a.dq ? a.n_x * a.B * a.Hk * a.splits : 0;
   const int k_end = (n_k + 7) & ~7, id = blockIdx.x;
   const int item = id < k_end ? item_of(n_k, id) : item_of(n_q, id - k_end);
@@ -798,19 +821,28 @@ struct Plan {
 
 constexpr int64_t CUS = 256;
 // A workgroup's time alone on its CU, of the time beside another, and what the
-// smaller workgroups cost in full rounds.
+// smaller workgroups cost in full rounds (2048 x 1024, heads of 128, us, forward in
+// 256-row and in 128-row workgroups: 32 heads 45.7 and 46.0, 36: 70.7 and 59.2, 40:
+// 68.9 and 58.1, 48: 69.3 and 60.5, 56: 73.7 and 73.5, 100: 144.7 and 127.4; two full
+// rounds of 4096 keys 266 and 276.  dQ alike: 40 heads 104 and 82, 56: 111 and 107).
 constexpr double ALONE = 0.6, SHARE = 1.05;
 // Tiles of 64 x 64 for each of two workgroups a CU, of both sides, up to which
-// the backward is one launch.
+// the backward is one launch.  In two launches and in one, us: heads of 128, 8
+// tiles (2 x 512 x 512, 16 heads) 47 and 34, 12 tiles 44 and 48 (3 x 512 x 512), 55
+// and 52 (1000 x 333, 32 heads), 16 tiles 49 and 59, 32 tiles 75 and 100; heads of
+// 64, 16 tiles 28 and 34, 22 to 24 tiles 46 and 43, 47 and 45.
 constexpr int64_t SMALL_TILES_64 = 12, SMALL_TILES_128 = 8;
-// Tiles that ranges have to save a workgroup.
+// Tiles that ranges have to save a workgroup (1 to 6 measured the same).
 constexpr int64_t RANGE_GAIN = 2;
 
-// Blocks of `big` rows where they fill the card, of 64 where not; with few of
+// Blocks of 128 or 256 rows where they fill the card, of 64 where not; with few of
 // those too, the other side in ranges.  One block of rows for each sequence and
 // head is a call that reads its keys for little work (single tokens): it takes
 // more ranges, so that many loads are in flight and long sequences do not wait
-// for one workgroup.
+// for one workgroup.  (Workgroups wanted, and tiles of keys a range has at least,
+// us of 8 x 1 x 2048 of 40 heads of 128, ragged, and of 16 x 1 x 4000 of 32 heads on
+// 4: one range 72, -; 1024, 8: 52.3, 33.4; 1024, 4: 52.5, 39.1; 2048, 4: 53.8, 39.3;
+// 2048, 2: 53.8, 48.7; 4096, 2: 61.7, 49.0.)
 constexpr int64_t TOKEN_WGS = 1024, TOKEN_TILES = 8;
 // Rounds of workgroups that a launch of n takes where `each` share a CU; a last
 // round that leaves every CU at most one of two is shorter.
