@@ -37,20 +37,23 @@ class Case:
         self.__dict__.update(dtype=dtype, B=B, Tq=Tq, Tk=Tk, Hq=Hq, Hk=Hk, dh=dh, rows=rows)
         self.scale = float(np.float32(dh ** -0.5))
 
-        def side(T, given, lo):
-            if rows == "full":
+        # how each side's sequences lie: "mixed" is padded queries on packed keys
+        self.lay = {k: (("padded", "packed")[k == "k"] if rows == "mixed" else rows) for k in "qk"}
+
+        def side(T, given, lay):
+            if lay == "full":
                 n = [T] * B
             else:
-                n = list(given) if given is not None else [T] + [int(v) for v in r.integers(lo, T + 1, B - 1)]
-            if rows != "packed":
+                n = list(given) if given is not None else [T] + [int(v) for v in r.integers(0, T + 1, B - 1)]
+            if lay != "packed":
                 return n, [b * T for b in range(B)], B * T
             start = [3]
             for v in n[:-1]:
                 start.append(start[-1] + v + 2)
             return n, start, start[-1] + n[-1] + 4
 
-        self.qn, self.qs, self.nq = side(Tq, q_len, 0)
-        self.kn, self.ks, self.nk = side(Tk, k_len, 0)
+        self.qn, self.qs, self.nq = side(Tq, q_len, self.lay["q"])
+        self.kn, self.ks, self.nk = side(Tk, k_len, self.lay["k"])
         i32 = lambda v: t.tensor(v, device="cuda", dtype=t.int32)  # noqa: E731
         self.idx = dict(q_start=i32(self.qs), q_len=i32(self.qn), k_start=i32(self.ks), k_len=i32(self.kn))
 
@@ -66,10 +69,11 @@ class Case:
         self.dout = rows_of(self.nq, Hq, self.qs, self.qn, 0.1)
         self.pad = pad
         ptr = {k: v.data_ptr() for k, v in self.idx.items()}
-        if rows != "packed":
-            ptr.update(q_start=None, k_start=None)
-        if rows == "full":
-            ptr.update(q_len=None, k_len=None)
+        for k, lay in self.lay.items():
+            if lay != "packed":
+                ptr[k + "_start"] = None
+            if lay == "full":
+                ptr[k + "_len"] = None
         self.shape = A.atom_cross_shape(B, Tq, Tk, Hq, Hk, dh, self.nq, self.nk, **ptr)
 
     def empty(self, like):
@@ -121,7 +125,7 @@ class Case:
         on[n] = False
         rest = x[~on][:, :width]
         keep = FILL
-        if self.rows != "packed":
+        if self.lay[side] != "packed":
             assert bool((rest[:-1] == 0).all())
             rest = rest[-1:]
         assert bool((rest == keep).all()) and bool((x[:, width:] == keep).all())
@@ -174,7 +178,11 @@ SHAPES = [
     (1, 65, 65, 2, 2, 128, "full", 0), (5, 33, 130, 5, 5, 64, "padded", 0), (4, 130, 129, 6, 2, 128, "packed", 8),
     (4, 129, 1000, 4, 4, 64, "padded", 0), (1, 3, 4100, 4, 2, 128, "full", 0), (2, 500, 17, 40, 5, 64, "packed", 0),
     (9, 200, 200, 16, 16, 128, "padded", 0), (12, 150, 90, 24, 24, 64, "packed", 8), (1, 700, 3, 1, 1, 128, "full", 0),
-    (2, 1024, 260, 16, 4, 64, "full", 0), (2, 300, 700, 40, 40, 128, "full", 0)]
+    (2, 1024, 260, 16, 4, 64, "full", 0), (2, 300, 700, 40, 40, 128, "full", 0),
+    # workgroups of 128 rows at d_h 128; one head of keys for 64; D of more queries than one range holds; many ranges
+    (5, 259, 70, 64, 64, 128, "padded", 0), (2, 40, 200, 64, 1, 128, "packed", 0), (1, 2100, 130, 8, 1, 64, "full", 0),
+    (3, 60, 150, 6, 2, 64, "mixed", 0), (3, 7, 1000, 6, 2, 128, "mixed", 8), (1, 16, 3000, 1, 1, 64, "full", 0),
+    (1, 17, 3000, 1, 1, 128, "full", 0), (2, 2000, 64, 2, 1, 128, "full", 0)]
 
 
 @pytest.mark.gpu
@@ -187,7 +195,7 @@ def test_forward(dtype, B, Tq, Tk, Hq, Hk, dh, rows, pad):
     c.fwd(o, lse)
     _check_fwd(c, o, lse)
     on = c.covered(c.nq, c.qs, c.qn)[:c.nq]
-    assert bool((lse[:c.nq][~on] == (FILL if rows == "packed" else -math.inf)).all()) and bool((lse[c.nq] == FILL).all())
+    assert bool((lse[:c.nq][~on] == (FILL if c.lay["q"] == "packed" else -math.inf)).all()) and bool((lse[c.nq] == FILL).all())
     # without lse; again: the same bits
     o2 = c.empty(c.q)
     c.fwd(o2, None)
