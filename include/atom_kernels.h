@@ -186,9 +186,10 @@ typedef struct {
  * leading dimensions multiples of 8 (bf16) or 4 (fp32), below 2^24; tensors and ws
  * 16-byte aligned; less than 2^26 pairs of query and head, and of key and head of keys, in
  * padded lengths; Tq (Hq/Hk)^2 < 2^32, and less than 2^22 workgroups of 64 rows.
- * o must not overlap the inputs.  ws: device scratch of at least the bytes
- * that the query returns (0: none needed, or sizes refused); calls that may
- * overlap need scratch of their own. */
+ * o must not overlap the inputs.  Finite scores have to be below 2^30 in magnitude
+ * (beyond, the exponent's rounding alone overflows).  ws: device scratch of at least
+ * the bytes that the query returns (0: none needed, or sizes refused); calls that
+ * may overlap need scratch of their own. */
 uint64_t atom_k_cross_attn_fwd_ws_bytes(int dtype, const atom_cross_shape* shape);
 int atom_k_cross_attn_fwd(int dtype, const atom_cross_shape* shape, const void* q, int64_t ldq, const void* k,
                           int64_t ldk, const void* v, int64_t ldv, float scale, void* o, int64_t ldo, float* lse,
@@ -197,7 +198,8 @@ int atom_k_cross_attn_fwd(int dtype, const atom_cross_shape* shape, const void* 
 /* Backward, from the forward's o and lse and the gradient dout of o, with the same
  * shape and scale: with p = exp(z - lse) and D = sum_c dout o,
  *   dv = p^T dout,  ds = p (dout v^T - D),  dq = scale ds k,  dk = scale ds^T q,
- * dk and dv summed over the heads that share them, in a fixed order.  dq may be
+ * dk and dv summed over the heads that share them, in a fixed order.  lse being
+ * fp32, p is off by up to |lse| 2^-22 of itself (scores in the thousands: 10^-3).  dq may be
  * NULL (not wanted), or dk and dv both.  The gradients must not overlap the inputs
  * or one another.  Requirements as above, for every tensor. */
 uint64_t atom_k_cross_attn_bwd_ws_bytes(int dtype, const atom_cross_shape* shape);

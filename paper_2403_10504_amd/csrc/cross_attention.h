@@ -77,12 +77,15 @@ ATOM_DEV float exp_near(float t) {
   return t < -104.f ? 0.f : __builtin_fmaf(p, r * attn::LN2, p);
 }
 
-// A row's output from the sums of its ranges, in range order: 64 lanes a row.
-template <typename T, int DH>
-__global__ void __launch_bounds__(256) cross_join_kernel(const CrossArgs a) {
-  const int lane = threadIdx.x & 63;
+// A row's output from the sums of its ranges: W waves a row, each with every W-th
+// range in order, then the waves in order.  A lane takes the weight of one range in
+// 64, the wave their sums, eight loads in flight.
+template <typename T, int DH, int W>
+__global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) cross_join_kernel(const CrossArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t P = static_cast<int64_t>(a.Tq) * a.G, n = P * a.B * a.Hk;
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t r = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x;
+  const int first = W == 1 ? 0 : wave;
   if (r >= n) return;
   const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh % a.B, hk = bh / a.B;
   const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b);
@@ -92,12 +95,38 @@ __global__ void __launch_bounds__(256) cross_join_kernel(const CrossArgs a) {
   constexpr bool NATURAL = sizeof(T) == 4;  // the maxima's units
   float m = NO_MAX, l = 0.f, o[E] = {};
   if (on) {
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.ml[2 * (s * n + r)]);
-    for (int s = 0; s < a.splits; ++s) {
-      const float t = a.ml[2 * (s * n + r)] - m, f = NATURAL ? exp_near(t) : attn::ex2(t);
-      l += f * a.ml[2 * (s * n + r) + 1];
+    for (int s = lane; s < a.splits; s += 64) m = fmaxf(m, a.ml[2 * (s * n + r)]);
+    m = wave_max(m);
+    for (int s0 = first; s0 < a.splits; s0 += 64 * W) {
+      const int s = s0 + lane * W, count = min(64, (a.splits - s0 + W - 1) / W);
+      float f = 0.f;
+      if (s < a.splits) {
+        const float t = a.ml[2 * (s * n + r)] - m;
+        f = NATURAL ? exp_near(t) : attn::ex2(t);
+        l += f * a.ml[2 * (s * n + r) + 1];
+      }
+      const float* part = a.part + (s0 * n + r) * DH + E * lane;
+#pragma unroll 8
+      for (int i = 0; i < count; ++i) {
+        const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i));
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] += f * a.part[(s * n + r) * DH + E * lane + e];
+        for (int e = 0; e < E; ++e) o[e] += fi * part[i * (W * n * DH) + e];
+      }
+    }
+    l = wave_sum(l);
+  }
+  if constexpr (W > 1) {
+    __shared__ float sums[W][64][E + 1];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[wave][lane][e] = o[e];
+    sums[wave][lane][E] = l;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += sums[w][lane][e];
+      l += sums[w][lane][E];
     }
   }
   const int64_t lo = at<DH>(a, qs, hk, p, a.ldo) + E * lane;

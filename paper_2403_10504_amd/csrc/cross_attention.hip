@@ -820,12 +820,63 @@ struct Plan {
 };
 
 constexpr int64_t CUS = 256;
-// A workgroup's time alone on its CU, of the time beside another, and what the
-// smaller workgroups cost in full rounds (2048 x 1024, heads of 128, us, forward in
-// 256-row and in 128-row workgroups: 32 heads 45.7 and 46.0, 36: 70.7 and 59.2, 40:
-// 68.9 and 58.1, 48: 69.3 and 60.5, 56: 73.7 and 73.5, 100: 144.7 and 127.4; two full
-// rounds of 4096 keys 266 and 276.  dQ alike: 40 heads 104 and 82, 56: 111 and 107).
-constexpr double ALONE = 0.6, SHARE = 1.05;
+// What a launch takes, in us, for the choice of its workgroups' rows and ranges: a
+// workgroup that has its CU to itself takes start + tile for each tile of the other
+// side, w of them on a CU share w times as much (where several fit; where one does,
+// they follow each other), and a last round that leaves most CUs idle takes `last`
+// of a full one.  Measured with all CUs busy, and rounded.  (us, heads of 128, forward
+// in 256-row and in 128-row workgroups: 2048 x 1024, 32 heads 45.7 and 46.0, 40: 68.9
+// and 58.1, 56: 73.7 and 73.5; 20,000 x 300, 16 heads 95 and 84; 2 x 2048 x 4096, 32
+// heads 266 and 276.  Heads of 64, 128 and 64 rows: 8 x 300 x 1500, 12 heads 37 and 27;
+// 8 x 1024 x 1024 38 and 42.  dQ in 256 and 128 rows, 40 heads 104 and 82.)
+struct Cost {
+  int blk;  // rows; 0: no such kernel
+  double tile, start, share, last;
+};
+using Costs = Cost[3];
+constexpr Costs FWD[2] = {{{64, 0.45, 1.2, 0.78, 0.55}, {128, 0.76, 1.8, 0.77, 0.55}, {}},
+                          {{64, 0.92, 2.0, 0.76, 0.55}, {128, 1.28, 2.75, 0.91, 0.55}, {256, 2.2, 7.5, 1.0, 0.55}}};
+constexpr Costs DQ[2] = {{{128, 1.15, 2.0, 0.77, 0.55}, {}, {}},
+                         {{128, 1.6, 3.0, 0.94, 0.55}, {256, 2.65, 10.0, 1.0, 1.0}, {}}};
+constexpr Costs DKDV[2] = {{{128, 1.5, 3.0, 0.77, 0.55}, {}, {}}, {{128, 1.9, 6.0, 1.0, 0.8}, {}, {}}};
+constexpr Costs FWD_F32[2] = {{{64, 2.7, 2.0, 0.8, 0.55}, {}, {}}, {{64, 5.3, 2.0, 0.8, 0.55}, {}, {}}};
+constexpr Costs DQ_F32[2] = {{{64, 4.0, 3.0, 0.8, 0.55}, {}, {}}, {{64, 8.0, 3.0, 0.8, 0.55}, {}, {}}};
+constexpr Costs DKDV_F32[2] = {{{64, 5.0, 3.0, 0.8, 0.55}, {}, {}}, {{64, 10.0, 3.0, 0.8, 0.55}, {}, {}}};
+// Ranges cost a launch that joins their sums, and the way of those to memory and
+// back, by the 1000 numbers that each CU has.  (4 x 300 x 500, 12 heads of 64, 240
+// workgroups: 10.3 us, in two ranges 20.0; 2 x 512 x 16000, 8 heads of 128, 32 of 256
+// rows: 415, in 8 ranges 84, in 12 105; 20,000 x 300, 16 heads, gradients: 713 with one
+// range of queries, 281 with five, which fill a round of CUs, 340 with six.)
+constexpr double JOIN = 8.0, JOIN_KILO = 0.15;
+// More ranges have to be faster by this (8 x 128 x 1500, 16 heads of 64, gradients: dQ
+// in two ranges 59 us, in four, the same by these figures, 63).
+constexpr double GAIN = 0.95;
+
+// Blocks of `rows` rows of `heads` heads over `tiles` tiles, `width` numbers in a
+// row's sums: the kernel and the ranges (as many as fit one to four workgroups a
+// CU) that take least.
+Plan plan_of(const Costs& kernels, int64_t rows, int64_t heads, int64_t tiles, int width) {
+  Plan best{};
+  double least = 0;
+  for (const Cost& c : kernels) {
+    if (!c.blk) continue;
+    const int64_t n_x = (rows + c.blk - 1) / c.blk, n = n_x * heads;
+    int64_t splits = 0;
+    double mine = 0;
+    for (int64_t k = 0; k <= 4; ++k) {
+      if (k && k * CUS < 2 * n) continue;
+      const int64_t s = k == 0 || n == 0 ? 1 : std::min(k * CUS / n, tiles / 2);
+      if (k && s <= 1) continue;
+      const int64_t rem = n * s % CUS;
+      const double w = std::max(1.0, static_cast<double>(n * s / CUS) + (rem ? std::max(c.last, 1.0 * rem / CUS) : 0.0));
+      double t = std::max(1.0, c.share * w) * (c.tile * ((tiles + s - 1) / s) + c.start);
+      if (s > 1) t += JOIN + JOIN_KILO * 1e-3 * w * c.blk * width;
+      if (splits == 0 || t < GAIN * mine) splits = s, mine = t;
+    }
+    if (best.blk == 0 || mine < least) best = Plan{c.blk, static_cast<int>(n_x), static_cast<int>(splits)}, least = mine;
+  }
+  return best;
+}
 // Tiles of 64 x 64 for each of two workgroups a CU, of both sides, up to which
 // the backward is one launch.  In two launches and in one, us: heads of 128, 8
 // tiles (2 x 512 x 512, 16 heads) 47 and 34, 12 tiles 44 and 48 (3 x 512 x 512), 55
@@ -835,39 +886,22 @@ constexpr int64_t SMALL_TILES_64 = 12, SMALL_TILES_128 = 8;
 // Tiles that ranges have to save a workgroup (1 to 6 measured the same).
 constexpr int64_t RANGE_GAIN = 2;
 
-// Blocks of 128 or 256 rows where they fill the card, of 64 where not; with few of
-// those too, the other side in ranges.  One block of rows for each sequence and
-// head is a call that reads its keys for little work (single tokens): it takes
-// more ranges, so that many loads are in flight and long sequences do not wait
-// for one workgroup.  (Workgroups wanted, and tiles of keys a range has at least,
-// us of 8 x 1 x 2048 of 40 heads of 128, ragged, and of 16 x 1 x 4000 of 32 heads on
-// 4: one range 72, -; 1024, 8: 52.3, 33.4; 1024, 4: 52.5, 39.1; 2048, 4: 53.8, 39.3;
-// 2048, 2: 53.8, 48.7; 4096, 2: 61.7, 49.0.)
+// One block of rows for each sequence and head is a call that reads its keys for
+// little work (single tokens): it takes more ranges, so that many loads are in
+// flight and long sequences do not wait for one workgroup.  (Workgroups wanted, and
+// tiles of keys a range has at least, us of 8 x 1 x 2048 of 40 heads of 128, ragged,
+// and of 16 x 1 x 4000 of 32 heads on 4: one range 72, -; 1024, 8: 52.3, 33.4; 1024,
+// 4: 52.5, 39.1; 2048, 4: 53.8, 39.3; 2048, 2: 53.8, 48.7; 4096, 2: 61.7, 49.0.)
 constexpr int64_t TOKEN_WGS = 1024, TOKEN_TILES = 8;
-// Rounds of workgroups that a launch of n takes where `each` share a CU; a last
-// round that leaves every CU at most one of two is shorter.
-double rounds(int64_t n, int each) {
-  const int64_t slots = CUS * each, rem = n % slots;
-  return static_cast<double>(n / slots) + (rem == 0 ? 0.0 : each == 2 && rem <= CUS ? ALONE : 1.0);
-}
-// Of workgroups of 256 rows, one a CU, and of 128, two: the one whose rounds take
-// less, of which both take the same but for SHARE.
-int rows_of(int64_t rows, int64_t heads) {
-  const double big = rounds((rows + 255) / 256 * heads, 1), mid = SHARE * rounds((rows + 127) / 128 * heads, 2);
-  return mid < big ? 128 : 256;
-}
-Plan plan_of(int64_t rows, int64_t heads, int64_t other, bool most64, int dh) {
-  Plan p{};
-  p.blk = most64 || rows <= 64 || (rows + 127) / 128 * heads < CUS ? 64 : dh == 64 ? 128 : rows_of(rows, heads);
-  p.n_x = static_cast<int>((rows + p.blk - 1) / p.blk);
-  const int64_t n = p.n_x * heads, tiles = (other + attn::BT - 1) / attn::BT;
-  const int64_t want = rows <= 64 ? TOKEN_WGS : n < CUS ? 2 * CUS : 0, least = rows <= 64 ? TOKEN_TILES : 2;
-  p.splits = n > 0 ? static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want / n, tiles / least))) : 1;
-  return p;
-}
 
 Plan fwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
-  return plan_of(static_cast<int64_t>(Tq) * G, static_cast<int64_t>(B) * Hk, Tk, dtype != DT_BF16, dh);
+  const int64_t rows = static_cast<int64_t>(Tq) * G, heads = static_cast<int64_t>(B) * Hk;
+  const int64_t tiles = (Tk + attn::BT - 1) / attn::BT;
+  if (rows <= 64) {
+    const int64_t s = heads > 0 ? std::min<int64_t>(TOKEN_WGS / heads, tiles / TOKEN_TILES) : 1;
+    return Plan{64, static_cast<int>((rows + 63) / 64), static_cast<int>(std::max<int64_t>(1, s))};
+  }
+  return plan_of(dtype == DT_BF16 ? FWD[dh == 128] : FWD_F32[dh == 128], rows, heads, tiles, dh);
 }
 // The backward's two sides: q (blocks of queries, ranges of keys) and k.
 struct BwdPlan {
@@ -886,21 +920,17 @@ BwdPlan bwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
   BwdPlan p{};
   const int64_t fair = (2 * tq * tk * heads + 2 * CUS - 1) / (2 * CUS);
   p.small = fair <= (dh == 64 ? SMALL_TILES_64 : SMALL_TILES_128);
-  const bool most64 = p.small || dtype != DT_BF16;
-  p.q.blk = most64 ? 64 : dh == 64 ? 128 : rows_of(rows, heads);
-  p.k.blk = most64 ? 64 : 128;
-  p.q.n_x = static_cast<int>((rows + p.q.blk - 1) / p.q.blk);
-  p.k.n_x = static_cast<int>((Tk + p.k.blk - 1) / p.k.blk);
   if (p.small) {
     // both sides share two workgroups a CU
-    p.q.splits = ranges_of(tk, fair, 2);
+    p.q = Plan{64, static_cast<int>(tq), ranges_of(tk, fair, 2)};
     // (and D of a range of queries has to fit the LDS)
-    p.k.splits = std::max(ranges_of(tq, fair, 2), static_cast<int>((tq + SMALL_ROWS / attn::BT - 1) / (SMALL_ROWS / attn::BT)));
+    p.k = Plan{64, static_cast<int>(tk),
+               std::max(ranges_of(tq, fair, 2), static_cast<int>((tq + SMALL_ROWS / attn::BT - 1) / (SMALL_ROWS / attn::BT)))};
+    p.q.splits = std::max(1, p.q.splits), p.k.splits = std::max(1, p.k.splits);
   } else {
-    p.q.splits = ranges_of(tk, (p.q.n_x * heads * tk + CUS - 1) / CUS, 4);
-    p.k.splits = ranges_of(tq, (p.k.n_x * heads * tq + CUS - 1) / CUS, 4);
+    p.q = plan_of(dtype == DT_BF16 ? DQ[dh == 128] : DQ_F32[dh == 128], rows, heads, tk, dh);
+    p.k = plan_of(dtype == DT_BF16 ? DKDV[dh == 128] : DKDV_F32[dh == 128], Tk, heads, tq, 2 * dh);
   }
-  p.q.splits = std::max(1, p.q.splits), p.k.splits = std::max(1, p.k.splits);
   return p;
 }
 
@@ -909,45 +939,64 @@ unsigned grid_of(const CrossArgs& a, int64_t x, int64_t splits) {
   return static_cast<unsigned>((x * splits * a.B * a.Hk + 7) / 8 * 8);
 }
 
-// Sums of the ranges, in range order, to dq (packed rows, times the scale) and
-// to dk and dv (which hold it): 64 lanes a row, a side that has none left out.
-template <typename T, int DH>
-__global__ void __launch_bounds__(256) cross_sum_kernel(const CrossArgs a, int64_t n_q, int64_t n_k) {
+// Sums of the ranges to dq (packed rows, times the scale) and to dk and dv (which
+// hold it), a side that has none left out: W waves a row, each every W-th range in
+// order, then the waves in order.
+template <typename T, int DH, int W>
+__global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) cross_sum_kernel(const CrossArgs a, int64_t n_q, int64_t n_k) {
   constexpr int E = DH / 64;
-  const int lane = threadIdx.x & 63;
-  int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (r < n_q) {
-    const int64_t P = static_cast<int64_t>(a.Tq) * a.G;
-    const int bh = static_cast<int>(r / P), p = static_cast<int>(r % P), b = bh % a.B, hk = bh / a.B;
-    const Seq qs = seq(a.q_start, a.q_len, a.Tq, a.q_rows, b);
-    const bool on = p < qs.n * a.G;
-    if (!on && a.q_start) return;
-    float v[E] = {};
-    for (int s = 0; s < a.splits && on; ++s)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int first = W == 1 ? 0 : wave;
+  int64_t r = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x;
+  const bool q_side = r < n_q;
+  if (!q_side) r -= n_q;
+  const int64_t n = q_side ? n_q : n_k, per = q_side ? static_cast<int64_t>(a.Tq) * a.G : a.Tk;
+  if (r >= n) return;
+  const int bh = static_cast<int>(r / per), i = static_cast<int>(r % per), b = bh % a.B, hk = bh / a.B;
+  const Seq s = q_side ? seq(a.q_start, a.q_len, a.Tq, a.q_rows, b) : seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
+  const bool on = i < (q_side ? s.n * a.G : s.n);
+  if (!on && (q_side ? a.q_start : a.k_start)) return;
+  const int splits = !on ? 0 : q_side ? a.splits : a.k_splits;
+  float v[2][E] = {};
+  const int64_t at_r = (first * n + r) * DH + E * lane, step = W * n * DH;
+  if (q_side) {
+    const float* p = a.part + at_r;
+#pragma unroll 8
+    for (int j = first; j < splits; j += W, p += step)
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] += a.part[(s * n_q + r) * DH + E * lane + e];
-    const int64_t lo = at<DH>(a, qs, hk, p, a.lddq) + E * lane;
+      for (int e = 0; e < E; ++e) v[0][e] += p[e];
+  } else {
+    const float *pk = a.part_k + at_r, *pv = a.part_v + at_r;
+#pragma unroll 8
+    for (int j = first; j < splits; j += W, pk += step, pv += step)
 #pragma unroll
-    for (int e = 0; e < E; ++e) static_cast<T*>(a.dq)[lo + e] = from_f<T>(v[e] * a.scale);
-    return;
+      for (int e = 0; e < E; ++e) {
+        v[0][e] += pk[e];
+        v[1][e] += pv[e];
+      }
   }
-  r -= n_q;
-  if (r >= n_k) return;
-  const int bh = static_cast<int>(r / a.Tk), j = static_cast<int>(r % a.Tk), b = bh % a.B, hk = bh / a.B;
-  const Seq ks = seq(a.k_start, a.k_len, a.Tk, a.k_rows, b);
-  const bool on = j < ks.n;
-  if (!on && a.k_start) return;
-  float vk[E] = {}, vv[E] = {};
-  for (int s = 0; s < a.k_splits && on; ++s)
+  if constexpr (W > 1) {
+    __shared__ float sums[W][64][2 * E];
+#pragma unroll
+    for (int e = 0; e < 2 * E; ++e) sums[wave][lane][e] = v[e / E][e % E];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int w = 1; w < W; ++w)
+#pragma unroll
+      for (int e = 0; e < 2 * E; ++e) v[e / E][e % E] += sums[w][lane][e];
+  }
+  if (q_side) {
+    const int64_t lo = at<DH>(a, s, hk, i, a.lddq) + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) static_cast<T*>(a.dq)[lo + e] = from_f<T>(v[0][e] * a.scale);
+  } else {
+    const int64_t row = s.row0 + i, col = hk * DH + E * lane;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      vk[e] += a.part_k[(s * n_k + r) * DH + E * lane + e];
-      vv[e] += a.part_v[(s * n_k + r) * DH + E * lane + e];
+      static_cast<T*>(a.dk)[row * a.lddk + col + e] = from_f<T>(v[0][e]);
+      static_cast<T*>(a.dv)[row * a.lddv + col + e] = from_f<T>(v[1][e]);
     }
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    static_cast<T*>(a.dk)[(ks.row0 + j) * a.lddk + hk * DH + E * lane + e] = from_f<T>(vk[e]);
-    static_cast<T*>(a.dv)[(ks.row0 + j) * a.lddv + hk * DH + E * lane + e] = from_f<T>(vv[e]);
   }
 }
 
@@ -971,11 +1020,21 @@ hipError_t fwd_bf16(const CrossArgs& a, int blk, int dh, hipStream_t s) {
 
 unsigned rows_grid(int64_t rows) { return static_cast<unsigned>((rows + 3) / 4); }
 
+// Ranges from which a row's sums are joined by JOIN_WAVES waves (one token of 32 heads
+// on 100,000 keys of 4, 195 ranges: 100 us by one wave, serially; 11).
+constexpr int JOIN_WIDE = 16, JOIN_WAVES = 8;
+constexpr int64_t JOIN_ROWS = 1 << 14;  // (more rows fill the card with a wave each)
+template <typename T, int DH>
+void join_launch(const CrossArgs& a, int64_t rows, hipStream_t s) {
+  if (a.splits >= JOIN_WIDE && rows <= JOIN_ROWS)
+    hipLaunchKernelGGL((cross_join_kernel<T, DH, JOIN_WAVES>), dim3(static_cast<unsigned>(rows)), dim3(64 * JOIN_WAVES), 0, s, a);
+  else hipLaunchKernelGGL((cross_join_kernel<T, DH, 1>), dim3(rows_grid(rows)), dim3(256), 0, s, a);
+}
 template <typename T>
 hipError_t join(const CrossArgs& a, int dh, hipStream_t s) {
-  const dim3 grid(rows_grid(static_cast<int64_t>(a.Tq) * a.G * a.B * a.Hk));
-  if (dh == 64) hipLaunchKernelGGL((cross_join_kernel<T, 64>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((cross_join_kernel<T, 128>), grid, dim3(256), 0, s, a);
+  const int64_t rows = static_cast<int64_t>(a.Tq) * a.G * a.B * a.Hk;
+  if (dh == 64) join_launch<T, 64>(a, rows, s);
+  else join_launch<T, 128>(a, rows, s);
   return hipGetLastError();
 }
 
@@ -999,14 +1058,21 @@ hipError_t bwd_bf16(const CrossArgs& a, const BwdPlan& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename T, int DH>
+void sum_launch(const CrossArgs& a, int64_t n_q, int64_t n_k, hipStream_t s) {
+  const int64_t rows = n_q + n_k;
+  // (a side that has no ranges has no rows here)
+  if (std::max(n_q ? a.splits : 0, n_k ? a.k_splits : 0) >= JOIN_WIDE && rows <= JOIN_ROWS)
+    hipLaunchKernelGGL((cross_sum_kernel<T, DH, JOIN_WAVES>), dim3(static_cast<unsigned>(rows)), dim3(64 * JOIN_WAVES), 0, s, a, n_q, n_k);
+  else hipLaunchKernelGGL((cross_sum_kernel<T, DH, 1>), dim3(rows_grid(rows)), dim3(256), 0, s, a, n_q, n_k);
+}
 template <typename T>
 hipError_t sum(const CrossArgs& a, int dh, hipStream_t s) {
   const int64_t heads = static_cast<int64_t>(a.B) * a.Hk;
   const int64_t n_q = a.dq && a.splits > 1 ? a.Tq * heads * a.G : 0, n_k = a.dk && a.k_splits > 1 ? a.Tk * heads : 0;
   if (n_q + n_k == 0) return hipSuccess;
-  const dim3 grid(rows_grid(n_q + n_k));
-  if (dh == 64) hipLaunchKernelGGL((cross_sum_kernel<T, 64>), grid, dim3(256), 0, s, a, n_q, n_k);
-  else hipLaunchKernelGGL((cross_sum_kernel<T, 128>), grid, dim3(256), 0, s, a, n_q, n_k);
+  if (dh == 64) sum_launch<T, 64>(a, n_q, n_k, s);
+  else sum_launch<T, 128>(a, n_q, n_k, s);
   return hipGetLastError();
 }
 
@@ -1022,11 +1088,10 @@ bool cross_attn_ok(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
   if (heads >= 1 << 30) return false;
   // rows of the launches that join ranges, four a workgroup
   if (heads * (Tq * G + Tk) >= MAX_WORKGROUPS * 4 - 4) return false;
-  const BwdPlan p = bwd_plan(dtype, B, Tq, Tk, Hk, G, dh);
-  const int64_t n_q = static_cast<int64_t>(p.q.n_x) * p.q.splits, n_k = static_cast<int64_t>(p.k.n_x) * p.k.splits;
-  const Plan f = fwd_plan(dtype, B, Tq, Tk, Hk, G, dh);
-  // below half of what a dispatch counts (512 threads each)
-  return (n_q + n_k) * heads < MAX_WORKGROUPS / 2 - 16 && static_cast<int64_t>(f.n_x) * f.splits * heads < MAX_WORKGROUPS / 2 - 16;
+  // Workgroups of either call, below half of what a dispatch counts (512 threads
+  // each): of 64 rows, or where ranges multiply them, a few thousand.
+  const int64_t n = ((Tq * G + 63) / 64 + (Tk + 63) / 64) * heads;
+  return n + (1 << 14) < MAX_WORKGROUPS / 2;
 }
 
 uint64_t cross_attn_fwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {

@@ -484,7 +484,7 @@ template <int DH>
 __global__ void __launch_bounds__(256, 2) cross_bwd_small_f32_kernel(const CrossArgs a) {
   __shared__ __attribute__((aligned(16))) float tiles[2][BT * Tile<DH>::RP];
   __shared__ float rows[2][BT], d_own[SMALL_ROWS];
-const int n_k = a.dk ? a.k_x * a.B * a.Hk * a.k_splits : 0, n_q = a.dq ? a.n_x * a.B * a.Hk * a.splits : 0;
+  const int n_k = a.dk ? a.k_x * a.B * a.Hk * a.k_splits : 0, n_q = a.dq ? a.n_x * a.B * a.Hk * a.splits : 0;
   const int k_end = (n_k + 7) & ~7, id = blockIdx.x;
   const int i = id < k_end ? item_of(n_k, id) : item_of(n_q, id - k_end);
   if (i < 0) return;

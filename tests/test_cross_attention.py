@@ -202,6 +202,40 @@ def test_forward(dtype, B, Tq, Tk, Hq, Hk, dh, rows, pad):
     assert t.equal(o, o2)
 
 
+# ranges: more than one for each lane of the waves that join them, and for each wave; workgroups of 64, 128 and 256
+# rows in ranges and without; ranges that a short sequence leaves empty; ranges of queries in one launch and in two
+RANGES = [
+    (1, 1, 300000, 1, 1, 64, "full", 0), (2, 1, 20000, 4, 2, 128, "packed", 0), (3, 2, 9000, 2, 1, 64, "padded", 8),
+    (1, 200, 5000, 2, 2, 128, "packed", 0), (1, 300, 2000, 2, 1, 64, "full", 0), (1, 5000, 60, 4, 2, 128, "packed", 0),
+    (1, 3000, 600, 8, 1, 128, "full", 0), (3, 500, 3000, 4, 4, 128, "padded", 0), (2, 1030, 600, 16, 16, 64, "packed", 0),
+    (16, 256, 1300, 16, 16, 128, "padded", 0), (2, 512, 16000, 8, 8, 128, "full", 0)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh,rows,pad", RANGES)
+def test_ranges(dtype, B, Tq, Tk, Hq, Hk, dh, rows, pad):
+    """Both directions, by the bounds of the others (a sum of n terms in any order is off by n u at most, and each
+    join by one rounding more); twice: the same bits."""
+    t = U.torch()
+    c = Case(dtype, B, Tq, Tk, Hq, Hk, dh, rows, seed=B * 13 + Tq + Tk, pad=pad)
+    outs = []
+    for _ in range(2):
+        o, lse = c.empty(c.q), t.full((c.nq + 1, Hq), FILL, device="cuda")
+        c.fwd(o, lse)
+        outs.append((o, lse))
+    _check_fwd(c, *outs[0])
+    assert t.equal(outs[0][0], outs[1][0]) and t.equal(outs[0][1], outs[1][1])
+    o, lse = _reference_fwd(c)
+    outs = []
+    for _ in range(2):
+        g = c.empty(c.q), c.empty(c.k), c.empty(c.v)
+        c.bwd(o, lse, *g)
+        outs.append(g)
+    _check_bwd(c, o, lse, *outs[0])
+    assert all(t.equal(a, b) for a, b in zip(*outs))
+
+
 def _gradients(c, o, lse):
     """Per sequence (qr, kr, dq, dk, dv and their bounds) from the given o and lse."""
     t = U.torch()
@@ -403,6 +437,30 @@ def test_large_and_infinite_scores(dtype):
     c.bwd(o, lse, dq, dk, dv)
     assert bool((dv[:130, :64] == 0).all())  # no weight: no gradient
     assert bool(dv[:130, 64:].isfinite().all()) and bool(dv[130:260, :64].isfinite().all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Tq,Tk", [(3, 127), (140, 127), (3, 2000)])
+def test_scores_up_to_the_limit(dtype, Tq, Tk):
+    """Scores to just below 2^30, exact, and 2^21 apart at least: the largest key has all the weight, to the bit."""
+    t = U.torch()
+    c = Case(dtype, 1, Tq, Tk, 2, 2, 64, seed=14)
+    c.scale = 0.25
+    c.q[:-1], c.k[:-1] = 0.0, 0.0
+    j = t.arange(Tk, device="cuda")
+    for h in (0, 64):
+        c.q[:-1, h] = 2.0 ** 15 * (1 - 2 * (t.arange(Tq, device="cuda") % 2)).float()
+        c.k[:-1, h] = 2.0 ** 15 * (1 + (j * 50 % 127).clamp(max=126) / 128.0) * (j < 127)  # (0 behind the first 127)
+    best = int((c.k[:Tk, 0]).argmax())
+    worst = int(t.where(j < 127, c.k[:Tk, 0].float(), t.full((Tk,), math.inf, device="cuda")).argmin()) if Tk == 127 else None
+    o, lse = c.empty(c.q), t.full((c.nq + 1, 2), FILL, device="cuda")
+    c.fwd(o, lse)
+    assert t.equal(o[0:Tq:2], c.v[best].expand(len(range(0, Tq, 2)), -1))
+    if worst is not None:
+        assert t.equal(o[1:Tq:2], c.v[worst].expand(len(range(1, Tq, 2)), -1))
+    z = c.scale * 2.0 ** 15 * c.k[best, 0].double()
+    assert (lse[0:Tq:2].double() - z).abs().max() <= 4 * u * z
 
 
 @pytest.mark.gpu
