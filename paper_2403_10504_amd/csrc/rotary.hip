@@ -20,7 +20,8 @@
 // 2 V, which do not turn.  So a pair never leaves its lane, P lanes (a power of
 // two) hold a head, and a wave 64 / P heads at a time.  A wave takes a whole
 // row, so the angles of its V pairs, and their sines, are computed once for all
-// of the row's heads; where rows are few a row's heads go to several waves.
+// of the row's heads; where rows are few a row's heads go to several waves, where a
+// row's heads are few several rows to one.
 //
 // Sines are computed one a lane and passed on through LDS inside the wave: they are
 // the same in every head, and a lane alone would compute V of them.
@@ -55,8 +56,9 @@ struct Args {
   uint32_t rows, T;
   int Hq, Hk, Hv;  // (rope: Hq alone)
   int dh, rot;
-  int plog, per;  // log2 of P; groups of 64 / P heads that a workgroup takes of a row
-  int copy;       // the value heads are copied
+  int plog, rlog;  // log2 of P, and of the rows that a wave takes at a time
+  int per;         // groups of heads that a workgroup takes of a row
+  int copy;        // the value heads are copied
 };
 
 enum { ROPE, NORM, NORM_BWD };
@@ -147,14 +149,16 @@ ATOM_DEV float sum_inside(float v, int P) {
 // NC chunks of a lane (two for heads of more than 128 elements in single pairs).
 // (Waves a SIMD: the norms within 128 registers 44.6 us, 135 unbounded 47.0, 96 48;
 // the gradients within 168 49.3, within 256 48.8, 128 spill: 92.)
-template <typename T, int V, int NC, bool PAIRS, int OP>
+// MIX: groups of several sides (kind_of), and several rows a wave.
+template <typename T, int V, int NC, bool PAIRS, int OP, bool MIX>
 __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_kernel(const Args a) {
   using C = Chunk<T, V, PAIRS>;
   using R = Raw<T, V>;
-  __shared__ float2 turns[WAVES][128];  // cosine and sine of a row's pairs, times mscale
+  constexpr int PAIRS_MAX = MIX ? 64 * V : 128;  // (64 lanes of V pairs; a row has 128 at most)
+  __shared__ float2 turns[WAVES][PAIRS_MAX];       // cosine and sine of the rows' pairs, times mscale
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int P = 1 << a.plog, HS = 64 >> a.plog;
-  const int slot = lane >> a.plog, lp = lane & (P - 1);
+  const int P = 1 << a.plog, rlog = MIX ? a.rlog : 0, slog = 6 - a.plog - rlog, S = 1 << slog;
+  const int lp = lane & (P - 1), slot = (lane >> a.plog) & (S - 1), ri = MIX ? lane >> (a.plog + slog) : 0;
   const int L = a.dh / (2 * V), rc = a.rot / (2 * V);
   const float inv_dh = 1.f / a.dh;
   int o0[NC], o1[NC];
@@ -167,8 +171,9 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
     if (!turn[k] || PAIRS) o0[k] = 2 * V * c, o1[k] = o0[k] + V;
     else o0[k] = V * c, o1[k] = a.rot / 2 + V * c;
   }
-  const int gq = (a.Hq + HS - 1) / HS, gk = (a.Hk + HS - 1) / HS, gv = a.copy ? (a.Hv + HS - 1) / HS : 0;
-  const int g0 = blockIdx.y * a.per, g1 = min(g0 + a.per, gq + gk + gv);
+  const int Hq = a.Hq, Hk = a.Hk, Hv = a.copy ? a.Hv : 0, H = Hq + Hk + Hv;
+  const int gq = (Hq + S - 1) >> slog, gk = (Hk + S - 1) >> slog, gv = (Hv + S - 1) >> slog;
+  const int g0 = blockIdx.y * a.per, g1 = min(g0 + a.per, MIX ? (H + S - 1) >> slog : gq + gk + gv);
 
   C gain[NC];
   float acc[2][NC][2 * V];  // of queries and of keys
@@ -192,22 +197,38 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
       }
     }
   };
-  // group g: its side, and the lane's head
+  // Group g: what its heads are (ALL_Q, ALL_K, ALL_V, or g itself if of several
+  // sides), and the lane's head.
+  enum { ALL_Q = -1, ALL_K = -2, ALL_V = -3 };
+  auto kind_of = [&](int g) -> int {
+    if (!MIX) return g < gq ? ALL_Q : g < gq + gk ? ALL_K : ALL_V;
+    const int first = g << slog, last = min(first + S, H) - 1;
+    return last < Hq ? ALL_Q : first >= Hq + Hk ? ALL_V : first >= Hq && last < Hq + Hk ? ALL_K : g;
+  };
   struct Head {
     bool is_q, is_v, there;
     int at;  // of its first element in the row (2^16 heads of 256 at most)
   };
-  auto head_of = [&](int g) {
-    Head h;
-    h.is_q = g < gq, h.is_v = g >= gq + gk;
-    const int i = (h.is_q ? g : h.is_v ? g - gq - gk : g - gq) * HS + slot;
-    h.there = i < (h.is_q ? a.Hq : h.is_v ? a.Hv : a.Hk);
-    h.at = (h.is_q ? i : h.is_v ? a.Hq + a.Hk + i : a.Hq + i) * a.dh;
-    return h;
+  bool row_there = true;
+  // (by value: between variables captured by reference the compiler selects an
+  // address, which puts them in memory)
+  auto head_at = [](int g, int slog, int slot, int gq, int gk, int Hq, int Hk, int Hv, int dh, bool row_there) {
+    if (MIX) {
+      const int i = (g << slog) + slot;
+      return Head{i < Hq, i >= Hq + Hk, i < Hq + Hk + Hv && row_there, i * dh};
+    }
+    const bool is_q = OP == ROPE || g < gq, is_v = OP != ROPE && g >= gq + gk;
+    const int i = ((is_q ? g : is_v ? g - gq - gk : g - gq) << slog) + slot;
+    return Head{is_q, is_v, i < (is_q ? Hq : is_v ? Hv : Hk), (is_q ? i : is_v ? Hq + Hk + i : Hq + i) * dh};
   };
+  auto head_of = [&](int g) { return head_at(g, slog, slot, gq, gk, Hq, Hk, Hv, a.dh, row_there); };
+  // (several rows are within 2^31 elements)
+  const int rx_off = MIX ? ri * static_cast<int>(a.ldx) : 0, rd_off = MIX ? ri * static_cast<int>(a.lddy) : 0;
+  const int ry_off = MIX ? ri * static_cast<int>(a.ldy) : 0;
 
-  for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * WAVES + wave; row < a.rows;
-       row += static_cast<uint64_t>(gridDim.x) * WAVES) {
+  for (uint64_t row = (static_cast<uint64_t>(blockIdx.x) * WAVES + wave) << rlog; row < a.rows;
+       row += static_cast<uint64_t>(gridDim.x) * WAVES << rlog) {
+    if (MIX) row_there = row + ri < a.rows;
     const T* x = static_cast<const T*>(a.x) + static_cast<int64_t>(row) * a.ldx;
     const T* dy = OP == NORM_BWD ? static_cast<const T*>(a.dy) + static_cast<int64_t>(row) * a.lddy : x;
     T* y = static_cast<T*>(a.y) + static_cast<int64_t>(row) * a.ldy;
@@ -220,8 +241,8 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
 #pragma unroll
         for (int i = 0; i < V; ++i) rx[k].a.e[i] = rx[k].b.e[i] = rd[k].a.e[i] = rd[k].b.e[i] = 0;
         if (h.there && on[k]) {
-          if (OP == NORM_BWD) rd[k].load(dy + h.at, o0[k], o1[k]);
-          if (OP != NORM_BWD || !h.is_v) rx[k].load(x + h.at, o0[k], o1[k]);
+          if (OP == NORM_BWD) rd[k].load(dy + rd_off + h.at, o0[k], o1[k]);
+          if (OP != NORM_BWD || !h.is_v) rx[k].load(x + rx_off + h.at, o0[k], o1[k]);
         }
       }
     };
@@ -231,10 +252,21 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
     if (a.rot) {
       // each lane one pair in 64 (they are the same in every head), passed on
       // through LDS inside the wave
-      const double p = a.pos ? static_cast<double>(a.pos[row]) : static_cast<double>(static_cast<uint32_t>(row) % a.T);
-      for (int i = lane; i < a.rot / 2; i += 64) {
+      const int half = a.rot / 2, inv = (0x10000 + half - 1) / half;  // (i inv >> 16 is i / half below 512)
+      const uint32_t t0 = a.pos ? 0 : static_cast<uint32_t>(row) % a.T;
+      double p = 0.0;
+      if (!MIX) p = a.pos ? static_cast<double>(a.pos[row]) : static_cast<double>(t0);
+      for (int i = lane; i < half << rlog; i += 64) {
+        const int r = MIX ? i * inv >> 16 : 0, pair = i - r * half;
+        if (MIX && !a.pos) {
+          uint32_t t = t0 + r;
+          while (t >= a.T) t -= a.T;
+          p = static_cast<double>(t);
+        } else if (MIX && row + r < a.rows) {
+          p = static_cast<double>(a.pos[row + r]);
+        }
         // half turns, reduced to [-1, 1] in 64 bits; then exact in fp32 to 2^-25
-        const double t = p * (a.freq[i] * 0.31830988618379067154);
+        const double t = p * (a.freq[pair] * 0.31830988618379067154);
         float s, c;
         sincospif(static_cast<float>(t - 2.0 * rint(0.5 * t)), &s, &c);
         turns[wave][i] = make_float2(c * a.mscale, (OP == NORM_BWD || (OP == ROPE && a.back) ? -s : s) * a.mscale);
@@ -246,7 +278,7 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
         if (turn[k]) {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const float2 t = turns[wave][V * (lp + 64 * k) + i];
+            const float2 t = turns[wave][(MIX ? ri * (a.rot / 2) : 0) + V * (lp + 64 * k) + i];
             cs[k][i] = t.x;
             sn[k][i] = t.y;
           }
@@ -276,13 +308,17 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
         h = head_of(g + 1);
         fetch(h);
       }
-      if (cur.is_v) {  // values: as they are
+      const int kind = OP == ROPE ? ALL_Q : kind_of(g);
+      auto copy = [&] {  // values: as they are
 #pragma unroll
         for (int k = 0; k < NC; ++k)
-          if (cur.there && on[k]) (OP == NORM_BWD ? cd[k] : cx[k]).store(y + cur.at, o0[k], o1[k]);
+          if (cur.there && on[k]) (OP == NORM_BWD ? cd[k] : cx[k]).store(y + ry_off + cur.at, o0[k], o1[k]);
+      };
+      if (kind == ALL_V) {
+        copy();
         continue;
       }
-      if (OP != ROPE && (g == g0 || g == gq)) load_gain(cur.is_q ? a.gq : a.gk);
+      if (OP != ROPE && (MIX || g == g0 || g == gq)) load_gain(cur.is_q ? a.gq : a.gk);
       C v[NC];
 #pragma unroll
       for (int k = 0; k < NC; ++k) v[k].set(cx[k]);
@@ -307,7 +343,16 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
         } else {
           C d[NC];
 #pragma unroll
-          for (int k = 0; k < NC; ++k) d[k].set(cd[k]);
+          for (int k = 0; k < NC; ++k) {
+            d[k].set(cd[k]);
+            if (MIX && kind >= 0) {  // (values add nothing to the gains, whatever they are)
+#pragma unroll
+              for (int i = 0; i < V; ++i) {
+                d[k].u[i] = cur.is_v ? 0.f : d[k].u[i];
+                d[k].w[i] = cur.is_v ? 0.f : d[k].w[i];
+              }
+            }
+          }
           rotate(d);
           float m = 0.f;
 #pragma unroll
@@ -317,8 +362,13 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
               v[k].u[i] *= r;
               v[k].w[i] *= r;
               const float tu = d[k].u[i] * v[k].u[i], tw = d[k].w[i] * v[k].w[i];
-              if (cur.is_q) acc[0][k][2 * i] += tu, acc[0][k][2 * i + 1] += tw;
-              else acc[1][k][2 * i] += tu, acc[1][k][2 * i + 1] += tw;
+              if (MIX) {
+                if (kind != ALL_K) acc[0][k][2 * i] += cur.is_q ? tu : 0.f, acc[0][k][2 * i + 1] += cur.is_q ? tw : 0.f;
+                if (kind != ALL_Q) acc[1][k][2 * i] += cur.is_q ? 0.f : tu, acc[1][k][2 * i + 1] += cur.is_q ? 0.f : tw;
+              } else {
+                if (cur.is_q) acc[0][k][2 * i] += tu, acc[0][k][2 * i + 1] += tw;
+                else acc[1][k][2 * i] += tu, acc[1][k][2 * i + 1] += tw;
+              }
               m += tu * gain[k].u[i] + tw * gain[k].w[i];
             }
           m = sum_inside(m, P) * inv_dh;
@@ -333,7 +383,8 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
       }
 #pragma unroll
       for (int k = 0; k < NC; ++k)
-        if (cur.there && on[k]) v[k].get().store(y + cur.at, o0[k], o1[k]);
+        if (cur.there && on[k] && !(MIX && kind >= 0 && cur.is_v)) v[k].get().store(y + ry_off + cur.at, o0[k], o1[k]);
+      if (MIX && kind >= 0 && cur.is_v) copy();
     }
   }
 
@@ -365,7 +416,7 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
         return p + q;
       });
     __shared__ float sums[WAVES][2][256];
-    if (slot == 0) {
+    if (lane < P) {
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -413,7 +464,7 @@ __global__ void __launch_bounds__(1024) gain_sum_kernel(const float* __restrict_
 
 // The grid: workgroups of four rows, and the parts of a row's heads.
 struct Shape {
-  int v, plog, per;
+  int per;
   unsigned gx, gy;
 };
 
@@ -432,16 +483,18 @@ int pairs_of(int dtype, int dh, int rot, uint64_t align) {
 constexpr int64_t FULL_WAVES = 2048;
 constexpr int64_t MAX_PARTS = 64;
 // Workgroups of the backward at most: each leaves a partial sum of the gains,
-// and gain_sum_kernel takes 4 us for 1024 of them.
+// and gain_sum_kernel takes 4 us for 1024 of them.  As many as run at once: half of
+// them where a lane has 8 pairs, for its registers (8192 rows of 3 x 16 heads of 128,
+// 1024 and 512: 61.9 and 59.6 us; fp32, 3 x 8 heads of 80, 42.1 and 47.5).
 constexpr int64_t BWD_BLOCKS = 1024;
 
-Shape shape_of(int op, int64_t rows, int groups, int dh, int v, int plog) {
-  Shape s{v, plog, groups, 0, 1};
-  const int64_t wgs = (rows + WAVES - 1) / WAVES;
+Shape shape_of(int op, int64_t rows, int rlog, int groups, int v) {
+  Shape s{groups, 0, 1};
+  const int64_t wgs = (((rows - 1) >> rlog) + WAVES) / WAVES;
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({groups, FULL_WAVES / rows, MAX_PARTS}));
   s.per = static_cast<int>((groups + parts - 1) / parts);
   s.gy = static_cast<unsigned>((groups + s.per - 1) / s.per);
-  s.gx = static_cast<unsigned>(std::min<int64_t>(wgs, op == NORM_BWD ? std::max<int64_t>(1, BWD_BLOCKS / s.gy) : MAX_WORKGROUPS / s.gy - 1));
+  s.gx = static_cast<unsigned>(std::min<int64_t>(wgs, op == NORM_BWD ? std::max<int64_t>(1, BWD_BLOCKS / (v == 8 ? 2 : 1) / s.gy) : MAX_WORKGROUPS / s.gy - 1));
   return s;
 }
 
@@ -452,41 +505,61 @@ int plog_of(int dh, int v) {
   return p;
 }
 
-template <typename T, int V, int OP>
+// Whether groups of several sides, and 2^rlog rows a wave, take half the passes or
+// less (the registers that they need cost more than a few passes less: 16 + 2 + 2 heads,
+// three for four, 20.1 -> 23.4 us; fp32 gradients of 8 + 2 + 2, two for three, 132 ->
+// 166).  100,000 rows of 1 + 1 + 1 heads of 128: 137 -> 53 us, gradients 257 -> 100;
+// 16,384 of 4 + 1 + 1 heads of 64: 25 -> 12, 52 -> 22.
+bool mixed(int64_t rows, int Hq, int Hk, int Hv, int hlog, int64_t ld, int* rlog) {
+  const int heads = Hq + Hk + Hv, S = 1 << hlog;
+  const int apart = (Hq + S - 1) / S + (Hk + S - 1) / S + (Hv + S - 1) / S;
+  int r = 0;
+  while (r < hlog && (1 << (hlog - r - 1)) >= heads && rows >> (r + 1) >= FULL_WAVES && ld << (r + 1) < 1ll << 31) ++r;
+  *rlog = r;
+  return 2 * ((heads + S - 1) / S) <= apart << r;
+}
+
+template <typename T, int V, int OP, bool MIX>
 void launch(const Args& a, bool pairs, const Shape& g, hipStream_t s) {
   const dim3 grid(g.gx, g.gy), block(64 * WAVES);
   if constexpr (V == 1) {
     if (a.dh > 128) {
-      if (pairs) hipLaunchKernelGGL((rotary_kernel<T, V, 2, true, OP>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((rotary_kernel<T, V, 2, false, OP>), grid, block, 0, s, a);
+      if (pairs) hipLaunchKernelGGL((rotary_kernel<T, V, 2, true, OP, MIX>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((rotary_kernel<T, V, 2, false, OP, MIX>), grid, block, 0, s, a);
       return;
     }
   }
-  if (pairs) hipLaunchKernelGGL((rotary_kernel<T, V, 1, true, OP>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((rotary_kernel<T, V, 1, false, OP>), grid, block, 0, s, a);
+  if (pairs) hipLaunchKernelGGL((rotary_kernel<T, V, 1, true, OP, MIX>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((rotary_kernel<T, V, 1, false, OP, MIX>), grid, block, 0, s, a);
 }
 
 template <int OP>
 hipError_t run(int dtype, Args& a, int layout, uint64_t align, hipStream_t s, unsigned* blocks) {
   const int v = pairs_of(dtype, a.dh, a.rot, align);
   a.plog = plog_of(a.dh, v);
-  const int HS = 64 >> a.plog;
-  const int groups = (a.Hq + HS - 1) / HS + (a.Hk + HS - 1) / HS + (a.copy ? (a.Hv + HS - 1) / HS : 0);
+  const int hlog = 6 - a.plog, Hv = a.copy ? a.Hv : 0;
   *blocks = 0;
-  if (a.rows == 0 || groups == 0) return hipSuccess;
-  const Shape g = shape_of(OP, a.rows, groups, a.dh, v, a.plog);
+  if (a.rows == 0 || a.Hq + a.Hk + Hv == 0) return hipSuccess;
+  // (in the widest accesses alone)
+  const bool mix = v == (dtype == DT_BF16 ? 8 : 4) && mixed(a.rows, a.Hq, a.Hk, Hv, hlog, std::max({a.ldx, a.lddy, a.ldy}), &a.rlog);
+  if (!mix) a.rlog = 0;
+  const int slog = hlog - a.rlog, S = 1 << slog;
+  auto groups = [&](int heads) { return (heads + S - 1) >> slog; };
+  const Shape g = shape_of(OP, a.rows, a.rlog, mix ? groups(a.Hq + a.Hk + Hv) : groups(a.Hq) + groups(a.Hk) + groups(Hv), v);
   a.per = g.per;
   *blocks = g.gx * g.gy;
   const bool pairs = layout == ATOM_ROPE_PAIRS;
   if (dtype == DT_BF16) {
-    if (v == 8) launch<bf16_t, 8, OP>(a, pairs, g, s);
-    else if (v == 4) launch<bf16_t, 4, OP>(a, pairs, g, s);
-    else if (v == 2) launch<bf16_t, 2, OP>(a, pairs, g, s);
-    else launch<bf16_t, 1, OP>(a, pairs, g, s);
+    if (mix) launch<bf16_t, 8, OP, true>(a, pairs, g, s);
+    else if (v == 8) launch<bf16_t, 8, OP, false>(a, pairs, g, s);
+    else if (v == 4) launch<bf16_t, 4, OP, false>(a, pairs, g, s);
+    else if (v == 2) launch<bf16_t, 2, OP, false>(a, pairs, g, s);
+    else launch<bf16_t, 1, OP, false>(a, pairs, g, s);
   } else {
-    if (v == 4) launch<float, 4, OP>(a, pairs, g, s);
-    else if (v == 2) launch<float, 2, OP>(a, pairs, g, s);
-    else launch<float, 1, OP>(a, pairs, g, s);
+    if (mix) launch<float, 4, OP, true>(a, pairs, g, s);
+    else if (v == 4) launch<float, 4, OP, false>(a, pairs, g, s);
+    else if (v == 2) launch<float, 2, OP, false>(a, pairs, g, s);
+    else launch<float, 1, OP, false>(a, pairs, g, s);
   }
   return hipGetLastError();
 }

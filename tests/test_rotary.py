@@ -247,6 +247,55 @@ def test_norm_backward(dtype, layout, rows, Hq, Hk, Hv, dh, rot, pad):
     assert _kept(dy, rows, width)
 
 
+# The widest accesses: every buffer aligned, in leading dimensions of its own.  One side and all of them in a group, two
+# groups, several rows a wave (to 32) with some behind the last one, and as many heads as lanes for them.
+ALIGNED = [  # rows, Hq, Hk, Hv, dh, rot, T
+    (1, 1, 1, 1, 64, 64, 1), (37, 12, 2, 2, 128, 128, 5), (300, 8, 2, 2, 96, 0, 1), (4101, 4, 1, 1, 64, 64, 3),
+    (4101, 1, 1, 1, 128, 96, 2048), (9001, 2, 1, 0, 64, 32, 1), (9001, 0, 1, 1, 64, 64, 100), (8200, 3, 0, 2, 32, 32, 7),
+    (40003, 1, 0, 0, 64, 64, 3), (70001, 1, 0, 0, 16, 16, 1), (70001, 1, 1, 0, 16, 16, 40000), (2050, 5, 3, 2, 80, 80, 9),
+    (600, 20, 4, 4, 256, 256, 77), (1030, 16, 16, 16, 128, 64, 1030)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("rows,Hq,Hk,Hv,dh,rot,T", ALIGNED)
+def test_aligned_rows(dtype, layout, rows, Hq, Hk, Hv, dh, rot, T):
+    t = U.torch()
+    n, heads, mscale = Hq + Hk, Hq + Hk + Hv, 1.25
+    width = heads * dh
+    for far in (False, True):
+        x, pos, freq, gq, gk, g = _norm_case(dtype, rows, Hq, Hk, Hv, dh, rot, 0, rows + dh + far, far)
+        angle = _angles(rows, T, pos, freq) if rot else None
+        y = _padded(rows, width, 16, dtype)
+        A.atom_k_rope(U.dt_code(dtype), x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0), _ptr(pos), _ptr(freq), mscale,
+                      LAYOUTS[layout], 0, rows, T, heads, dh, rot)
+        ref = _split(x, rows, heads, dh)
+        ref, bound = _turn(ref, angle, mscale, layout) if rot else (ref, t.zeros_like(ref))
+        _within(_split(y, rows, heads, dh), ref, bound, dtype)
+        assert _kept(y, rows, width)
+        y = _padded(rows, width, 16, dtype)
+        _fwd(dtype, x, y, gq, gk, pos, freq, mscale, layout, rows, T, Hq, Hk, Hv, dh, rot)
+        ref, bound, *_ = _forward(x, gq, gk, rows, Hq, Hk, dh, angle, mscale, layout)
+        _within(_split(y, rows, n, dh), ref, bound, dtype)
+        assert t.equal(y[:rows, n * dh:width], x[:rows, n * dh:width]) and _kept(y, rows, width)
+        # gradients; infinities and NaN in the values' part are copied and touch nothing else
+        dy, dx = _padded(rows, width, 8, dtype), _padded(rows, width, 24, dtype)
+        dy[:rows, :width] = t.randn(rows, width, device="cuda", generator=g) * 0.01
+        if Hv:
+            dy[0, n * dh], dy[rows - 1, width - 1] = math.inf, float("nan")
+        dg = t.full((2, dh), 55.0, device="cuda")
+        _bwd(dtype, dy, x, dx, gq, gk, dg[0], dg[1], pos, freq, mscale, layout, rows, T, Hq, Hk, Hv, dh, rot,
+             _ws(rows, Hq, Hk, dh))
+        refs = _gradients(dy, x, gq, gk, rows, Hq, Hk, dh, angle, mscale, layout)
+        _within(_split(dx, rows, n, dh), *refs[0], dtype)
+        bits = t.int16 if dtype == "bf16" else t.int32
+        assert t.equal(dx[:rows, n * dh:width].contiguous().view(bits), dy[:rows, n * dh:width].contiguous().view(bits))
+        assert _kept(dx, rows, width)
+        for k in (0, 1):
+            _within(dg[k], *refs[1 + k], "f32")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("layout", ["half", "pairs"])
 def test_gradient_against_differences(layout):
