@@ -68,7 +68,9 @@ ATOM_DEV Range range_of(int n_rows, int splits, int s) {
 // us, 32 rows 308 to 310; ahead 275 in 256-row workgroups, 289 in 128-row ones, 360
 // with 16 rows a wave; without branches between the score and the second product 260
 // and 275.  Orders asked for by scheduling groups: 266 to 270; two score tiles' sums
-// side by side, 3 to 6 fragments of V ahead: within 2 us.)
+// side by side, 3 to 6 fragments of V ahead: within 2 us; the two halves of a
+// workgroup in turns, one in its products while the other has its exponentials, two
+// barriers a tile: 262; 64 rows a wave at one wave a SIMD spill: 349.)
 template <int DH, int GR, int NW, int WPS, bool SPLIT>
 __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs a) {
   constexpr int NT = 64 * NW;
@@ -206,6 +208,9 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
   // first score on, so that the compiler's order is the one asked for.
   auto step = [&](auto NEXT_, float (&z)[GR][4][4], float (&next)[GR][4][4], int kt) {
     constexpr int NEXT = decltype(NEXT_)::value;
+    // of a SIMD's waves the one that has exponentials to do goes first, so that they
+    // come apart (cross_small 32.0 -> 30.9 us, cross_6.7b 261 -> 257)
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int g = 0; g < GR; ++g) {
       const float mx = rows4_max(mloc[g]) * sc;
@@ -237,6 +242,7 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
 #pragma unroll
       for (int jt = 0; jt < 4; ++jt) exps(jt);
     }
+    __builtin_amdgcn_s_setprio(0);
     const uint8_t* vst = lds + (2 + (kt & 1)) * F::TILE;
     constexpr int AHEAD = 4;  // fragments of V in flight
     Frag<bf16_t> vf[AHEAD];
@@ -707,6 +713,7 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
       };
       constexpr int AHEAD = 2;
       Frag<bf16_t> ot2[AHEAD], qt2[AHEAD];
+      __builtin_amdgcn_s_setprio(1);  // (as in the forward: 219 -> 217 us)
       read(0);
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
@@ -733,6 +740,7 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
           ds[it][r] = p[it][r] * (dp[r] - del_s[il]);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
         Frag<bf16_t> pf, dsf;
