@@ -106,11 +106,19 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) cross_join_kernel(const
         l += f * a.ml[2 * (s * n + r) + 1];
       }
       const float* part = a.part + (s0 * n + r) * DH + E * lane;
-#pragma unroll 8
-      for (int i = 0; i < count; ++i) {
-        const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i));
+      for (int i0 = 0; i0 < count; i0 += 8) {
+        float v[8][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += fi * part[i * (W * n * DH) + e];
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[i][e] = part[min(i0 + i, count - 1) * (W * n * DH) + e];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (i0 + i >= count) break;
+          const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i0 + i));
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] += fi * v[i][e];
+        }
       }
     }
     l = wave_sum(l);

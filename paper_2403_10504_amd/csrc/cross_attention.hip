@@ -60,6 +60,40 @@ ATOM_DEV Range range_of(int n_rows, int splits, int s) {
   return Range{min(s * per, n), min(s * per + per, n)};
 }
 
+// Every wave is done with the stages in LDS.
+ATOM_DEV void stages_done() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  asm volatile("s_barrier" ::: "memory");
+}
+// A wave's results go out through LDS (the stages' place), N rows of DH, so that a
+// store covers whole rows instead of 32 bytes of each (one tile of keys 25.5 -> 22.6
+// us; gradients of 4 x 64 x 1500, 32 heads of 128, 108 -> 96, of 2 x 512 x 16000, 8 heads,
+// 291 -> 281).
+template <int DH, int N>
+struct Rows {
+  static constexpr int RB = DH * 2, CPR = DH / 8;  // bytes and chunks of 16 bytes in a row
+  uint8_t* mine;
+  // columns 16 c + 4 lg + 0..3 of a row
+  ATOM_DEV void put(int row, int c, int lg, float (&v)[4]) const {
+    const int chunk = (2 * c + (lg >> 1)) ^ (row & (CPR - 1));
+    store_row4<bf16_t>(reinterpret_cast<bf16_t*>(mine + row * RB + chunk * 16 + 8 * (lg & 1)), v);
+  }
+  // to(row, on): where a row goes, and whether it does
+  template <typename TO>
+  ATOM_DEV void store(int lane, TO to) const {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < N * CPR / 64; ++i) {
+      const int row = i * (64 / CPR) + lane / CPR, chunk = lane % CPR;
+      const uint4 v = *reinterpret_cast<const uint4*>(mine + row * RB + (chunk ^ (row & (CPR - 1))) * 16);
+      bool on;
+      bf16_t* p = to(row, on);
+      if (on) *reinterpret_cast<uint4*>(p + chunk * 8) = v;
+    }
+  }
+};
+
 // ------------------------------------------------------------------ forward
 // A tile's scores are computed one tile ahead: the matrix instructions of
 // S(t+1) = K Q^T stand between the exponentials of P(t), which need nothing of
@@ -322,11 +356,9 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
     }
     return;
   }
-  // Results go out through LDS (a wave's rows in the stages, which every wave is
-  // done with), so that a store covers whole rows instead of 32 bytes of each.
   constexpr int WROWS = 16 * GR;
   static_assert(NW * WROWS * RB <= 4 * F::TILE, "results in the stages' place");
-  uint8_t* mine = lds + w * WROWS * RB;
+  Rows<DH, WROWS> out{lds + w * WROWS * RB};
   fence();
   // padded queries of a padded batch get zeros (P up to Tq G)
   const int p_end = a.q_start ? P : a.Tq * a.G;
@@ -341,22 +373,17 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
       float v[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) v[r] = none ? 0.f : acc_o[g][c][r] * inv;
-      const int chunk = (2 * c + (lg >> 1)) ^ (row & (F::CPR - 1));
-      store_row4<bf16_t>(reinterpret_cast<bf16_t*>(mine + row * RB + chunk * 16 + 8 * (lg & 1)), v);
+      out.put(row, c, lg, v);
     }
     if (lg == 0 && a.lse && pi < p_end) {
       const Row rw = row_of(a, pi);
       a.lse[(qs.row0 + rw.t) * a.Hq + hk * a.G + rw.g] = none ? -INFINITY : (m_i[g] + log2f(l_tot)) * LN2;
     }
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-#pragma unroll
-  for (int i = 0; i < WROWS * F::CPR / 64; ++i) {
-    const int row = i * (64 / F::CPR) + lane / F::CPR, chunk = lane % F::CPR, pi = qw + row;
-    const uint4 v = *reinterpret_cast<const uint4*>(mine + row * RB + (chunk ^ (row & (F::CPR - 1))) * 16);
-    if (pi < p_end) *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.o) + at<DH>(a, qs, hk, pi, a.ldo) + chunk * 8) = v;
-  }
+  out.store(lane, [&](int row, bool& on) {
+    on = qw + row < p_end;
+    return static_cast<bf16_t*>(a.o) + (on ? at<DH>(a, qs, hk, qw + row, a.ldo) : 0);
+  });
 }
 
 // ------------------------------------------------------------ backward: dQ
@@ -522,6 +549,9 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
     }
   }
 
+  Rows<DH, 16 * GR> out{lds + w * 16 * GR * RB};
+  static_assert(NW * 16 * GR * RB <= 2 * F::STAGE, "results in the stages' place");
+  if (!ranges) stages_done();
 #pragma unroll
   for (int g = 0; g < GR; ++g) {
     const int pi = qw + g * 16 + lr;
@@ -535,16 +565,20 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
       }
       continue;
     }
-    if (pi >= (a.q_start ? P : n_p)) continue;
-    bf16_t* row = static_cast<bf16_t*>(a.dq) + at<DH>(a, qs, hk, pi, a.lddq);
 #pragma unroll
     for (int c = 0; c < NCT; ++c) {
       float v[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) v[r] = pi < P ? acc[g][c][r] * a.scale : 0.f;  // (padding: zeros)
-      store_row4<bf16_t>(row + c * 16 + 4 * lg, v);
+      out.put(g * 16 + lr, c, lg, v);
     }
   }
+  if (ranges) return;
+  const int64_t p_end = a.q_start ? P : n_p;
+  out.store(lane, [&](int row, bool& on) {
+    on = qw + row < p_end;
+    return static_cast<bf16_t*>(a.dq) + (on ? at<DH>(a, qs, hk, qw + row, a.lddq) : 0);
+  });
 }
 
 // -------------------------------------------------------- backward: dK, dV
@@ -761,24 +795,38 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
     if (more) store_rows(cur ^ 1);
   }
 
-  if (kj >= (ranges || a.k_start ? n_keys : a.Tk)) return;
-  const int64_t r = ranges ? (static_cast<int64_t>(split) * BH + bh) * a.Tk + kj : ks.row0 + kj;
-#pragma unroll
-  for (int c = 0; c < NCT; ++c) {
-    float vk[4], vv[4];
+  auto sums = [&](int c, float (&vk)[4], float (&vv)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       vk[i] = kj < n_keys ? acc_dk[c][i] * a.scale : 0.f;  // (padding: zeros)
       vv[i] = kj < n_keys ? acc_dv[c][i] : 0.f;
     }
-    if (ranges) {
+  };
+  if (ranges) {
+    if (kj >= n_keys) return;
+    const int64_t r = (static_cast<int64_t>(split) * BH + bh) * a.Tk + kj;
+#pragma unroll
+    for (int c = 0; c < NCT; ++c) {
+      float vk[4], vv[4];
+      sums(c, vk, vv);
       store_row4<float>(a.part_k + r * DH + c * 16 + 4 * lg, vk);
       store_row4<float>(a.part_v + r * DH + c * 16 + 4 * lg, vv);
-    } else {
-      store_row4<bf16_t>(static_cast<bf16_t*>(a.dk) + r * a.lddk + hk * DH + c * 16 + 4 * lg, vk);
-      store_row4<bf16_t>(static_cast<bf16_t*>(a.dv) + r * a.lddv + hk * DH + c * 16 + 4 * lg, vv);
     }
+    return;
   }
+  Rows<DH, 16> out{lds + w * 2 * 16 * RB}, out_v{lds + (w * 2 + 1) * 16 * RB};
+  stages_done();
+#pragma unroll
+  for (int c = 0; c < NCT; ++c) {
+    float vk[4], vv[4];
+    sums(c, vk, vv);
+    out.put(lr, c, lg, vk);
+    out_v.put(lr, c, lg, vv);
+  }
+  const int k_end = a.k_start ? n_keys : a.Tk;
+  bf16_t *dk = static_cast<bf16_t*>(a.dk) + ks.row0 * a.lddk + hk * DH, *dv = static_cast<bf16_t*>(a.dv) + ks.row0 * a.lddv + hk * DH;
+  out.store(lane, [&](int row, bool& on) { return on = kw + row < k_end, dk + (kw + row) * a.lddk; });
+  out_v.store(lane, [&](int row, bool& on) { return on = kw + row < k_end, dv + (kw + row) * a.lddv; });
 }
 
 // Large problems: a launch each.  dQ in workgroups of NW waves of 32 queries, dK
