@@ -829,13 +829,13 @@ ATOM_DEV void dkdv_body(uint8_t* lds, float* d_own, const CrossArgs& a, int item
   out_v.store(lane, [&](int row, bool& on) { return on = kw + row < k_end, dv + (kw + row) * a.lddv; });
 }
 
-// Large problems: a launch each.  dQ in workgroups of NW waves of 32 queries, dK
-// and dV of eight waves of 16 keys, two tiles a barrier.
-template <int DH, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) cross_dq_kernel(const CrossArgs a) {
+// Large problems: a launch each.  dQ in workgroups of four waves of 16 or 32 queries,
+// dK and dV of eight waves of 16 keys, two tiles a barrier.
+template <int DH, int GR>
+__global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * FwdDL<DH>::STAGE];
   const int item = item_of(a.n_x * a.B * a.Hk * a.splits, blockIdx.x);
-  if (item >= 0) dq_body<DH, 2, NW, 1>(lds, a, item);
+  if (item >= 0) dq_body<DH, GR, 4, 1>(lds, a, item);
 }
 template <int DH>
 __global__ void __launch_bounds__(512, DH == 64 ? 4 : 2) cross_dkdv_kernel(const CrossArgs a) {
@@ -884,7 +884,9 @@ constexpr int64_t CUS = 256;
 // in 256-row and in 128-row workgroups: 2048 x 1024, 32 heads 45.7 and 46.0, 40: 68.9
 // and 58.1, 56: 73.7 and 73.5; 20,000 x 300, 16 heads 95 and 84; 2 x 2048 x 4096, 32
 // heads 266 and 276.  Heads of 64, 128 and 64 rows: 8 x 300 x 1500, 12 heads 37 and 27;
-// 8 x 1024 x 1024 38 and 42.  dQ in 256 and 128 rows, 40 heads 104 and 82.)
+// 8 x 1024 x 1024 38 and 42.  Gradients with dQ in 128 and 64 rows: 8 x 300 x 1500, 12
+// heads of 64, 81 and 69; 8 x 128 x 1500, 16 heads of 128, 113 and 107, 2 x 2048 x 4096, 32
+// heads 923 and 1017; 2 x 2048 x 1500, 32 heads 360, in 256 rows 367.)
 struct Cost {
   int blk;  // rows; 0: no such kernel
   double tile, start, share, last;
@@ -892,8 +894,8 @@ struct Cost {
 using Costs = Cost[3];
 constexpr Costs FWD[2] = {{{64, 0.45, 1.2, 0.78, 0.55}, {128, 0.76, 1.8, 0.77, 0.55}, {}},
                           {{64, 0.92, 2.0, 0.76, 0.55}, {128, 1.28, 2.75, 0.91, 0.55}, {256, 2.2, 7.5, 1.0, 0.55}}};
-constexpr Costs DQ[2] = {{{128, 1.15, 2.0, 0.77, 0.55}, {}, {}},
-                         {{128, 1.6, 3.0, 0.94, 0.55}, {256, 2.65, 10.0, 1.0, 1.0}, {}}};
+constexpr Costs DQ[2] = {{{64, 0.68, 1.3, 0.80, 0.55}, {128, 1.15, 2.0, 0.77, 0.55}, {}},
+                         {{64, 1.15, 2.5, 0.85, 0.55}, {128, 1.6, 3.0, 0.94, 0.55}, {}}};
 constexpr Costs DKDV[2] = {{{128, 1.5, 3.0, 0.77, 0.55}, {}, {}}, {{128, 1.9, 6.0, 1.0, 0.8}, {}, {}}};
 constexpr Costs FWD_F32[2] = {{{64, 2.7, 2.0, 0.8, 0.55}, {}, {}}, {{64, 5.3, 2.0, 0.8, 0.55}, {}, {}}};
 constexpr Costs DQ_F32[2] = {{{64, 4.0, 3.0, 0.8, 0.55}, {}, {}}, {{64, 8.0, 3.0, 0.8, 0.55}, {}, {}}};
@@ -1103,10 +1105,8 @@ hipError_t bwd_bf16(const CrossArgs& a, const BwdPlan& p, hipStream_t s) {
   }
   // dQ first: it computes D
   if (nq) {
-    if constexpr (DH == 128) {
-      if (p.q.blk == 256) hipLaunchKernelGGL((cross_dq_kernel<DH, 8>), dim3(nq), dim3(512), 0, s, a);
-    }
-    if (p.q.blk == 128) hipLaunchKernelGGL((cross_dq_kernel<DH, 4>), dim3(nq), dim3(256), 0, s, a);
+    if (p.q.blk == 128) hipLaunchKernelGGL((cross_dq_kernel<DH, 2>), dim3(nq), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((cross_dq_kernel<DH, 1>), dim3(nq), dim3(256), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
