@@ -15,7 +15,7 @@
 //
 // What bounds it: long sequences the vector unit and the matrix cores, which
 // share a SIMD's issue slots (2 x 2048 queries, 4096 keys, 32 heads of 128: 259 us,
-// 1.06 PFLOP/s, matrix cores busy 48 %; a library product here 1.43); short ones
+// 1.06 PFLOP/s, matrix cores busy 46 %; a library product here 1.43); short ones
 // the bytes of q and o and the start of a workgroup (8 x 2048 queries on 48 to 500
 // keys, 12 heads of 64: 31 us, of which 15 remain with 64 keys); single tokens the
 // keys' bytes (8 x 1 on 261 to 2048 keys, 40 heads of 128: 51 us, 4.5 TB/s).
@@ -586,8 +586,8 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
 // (LDS); otherwise it is read from a.delta.
 // Two waves a SIMD, which the accumulators of dK and dV and the fragments of K and V
 // leave room for, do not hide all of the LDS reads and exponentials (2 x 2048 x 1500,
-// 32 heads of 128: 219 us, 0.92 PFLOP/s of its four products, matrix cores busy 37 %,
-// LDS 41 %).  Slower there: 32 keys a wave at one wave a SIMD (250), row fragments
+// 32 heads of 128: 217 us, 0.93 PFLOP/s of its four products, matrix cores busy 40 %,
+// LDS 46 %).  Slower there: 32 keys a wave at one wave a SIMD (250), row fragments
 // of two steps held (233), the second products beside the next step's scores (235),
 // workgroups of four waves (246), three or four fragments ahead (224).
 template <int DH, int W, int SUB, bool OWN_D>
