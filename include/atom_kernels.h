@@ -122,9 +122,9 @@ int atom_rope_freqs(int rot, double base, int scaling, double factor, double tra
  * and y [rows][ldy] (queries and keys of a fused qkv: heads = 2 H, ldx = 3 d).
  * transposed: by -a, the gradient dx = mscale R^T dy of y = mscale R x.
  * pos: device positions [rows], any int32; NULL: row % T (T >= 1; not read
- * otherwise).  freq: device, [rot/2].  Angles are computed in 64 bits (at
- * p freq = 10^9 they are off by 10^-7).  y may be x (with ldy = ldx), else they
- * must not overlap.  Requirements: rows from 0 to 2^31 - 1; heads from 0 to 2^16
+ * otherwise).  freq: device, [rot/2].  Angles are off by 2^-25 half turns (10^-7)
+ * at most, at any position.  y may be x (with ldy = ldx), else they must not overlap.
+ * Requirements: rows from 0 to 2^31 - 1; heads from 0 to 2^16
  * (rows or heads 0: nothing is done, and no pointer looked at); dh even, 2 to 256;
  * rot even, 0 to dh (0: pos and freq are not read); mscale finite; ldx, ldy >=
  * heads * dh, up to 2^29; x and y aligned to their elements (to 16 bytes, with dh, rot

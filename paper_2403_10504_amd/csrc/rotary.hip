@@ -26,8 +26,9 @@
 // Sines are computed one a lane and passed on through LDS inside the wave: they are
 // the same in every head, and a lane alone would compute V of them.
 //
-// Angles are exact in 64 bits before they are reduced: p freq_i in fp32 is off
-// by a whole turn's part from p = 10^5 on (2^-24 of 10^5 radians: 0.006).
+// Angles are computed in 64 bits, with what those round off kept (half_turns): p
+// freq_i in fp32 is off by a whole turn's part from p = 10^5 on (2^-24 of 10^5
+// radians: 0.006).
 #include <math.h>
 
 #include <algorithm>
@@ -144,6 +145,20 @@ ATOM_DEV float sum_inside(float v, int P) {
   if (P > 16) pair16(v, a, b), v = a + b;
   if (P > 32) pair32(v, a, b), v = a + b;
   return v;
+}
+
+// p freq / pi, less the whole turns, to 2^-25 (fp32's half step below 1): what the
+// products with 1/pi (in two doubles) and with p round off is added behind the
+// reduction, which is exact.  (Rounded to 64 bits alone, angles of 2 10^9 radians are
+// off by up to 5 10^-7.)  Not contracted: in a fused product t would not be the value
+// that its rest was taken of.
+ATOM_DEV float half_turns(double p, double freq) {
+#pragma clang fp contract(off)
+  constexpr double INV_PI = 0x1.45f306dc9c883p-2, INV_PI_LOW = -0x1.6b01ec5417056p-56;
+  const double q = freq * INV_PI, q_low = __builtin_fma(freq, INV_PI, -q) + freq * INV_PI_LOW;
+  const double t = p * q, t_low = __builtin_fma(p, q, -t) + p * q_low;
+  const double rest = (t - 2.0 * rint(0.5 * t)) + t_low;
+  return static_cast<float>(rest - 2.0 * rint(0.5 * rest));  // (beyond 1 fp32's step is twice as long)
 }
 
 // NC chunks of a lane (two for heads of more than 128 elements in single pairs).
@@ -265,10 +280,8 @@ __global__ void __launch_bounds__(64 * WAVES, OP == NORM_BWD ? 2 : 4) rotary_ker
         } else if (MIX && row + r < a.rows) {
           p = static_cast<double>(a.pos[row + r]);
         }
-        // half turns, reduced to [-1, 1] in 64 bits; then exact in fp32 to 2^-25
-        const double t = p * (a.freq[pair] * 0.31830988618379067154);
         float s, c;
-        sincospif(static_cast<float>(t - 2.0 * rint(0.5 * t)), &s, &c);
+        sincospif(half_turns(p, a.freq[pair]), &s, &c);
         turns[wave][i] = make_float2(c * a.mscale, (OP == NORM_BWD || (OP == ROPE && a.back) ? -s : s) * a.mscale);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -7,6 +7,7 @@ a turned pair (u, w) is off by E = (|u| + |w|) mscale (2^-21 + p freq 2^-52).  r
 squares at most in 16 terms of a lane and 6 shuffles, a root and a division: 2^-20 relative, 2^-19 with the products
 behind it.  A result is rounded to its type: eps / 2 of the value.  fp32's denormal results may be off by 2^-126."""
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -135,6 +136,32 @@ def test_rope_far_and_negative_positions(layout):
     ref, bound = _turn(_split(x, rows, heads, dh), _angles(rows, 1, pos, freq), 1.0, layout)
     _within(_split(y, rows, heads, dh), ref, bound, "f32")
     assert t.equal(y[0], x[0])  # position 0: nothing turns
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("back", [0, 1])
+def test_angles_at_the_farthest_positions(layout, back):
+    """Angles of 10^9 and more, the reference p freq reduced in rational numbers: heads of pairs (1, 0) give cosines and
+    sines, off by the angle's cut to 2^-25 half turns and the function's own 2^-23, and nothing by the angle's size."""
+    t = U.torch()
+    r = np.random.default_rng(40)
+    pos = np.concatenate([r.integers(2 ** 30, 2 ** 31, 40), [2 ** 31 - 1, -2 ** 31]]).astype(np.int32)
+    freq = np.concatenate([r.uniform(0.4, 1.0, 124), [1.0, np.pi / 4, 1 / 3, 10000.0 ** (-1 / 64)]])
+    rows, dh = len(pos), 256
+    first = slice(0, 128) if layout == "half" else slice(0, dh, 2)
+    second = slice(128, dh) if layout == "half" else slice(1, dh, 2)
+    x = t.zeros(rows, dh, device="cuda")
+    x[:, first] = 1.0
+    y, p, f = t.empty_like(x), t.from_numpy(pos).cuda(), t.from_numpy(freq).cuda()
+    A.atom_k_rope(A.ATOM_F32, x.data_ptr(), dh, y.data_ptr(), dh, p.data_ptr(), f.data_ptr(), 1.0, LAYOUTS[layout], back, rows,
+                  0, 1, dh, dh)
+    two_pi = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494459")
+    a = np.array([[float(int(i) * Fraction(w) % two_pi) for w in freq] for i in pos])
+    bound = math.pi * 2.0 ** -25 + 2.0 ** -23
+    got = y.double().cpu().numpy()
+    off = max(np.abs(got[:, first] - np.cos(a)).max(), np.abs(got[:, second] - (-1) ** back * np.sin(a)).max())
+    assert off <= bound, off
 
 
 def _forward(x, gq, gk, rows, Hq, Hk, dh, angle, mscale, layout):
