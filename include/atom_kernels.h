@@ -112,7 +112,8 @@ int atom_k_attn_bwd_noalloc(int dtype, const void* qkv, const void* o, const voi
  *                     those of n >= fast stay, those of n <= slow are divided by
  *                     factor, between them (linear in n) a mean of both.
  * ATOM_EINVAL: rot odd, below 2 or above 256, base or factor not finite and
- * above 0, PARTS without 0 <= slow < fast and trained >= 1. */
+ * above 0, PARTS without 0 <= slow < fast and trained >= 1, a frequency that is
+ * not finite (freq stays as it was). */
 enum { ATOM_ROPE_HALF = 0, ATOM_ROPE_PAIRS = 1 };
 enum { ATOM_ROPE_PLAIN = 0, ATOM_ROPE_LINEAR = 1, ATOM_ROPE_BASE = 2, ATOM_ROPE_PARTS = 3 };
 int atom_rope_freqs(int rot, double base, int scaling, double factor, double trained, double slow, double fast,

@@ -127,16 +127,20 @@ int atom_rope_freqs(int rot, double base, int scaling, double factor, double tra
   if (scaling != ATOM_ROPE_PLAIN && (!(factor > 0) || !isfinite(factor))) return ATOM_EINVAL;
   if (scaling == ATOM_ROPE_PARTS && !(slow >= 0 && slow < fast && isfinite(fast) && trained >= 1 && isfinite(trained)))
     return ATOM_EINVAL;
-  if (scaling == ATOM_ROPE_BASE && rot > 2) base *= pow(factor, rot / (rot - 2.0));
+  double out[128];
   for (int i = 0; i < rot / 2; ++i) {
     double f = pow(base, -2.0 * i / rot);
     if (scaling == ATOM_ROPE_LINEAR) f /= factor;
+    // (the other base's power apart: that base itself may be beyond the numbers)
+    if (scaling == ATOM_ROPE_BASE && i > 0) f *= pow(factor, -2.0 * i / (rot - 2));
     if (scaling == ATOM_ROPE_PARTS) {
       const double keep = fmin(1.0, fmax(0.0, (trained * f / (2.0 * M_PI) - slow) / (fast - slow)));
       f *= keep + (1.0 - keep) / factor;
     }
-    freq[i] = f;
+    if (!isfinite(f)) return ATOM_EINVAL;
+    out[i] = f;
   }
+  for (int i = 0; i < rot / 2; ++i) freq[i] = out[i];
   return ATOM_OK;
 }
 

@@ -460,6 +460,25 @@ def test_frequencies():
     assert A.atom_rope_freqs(2, scaling=A.ATOM_ROPE_BASE, factor=8.0) == [1.0]
 
 
+@pytest.mark.parametrize("rot,factor", [(4, 1e160), (4, 1e-200), (6, 1e250), (64, 1e300), (256, 1e-290)])
+def test_frequencies_of_bases_beyond_the_numbers(rot, factor):
+    """base factor^(rot/(rot-2)) need not be a double where the frequencies are: by logarithms, off by 2^-52 of 1000
+    and a rounding of each power."""
+    i = np.arange(rot // 2)
+    got = A.atom_rope_freqs(rot, scaling=A.ATOM_ROPE_BASE, factor=factor)
+    ref = -2.0 * i / rot * math.log(1e4) - 2.0 * i / (rot - 2) * math.log(factor)
+    assert got[0] == 1.0 and np.abs(np.log(got) - ref).max() <= 1000 * 2.0 ** -50
+    assert abs(got[-1] * factor * 1e4 ** ((rot - 2) / rot) - 1) <= 2.0 ** -50
+
+
+@pytest.mark.parametrize("kw", [dict(rot=256, base=5e-324), dict(rot=64, scaling=1, factor=1e-320),
+                                dict(rot=4, base=1e-300, scaling=2, factor=1e-300), dict(rot=64, scaling=3, factor=1e-320)])
+def test_frequencies_that_are_not_finite(kw):
+    with pytest.raises(A.AtomError) as e:
+        A.atom_rope_freqs(**kw)
+    assert e.value.status == A.ATOM_EINVAL
+
+
 @pytest.mark.parametrize("kw", [dict(rot=0), dict(rot=3), dict(rot=258), dict(rot=64, base=0.0), dict(rot=64, base=math.inf),
                                 dict(rot=64, base=math.nan), dict(rot=64, scaling=4), dict(rot=64, scaling=1, factor=0.0),
                                 dict(rot=64, scaling=3, slow=2.0, fast=2.0), dict(rot=64, scaling=3, trained=0.0),
