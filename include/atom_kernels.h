@@ -185,8 +185,9 @@ typedef struct {
  * divides Hq, B, Tq, Tk >= 0 (B or Tq 0: nothing is done), q_start with q_len only
  * (k alike); without a start, q_rows >= B * Tq (k alike); scale finite, above 0;
  * leading dimensions multiples of 8 (bf16) or 4 (fp32), below 2^24; tensors and ws
- * 16-byte aligned; less than 2^26 pairs of query and head, and of key and head of keys, in
- * padded lengths; Tq (Hq/Hk)^2 < 2^32, and less than 2^22 workgroups of 64 rows.
+ * 16-byte aligned; in padded lengths B Hk, Tq Hq/Hk and Tk below 2^30, rows and heads
+ * B (Tq Hq + Tk Hk) below 2^26 - 4, blocks of 64 of them B Hk (ceil(Tq Hq/Hk / 64) +
+ * ceil(Tk / 64)) below 2^23 - 2^14, and Tq (Hq/Hk)^2 below 2^32.
  * o must not overlap the inputs.  Finite scores have to be below 2^30 in magnitude
  * (beyond, the exponent's rounding alone overflows).  ws: device scratch of at least
  * the bytes that the query returns (0: none needed, or sizes refused); calls that

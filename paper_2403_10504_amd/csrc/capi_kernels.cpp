@@ -37,7 +37,7 @@ inline bool positions_ok(const int32_t* pos, const double* freq, int T, int rot)
                       (pos || T >= 1));
 }
 inline bool cross_ok(int dt, const atom_cross_shape* s) {
-  return dt_ok(dt) && s && cross_attn_ok(dt, s->B, s->Tq, s->Tk, s->Hq, s->Hk, s->dh);
+  return dt_ok(dt) && s && cross_attn_ok(s->B, s->Tq, s->Tk, s->Hq, s->Hk, s->dh);
 }
 // starts come with lengths; without them the rows hold the padded batch
 inline bool side_ok(const int32_t* start, const int32_t* len, int64_t rows, int64_t B, int64_t T) {

@@ -1137,11 +1137,12 @@ uint64_t up4(uint64_t n) { return (n + 3) / 4 * 4; }
 
 }  // namespace
 
-bool cross_attn_ok(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh) {
+bool cross_attn_ok(int B, int Tq, int Tk, int Hq, int Hk, int dh) {
   if (B < 0 || Tq < 0 || Tk < 0 || Hq < 1 || Hk < 1 || Hq % Hk || (dh != 64 && dh != 128)) return false;
   const int64_t G = Hq / Hk, heads = static_cast<int64_t>(B) * Hk;
-  if (G > 1 << 15 || Tq * G > (1ll << 32) / G - 1 || Tq * G >= 1ll << 30 || Tk >= 1 << 30) return false;
-  if (heads >= 1 << 30) return false;
+  // (row_of's products)
+  if (Tq > 0 && (G >= 1 << 16 || Tq * G * G >= 1ll << 32)) return false;
+  if (Tq * G >= 1ll << 30 || Tk >= 1 << 30 || heads >= 1 << 30) return false;
   // rows of the launches that join ranges, four a workgroup
   if (heads * (Tq * G + Tk) >= MAX_WORKGROUPS * 4 - 4) return false;
   // Workgroups of either call, below half of what a dispatch counts (512 threads

@@ -268,7 +268,7 @@ struct CrossArgs {
 };
 
 // Whether the sizes are taken, by the forward and the backward alike.
-bool cross_attn_ok(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh);
+bool cross_attn_ok(int B, int Tq, int Tk, int Hq, int Hk, int dh);
 uint64_t cross_attn_fwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh);
 hipError_t cross_attn_fwd(int dtype, CrossArgs& a, int dh, void* ws, hipStream_t s);
 uint64_t cross_attn_bwd_ws(int dtype, int B, int Tq, int Tk, int Hq, int Hk, int dh);

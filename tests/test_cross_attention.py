@@ -611,3 +611,46 @@ def test_refusals(dtype):
     for change in BAD_SHAPES[:9] + BAD_SHAPES[17:]:
         s = A.atom_cross_shape(**{**SHAPE, **change})
         assert A.atom_k_cross_attn_fwd_ws_bytes(dtype, s) == 0 and A.atom_k_cross_attn_bwd_ws_bytes(dtype, s) == 0
+
+
+@pytest.mark.parametrize("dtype", [A.ATOM_BF16, A.ATOM_F32])
+def test_limits_are_the_documented_ones(dtype):
+    """The last size that each limit takes and the first that it refuses, on the host: shapes without queries have
+    nothing to do in the forward; large gradients need scratch."""
+
+    def forward(B, Tk, Hk):
+        s = A.atom_cross_shape(**{**SHAPE, "B": B, "Tq": 0, "Tk": Tk, "Hq": Hk, "Hk": Hk, "q_rows": 0, "k_rows": B * Tk})
+        A.atom_k_cross_attn_fwd(dtype, s, None, 0, None, 0, None, 0, 1.0, None, 0, None, None, 0)
+
+    forward(1, 2 ** 26 - 5, 1)
+    _refused(forward, 1, 2 ** 26 - 4, 1)
+    forward(2 ** 23 - 2 ** 14 - 1, 1, 1)
+    _refused(forward, 2 ** 23 - 2 ** 14, 1, 1)
+    forward(2 ** 12, 1, 2 ** 11 - 2 ** 2 - 1)
+    _refused(forward, 2 ** 12, 1, 2 ** 11 - 2 ** 2)
+    forward(0, 2 ** 30 - 1, 1)
+    _refused(forward, 0, 2 ** 30, 1)
+
+    def scratch(Tq, Hq):
+        s = A.atom_cross_shape(**{**SHAPE, "B": 1, "Tq": Tq, "Tk": 4096, "Hq": Hq, "Hk": 1, "q_rows": Tq, "k_rows": 4096})
+        return A.atom_k_cross_attn_bwd_ws_bytes(dtype, s)
+
+    for G in (2 ** 16 - 1, 2 ** 15 + 1, 2 ** 15, 46340, 641, 64):
+        most = min((2 ** 32 - 1) // G ** 2, (2 ** 26 - 5 - 4096) // G)
+        assert scratch(most, G) > 0 and scratch(most + 1, G) == 0, G
+    assert scratch(1, 2 ** 16) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Tq", [(2 ** 16 - 1, 1), (2 ** 15 + 1, 3)])
+def test_most_heads_on_one(dtype, Hq, Tq):
+    t = U.torch()
+    c = Case(dtype, 1, Tq, 10, Hq, 1, 64, seed=31)
+    o, lse = c.empty(c.q), t.full((c.nq + 1, Hq), FILL, device="cuda")
+    c.fwd(o, lse)
+    _check_fwd(c, o, lse)
+    o, lse = _reference_fwd(c)
+    g = c.empty(c.q), c.empty(c.k), c.empty(c.v)
+    c.bwd(o, lse, *g)
+    _check_bwd(c, o, lse, *g)
