@@ -105,8 +105,8 @@ struct Rows {
 // side by side, 3 to 6 fragments of V ahead: within 2 us; the two halves of a
 // workgroup in turns, one in its products while the other has its exponentials, two
 // barriers a tile: 262; 64 rows a wave at one wave a SIMD spill: 349.)
-template <int DH, int GR, int NW, int WPS, bool SPLIT>
-__global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs a) {
+template <int DH, int GR, int NW, bool SPLIT>
+__global__ void __launch_bounds__(64 * NW, 2) cross_fwd_kernel(const CrossArgs a) {
   constexpr int NT = 64 * NW;
   using F = FwdDL<DH, NT>;
   constexpr int NS = DH / 32, NCT = DH / 16, BQ = NW * 16 * GR, RB = DH * 2;
@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(64 * NW, WPS) cross_fwd_kernel(const CrossArgs
 // 32 queries a wave in large problems, which halves the LDS reads of K and V (2 x
 // 2048 x 1500, 32 heads of 128: 203 us with 16, 155 with 32: 0.98 PFLOP/s of its
 // three products).
-template <int DH, int GR, int NW, int SUB>
+template <int DH, int GR, int NW>
 ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
   using F = FwdDL<DH>;
   constexpr int NS = DH / 32, NCT = DH / 16, BQ = NW * 16 * GR, NT = 64 * NW, RB = DH * 2;
@@ -429,12 +429,7 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
     }
   };
   const Range rg = q0 < P && a.dq ? range_of(n_keys, a.splits, split) : Range{0, 0};
-  auto load_stage = [&](int st, int kt) {
-#pragma unroll
-    for (int u = 0; u < SUB; ++u)
-      if (kt + u < rg.t1) load_tile(st * SUB + u, (kt + u) * BT);
-  };
-  load_stage(0, rg.t0);
+  if (rg.t0 < rg.t1) load_tile(0, rg.t0 * BT);
 
   Frag<bf16_t> qf[GR][NS], of[GR][NS];
   float lse_i[GR], del_i[GR];
@@ -475,18 +470,20 @@ ATOM_DEV void dq_body(uint8_t* lds, const CrossArgs& a, int item) {
     const uint2 hi = ds_read_tr8(st + r1 * RB + (chunk ^ dsw<DH>(r1)) * 16 + 8 * (lr & 1));
     f.v = make_uint4(lo.x, lo.y, hi.x, hi.y);
   };
-  for (int ks0 = rg.t0; ks0 < rg.t1; ks0 += SUB) {
-    const int cur = ((ks0 - rg.t0) / SUB) & 1;
+  for (int kt = rg.t0; kt < rg.t1; ++kt) {
+    const int cur = (kt - rg.t0) & 1;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     asm volatile("s_barrier" ::: "memory");
-    if (ks0 + SUB < rg.t1) load_stage(cur ^ 1, ks0 + SUB);
+    if (kt + 1 < rg.t1) load_tile(cur ^ 1, (kt + 1) * BT);
     if (qw >= P) continue;
+    // A loop of one trip, for the compiler: without it the same code takes more
+    // registers (dQ of heads of 128, 32 queries a wave: 63 spilled in place of none,
+    // 2 x 2048 x 1500, 32 heads, both gradients 366 -> 578 us).
 #pragma unroll 1
-    for (int u = 0; u < SUB; ++u) {
-      const int kt = ks0 + u, j0 = kt * BT;
-      if (kt >= rg.t1) break;
-      const uint8_t* kst = lds + (cur * SUB + u) * F::STAGE;
+    for (int once = 0; once < 1; ++once) {
+      const int j0 = kt * BT;
+      const uint8_t* kst = lds + cur * F::STAGE;
       const uint8_t* vst = kst + F::TILE;
       float ds[GR][4][4];
       auto score_tile = [&](auto MASK_) {
@@ -835,7 +832,7 @@ template <int DH, int GR>
 __global__ void __launch_bounds__(256, 2) cross_dq_kernel(const CrossArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * FwdDL<DH>::STAGE];
   const int item = item_of(a.n_x * a.B * a.Hk * a.splits, blockIdx.x);
-  if (item >= 0) dq_body<DH, GR, 4, 1>(lds, a, item);
+  if (item >= 0) dq_body<DH, GR, 4>(lds, a, item);
 }
 template <int DH>
 __global__ void __launch_bounds__(512, DH == 64 ? 4 : 2) cross_dkdv_kernel(const CrossArgs a) {
@@ -860,7 +857,7 @@ __global__ void __launch_bounds__(256, DH == 64 ? 3 : 2) cross_bwd_small_kernel(
   const int item = id < k_end ? item_of(n_k, id) : item_of(n_q, id - k_end);
   if (item < 0) return;
   if (id < k_end) dkdv_body<DH, 4, 1, true>(lds, reinterpret_cast<float*>(lds + STAGES), a, item);
-  else dq_body<DH, 1, 4, 1>(lds, a, item);
+  else dq_body<DH, 1, 4>(lds, a, item);
 }
 
 }  // namespace cross
@@ -984,7 +981,6 @@ BwdPlan bwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
     // (and D of a range of queries has to fit the LDS)
     p.k = Plan{64, static_cast<int>(tk),
                std::max(ranges_of(tq, fair, 2), static_cast<int>((tq + SMALL_ROWS / attn::BT - 1) / (SMALL_ROWS / attn::BT)))};
-    p.q.splits = std::max(1, p.q.splits), p.k.splits = std::max(1, p.k.splits);
   } else {
     p.q = plan_of(dtype == DT_BF16 ? DQ[dh == 128] : DQ_F32[dh == 128], rows, heads, tk, dh);
     p.k = plan_of(dtype == DT_BF16 ? DKDV[dh == 128] : DKDV_F32[dh == 128], Tk, heads, tq, 2 * dh);
@@ -1061,8 +1057,8 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) cross_sum_kernel(const 
 template <int DH, int GR, int NW>
 void fwd_launch(const CrossArgs& a, hipStream_t s) {
   const dim3 grid(grid_of(a, a.n_x, a.splits)), block(64 * NW);
-  if (a.splits > 1) hipLaunchKernelGGL((cross_fwd_kernel<DH, GR, NW, 2, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((cross_fwd_kernel<DH, GR, NW, 2, false>), grid, block, 0, s, a);
+  if (a.splits > 1) hipLaunchKernelGGL((cross_fwd_kernel<DH, GR, NW, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((cross_fwd_kernel<DH, GR, NW, false>), grid, block, 0, s, a);
 }
 hipError_t fwd_bf16(const CrossArgs& a, int blk, int dh, hipStream_t s) {
   if (dh == 64) {
