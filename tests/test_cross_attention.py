@@ -654,3 +654,99 @@ def test_most_heads_on_one(dtype, Hq, Tq):
     g = c.empty(c.q), c.empty(c.k), c.empty(c.v)
     c.bwd(o, lse, *g)
     _check_bwd(c, o, lse, *g)
+
+
+# small gradients (one launch) and large ones, heads of keys alone and shared by three (tiles start inside a token);
+# leading dimensions up to the largest, where 64 rows span 2^31 bytes and more
+FAR = [(2, 150, 300, 2, 2, 64, 2 ** 24 - 8), (2, 150, 300, 6, 2, 64, 2 ** 24 - 8), (2, 150, 2300, 15, 15, 64, 2 ** 20 + 8),
+       (2, 150, 2300, 12, 4, 128, 2 ** 20 + 8)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hk,dh,ldk", FAR)
+def test_far_rows_of_every_tensor(dtype, B, Tq, Tk, Hq, Hk, dh, ldk):
+    """Packed rows up to 2^24 - 8 elements apart, the last ones behind 2^32: the bits of rows side by side."""
+    t = U.torch()
+    args = dict(rows="packed", seed=32, q_len=[Tq, Tq - 3], k_len=[Tk, Tk - 1])
+    near, far = Case(dtype, B, Tq, Tk, Hq, Hk, dh, **args), Case(dtype, B, Tq, Tk, Hq, Hk, dh, **args)
+    nq, nk, wq, wk, ldq = near.nq, near.nk, Hq * dh, Hk * dh, 2 ** 24 - 8
+    assert nq * ldq > 2 ** 32 and nk * ldk > 2 ** 32
+    bq, bk = (t.empty(n * ld, device="cuda", dtype=_type(dtype)).view(n, ld) for n, ld in ((nq, ldq), (nk, ldk)))
+    q, do, o, dq = (bq[:, i * wq:(i + 1) * wq] for i in range(4))
+    k, v, dk, dv = (bk[:, i * wk:(i + 1) * wk] for i in range(4))
+    for x, y in ((q, near.q), (do, near.dout)):
+        x.copy_(y[:nq])
+    for x, y in ((k, near.k), (v, near.v)):
+        x.copy_(y[:nk])
+    far.q, far.dout, far.k, far.v = q, do, k, v
+    lse = t.full((2, nq + 1, Hq), FILL, device="cuda")
+    out = near.empty(near.q), near.empty(near.q), near.empty(near.k), near.empty(near.v)
+    near.fwd(out[0], lse[0])
+    near.bwd(out[0], lse[0], *out[1:])
+    _check_fwd(near, out[0], lse[0])
+    _check_bwd(near, out[0], lse[0], *out[1:])
+    far.fwd(o, lse[1])
+    far.bwd(o, lse[1], dq, dk, dv)
+    assert t.equal(lse[0], lse[1])
+    on = {"q": near.covered(nq, near.qs, near.qn)[:nq], "k": near.covered(nk, near.ks, near.kn)[:nk]}
+    for side, a, b in (("q", out[0], o), ("q", out[1], dq), ("k", out[2], dk), ("k", out[3], dv)):
+        assert t.equal(a[:-1][on[side]], b[on[side]])
+
+
+class Head(Case):
+    """One head of one sequence of a case without shared keys, on its keys from the n-th on alone."""
+
+    def __init__(self, c, b, h, n=0):
+        self.__dict__.update(c.__dict__)
+        self.Hq = self.Hk = 1
+        qr, kr = slice(c.qs[b], c.qs[b] + c.qn[b]), slice(c.ks[b] + n, c.ks[b] + c.kn[b])
+        self.cols = slice(h * c.dh, (h + 1) * c.dh)
+        one = lambda x, r: x[r, self.cols].double().unsqueeze(0)  # noqa: E731
+        self.only = qr, kr, one(c.q, qr), one(c.k, kr), one(c.v, kr), one(c.dout, qr)
+
+    def sequences(self):
+        yield self.only
+
+    def outside(self, *_):
+        pass
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Tq,Tk,gone", [(20, 130, 70), (300, 130, 64), (3, 2000, 1100), (70, 130, 129)])
+def test_keys_of_infinity_and_nan(dtype, Tq, Tk, gone):
+    """The first keys of a head at -infinity leave the others' results, by the bounds of those alone, and get no
+    gradient; all of them leave nothing; a NaN spoils its own sequence and head and no other."""
+    t = U.torch()
+
+    def run(c):
+        o, lse = c.empty(c.q), t.full((c.nq + 1, 2), FILL, device="cuda")
+        c.fwd(o, lse)
+        g = c.empty(c.q), c.empty(c.k), c.empty(c.v)
+        c.bwd(o, lse, *g)
+        return o, lse, g
+
+    def check(c, o, lse, g, b, h, n=0):
+        x = Head(c, b, h, n)
+        at = lambda y: y[:, x.cols]  # noqa: E731
+        _check_fwd(x, at(o)[:c.nq], lse[:c.nq, h:h + 1])
+        # (dq of infinite keys: 0 times infinity)
+        _check_bwd(x, at(o), lse[:, h:h + 1], None if n else at(g[0]), at(g[1]), at(g[2]))
+
+    c = Case(dtype, 2, Tq, Tk, 2, 2, 64, seed=33)
+    c.q[:, :] = c.q.abs()
+    c.k[:gone, :64] = -math.inf  # sequence 0, head 0
+    o, lse, g = run(c)
+    check(c, o, lse, g, 0, 0, gone)
+    assert bool((g[1][:gone, :64] == 0).all()) and bool((g[2][:gone, :64] == 0).all())
+    for b, h in ((0, 1), (1, 0), (1, 1)):
+        check(c, o, lse, g, b, h)
+    c.k[:Tk, :64] = -math.inf
+    c.k[Tk + Tk // 2, 64 + 3] = float("nan")  # sequence 1, head 1
+    o, lse, g = run(c)
+    assert bool((o[:Tq, :64] == 0).all()) and bool((lse[:Tq, 0] == -math.inf).all())
+    assert bool((g[1][:Tk, :64] == 0).all()) and bool((g[2][:Tk, :64] == 0).all())
+    assert bool(o[Tq:2 * Tq, 64:].isnan().all()) and bool(lse[Tq:2 * Tq, 1].isnan().all())
+    for b, h in ((0, 1), (1, 0)):
+        check(c, o, lse, g, b, h)

@@ -443,6 +443,33 @@ def test_far_rows():
     assert t.equal(x[:, :2 * dh], y)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_far_rows_several_a_wave(dtype):
+    """Few heads of many rows, several rows a wave, 2^19 elements apart and the last of them behind 2^32: the bits of rows
+    side by side, in every call."""
+    t = U.torch()
+    rows, T, dh, H = 8200, 77, 64, 3
+    width, ld = H * dh, 2 ** 19 + 16
+    near = _norm_case(dtype, rows, 1, 1, 1, dh, dh, 0, 41)
+    x, _, freq, gq, gk, g = near
+    dy = t.randn(rows, width, device="cuda", generator=g).to(_type(dtype))
+    far = t.empty(rows * ld, device="cuda", dtype=_type(dtype)).view(rows, ld)
+    fx, fdy, fy, fdx = (far[:, i * width:(i + 1) * width] for i in range(4))
+    fx.copy_(x[:rows])
+    fdy.copy_(dy)
+    out = []
+    for a, b, y, dx in ((x, dy, t.empty_like(x), t.empty_like(dy)), (fx, fdy, fy, fdx)):
+        dg = t.empty(2, dh, device="cuda")
+        A.atom_k_rope(U.dt_code(dtype), a.data_ptr(), a.stride(0), y.data_ptr(), y.stride(0), None, freq.data_ptr(), 1.0,
+                      A.ATOM_ROPE_HALF, 0, rows, T, H, dh, dh)
+        turned = y[:rows].clone()
+        _fwd(dtype, a, y, gq, gk, None, freq, 1.0, "pairs", rows, T, 1, 1, 1, dh, dh)
+        _bwd(dtype, b, a, dx, gq, gk, dg[0], dg[1], None, freq, 1.0, "pairs", rows, T, 1, 1, 1, dh, dh, _ws(rows, 1, 1, dh))
+        out.append((turned, y[:rows].clone(), dx.clone(), dg))
+    assert all(t.equal(p, q) for p, q in zip(*out))
+
+
 def test_frequencies():
     i = np.arange(32)
     plain = 10000.0 ** (-i / 32)
