@@ -135,7 +135,8 @@ int atom_k_rope(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy, con
 
 /* Norms of queries and keys, and the turn, in one pass over rows of Hq heads of
  * queries, Hk of keys and Hv of values (a fused qkv: H each; one side alone: 0
- * for the others), before atom_k_attn_fwd or atom_k_cross_attn_fwd:
+ * for the others), before atom_k_attn_fwd (which takes H heads of each side, of 64 or
+ * 128) or atom_k_cross_attn_fwd (those sizes too, shared heads of keys, no causal mask):
  *   u = g x / sqrt(mean(x^2) + eps) over a head's dh elements,  y = mscale R u,
  * g = gq or gk [dh] in dtype, shared by the heads of a side (NULL: 1).  Heads of
  * values are copied (nothing is done where y is x).  rot 0: the norms alone.
@@ -163,7 +164,10 @@ int atom_k_qknorm_rope_bwd(int dtype, const void* dy, int64_t lddy, const void* 
  * values, query head h on head h / (Hq / Hk).  For each sequence and head
  *   z = scale q k^T,  lse = log sum_j exp z_j,  o = exp(z - lse) v.
  * Every key of a sequence is visible to every query of it.  A row without keys
- * (or with scores of -infinity alone) gives o 0 and lse -infinity.
+ * (or with scores of -infinity alone) gives o 0 and lse -infinity.  Sums and
+ * statistics are fp32; bf16 calls round exp(z - max) to bf16 before its product with
+ * v, the backward p and ds before theirs (half a step, 2^-8 of each term).  An infinity
+ * in v or dout makes the results that it enters infinite or NaN.
  *
  * Rows: q and o [q_rows][Hq * dh], lse fp32 [q_rows][Hq], k and v [k_rows][Hk * dh],
  * each with its leading dimension.  Padded: sequence b's queries are rows b * Tq

@@ -883,7 +883,12 @@ constexpr int64_t CUS = 256;
 // heads 266 and 276.  Heads of 64, 128 and 64 rows: 8 x 300 x 1500, 12 heads 37 and 27;
 // 8 x 1024 x 1024 38 and 42.  Gradients with dQ in 128 and 64 rows: 8 x 300 x 1500, 12
 // heads of 64, 81 and 69; 8 x 128 x 1500, 16 heads of 128, 113 and 107, 2 x 2048 x 4096, 32
-// heads 923 and 1017; 2 x 2048 x 1500, 32 heads 360, in 256 rows 367.)
+// heads 923 and 1017; 2 x 2048 x 1500, 32 heads 360, in 256 rows 367.  fp32, one range
+// of 16 and of 32 tiles, 256 workgroups: heads of 64 and of 128, forward 60 and 103, 102
+// and 195, dQ 73 and 139, 141 and 270; 512 workgroups 32 tiles 183, 344, 239, 458.  dK
+// and dV, with the pass for D, 148 and 293, 366 and 679, 512 workgroups 489 and 1087: a
+// tile takes a third more than its row says.  Two ranges, 256 workgroups: 139 and 266,
+// 320 and 567, taken by these figures but for the first.)
 struct Cost {
   int blk;  // rows; 0: no such kernel
   double tile, start, share, last;
@@ -938,7 +943,8 @@ Plan plan_of(const Costs& kernels, int64_t rows, int64_t heads, int64_t tiles, i
 // and 52 (1000 x 333, 32 heads), 16 tiles 49 and 59, 32 tiles 75 and 100; heads of
 // 64, 16 tiles 28 and 34, 22 to 24 tiles 46 and 43, 47 and 45.
 constexpr int64_t SMALL_TILES_64 = 12, SMALL_TILES_128 = 8;
-// Tiles that ranges have to save a workgroup (1 to 6 measured the same).
+// Tiles that ranges have to save a workgroup of a small backward, to be worth their
+// join's launch (1 to 6 measured the same).
 constexpr int64_t RANGE_GAIN = 2;
 
 // One block of rows for each sequence and head is a call that reads its keys for
@@ -946,7 +952,10 @@ constexpr int64_t RANGE_GAIN = 2;
 // flight and long sequences do not wait for one workgroup.  (Workgroups wanted, and
 // tiles of keys a range has at least, us of 8 x 1 x 2048 of 40 heads of 128, ragged,
 // and of 16 x 1 x 4000 of 32 heads on 4: one range 72, -; 1024, 8: 52.3, 33.4; 1024,
-// 4: 52.5, 39.1; 2048, 4: 53.8, 39.3; 2048, 2: 53.8, 48.7; 4096, 2: 61.7, 49.0.)
+// 4: 52.5, 39.1; 2048, 4: 53.8, 39.3; 2048, 2: 53.8, 48.7; 4096, 2: 61.7, 49.0.  Both
+// shapes have the card full.  One sequence of few heads has not, and its workgroups
+// still walk eight tiles: one token of 32 heads of 128 on 2048 keys of 8 heads, 32
+// workgroups, 13.5 us, fp32 26; fewer tiles a range are not measured there.)
 constexpr int64_t TOKEN_WGS = 1024, TOKEN_TILES = 8;
 
 Plan fwd_plan(int dtype, int B, int Tq, int Tk, int Hk, int G, int dh) {
@@ -963,8 +972,8 @@ struct BwdPlan {
   bool small;
   Plan q, k;
 };
-// Ranges of a side: none where they would not shorten a workgroup's tiles from
-// `all` to the `fair` share by more than the launch that joins them costs.
+// Ranges of a side that bring a workgroup's tiles from `all` to the `fair` share, but
+// not below `least`; none where that saves RANGE_GAIN tiles or fewer.
 int ranges_of(int64_t all, int64_t fair, int64_t least) {
   const int64_t per = std::max(fair, least);
   return static_cast<int>(all > per + RANGE_GAIN ? (all + per - 1) / per : 1);

@@ -3,7 +3,10 @@
 // rows in their natural layout, through registers into padded LDS, two stages.
 // A transposed operand is read by elements: a fragment's eight matrix
 // instructions take 256 cycles, its eight LDS reads 16.  2 x 512 x 512, 16 heads of
-// 128: 50 us forward, 152 backward (86 and 99 TFLOP/s; a library product 142).
+// 128: 50 us forward, 150 backward (86 and, with the scores and dP that are computed
+// twice, 100 TFLOP/s; a library product 142).  dK and dV at heads of 128 need more than
+// 256 registers, two tiles on their way to LDS beside K, V and both sums: 84 are
+// spilled, 78 in the small backward.
 #include "cross_attention.h"
 
 namespace atom {

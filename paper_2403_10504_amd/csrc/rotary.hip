@@ -13,7 +13,10 @@
 // kept, the whole head being in registers anyway).  4096 rows of 3 x 32 heads of 128:
 // 39 us, 5.2 TB/s (a large copy: 5.1); gradients of 2048 rows of 3 x 40: 35 us, 4.8
 // TB/s, and 4 for the gains' sums; queries and keys of 8192 rows of 16 heads turned:
-// 29.8 us, 4.5 TB/s.
+// 29.8 us, 4.5 TB/s.  Where head, rot or a pitch allows less than 16 bytes an access
+// (pairs_of), less: 4096 rows of 3 x 32 heads of 128, bf16, 41 us in 16 bytes, 48 in 8,
+// 61 in 4, 95 in 2; fp32, 2048 rows, 45, 61 and 94 in 16, 8 and 4; heads of 130 123 and
+// 112; gradients, 2048 rows bf16, 32, 45, 64 and 83.
 //
 // A lane holds V pairs of a head: in the half layout V elements at c V and V at
 // rot/2 + c V, in the pairs layout 2 V in a row; elements past rot in chunks of
