@@ -375,6 +375,77 @@ def test_rows_do_not_mix():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,Hq,Hk,Hv,dh,rot,T", ALIGNED)
+def test_aligned_rows_in_place(dtype, rows, Hq, Hk, Hv, dh, rot, T):
+    """The widest accesses, several rows a wave, with results where the inputs were."""
+    t = U.torch()
+    n, width = Hq + Hk, (Hq + Hk + Hv) * dh
+    x, pos, freq, gq, gk, g = _norm_case(dtype, rows, Hq, Hk, Hv, dh, rot, 16, rows + dh + 7)
+    angle = _angles(rows, T, pos, freq) if rot else None
+    dy = _padded(rows, width, 8, dtype)
+    dy[:rows, :width] = t.randn(rows, width, device="cuda", generator=g) * 0.01
+    dg, values = t.full((2, dh), 55.0, device="cuda"), dy[:rows, n * dh:width].clone()
+    refs = _gradients(dy, x, gq, gk, rows, Hq, Hk, dh, angle, 0.75, "half")
+    _bwd(dtype, dy, x, dy, gq, gk, dg[0], dg[1], pos, freq, 0.75, "half", rows, T, Hq, Hk, Hv, dh, rot, _ws(rows, Hq, Hk, dh))
+    _within(_split(dy, rows, n, dh), *refs[0], dtype)
+    assert t.equal(dy[:rows, n * dh:width], values) and _kept(dy, rows, width)
+    for k in (0, 1):
+        _within(dg[k], *refs[1 + k], "f32")
+    y, values = x.clone(), x[:rows, n * dh:width].clone()
+    ref, bound, *_ = _forward(x, gq, gk, rows, Hq, Hk, dh, angle, 0.75, "half")
+    _fwd(dtype, y, y, gq, gk, pos, freq, 0.75, "half", rows, T, Hq, Hk, Hv, dh, rot)
+    _within(_split(y, rows, n, dh), ref, bound, dtype)
+    assert t.equal(y[:rows, n * dh:width], values) and _kept(y, rows, width)
+    if rot:
+        ref, bound = _turn(_split(x, rows, n, dh), angle, 0.75, "half")
+        A.atom_k_rope(U.dt_code(dtype), x.data_ptr(), x.stride(0), x.data_ptr(), x.stride(0), None, _ptr(freq), 0.75,
+                      A.ATOM_ROPE_HALF, 0, rows, T, n, dh, rot)
+        _within(_split(x, rows, n, dh), ref, bound, dtype)
+        assert t.equal(x[:rows, n * dh:width], values) and _kept(x, rows, width)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hk,Hv,dh,rot", [(65534, 1, 1, 2, 2), (1, 65535, 0, 16, 16), (0, 1, 65535, 4, 0)])
+def test_most_heads(dtype, Hq, Hk, Hv, dh, rot):
+    t = U.torch()
+    rows, T, n, width = 3, 2, Hq + Hk, (Hq + Hk + Hv) * dh
+    x, pos, freq, gq, gk, g = _norm_case(dtype, rows, Hq, Hk, Hv, dh, rot, 0, 61)
+    angle = _angles(rows, T, pos, freq) if rot else None
+    y, dx = _padded(rows, width, 0, dtype), _padded(rows, width, 0, dtype)
+    _fwd(dtype, x, y, gq, gk, pos, freq, 1.0, "half", rows, T, Hq, Hk, Hv, dh, rot)
+    ref, bound, *_ = _forward(x, gq, gk, rows, Hq, Hk, dh, angle, 1.0, "half")
+    _within(_split(y, rows, n, dh), ref, bound, dtype)
+    dy = t.randn(rows + 1, width, device="cuda", generator=g).to(_type(dtype))
+    dg = t.full((2, dh), 55.0, device="cuda")
+    _bwd(dtype, dy, x, dx, gq, gk, dg[0], dg[1], pos, freq, 1.0, "half", rows, T, Hq, Hk, Hv, dh, rot, _ws(rows, Hq, Hk, dh))
+    refs = _gradients(dy, x, gq, gk, rows, Hq, Hk, dh, angle, 1.0, "half")
+    _within(_split(dx, rows, n, dh), *refs[0], dtype)
+    for k in (0, 1):
+        _within(dg[k], *refs[1 + k], "f32")
+    for a, b in ((x, y), (dy, dx)):
+        assert t.equal(a[:rows, n * dh:], b[:rows, n * dh:]) and _kept(b, rows, width)
+
+
+@pytest.mark.gpu
+def test_most_rows():
+    """2^31 - 1 rows, in place: they repeat with the positions, so every period has the first one's bits."""
+    t = U.torch()
+    rows, T = 2 ** 31 - 1, 1021
+    base = t.randn(T, 2, device="cuda", generator=t.Generator(device="cuda").manual_seed(62)).to(t.bfloat16)
+    x = base.repeat(rows // T + 1, 1)
+    x[rows:] = 77.0
+    freq, y = _freq(2), t.empty_like(base)
+    for a, b, n in ((base, y, T), (x, x, rows)):
+        A.atom_k_rope(A.ATOM_BF16, a.data_ptr(), 2, b.data_ptr(), 2, None, freq.data_ptr(), 1.0, A.ATOM_ROPE_HALF, 0, n, T, 1,
+                      2, 2)
+    whole, rest = rows // T, rows % T
+    assert bool((x[:whole * T].view(whole, 2 * T) == y.view(1, 2 * T)).all())
+    assert t.equal(x[whole * T:rows], y[:rest]) and bool((x[rows:] == 77.0).all())
+
+
+@pytest.mark.gpu
 def test_no_rows_and_no_heads():
     t = U.torch()
     A.atom_k_rope(A.ATOM_BF16, None, 0, None, 0, None, None, 1.0, 0, 0, 0, 0, 4, 64, 64)
